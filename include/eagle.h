@@ -244,6 +244,135 @@ int eagle_feature_noise(eagle_ctx *ctx, const float *in_dev, float *out_dev, int
  * events; *gb_per_s = bytes read / summed kernel time.  The buffer is only read.  Synchronises the stream. */
 int eagle_probe_stream_read(const void *buf_dev, size_t bytes, int32_t iters, void *hip_stream, double *gb_per_s);
 
+/* ---- Operators on the caller's own tensors ----------------------------------------------------------------------
+ * Rotary positions with the append to a paged cache, attention of a chunk of new tokens over it, and the rules logits pass before a token is
+ * chosen: what a step does inside a context, for tensors of the caller (another head, a model of another layout, a scheduler of its own).
+ *   - They need no context.  Every tensor lies on the device that `hip_stream` belongs to, which must be the calling thread's current device; work
+ *     is enqueued on that stream only, nothing is allocated and nothing synchronises, so the calls may be captured into graphs.
+ *   - Calls on different streams or threads may overlap as long as they share no output and no workspace (two captured graphs that share a
+ *     workspace must not run at the same time).
+ *   - Arguments the host holds are checked: EAGLE_EINVAL, nothing launched.  What lies in device memory (lengths, page numbers, token ids) cannot
+ *     be; the kernels bound every access instead, as said at each field.
+ *   - Types are EAGLE_F32 and EAGLE_BF16; sums and statistics are kept in 32 bits. */
+
+/* New tokens of a batch of sequences: sequence s has the rows row_start[s] .. row_start[s+1]-1 of the row tensors, and with them key_len[s] tokens in
+ * the cache (row i of n is token key_len[s] - n + i).  A draft tree instead of consecutive tokens: tree_base[s] tokens are in front of the tree, node u lies
+ * at token tree_base[s] + u, and bit u of tree_mask[row] says that node u is the row's own node or an ancestor (parents before children, so the
+ * highest bit is the row's own); a node's position is tree_base[s] + its number of ancestors.  key_len[s] counts all nodes in the cache, also those that
+ * have no row in this call.
+ * max_rows and max_keys bound the rows of a sequence and key_len: rows and tokens beyond are not processed. */
+typedef struct {
+  int32_t n_seqs, n_rows, max_rows, max_keys;
+  const int32_t *row_start;           /* dev int32 [n_seqs + 1] */
+  const int32_t *key_len;             /* dev int32 [n_seqs] */
+  const int32_t *tree_base;           /* dev int32 [n_seqs], with tree_mask; or both null */
+  const uint64_t *tree_mask;          /* dev uint64 [n_rows] */
+} eagle_chunk;
+
+/* Paged keys and values: element (page, kv head, token in page, i) of k and v at page * page_stride + head * head_stride + token * token_stride + i
+ * (strides in elements, the same for both).  page_table[s * table_stride + t / page_tokens] is the page of token t of sequence s; a number outside
+ * 0..n_pages-1 (-1, say) is a page that is not there: its tokens are invisible and rows are not stored to it. */
+typedef struct {
+  void *k, *v;
+  int32_t dtype, n_kv_heads, head_dim, page_tokens /* power of two */, n_pages, pages_per_seq;
+  int64_t page_stride, head_stride, token_stride, table_stride;
+  const int32_t *page_table;          /* dev int32 [n_seqs][table_stride >= pages_per_seq] */
+} eagle_paged_kv;
+
+/* How positions turn a head: pair p (p < rot_dim / 2) of the first rot_dim elements by the angle position * f_p, f_p = theta^(-2p/rot_dim), scaled:
+ *   EAGLE_ROPE_LINEAR  f / factor
+ *   EAGLE_ROPE_BASE    theta * factor^(rot_dim / (rot_dim - 2)) in place of theta
+ *   EAGLE_ROPE_BANDS   by wavelength w = 2 pi / f against L = trained_len: f where w < L / high, f / factor where w > L / low, between them
+ *                      f * (s + (1 - s) / factor) with s = (L / w - low) / (high - low)
+ *   EAGLE_ROPE_RAMP    by pair: f up to pair a, f / factor from pair b, linear between, with a = max(0, floor(P(high))), b = min(rot_dim - 1, ceil(P(low))),
+ *                      P(n) = rot_dim * ln(L / (2 pi n)) / (2 ln theta): the pair that turns n times over L positions
+ * Cosines and sines are multiplied by mscale.  Pair p is (p, p + rot_dim / 2), or (2p, 2p + 1) if interleaved.  rot_dim is even, at most head_dim <= 256. */
+enum { EAGLE_ROPE_NONE = 0, EAGLE_ROPE_LINEAR, EAGLE_ROPE_BASE, EAGLE_ROPE_BANDS, EAGLE_ROPE_RAMP };
+typedef struct {
+  int32_t head_dim, rot_dim, interleaved, scaling;
+  double theta, factor, low, high;    /* low < high: BANDS and RAMP only; factor >= 1: unread with NONE */
+  int32_t trained_len;                /* BANDS and RAMP */
+  float mscale;
+} eagle_rope_config;
+/* The same, worked out: turn[p] = f_p / (2 pi) as a fraction of 2^64.  Host memory; made once, passed to every call. */
+typedef struct {
+  int32_t head_dim, rot_dim, interleaved;
+  float mscale;
+  uint64_t turn[128];
+} eagle_rope_plan;
+int eagle_rope_plan_init(const eagle_rope_config *cfg, eagle_rope_plan *out);
+
+/* Rotates q [n_rows][n_heads][head_dim] into q_out and k [n_rows][n_kv_heads][head_dim] into the cache, together with v -- or, without a cache (kv null), k into
+ * k_out.  Row and head strides in elements, elements of a head consecutive; outputs may be the inputs.  With a cache `chunk` is needed; v null leaves the
+ * cache's values alone.  positions (dev int32 [n_rows]) overrides the positions that `chunk` gives; without a chunk (null: n_rows is the field here) it
+ * is needed.  q (with q_out) or k may be null.  Rows that no sequence owns are left as they are, in the outputs too (without a chunk there are none), and
+ * a token at or behind max_keys, or on a page that is not there, is not stored.
+ * inverse: the transposed map (angles negated, the same mscale): the gradient of the rotation with respect to its input; without a cache only.
+ * Two rows of one call must not be the same token of the cache. */
+typedef struct {
+  int32_t n_rows, n_heads, n_kv_heads, dtype, inverse;
+  const void *q, *k, *v;
+  void *q_out, *k_out;
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head, q_out_row, q_out_head, k_out_row, k_out_head;
+  const int32_t *positions;
+} eagle_rope_args;
+int eagle_rope(const eagle_rope_plan *plan, const eagle_rope_args *args, const eagle_chunk *chunk, const eagle_paged_kv *kv, void *hip_stream);
+
+/* out = softmax(score) v over the visible tokens of the cache, for every row and head (query head h uses kv head h / (n_heads / n_kv_heads)):
+ *   score(row, j) = scale * q . k_j;  softcap > 0: softcap * tanh(score / softcap);  slopes: minus slopes[h] * |distance|
+ * distance = the row's position - token j's (a token in front of the chunk lies at its index).  Token j is visible to a row if j < key_len[s], its page is there, and
+ *   - j comes before the row or is the row itself (tree: is in front of the tree, or the row's node or an ancestor), and distance < window if window > 0, or
+ *   - j < prefix[s] (tree: at most the tokens in front of the tree): a prefix every row of the sequence sees, in front of the window and ahead of the row.
+ * A row that sees nothing gets zeros.  q, out: EAGLE_F32 over a cache of either type, or EAGLE_BF16 over EAGLE_BF16; out is of q's type and may be q.
+ * head_dim: a multiple of 8, 8..128.  q's rows and the cache's tokens start on multiples of 16 bytes, out's of 8 elements.  NaN and infinities in a token stay with
+ * the rows that see it.  Rows that no sequence owns are left as they are.
+ * workspace (dev, 256-byte aligned): eagle_chunk_attention_workspace() bytes, for the same arguments; its contents need not be kept or cleared. */
+typedef struct {
+  int32_t n_heads, dtype, window;
+  const void *q;
+  void *out;
+  int64_t q_row, q_head, out_row, out_head;   /* elements */
+  float scale, softcap;
+  const float *slopes;                /* dev [n_heads] or null */
+  const int32_t *prefix;              /* dev [n_seqs] or null */
+} eagle_attention_args;
+size_t eagle_chunk_attention_workspace(const eagle_attention_args *args, const eagle_chunk *chunk, const eagle_paged_kv *kv);
+int eagle_chunk_attention(const eagle_attention_args *args, const eagle_chunk *chunk, const eagle_paged_kv *kv, void *workspace_dev, size_t workspace_bytes,
+                          void *hip_stream);
+
+/* What logits pass before a token is chosen.  The text of row r is its sequence's tokens and, along a draft tree, the tokens of the nodes on its path; with
+ * c = how often token t occurs in it behind the sequence's first n_prompt tokens:
+ *   x = logit;  t anywhere in the text: x / repetition if x > 0, else x * repetition;  c > 0: x - presence - frequency * c;  x + bias[t];
+ *   t not allowed: -inf
+ * Every array may be null (no such rule).  Token ids outside the vocabulary count for nothing.  A token may stand in a bias list more than once: the last entry
+ * counts.  A repetition that is not above 0 counts as 1.  A mask may leave a row empty: all of it is -inf. */
+typedef struct {
+  int32_t n_seqs;
+  const int32_t *tokens;              /* dev [n_seqs][token_stride] */
+  int64_t token_stride;
+  const int32_t *n_tokens, *n_prompt; /* dev [n_seqs]; n_tokens at most token_stride (more is not read); n_prompt null: 0 */
+  const float *repetition, *presence, *frequency;   /* dev [n_seqs] */
+  const int32_t *bias_start, *bias_token;           /* dev [n_seqs + 1], [bias_start[n_seqs]]; entries beyond n_bias are not read */
+  const float *bias_value;
+  int32_t n_bias;
+} eagle_logit_rules;
+/* in, out: [n_rows][vocab] of `dtype`, row strides in elements; out may be in.  Sequence s has the rows row_start[s] .. row_start[s+1]-1 (null: row r is
+ * sequence r's, and n_rows = n_seqs); rows that no sequence owns are left as they are.  path_token (dev [n_rows]) and path_mask (dev uint64 [n_rows]), or both
+ * null: bit u of a row's mask adds the token of its sequence's row u to its text (u < 64).  allowed: bit t % 32 of word t / 32 of row allowed_row[r] of
+ * [n_masks][mask_stride] words (allowed_row null: row r); a row number outside 0..n_masks-1 (-1, say): no mask. */
+typedef struct {
+  int32_t n_rows, vocab, dtype, n_masks;
+  const void *in;
+  void *out;
+  int64_t in_stride, out_stride, mask_stride;
+  const int32_t *row_start;
+  const int32_t *path_token;
+  const uint64_t *path_mask;
+  const uint32_t *allowed;
+  const int32_t *allowed_row;
+} eagle_logits;
+int eagle_apply_logit_rules(const eagle_logits *logits, const eagle_logit_rules *rules, void *hip_stream);
+
 const char *eagle_last_error(void);   /* thread-local text of the last failure */
 const char *eagle_version(void);
 

@@ -30,7 +30,8 @@ EXPORTS = ["eagle_workspace_bytes", "eagle_init", "eagle_free", "eagle_load_weig
            "eagle_draft_tree", "eagle_verify", "eagle_accept", "eagle_accept_static", "eagle_step", "eagle_vanilla_step", "eagle_generate",
            "eagle_set_hint", "eagle_set_page_table", "eagle_set_buffer", "eagle_force_tree", "eagle_expand_level",
            "eagle_force_accept", "eagle_get_buffer", "eagle_get_kv_row", "eagle_set_profiling", "eagle_get_profile", "eagle_get_kernel_stats", "eagle_probe_stream_read",
-           "eagle_head_loss", "eagle_feature_noise", "eagle_last_error", "eagle_version"]
+           "eagle_head_loss", "eagle_feature_noise", "eagle_rope_plan_init", "eagle_rope", "eagle_chunk_attention_workspace", "eagle_chunk_attention",
+           "eagle_apply_logit_rules", "eagle_last_error", "eagle_version"]
 
 
 class EagleConfig(ctypes.Structure):
@@ -108,6 +109,9 @@ def load_library(need_gpu_runtime: bool = True):
     lib.eagle_probe_stream_read.argtypes = [vp, sz, i32, vp, ctypes.POINTER(ctypes.c_double)]
     lib.eagle_head_loss.argtypes = [vp, vp, vp, i32, ctypes.c_float, vp, ctypes.POINTER(ctypes.c_float)]
     lib.eagle_feature_noise.argtypes = [vp, vp, vp, i32, ctypes.c_float, ctypes.c_uint64, ctypes.c_uint64]
+    if need_gpu_runtime:
+        from . import operators
+        operators.declare(lib)
     lib.eagle_last_error.restype = ctypes.c_char_p
     lib.eagle_version.restype = ctypes.c_char_p
     _lib = lib
@@ -397,3 +401,12 @@ class Eagle:
         self._chk(self.lib.eagle_get_kernel_stats(self.h, phase, arr, 16, ctypes.byref(n), int(reset)))
         return [{"name": arr[i].name.decode(), "kernel": arr[i].kernel.decode(), "ms": arr[i].ms,
                  "launches": int(arr[i].launches), "bytes": arr[i].bytes} for i in range(n.value)]
+
+
+def __getattr__(name):
+    """The operators on the caller's own tensors live in `operators`, which imports torch; their names are this package's too."""
+    if name in ("operators", "Chunk", "PagedKV", "LogitRules", "rope_plan", "rope", "chunk_attention", "chunk_attention_workspace", "apply_logit_rules"):
+        import importlib
+        mod = importlib.import_module(__name__ + ".operators")
+        return mod if name == "operators" else getattr(mod, name)
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

@@ -1,12 +1,13 @@
 """Build libeagle.so (hipcc, gfx950) in-tree."""
 import os
 import subprocess
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libeagle.so")
-SOURCES = ["eagle.hip"]
-HEADERS = ["kernels.h", "kernels2.h", "plans.h", "common.h", os.path.join("..", "..", "include", "eagle.h")]
+SOURCES = ["eagle.hip", "operators.hip"]
+HEADERS = ["kernels.h", "kernels2.h", "plans.h", "common.h", "host.h", "rows.h", "rope.h", "chunk_attn.h", "logit_rules.h", os.path.join("..", "..", "include", "eagle.h")]
 
 
 def needs_build() -> bool:
@@ -20,17 +21,21 @@ def build(force: bool = True, verbose: bool = False) -> str:
     """Compile every HIP source for gfx950 into libeagle.so.  Raises on failure."""
     if not force and not needs_build():
         return LIB
-    cmd = ["hipcc", "--offload-arch=gfx950", "-O3", "-std=c++17", "-shared", "-fPIC",
-           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-           "-Wno-unused-result", "-Wno-unused-command-line-argument",
-           *[os.path.join(CSRC, s) for s in SOURCES], "-o", LIB]
-    res = subprocess.run(cmd, capture_output=True, text=True)
+    flags = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+             "-Wno-unused-result", "-Wno-unused-command-line-argument"]
     noise = "is not a recognized feature for this target"
-    err = "\n".join(l for l in res.stderr.splitlines() if noise not in l)
-    if verbose or res.returncode:
-        print(err)
-    if res.returncode:
-        raise RuntimeError("hipcc failed:\n" + err)
+    with tempfile.TemporaryDirectory() as tmp:
+        objects = [os.path.join(tmp, s + ".o") for s in SOURCES]
+        jobs = [subprocess.Popen(["hipcc", *flags, "-c", os.path.join(CSRC, s), "-o", o], stderr=subprocess.PIPE, text=True) for s, o in zip(SOURCES, objects)]
+        for source, job in zip(SOURCES, jobs):
+            err = "\n".join(l for l in job.communicate()[1].splitlines() if noise not in l)
+            if verbose or job.returncode:
+                print(err)
+            if job.returncode:
+                raise RuntimeError(f"hipcc failed on {source}:\n" + err)
+        res = subprocess.run(["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", *objects, "-o", LIB], capture_output=True, text=True)
+        if res.returncode:
+            raise RuntimeError("hipcc failed to link:\n" + res.stderr)
     return LIB
 
 

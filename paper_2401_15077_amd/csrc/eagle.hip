@@ -1,6 +1,6 @@
 // libeagle: host side -- context, workspace layout, weight loading, and the orchestration of one EAGLE
 // speculative step (drafting: Sec. 3.1 / App. A.1; verification: Sec. 3.3; acceptance: Sec. 2 / App. A.2).
-#include "../../include/eagle.h"
+#include "host.h"
 #include "kernels.h"
 #include "kernels2.h"
 #include "plans.h"
@@ -16,19 +16,13 @@
 #include <mutex>
 
 static thread_local char g_err[512] = "";
-static int fail(int code, const char* fmt, ...) {
+int fail(int code, const char* fmt, ...) {
   va_list ap;
   va_start(ap, fmt);
   vsnprintf(g_err, sizeof(g_err), fmt, ap);
   va_end(ap);
   return code;
 }
-#define HIPCHK(x)                                                                                         \
-  do {                                                                                                    \
-    hipError_t e_ = (x);                                                                                  \
-    if (e_ != hipSuccess) return fail(EAGLE_EHIP, "%s failed: %s (%s:%d)", #x, hipGetErrorString(e_), __FILE__, __LINE__); \
-  } while (0)
-#define LAUNCH_CHECK() HIPCHK(hipGetLastError())
 
 // ---------------------------------------------------------------------------- static device scratch
 // Scratch of eagle_accept_static(): a fixed array in the code object instead of caller-provided memory, for callers

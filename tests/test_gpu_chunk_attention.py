@@ -1,0 +1,217 @@
+"""Attention of a chunk of new tokens over a paged cache against the oracle in 64 bits.
+
+Tolerances.  u = 2^-24.  fp32 queries: a score is a sum of up to 128 products, added up in 16s by pieces of 8 bits (six products of pieces, eight blocks: at most 64 roundings of
+partial sums that are at most B = scale * sum |q k|), so it is off by 64 u B, and 4 u of itself from scale, cap and slopes.  exp turns that into a relative error of a weight; sums over T tokens
+round T / 8 times at most.  So the output is off by (2 * (64 u B + 4 u (B + C)) + (T / 8 + 32) u) * A: A the weighted mean of |v|, C the largest cap or slope term.  bf16 queries: every weight rounds
+to bf16 (2^-8 A), and the result once more (2^-8 of itself); scores as above."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import operators as ref
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U = 2.0 ** -24
+TYPES = {"fp32": torch.float32, "bf16": torch.bfloat16}
+
+
+def pkg():
+    import paper_2401_15077_amd
+    return paper_2401_15077_amd
+
+
+def i32(a):
+    return torch.tensor(np.asarray(a), dtype=torch.int32, device=DEV)
+
+
+def tree(n, rng):
+    masks, depth = [1], [0]
+    for v in range(1, n):
+        p = int(rng.choice([u for u in range(v) if depth[u] < 15]))
+        masks.append(masks[p] | 1 << v)
+        depth.append(depth[p] + 1)
+    return masks
+
+
+def signed(m):
+    return [x - (1 << 64) if x >> 63 else x for x in m]
+
+
+def bound(want, mean, big, count, dtype, extra):
+    tol = (2 * (64 * U * big + 4 * U * (big + extra)) + (count[:, None] / 8 + 32) * U)[:, :, None] * mean + 1e-30
+    if dtype == torch.bfloat16:
+        tol = tol + 2.0 ** -8 * 1.001 * (mean + np.abs(want))
+    return tol
+
+
+def run(rows, keys, H, KVH, D, types, page, *, softcap=0.0, window=0, slopes=False, prefix=None, masks=None, base=None, scale=None, seed=0, poison=False, gap=()):
+    """One call against the oracle; masks: tree bits of all rows.  gap: (sequence, page number) pairs that are not there."""
+    p = pkg()
+    dtype, cdtype = (TYPES[t] for t in types.split("/"))
+    gen = torch.Generator(device=DEV).manual_seed(seed + 3)
+    R, S = sum(rows), len(rows)
+    need = [max(1, -(-k // page)) for k in keys]
+    n_pages = sum(need) + 2
+    order = np.random.default_rng(seed).permutation(n_pages).tolist()
+    table = np.full((S, max(need) + 1), -7, np.int32)
+    for s, n in enumerate(need):
+        table[s, :n] = [order.pop() for _ in range(n)]
+    for s, g in gap:
+        table[s, g] = n_pages + g if g % 2 else -1
+    kc, vc = (torch.randn(n_pages, KVH, page, D, device=DEV, generator=gen).to(cdtype) for _ in range(2))
+    if poison:                                                    # what no sequence owns holds NaN
+        owned = torch.zeros(n_pages, page, dtype=torch.bool, device=DEV)
+        for s, k in enumerate(keys):
+            for t in range(k):
+                if 0 <= table[s, t // page] < n_pages:
+                    owned[table[s, t // page], t % page] = True
+        for c in (kc, vc):
+            c.masked_fill_(~owned[:, None, :, None], float("nan"))
+    q = (torch.randn(R, H, D, device=DEV, generator=gen) * 1.5).to(dtype)
+    sl = torch.tensor(2.0 ** (-8.0 * np.arange(1, H + 1) / H), dtype=torch.float32, device=DEV) if slopes else None
+    start = np.cumsum([0] + list(rows))
+    tm = None if masks is None else torch.tensor(signed(masks), dtype=torch.int64, device=DEV)
+    chunk = p.Chunk(i32(start), i32(keys), R, max(max(rows), 1), max(keys) + 5, tree_base=None if base is None else i32(base), tree_mask=tm)
+    kv = p.PagedKV(kc, vc, i32(table))
+    out = torch.full_like(q, 5.0)
+    p.chunk_attention(q, kv, chunk, scale=scale, softcap=softcap, slopes=sl, window=window, prefix=None if prefix is None else i32(prefix), out=out)
+    torch.cuda.synchronize()
+    facts = ref.chunk_rows(start, keys, base, masks)
+    sc = D ** -0.5 if scale is None else scale
+    want, mean, big, count = ref.attention(q.double().cpu().numpy(), kc.double().cpu().numpy(), vc.double().cpu().numpy(), table, facts, R, keys, page=page, scale=sc, softcap=softcap,
+                                           slopes=None if sl is None else sl.double().cpu().numpy(), window=window, prefix=prefix, tree_base=base)
+    extra = softcap + (max(keys) * float(sl.max()) if slopes else 0.0)
+    got = out.double().cpu().numpy()
+    err = np.abs(got - want) / bound(want, mean, big, count, dtype, extra)
+    print(f"rows {rows} keys {keys} {types} worst {err.max():.3f} of the bound, rel {np.linalg.norm(got - want) / max(np.linalg.norm(want), 1e-30):.2e}", flush=True)
+    assert err.max() <= 1.0
+    assert (got[count == 0] == 0.0).all()
+    return q, kv, chunk, out, (kc, vc, table)
+
+
+ALL = ["fp32/fp32", "fp32/bf16", "bf16/bf16"]
+
+
+@pytest.mark.parametrize("types", ALL)
+@pytest.mark.parametrize("rows,keys,H,KVH,D,page", [
+    ([1], [1], 4, 4, 64, 64), ([1], [2], 1, 1, 8, 1), ([1], [31], 4, 2, 128, 16), ([1], [33], 8, 1, 128, 32), ([1], [701], 32, 32, 128, 64), ([1], [1500], 5, 5, 80, 64),
+    ([1, 1, 1], [64, 1, 129], 8, 2, 32, 32), ([2, 1, 5], [65, 700, 5], 6, 3, 40, 8), ([7], [7], 4, 4, 128, 64), ([33], [33], 2, 2, 64, 32), ([5, 40], [300, 40], 8, 2, 128, 16),
+    ([130], [200], 3, 1, 96, 64), ([257], [257], 2, 2, 128, 64), ([64, 1, 0, 3], [500, 90, 20, 3], 16, 2, 128, 128), ([1], [2100], 64, 8, 128, 256), ([20], [600], 12, 1, 72, 2),
+])
+def test_causal(rows, keys, H, KVH, D, page, types):
+    run(rows, keys, H, KVH, D, types, page, poison=True)
+
+
+@pytest.mark.parametrize("types", ALL)
+@pytest.mark.parametrize("nodes,base,H,KVH,D", [([26], [674], 8, 8, 128), ([26, 8, 1], [100, 0, 63], 8, 2, 64), ([64], [65], 4, 1, 128), ([63, 40], [31, 300], 4, 4, 32)])
+def test_trees(nodes, base, H, KVH, D, types):
+    rng = np.random.default_rng(sum(nodes))
+    masks = [m for n in nodes for m in tree(n, rng)]
+    run(nodes, [b + n for b, n in zip(base, nodes)], H, KVH, D, types, 64, masks=masks, base=base, poison=True)
+
+
+@pytest.mark.parametrize("types", ALL)
+def test_tree_level_rows_of_some_nodes(types):
+    rng = np.random.default_rng(5)
+    t = [tree(26, rng), tree(15, rng)]
+    masks = [t[0][u] for u in (1, 2, 5, 9)] + [t[1][u] for u in (3, 4)]
+    run([4, 2], [126, 45], 8, 2, 64, types, 32, masks=masks, base=[100, 30], poison=True)
+    run([4, 2], [126, 45], 8, 2, 64, types, 32, masks=masks, base=[100, 30], window=4, slopes=True, softcap=5.0, prefix=[7, 200])
+
+
+@pytest.mark.parametrize("types", ALL)
+@pytest.mark.parametrize("mods", [dict(softcap=3.0), dict(slopes=True), dict(window=1), dict(window=17), dict(window=100), dict(prefix=[40, 0]), dict(prefix=[300, 2]),
+                                  dict(window=33, prefix=[5, 70], softcap=20.0, slopes=True), dict(scale=0.3), dict(scale=-0.2), dict(scale=0.0), dict(window=400)], ids=str)
+@pytest.mark.parametrize("rows,keys", [([1, 1], [300, 77]), ([50, 9], [300, 77]), ([150, 64], [260, 64])])
+def test_modified_scores_and_masks(rows, keys, mods, types):
+    run(rows, keys, 8, 2, 64, types, 32, **mods)
+
+
+@pytest.mark.parametrize("types", ALL)
+@pytest.mark.parametrize("rows", [[1, 1, 2], [40, 3, 2]])
+def test_pages_that_are_not_there_and_rows_that_see_nothing(rows, types):
+    # sequence 0 lacks two pages, sequence 2 all it has: zeros
+    run(rows, [200, 64, 20], 8, 2, 64, types, 32, gap=[(0, 1), (0, 4), (2, 0)], poison=True)
+    # a window that ends on a missing page leaves the last rows nothing
+    run(rows, [200, 64, 20], 8, 2, 64, types, 32, gap=[(0, 5), (0, 6), (1, 1)], window=1, poison=True)
+
+
+@pytest.mark.parametrize("types", ALL)
+@pytest.mark.parametrize("rows,keys,H", [([40], [100], 4), ([6], [50], 4), ([200], [200], 2)])
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
+def test_what_a_row_does_not_see_does_not_reach_it(rows, keys, H, value, types):
+    """Keys and values of the newer tokens are not finite: rows in front of them are as they were, bit for bit; rows that see one get what is not finite."""
+    p = pkg()
+    q, kv, chunk, out, (kc, vc, table) = run(rows, keys, H, H, 64, types, 32)
+    n, K = rows[0], keys[0]
+    for c, name in ((vc, "v"), (kc, "k")):
+        old = c.clone()
+        first = n // 2                                            # row whose token is spoilt, and a later one
+        for i in (first, n - 1):
+            t = K - n + i
+            c[table[0, t // 32], :, t % 32, 3] = value
+        got = p.chunk_attention(q, kv, chunk)
+        assert torch.equal(got[:first], out[:first]), name
+        seen = got[first:] if name == "k" else got[first:, :, 3]
+        if name == "v":
+            assert not torch.isfinite(seen).any()
+            if value != value or n - 1 == first:
+                assert torch.isnan(seen).all() == (value != value)
+            else:
+                assert torch.equal(seen[0].float(), torch.full_like(seen[0].float(), value))
+            rest = [e for e in range(64) if e != 3]
+            assert torch.equal(got[:, :, rest], out[:, :, rest])
+        elif value != value:
+            assert torch.isnan(seen).all()
+        c.copy_(old)
+
+
+def test_strides_orders_and_rows_of_no_sequence():
+    p = pkg()
+    q, kv, chunk, out, (kc, vc, table) = run([3, 9], [50, 70], 4, 2, 64, "bf16/bf16", 16)
+    # queries and outputs as views of larger tensors, a cache laid out [page][token][head][dim], a table with longer rows
+    big = torch.zeros(12, 7, 64, dtype=torch.bfloat16, device=DEV)
+    view = big[:, 2:6]
+    view.copy_(q)
+    kt, vt = kc.transpose(1, 2).contiguous().transpose(1, 2), vc.transpose(1, 2).contiguous().transpose(1, 2)
+    wide = torch.full((2, table.shape[1] + 3), 0, dtype=torch.int32, device=DEV)
+    wide[:, :table.shape[1]] = i32(table)
+    kv2 = p.PagedKV(kt, vt, wide[:, :table.shape[1]])
+    obig = torch.full((12, 4, 72), 3.0, dtype=torch.bfloat16, device=DEV)
+    p.chunk_attention(view, kv2, chunk, out=obig[:, :, :64])
+    assert torch.equal(obig[:, :, :64], out) and torch.all(obig[:, :, 64:] == 3.0)
+    p.chunk_attention(view, kv2, chunk, out=view)                 # in place
+    assert torch.equal(view, out) and float(big[:, :2].abs().sum()) == 0.0 and float(big[:, 6].abs().sum()) == 0.0
+    # rows in front of the first and behind the last sequence stay as they are
+    q2 = torch.cat([q[:1], q, q[:2]])
+    o2 = torch.full_like(q2, 9.0)
+    chunk2 = p.Chunk(i32([1, 4, 13]), i32([50, 70]), 15, 9, 75)
+    p.chunk_attention(q2, kv, chunk2, out=o2)
+    assert torch.equal(o2[1:13], out) and torch.all(o2[0] == 9.0) and torch.all(o2[13:] == 9.0)
+
+
+@pytest.mark.parametrize("types", ALL)
+def test_the_same_call_gives_the_same_bits(types):
+    p = pkg()
+    q, kv, chunk, out, _ = run([1, 26, 1], [3000, 900, 40], 16, 2, 128, types, 64)
+    ws = torch.empty(p.chunk_attention_workspace(q, kv, chunk), dtype=torch.uint8, device=DEV)
+    for fill in (0, 255, 127):                                    # what the workspace holds does not matter
+        ws.fill_(fill)
+        assert torch.equal(p.chunk_attention(q, kv, chunk, workspace=ws), out)
+
+
+def test_lengths_beyond_what_the_host_said_are_not_read():
+    """key_len and row_start hold more than max_keys / the table / max_rows allow: the surplus is not processed, nothing is read or written out of bounds."""
+    p = pkg()
+    q, kv, chunk, out, _ = run([4], [64], 4, 4, 64, "fp32/fp32", 32)
+    lied = p.Chunk(i32([0, 4]), i32([1 << 30]), 4, 4, 64)
+    p.chunk_attention(q, kv, lied)                                # (the rows' own tokens lie far behind: they see all 64)
+    few = p.Chunk(i32([0, 4]), i32([64]), 4, 2, 64)
+    o = torch.full_like(q, 6.0)
+    p.chunk_attention(q, kv, few, out=o)
+    assert torch.equal(o[:2], out[:2]) and torch.all(o[2:] == 6.0)
+    none = p.Chunk(i32([0, 4]), i32([0]), 4, 4, 64)
+    assert float(p.chunk_attention(q, kv, none).abs().sum()) == 0.0
+    minus = p.Chunk(i32([0, 4]), i32([-5]), 4, 4, 64)
+    assert float(p.chunk_attention(q, kv, minus).abs().sum()) == 0.0
