@@ -1,75 +1,538 @@
 // Attention of a chunk of new tokens over a paged cache.
+//
+// A query head's rows and those of the other heads that share its kv head are COLUMNS of one problem (column c of a sequence: token c / g, head c % g of the group of g): they
+// read the same keys and values.  Scores and outputs are computed transposed on v_mfma_f32_32x32x16_bf16, S^T = K Q^T and O^T = V^T P^T, so a lane owns one column: its running
+// maximum and sum and the rescaling are lane-local, and a score's place in the accumulator is where the second product wants its weight.  One pass over the keys with the running
+// maximum and sum of the softmax; everything but the operands of the matrix instructions is fp32.
+//
+// fp32 operands are exact sums of three bf16 pieces (8 bits each of the 24), and of the nine products of two such sums the six of at least 2^-16 of the largest are kept: what is
+// left out is 2^-24 of a product.  bf16 operands are one piece.  Weights are one piece for bf16 queries (the output rounds by as much) and three for fp32.
+//
+// Two shapes.  WIDE (more than 32 columns a sequence and kv head): four waves of 32 columns share tiles of tokens in LDS.  Narrow: one block of 32 columns, the four waves take every
+// fourth tile and join at the end.  Where sequences, kv heads and column blocks do not fill the chip, the token range is split over work-groups and k_chunk_attn_join adds the parts up.
 #pragma once
 #include "rows.h"
 #include "rope.h"
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 struct ChunkAttnDev {
   const void* q; void* out;
   long long q_row, q_head, out_row, out_head;
   int H, window;
-  float scale, softcap;
+  float scale, softcap;                    // scale >= 0: the sign is q_flip's
+  uint32_t q_flip;                         // 0x8000 in both halves: the queries change sign
   const float* slopes; const int* prefix;
   ChunkDev chunk; PagedDev kv;
+  int col_blocks, splits, split_tiles;     // parts of the token range at most, tiles of one
+  float* part_o; float* part_ml;           // [row][head][split][DH], [row][head][split][maximum, sum]
 };
 
-// A work-group a row and head; a thread a token for the scores, a thread an element for the sums.
-template <typename T, typename CT>
-__global__ __launch_bounds__(256) void k_chunk_attn(const ChunkAttnDev A) {
-  __shared__ float qs[128], ps[256], sh[16];
-  __shared__ long long cell_s[256];
-  const int r = blockIdx.x, h = blockIdx.y, tid = threadIdx.x, dh = A.kv.head_dim;
-  const int s = wave_row_seq(A.chunk.row_start, A.chunk.n_seqs, r);
-  if (s < 0 || r - A.chunk.row_start[s] >= A.chunk.max_rows) return;
-  const int keys = chunk_keys(A.chunk, A.kv, s), kvh = h / (A.H / A.kv.n_kv_heads);
-  const bool tree = A.chunk.tree_mask;
-  const unsigned long long m = tree ? A.chunk.tree_mask[r] : 0;
-  const int base = tree ? A.chunk.tree_base[s] : 0;
-  const int own = tree ? base + __popcll(m) - 1 : A.chunk.key_len[s] - A.chunk.row_start[s + 1] + r;
-  const int prefix = A.prefix ? (tree ? min(A.prefix[s], base) : A.prefix[s]) : 0;
-  if (tid < dh) load_run<1>((const T*)A.q + r * A.q_row + h * A.q_head + tid, qs + tid);
-  __syncthreads();
-  float m_run = -INFINITY, l = 0.f, o = 0.f;
-  for (int j0 = 0; j0 < keys; j0 += 256) {
-    const int j = j0 + tid;
-    float x = -INFINITY;
-    long long cell = -1;
-    if (j < keys) {
-      const int page = token_page(A.kv, s, j);
-      bool seen;
-      int pos = j;
-      if (tree) {
-        const int u = j - base;
-        seen = u < 0 || (u < 64 && (m >> u & 1));
-        if (u >= 0) pos = base + __popcll(m & ((u < 64 ? 1ull << u : 0ull) - 1));
-      } else seen = j <= own;
-      const int dist = own - pos;
-      seen = (seen && (A.window <= 0 || dist < A.window)) || j < prefix;
-      if (seen && page >= 0) {
-        cell = page * A.kv.page_stride + kvh * A.kv.head_stride + (j & ((1 << A.kv.page_shift) - 1)) * A.kv.token_stride;
-        float acc = 0.f;
-        for (int d = 0; d < dh; ++d) { float kx; load_run<1>((const CT*)A.kv.k + cell + d, &kx); acc = fmaf(qs[d], kx, acc); }
-        x = acc * A.scale;
-        if (A.softcap > 0.f) x = A.softcap * tanhf(x / A.softcap);
-        if (A.slopes) x -= A.slopes[h] * (float)abs(dist);
+// What a column block of a sequence has to visit: tiles [0, n_prefix) and from first on, n_tiles in all; and what its rows have in common.
+struct ColumnRange {
+  int row0, n, keys, base, prefix, own0;   // first row, rows, tokens, tokens in front of the tree, prefix, index of row 0
+  bool tree;
+  int n_prefix, first, n_tiles;
+  int full_to, full_from;                  // tokens below full_to are in order for every row, tokens from full_from on inside every row's window
+};
+template <int KT>
+__device__ inline ColumnRange column_range(const ChunkAttnDev& A, int s, int col0, int cols, int g) {
+  ColumnRange c;
+  const int r0 = min(max(0, A.chunk.row_start[s]), A.chunk.n_rows), r1 = min(A.chunk.row_start[s + 1], A.chunk.n_rows);
+  const int n_all = max(0, r1 - r0);
+  c.row0 = r0;
+  c.n = min(n_all, A.chunk.max_rows);
+  c.keys = chunk_keys(A.chunk, A.kv, s);
+  c.tree = A.chunk.tree_mask != nullptr;
+  c.base = c.tree ? max(0, min(A.chunk.tree_base[s], c.keys)) : 0;
+  c.own0 = c.tree ? c.base : min(max(0, A.chunk.key_len[s]), 1 << 30) - n_all;
+  c.prefix = A.prefix ? min(A.prefix[s], c.tree ? c.base : c.keys) : 0;
+  c.prefix = max(0, c.prefix);
+  const int i_lo = col0 / g, i_hi = min(c.n - 1, (col0 + cols - 1) / g);
+  const int own_lo = c.tree ? c.base : c.own0 + i_lo, own_hi = c.tree ? c.base + 63 : c.own0 + i_hi;
+  const int end = min(c.keys, max(own_hi + 1, c.prefix));
+  const int lo = A.window > 0 ? max(0, own_lo - A.window + 1) : 0;
+  c.n_prefix = lo > 0 ? (min(c.prefix, end) + KT - 1) / KT : 0;
+  c.first = max(c.n_prefix, lo / KT);
+  c.n_tiles = i_lo >= c.n || end <= 0 ? 0 : c.n_prefix + max(0, (end + KT - 1) / KT - c.first);
+  c.full_to = min(c.keys, max(c.tree ? c.base : own_lo + 1, c.prefix));
+  c.full_from = A.window > 0 ? own_hi - A.window + 1 : 0;
+  return c;
+}
+
+__device__ __forceinline__ uint64_t low_ones(int n) { return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1ull; }
+
+// x as an exact sum of bf16 pieces; what is not finite stays in the first.
+template <int NP> __device__ __forceinline__ void pieces8(const float* x, bf16x8* p) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    p[0][i] = (__bf16)x[i];
+    if constexpr (NP == 3) {
+      float r = x[i] - (float)p[0][i];
+      p[1][i] = (__bf16)r;
+      r -= (float)p[1][i];
+      p[2][i] = (__bf16)r;
+    }
+  }
+}
+__device__ __forceinline__ bool not_finite(float x) { return (__builtin_bit_cast(uint32_t, x) & 0x7F800000u) == 0x7F800000u; }
+__device__ __forceinline__ bool pair_not_finite(uint32_t w) { return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u; }
+
+// Eight elements of a token in flight, and their pieces.
+template <typename CT> struct Raw8;
+template <> struct Raw8<bf16_t> {
+  u32x4 v;
+  __device__ __forceinline__ void load(const bf16_t* p) { v = *(const u32x4*)p; }
+  __device__ __forceinline__ void zero() { v = u32x4{0, 0, 0, 0}; }
+  __device__ __forceinline__ bool bad() const { return pair_not_finite(v.x) || pair_not_finite(v.y) || pair_not_finite(v.z) || pair_not_finite(v.w); }
+  __device__ __forceinline__ void split(bf16x8* p) const { p[0] = __builtin_bit_cast(bf16x8, v); }
+};
+template <> struct Raw8<float> {
+  f32x4 a, b;
+  __device__ __forceinline__ void load(const float* p) { a = *(const f32x4*)p; b = *(const f32x4*)(p + 4); }
+  __device__ __forceinline__ void zero() { a = b = f32x4{0.f, 0.f, 0.f, 0.f}; }
+  __device__ __forceinline__ bool bad() const {
+    bool r = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r = r || not_finite(a[i]) || not_finite(b[i]);
+    return r;
+  }
+  __device__ __forceinline__ void split(bf16x8* p) const {
+    const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    pieces8<3>(x, p);
+    if (bad()) {                                                  // (inf - inf in the later pieces)
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (not_finite(x[i])) { p[1][i] = (__bf16)0.f; p[2][i] = (__bf16)0.f; }
+    }
+  }
+};
+
+// Where 16 bytes (8 elements, piece c) of token t lie in a tile in LDS, in units of 8 elements.  Keys are read a token a lane: eight consecutive tokens' pieces lie in eight different
+// 16-byte columns.  Values are read transposed, four tokens by 64 bytes at a time: those lie in four different 64-byte columns.
+template <int DH> __device__ __forceinline__ int k_place(int t, int c) { return t * (DH / 8) + (c ^ (t & 7)); }
+template <int DH> __device__ __forceinline__ int v_place(int t, int c) { return t * (DH / 8) + (c ^ (DH == 128 ? (t & 3) << 2 : (t & 2) << 1)); }
+
+__device__ __forceinline__ s16x4 read_transposed(const bf16_t* p) {   // lane l of 16 gets element l of the four 16-element rows whose l / 4-th this address is in
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(uintptr_t)(p));
+}
+
+template <typename T, typename CT, int DH_, bool WIDE_, bool MODS_>
+struct ChunkAttn {
+  static constexpr int DH = DH_, NQ = sizeof(T) == 4 ? 3 : 1, NK = sizeof(CT) == 4 ? 3 : 1, NP = NQ > NK ? NQ : NK;
+  static constexpr bool WIDE = WIDE_, MODS = MODS_;
+  static constexpr int KT = WIDE && NK == 1 ? 64 : 32, KB = KT / 32, KSN = DH / 16, DB = DH / 32;
+  static constexpr int COLS = WIDE ? 128 : 32;
+  static constexpr int TILE = KT * DH;                            // elements of a piece of a tile
+  static constexpr int BUFS = WIDE ? 2 : 1;
+  static constexpr int K_ELTS = WIDE ? BUFS * NK * TILE : 0, V_ELTS = (WIDE ? BUFS : 4) * NK * TILE;
+  static constexpr size_t JOIN = WIDE ? 0 : (size_t)2 * (16 * DB + 2) * 64 * 4;
+  static constexpr size_t TILES = (size_t)(K_ELTS + V_ELTS) * 2;
+  static constexpr size_t LDS = TILES > JOIN ? TILES : JOIN;
+  static constexpr int WAVES = LDS > 80 * 1024 ? 1 : 2;           // a SIMD holds
+  static constexpr int GROUP = WIDE ? 256 : 64;                   // threads that fetch a tile together
+  static constexpr int ITEMS = KT * DH / 8 / GROUP;               // runs of 8 elements a thread fetches of the values (and of the keys if they go through LDS)
+};
+
+template <typename P, typename T, typename CT>
+__global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev A) {
+  constexpr int DH = P::DH, NQ = P::NQ, NK = P::NK, NP = P::NP, KT = P::KT, KB = P::KB, KSN = P::KSN, DB = P::DB, COLS = P::COLS, TILE = P::TILE, ITEMS = P::ITEMS;
+  constexpr bool WIDE = P::WIDE, MODS = P::MODS;
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem_c[];
+  __shared__ int s_bad[2];                                        // WIDE: number of the last tile in a buffer whose values are not all finite
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane & 31, hh = lane >> 5;
+  const int kvh = blockIdx.x % A.kv.n_kv_heads, part = blockIdx.x / A.kv.n_kv_heads, s = blockIdx.y, g = A.H / A.kv.n_kv_heads, dh = A.kv.head_dim;
+  const int cb = A.col_blocks - 1 - part % A.col_blocks, split = part / A.col_blocks;   // (blocks of the last rows see most: first)
+  const int col0 = cb * COLS;
+  const ColumnRange R = column_range<KT>(A, s, col0, COLS, g);
+  if (col0 >= R.n * g) return;
+  const int t_begin = split * A.split_tiles, t_end = min(R.n_tiles, t_begin + A.split_tiles);
+  if (t_begin >= t_end && split > 0) return;
+  const bool whole = R.n_tiles <= A.split_tiles;
+
+  // this lane's column
+  const int wave_col = col0 + (WIDE ? 32 * w : 0);
+  const int col = wave_col + q, tok_i = min(col / g, R.n - 1), head = kvh * g + col % g;
+  const bool live = col < R.n * g;
+  const int row = R.row0 + tok_i;
+  unsigned long long tmask = 0;
+  int own = R.own0 + tok_i;                                       // position (and, for consecutive tokens, index)
+  if (R.tree) {
+    tmask = A.chunk.tree_mask[row];
+    own = R.base + __popcll(tmask) - 1;
+  }
+  unsigned long long tnear = tmask;                               // nodes of the path inside the window
+  if (R.tree && A.window > 0) for (int i = __popcll(tmask) - A.window; i > 0; --i) tnear &= tnear - 1;
+  const float slope = MODS && A.slopes ? A.slopes[head] * 1.44269504088896341f : 0.f;
+
+  bf16x8 qf[NQ][KSN];
+  {
+    const T* qp = (const T*)A.q + row * A.q_row + head * A.q_head;
+#pragma unroll
+    for (int ks = 0; ks < KSN; ++ks) {
+      const int d = 16 * ks + 8 * hh;
+      Raw8<T> x;
+      x.zero();
+      if (live && d < dh) x.load(qp + d);
+      bf16x8 p[3];
+      x.split(p);
+#pragma unroll
+      for (int i = 0; i < NQ; ++i) qf[i][ks] = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, p[i]) ^ A.q_flip);
+    }
+  }
+
+  bf16_t* k_lds = (bf16_t*)smem_c;
+  bf16_t* v_lds = k_lds + P::K_ELTS + (WIDE ? 0 : w * NK * TILE);
+  if constexpr (WIDE) {
+    if (tid < 2) s_bad[tid] = -1;
+    __syncthreads();
+  }
+
+  // tile number -> first token
+  auto tile_token = [&](int it) { return (it < R.n_prefix ? it : it - R.n_prefix + R.first) * KT; };
+  // page of token k0 + lane (KT 32: lane % 32) of a tile, -1: not there or behind the last
+  auto pages_of = [&](int it) -> int {
+    const int t = tile_token(it) + (lane & (KT - 1));
+    return it < t_end && t < R.keys ? token_page(A.kv, s, t) : -1;
+  };
+  constexpr int STEP = WIDE ? 1 : 4;
+  Raw8<CT> kr[WIDE ? ITEMS : KSN], vr[ITEMS];
+  const int g_tid = WIDE ? tid : lane;
+  auto fetch = [&](int it, int pages) {
+    const int k0 = tile_token(it);
+    const int in_page = (1 << A.kv.page_shift) - 1;
+    const CT *kb = (const CT*)A.kv.k + kvh * A.kv.head_stride, *vb = (const CT*)A.kv.v + kvh * A.kv.head_stride;
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+      const int item = i * P::GROUP + g_tid, t = item / (DH / 8), c = item % (DH / 8);
+      const int page = __shfl(pages, t, 64);
+      const bool ok = page >= 0 && c * 8 < dh;
+      const long long at = page * A.kv.page_stride + ((k0 + t) & in_page) * A.kv.token_stride + c * 8;
+      if constexpr (WIDE) { kr[i].zero(); if (ok) kr[i].load(kb + at); }
+      vr[i].zero();
+      if (ok) vr[i].load(vb + at);
+    }
+    if constexpr (!WIDE) {
+      const int page = pages;                                     // (KT = 32: the lane's own token)
+      const long long at = page * A.kv.page_stride + ((k0 + q) & in_page) * A.kv.token_stride;
+#pragma unroll
+      for (int ks = 0; ks < KSN; ++ks) {
+        const int d = 16 * ks + 8 * hh;
+        kr[ks].zero();
+        if (page >= 0 && d < dh) kr[ks].load(kb + at + d);
       }
     }
-    float mx = x;
-    for (int i = 32; i; i >>= 1) mx = fmaxf(mx, __shfl_xor(mx, i, 64));
+  };
+  // the fetched tile to LDS; returns whether a value is not finite (to this thread's knowledge)
+  auto put = [&](int buf) -> bool {
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+      const int item = i * P::GROUP + g_tid, t = item / (DH / 8), c = item % (DH / 8);
+      bf16x8 p[3];
+      if constexpr (WIDE) {
+        kr[i].split(p);
+#pragma unroll
+        for (int j = 0; j < NK; ++j) *(bf16x8*)(k_lds + (buf * NK + j) * TILE + 8 * k_place<DH>(t, c)) = p[j];
+      }
+      vr[i].split(p);
+      bad = bad || vr[i].bad();
+#pragma unroll
+      for (int j = 0; j < NK; ++j) *(bf16x8*)(v_lds + (buf * NK + j) * TILE + 8 * v_place<DH>(t, c)) = p[j];
+    }
+    return bad;
+  };
+
+  const float c2 = MODS ? 1.44269504088896341f : A.scale * 1.44269504088896341f;   // scores to powers of two
+  const float cap2 = MODS && A.softcap > 0.f ? 2.f * 1.44269504088896341f / A.softcap : 0.f;
+  float m_run = -INFINITY, l_run = 0.f;                           // maximum (in powers of two) of the column, sum of this lane's half of the tokens
+  f32x16 oacc[DB];
+#pragma unroll
+  for (int b = 0; b < DB; ++b)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) oacc[b][r] = 0.f;
+
+  int it = t_begin + (WIDE ? 0 : w);
+  int pages = pages_of(it);
+  bool bad = false;
+  if (it < t_end) fetch(it, pages);
+  int pages_next = pages_of(it + STEP);
+  if constexpr (WIDE) {
+    if (it < t_end && __any(put(0)) && lane == 0) s_bad[0] = it;
     __syncthreads();
-    if ((tid & 63) == 0) sh[tid >> 6] = mx;
-    __syncthreads();
-    const float m_new = fmaxf(m_run, fmaxf(fmaxf(sh[0], sh[1]), fmaxf(sh[2], sh[3])));
-    const float p = cell >= 0 ? expf(x - (m_new > -INFINITY ? m_new : 0.f)) : 0.f;
-    const float f = m_run > -INFINITY ? expf(m_run - m_new) : 0.f;
-    ps[tid] = p; cell_s[tid] = cell;
-    __syncthreads();
-    m_run = m_new;
-    l *= f; o *= f;
-    for (int i = 0; i < 256; ++i)
-      if (cell_s[i] >= 0) {
-        l += ps[i];
-        if (tid < dh) { float v; load_run<1>((const CT*)A.kv.v + cell_s[i] + tid, &v); o = fmaf(ps[i], v, o); }
+  }
+  for (int step = 0; it < t_end; it += STEP, ++step) {
+    const int buf = WIDE ? step & 1 : 0, k0 = tile_token(it);
+    const uint64_t there = __ballot(pages >= 0) & low_ones(KT);
+    bf16x8 kf[NK];
+    f32x16 sacc[KB];
+    if constexpr (WIDE) {
+      if (it + 1 < t_end) fetch(it + 1, pages_next);
+      bad = s_bad[buf] == it;
+    } else {
+      bad = __any(put(0));
+    }
+#pragma unroll
+    for (int a = 0; a < KB; ++a) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sacc[a][r] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < KSN; ++ks) {
+        if constexpr (WIDE) {
+#pragma unroll
+          for (int j = 0; j < NK; ++j) kf[j] = *(const bf16x8*)(k_lds + (buf * NK + j) * TILE + 8 * k_place<DH>(32 * a + q, 2 * ks + hh));
+        } else {
+          bf16x8 p[3];
+          kr[ks].split(p);
+#pragma unroll
+          for (int j = 0; j < NK; ++j) kf[j] = p[j];
+        }
+#pragma unroll
+        for (int sum = NP - 1; sum >= 0; --sum)                   // small products first
+#pragma unroll
+          for (int i = 0; i < NQ; ++i)
+            if (sum - i >= 0 && sum - i < NK) sacc[a] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[sum - i], qf[i][ks], sacc[a], 0, 0, 0);
+      }
+    }
+    if constexpr (!WIDE) {
+      if (it + STEP < t_end) fetch(it + STEP, pages_next);        // (the keys' registers are free now)
+    }
+    const int pages_now = pages_next;
+    pages_next = pages_of(it + 2 * STEP);
+    // cap and slopes
+    if constexpr (MODS) {
+#pragma unroll
+      for (int a = 0; a < KB; ++a)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          float x = sacc[a][r] * A.scale;
+          if (A.softcap > 0.f) {
+            const float e = __builtin_amdgcn_exp2f(x * cap2);     // e^(2 x / cap); tanh = 1 - 2 / (e + 1)
+            float th = 1.f - 2.f * __builtin_amdgcn_rcpf(e + 1.f);
+            if constexpr (NQ == 3) {                              // fp32: near 0 that cancels; the Taylor polynomial to y^13 is within 10^-9 below 0.35
+              const float y = x / A.softcap, z = y * y;
+              float t = 3.59212803657248102e-3f;
+              t = fmaf(t, z, -8.86323552990219657e-3f);
+              t = fmaf(t, z, 2.18694885361552028e-2f);
+              t = fmaf(t, z, -5.39682539682539683e-2f);
+              t = fmaf(t, z, 0.133333333333333333f);
+              t = fmaf(t, z, -0.333333333333333333f);
+              t = fmaf(t * z, y, y);
+              th = fabsf(y) < 0.35f ? t : th;
+            }
+            x = A.softcap * th;
+          }
+          sacc[a][r] = x * c2;
+        }
+      if (slope != 0.f || __any(slope != 0.f)) {
+        const bool nodes = R.tree && k0 + KT > R.base;            // (uniform)
+#pragma unroll
+        for (int a = 0; a < KB; ++a)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int j = k0 + 32 * a + 8 * (r >> 2) + 4 * hh + (r & 3);
+            int pos = j;
+            if (nodes && j > R.base) pos = R.base + __popcll(tmask & low_ones(j - R.base));
+            sacc[a][r] = fmaf(-slope, (float)abs(own - pos), sacc[a][r]);
+          }
+      }
+    }
+    // what the column does not see
+    const bool full = k0 + KT <= R.full_to && (k0 >= R.full_from || k0 + KT <= R.prefix) && there == low_ones(KT);
+    if (!full) {
+      uint64_t vis;
+      if (R.tree) {
+        const int sh = k0 - R.base;                               // bit u of the path is token base + u
+        vis = low_ones(-sh) & ~(A.window > 0 ? low_ones(own - A.window + 1 - k0) : 0ull);
+        vis |= sh >= 64 || sh <= -64 ? 0ull : sh >= 0 ? tnear >> sh : tnear << -sh;
+      } else {
+        vis = low_ones(own + 1 - k0);
+        if (A.window > 0) vis &= ~low_ones(own - A.window + 1 - k0);
+      }
+      vis |= low_ones(R.prefix - k0);
+      vis &= there;
+      vis >>= 4 * hh;
+#pragma unroll
+      for (int a = 0; a < KB; ++a)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sacc[a][r] = (uint32_t)(vis >> (32 * a)) >> (8 * (r >> 2) + (r & 3)) & 1u ? sacc[a][r] : -INFINITY;
+    }
+    float top = sacc[0][0];
+#pragma unroll
+    for (int a = 0; a < KB; ++a)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) top = fmaxf(top, sacc[a][r]);
+    top = fmaxf(top, __shfl_xor(top, 32, 64));
+    if constexpr (!MODS) top *= c2;
+    // The maximum moves only when it grows by more than 8 (weights up to 2^8 lose nothing in fp32 or bf16), and lane by lane, so that a column's bits are its own.
+    const bool moved = top > m_run + 8.f || (m_run == -INFINITY && top > -INFINITY);
+    if (__any(moved)) {
+      const float f = moved ? __builtin_amdgcn_exp2f(m_run - top) : 1.f;
+      m_run = moved ? top : m_run;
+      l_run *= f;
+#pragma unroll
+      for (int b = 0; b < DB; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) oacc[b][r] *= f;
+    }
+    const float m_sub = m_run == -INFINITY ? 0.f : m_run;
+    float sum = 0.f;
+#pragma unroll
+    for (int a = 0; a < KB; ++a)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float e = __builtin_amdgcn_exp2f(MODS ? sacc[a][r] - m_sub : fmaf(sacc[a][r], c2, -m_sub));
+        sacc[a][r] = e;
+        sum += e;
+      }
+    l_run += sum;
+#pragma unroll
+    for (int jj = 0; jj < KT / 16; ++jj) {
+      bf16x8 pf[3];
+      {
+        float x[8];
+#pragma unroll
+        for (int t = 0; t < 8; ++t) x[t] = sacc[jj >> 1][8 * (jj & 1) + t];
+        pieces8<NQ>(x, pf);
+      }
+#pragma unroll
+      for (int b = 0; b < DB; ++b) {
+        bf16x8 vf[NK];
+        const int t = 16 * jj + 4 * hh + ((lane & 15) >> 2), c = 4 * b + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+#pragma unroll
+        for (int j = 0; j < NK; ++j) {
+          const bf16_t* vt = v_lds + (buf * NK + j) * TILE + 4 * (lane & 1);
+          const s16x4 lo = read_transposed(vt + 8 * v_place<DH>(t, c)), hi = read_transposed(vt + 8 * v_place<DH>(t + 8, c));
+          typedef short s16x8 __attribute__((ext_vector_type(8)));
+          vf[j] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+        if (bad) {
+          // 0 times what is not finite is not 0: it goes to the columns that see it by counting (NaN, then the infinities), and out of the product.
+          u32x4 v = __builtin_bit_cast(u32x4, vf[0]);
+#pragma unroll 1
+          for (int kind = 0; kind < 3; ++kind) {
+            u32x4 is;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              is[i] = 0;
+#pragma unroll
+              for (int x = 0; x < 2; ++x) {
+                const uint32_t e = v[i] >> (16 * x) & 0xFFFFu;
+                if (kind == 0 ? (e & 0x7FFFu) > 0x7F80u : e == (kind == 1 ? 0x7F80u : 0xFF80u)) is[i] |= 0x3F80u << (16 * x);
+              }
+            }
+            f32x16 hits;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) hits[r] = 0.f;
+            hits = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, is), pf[0], hits, 0, 0, 0);
+            const float add = kind == 0 ? __builtin_nanf("") : kind == 1 ? INFINITY : -INFINITY;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) oacc[b][r] += hits[r] > 0.f ? add : 0.f;
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if ((v[i] & 0x7F80u) == 0x7F80u) v[i] &= 0xFFFF0000u;
+            if ((v[i] & 0x7F800000u) == 0x7F800000u) v[i] &= 0xFFFFu;
+          }
+          vf[0] = __builtin_bit_cast(bf16x8, v);
+        }
+#pragma unroll
+        for (int sum2 = NP - 1; sum2 >= 0; --sum2)
+#pragma unroll
+          for (int i = 0; i < NQ; ++i)
+            if (sum2 - i >= 0 && sum2 - i < NK) oacc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[sum2 - i], pf[i], oacc[b], 0, 0, 0);
+      }
+    }
+    pages = pages_now;
+    if constexpr (WIDE) {
+      if (it + 1 < t_end && __any(put(buf ^ 1)) && lane == 0) s_bad[buf ^ 1] = it + 1;
+      __syncthreads();
+    }
+  }
+  l_run += __shfl_xor(l_run, 32, 64);
+  if constexpr (!WIDE) {
+    // waves 2 and 3 into 0 and 1, then 1 into 0
+    float* st = (float*)smem_c + lane;
+#pragma unroll
+    for (int half = 2; half > 0; half >>= 1) {
+      __syncthreads();
+      float* mine = st + (w & (half - 1)) * (16 * DB + 2) * 64;
+      if (w >= half && w < 2 * half) {
+        mine[0] = m_run; mine[64] = l_run;
+#pragma unroll
+        for (int b = 0; b < DB; ++b)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) mine[(2 + 16 * b + r) * 64] = oacc[b][r];
+      }
+      __syncthreads();
+      if (w < half) {
+        const float m1 = mine[0], m = fmaxf(m_run, m1);
+        const float w0 = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - m), w1 = m1 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m1 - m);
+        l_run = l_run * w0 + mine[64] * w1;
+        m_run = m;
+#pragma unroll
+        for (int b = 0; b < DB; ++b)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) oacc[b][r] = oacc[b][r] * w0 + mine[(2 + 16 * b + r) * 64] * w1;
+      }
+    }
+    if (w > 0) return;
+  }
+  if (!live) return;
+  if (whole) {
+    const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
+    T* o = (T*)A.out + row * A.out_row + head * A.out_head;
+#pragma unroll
+    for (int b = 0; b < DB; ++b)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int d = 32 * b + 8 * i + 4 * hh;
+        if (d >= dh) continue;
+        const float x[4] = {oacc[b][4 * i] * inv, oacc[b][4 * i + 1] * inv, oacc[b][4 * i + 2] * inv, oacc[b][4 * i + 3] * inv};
+        store_run<4>(o + d, x);
+      }
+  } else {
+    const size_t at = ((size_t)row * A.H + head) * A.splits + split;
+    if (hh == 0) { A.part_ml[2 * at] = m_run; A.part_ml[2 * at + 1] = l_run; }
+    float* o = A.part_o + at * DH;
+#pragma unroll
+    for (int b = 0; b < DB; ++b)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float x[4] = {oacc[b][4 * i], oacc[b][4 * i + 1], oacc[b][4 * i + 2], oacc[b][4 * i + 3]};
+        store_run<4>(o + 32 * b + 8 * i + 4 * hh, x);
       }
   }
-  if (tid < dh) { o = l == 0.f ? 0.f : o / l; store_run<1>((T*)A.out + r * A.out_row + h * A.out_head + tid, &o); }
+}
+
+// Adds up the parts of the (row, head) pairs whose tokens were split; a wave a pair.
+template <typename P, typename T>
+__global__ __launch_bounds__(256) void k_chunk_attn_join(const ChunkAttnDev A) {
+  constexpr int DH = P::DH, E = DH / 64;
+  const int row = blockIdx.x, head = blockIdx.y * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63, dh = A.kv.head_dim;
+  if (head >= A.H) return;
+  const int s = wave_row_seq(A.chunk.row_start, A.chunk.n_seqs, row);
+  if (s < 0) return;
+  const int g = A.H / A.kv.n_kv_heads, i = row - max(0, A.chunk.row_start[s]), col = i * g + head % g;
+  const ColumnRange R = column_range<P::KT>(A, s, col / P::COLS * P::COLS, P::COLS, g);
+  if (i >= R.n || R.n_tiles <= A.split_tiles) return;
+  const int n = (R.n_tiles + A.split_tiles - 1) / A.split_tiles;   // at most A.splits
+  const size_t at = ((size_t)row * A.H + head) * A.splits;
+  float m = -INFINITY;
+  for (int k = lane; k < n; k += 64) m = fmaxf(m, A.part_ml[2 * (at + k)]);
+  for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+  float l = 0.f, x[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) x[e] = 0.f;
+  for (int k = 0; k < n; ++k) {
+    const float mk = A.part_ml[2 * (at + k)], f = mk == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mk - m);
+    l = fmaf(f, A.part_ml[2 * (at + k) + 1], l);
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] = mk == -INFINITY ? x[e] : fmaf(f, A.part_o[(at + k) * DH + lane * E + e], x[e]);
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  T* o = (T*)A.out + row * A.out_row + head * A.out_head;
+#pragma unroll
+  for (int e = 0; e < E; ++e)
+    if (lane * E + e < dh) { x[e] *= inv; store_run<1>(o + lane * E + e, x + e); }
 }

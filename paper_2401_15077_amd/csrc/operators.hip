@@ -16,6 +16,7 @@ static bool aligned(const void* p, size_t n) { return (uintptr_t)p % n == 0; }
 static int check_chunk(const eagle_chunk* c, ChunkDev* d) {
   if (!c) return fail(EAGLE_EINVAL, "chunk is null");
   if (c->n_seqs < 1 || c->n_rows < 0 || c->max_rows < 1 || c->max_keys < 1) return fail(EAGLE_EINVAL, "chunk: n_seqs, max_rows and max_keys must be >= 1, n_rows >= 0");
+  if (c->n_rows > 1 << 30 || c->max_rows > 1 << 30 || c->max_keys > 1 << 30) return fail(EAGLE_EINVAL, "chunk: n_rows, max_rows and max_keys must be at most 2^30");
   if (!c->row_start || !c->key_len) return fail(EAGLE_EINVAL, "chunk: row_start or key_len is null");
   if (c->n_rows > 0 && !c->tree_base != !c->tree_mask) return fail(EAGLE_EINVAL, "chunk: tree_base and tree_mask belong together");
   *d = ChunkDev{c->n_seqs, c->n_rows, c->max_rows, c->max_keys, c->row_start, c->key_len, c->tree_base, (const unsigned long long*)c->tree_mask};
@@ -161,14 +162,59 @@ static int check_attention(const eagle_attention_args* a, const eagle_chunk* chu
   if (!aligned(kv->k, 16) || !aligned(kv->v, 16) || kv->page_stride * kelt % 16 || kv->head_stride * kelt % 16 || kv->token_stride * kelt % 16)
     return fail(EAGLE_EINVAL, "attention: the cache's tokens must start on multiples of 16 bytes");
   d->q = a->q; d->out = a->out; d->q_row = a->q_row; d->q_head = a->q_head; d->out_row = a->out_row; d->out_head = a->out_head;
-  d->H = a->n_heads; d->window = a->window; d->scale = a->scale; d->softcap = a->softcap; d->slopes = a->slopes; d->prefix = a->prefix;
+  d->H = a->n_heads; d->window = std::min(a->window, 1 << 30); d->slopes = a->slopes; d->prefix = a->prefix; d->softcap = a->softcap;
+  d->scale = std::fabs(a->scale);
+  d->q_flip = std::signbit(a->scale) ? 0x80008000u : 0u;
   return EAGLE_OK;
+}
+
+// Work-groups that the token range is split for where sequences, kv heads and column blocks are fewer, and the fewest tiles of a part.
+constexpr int ATTN_TARGET_WGS = 2048, ATTN_MIN_TILES = 4;
+
+// Columns and parts of a call; returns the bytes of workspace.
+static size_t plan_attention(ChunkAttnDev* d, int elt, int kv_elt, bool* wide) {
+  const int g = d->H / d->kv.n_kv_heads;
+  const long long cols = (long long)d->chunk.max_rows * g;
+  *wide = cols > 32;
+  const int KT = *wide && kv_elt == 2 ? 64 : 32;
+  d->col_blocks = (int)((cols + (*wide ? 127 : 31)) / (*wide ? 128 : 32));
+  const long long units = (long long)d->col_blocks * d->kv.n_kv_heads * d->chunk.n_seqs, tiles = ((long long)d->chunk.max_keys + KT - 1) / KT;
+  const long long parts = std::max(1ll, std::min(ATTN_TARGET_WGS / units, tiles / ATTN_MIN_TILES));
+  d->split_tiles = (int)((tiles + parts - 1) / parts);
+  d->splits = (int)((tiles + d->split_tiles - 1) / d->split_tiles);
+  if (d->splits == 1) return 256;
+  const size_t pairs = (size_t)d->chunk.n_rows * d->H * d->splits, DH = d->kv.head_dim <= 64 ? 64 : 128;
+  (void)elt;
+  return (pairs * 8 + 255) / 256 * 256 + pairs * DH * 4 + 256;
 }
 
 extern "C" size_t eagle_chunk_attention_workspace(const eagle_attention_args* a, const eagle_chunk* chunk, const eagle_paged_kv* kv) {
   ChunkAttnDev d;
+  bool wide;
   if (check_attention(a, chunk, kv, &d)) return 0;
-  return 256;
+  return plan_attention(&d, elt_of(a->dtype), elt_of(kv->dtype), &wide);
+}
+
+template <typename T, typename CT, int DH, bool WIDE, bool MODS>
+static int launch_attention(const ChunkAttnDev& d, hipStream_t stream) {
+  typedef ChunkAttn<T, CT, DH, WIDE, MODS> P;
+  auto kernel = k_chunk_attn<P, T, CT>;
+  HIPCHK(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)P::LDS));
+  kernel<<<dim3(d.kv.n_kv_heads * d.col_blocks * d.splits, d.chunk.n_seqs), 256, P::LDS, stream>>>(d);
+  LAUNCH_CHECK();
+  if (d.splits > 1) {
+    k_chunk_attn_join<P, T><<<dim3(d.chunk.n_rows, (d.H + 3) / 4), 256, 0, stream>>>(d);
+    LAUNCH_CHECK();
+  }
+  return EAGLE_OK;
+}
+template <typename T, typename CT>
+static int launch_attention(const ChunkAttnDev& d, bool wide, bool mods, hipStream_t stream) {
+  const bool big = d.kv.head_dim > 64;
+#define ATTEND(DH, WIDE) return mods ? launch_attention<T, CT, DH, WIDE, true>(d, stream) : launch_attention<T, CT, DH, WIDE, false>(d, stream)
+  if (big) { if (wide) ATTEND(128, true); else ATTEND(128, false); }
+  if (wide) ATTEND(64, true); else ATTEND(64, false);
+#undef ATTEND
 }
 
 extern "C" int eagle_chunk_attention(const eagle_attention_args* a, const eagle_chunk* chunk, const eagle_paged_kv* kv, void* workspace, size_t workspace_bytes,
@@ -176,16 +222,20 @@ extern "C" int eagle_chunk_attention(const eagle_attention_args* a, const eagle_
   ChunkAttnDev d;
   int rc = check_attention(a, chunk, kv, &d);
   if (rc) return rc;
+  bool wide;
+  const size_t need = plan_attention(&d, elt_of(a->dtype), elt_of(kv->dtype), &wide);
   if (!workspace || !aligned(workspace, 256)) return fail(EAGLE_EINVAL, "attention: workspace must be a 256-byte aligned device pointer");
-  if (workspace_bytes < eagle_chunk_attention_workspace(a, chunk, kv)) return fail(EAGLE_ENOMEM, "attention: workspace of %zu bytes is smaller than the %zu needed", workspace_bytes, eagle_chunk_attention_workspace(a, chunk, kv));
+  if (workspace_bytes < need) return fail(EAGLE_ENOMEM, "attention: workspace of %zu bytes is smaller than the %zu needed", workspace_bytes, need);
   if (chunk->n_rows == 0) return EAGLE_OK;
+  if (d.chunk.n_seqs > 65535 || (long long)d.kv.n_kv_heads * d.col_blocks * d.splits > 0x7FFFFFFF) return fail(EAGLE_EINVAL, "attention: more than 65535 sequences, or too many rows");
+  const size_t pairs = (size_t)d.chunk.n_rows * d.H * d.splits;
+  d.part_ml = (float*)workspace;
+  d.part_o = (float*)((char*)workspace + (pairs * 8 + 255) / 256 * 256);
+  const bool mods = d.softcap > 0.f || d.slopes || d.scale == 0.f;   // (a scale of 0 times a masked score)
   const hipStream_t stream = (hipStream_t)hip_stream;
-  const dim3 grid(chunk->n_rows, a->n_heads);
-  if (a->dtype == EAGLE_BF16) k_chunk_attn<bf16_t, bf16_t><<<grid, 256, 0, stream>>>(d);
-  else if (kv->dtype == EAGLE_BF16) k_chunk_attn<float, bf16_t><<<grid, 256, 0, stream>>>(d);
-  else k_chunk_attn<float, float><<<grid, 256, 0, stream>>>(d);
-  LAUNCH_CHECK();
-  return EAGLE_OK;
+  if (a->dtype == EAGLE_BF16) return launch_attention<bf16_t, bf16_t>(d, wide, mods, stream);
+  if (kv->dtype == EAGLE_BF16) return launch_attention<float, bf16_t>(d, wide, mods, stream);
+  return launch_attention<float, float>(d, wide, mods, stream);
 }
 
 // ---------------------------------------------------------------------------- logit rules
