@@ -76,6 +76,13 @@ template <int NP> __device__ __forceinline__ void pieces8(const float* x, bf16x8
   }
 }
 __device__ __forceinline__ bool not_finite(float x) { return (__builtin_bit_cast(uint32_t, x) & 0x7F800000u) == 0x7F800000u; }
+// Not 0 if one of the eight bf16 numbers is not finite: an exponent of ones carries into the sign's place.
+__device__ __forceinline__ uint32_t exponents(u32x4 v) {
+  uint32_t any = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) any |= (v[e] & 0x7F807F80u) + 0x00800080u;
+  return any & 0x80008000u;
+}
 __device__ __forceinline__ bool pair_not_finite(uint32_t w) { return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u; }
 
 // Eight elements of a token in flight, and their pieces.
@@ -114,32 +121,38 @@ template <int DH> __device__ __forceinline__ int k_place(int t, int c) { return 
 template <int DH> __device__ __forceinline__ int v_place(int t, int c) { return t * (DH / 8) + (c ^ (DH == 128 ? (t & 3) << 2 : (t & 2) << 1)); }
 
 __device__ __forceinline__ s16x4 read_transposed(const bf16_t* p) {   // lane l of 16 gets element l of the four 16-element rows whose l / 4-th this address is in
-  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(uintptr_t)(p));
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p);
 }
 
 template <typename T, typename CT, int DH_, bool WIDE_, bool MODS_>
 struct ChunkAttn {
   static constexpr int DH = DH_, NQ = sizeof(T) == 4 ? 3 : 1, NK = sizeof(CT) == 4 ? 3 : 1, NP = NQ > NK ? NQ : NK;
   static constexpr bool WIDE = WIDE_, MODS = MODS_;
+  // bf16 caches go from memory to LDS without passing through registers (DIRECT); fp32 ones are split into their pieces on the way.  The narrow shape has fp32 keys in registers.
+  static constexpr bool DIRECT = NK == 1, KEYS_IN_LDS = WIDE || DIRECT;
   static constexpr int KT = WIDE && NK == 1 ? 64 : 32, KB = KT / 32, KSN = DH / 16, DB = DH / 32;
   static constexpr int COLS = WIDE ? 128 : 32;
   static constexpr int TILE = KT * DH;                            // elements of a piece of a tile
-  static constexpr int BUFS = WIDE ? 2 : 1;
-  static constexpr int K_ELTS = WIDE ? BUFS * NK * TILE : 0, V_ELTS = (WIDE ? BUFS : 4) * NK * TILE;
-  static constexpr size_t JOIN = WIDE ? 0 : (size_t)2 * (16 * DB + 2) * 64 * 4;
-  static constexpr size_t TILES = (size_t)(K_ELTS + V_ELTS) * 2;
-  static constexpr size_t LDS = TILES > JOIN ? TILES : JOIN;
-  static constexpr int WAVES = LDS > 80 * 1024 ? 1 : 2;           // a SIMD holds
+  static constexpr int OWNERS = WIDE ? 1 : 4;                     // waves with a tile of their own
+  static constexpr int K_ELTS = KEYS_IN_LDS ? OWNERS * NK * TILE : 8, V_ELTS = OWNERS * NK * TILE;   // of one buffer
+  static constexpr bool TWO = WIDE || DIRECT;                     // buffers
+  static constexpr int JOIN = WIDE ? 0 : 2 * (16 * DB + 2) * 64 * 2;   // elements (of 2 bytes) that joining the waves takes
+  static constexpr int V0_ELTS = V_ELTS > JOIN ? V_ELTS : JOIN;
+  static constexpr int LDS = 2 * ((TWO ? 2 : 1) * K_ELTS + V0_ELTS + (TWO ? V_ELTS : 0));
+  static constexpr int WAVES = NK == 3 && DH == 128 ? 1 : 2;      // a SIMD holds (by registers)
   static constexpr int GROUP = WIDE ? 256 : 64;                   // threads that fetch a tile together
   static constexpr int ITEMS = KT * DH / 8 / GROUP;               // runs of 8 elements a thread fetches of the values (and of the keys if they go through LDS)
 };
 
+typedef __attribute__((address_space(3))) bf16_t* lds_ptr;
+
 template <typename P, typename T, typename CT>
 __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev A) {
   constexpr int DH = P::DH, NQ = P::NQ, NK = P::NK, NP = P::NP, KT = P::KT, KB = P::KB, KSN = P::KSN, DB = P::DB, COLS = P::COLS, TILE = P::TILE, ITEMS = P::ITEMS;
-  constexpr bool WIDE = P::WIDE, MODS = P::MODS;
-  extern __shared__ __attribute__((aligned(16))) unsigned char smem_c[];
-  __shared__ int s_bad[2];                                        // WIDE: number of the last tile in a buffer whose values are not all finite
+  constexpr bool WIDE = P::WIDE, MODS = P::MODS, DIRECT = P::DIRECT;
+  // (arrays of their own: the compiler tells reads of one from loads on their way into another)
+  __shared__ __attribute__((aligned(16))) bf16_t k_lds0[P::K_ELTS], k_lds1[P::TWO ? P::K_ELTS : 8], v_lds0[P::V0_ELTS], v_lds1[P::TWO ? P::V_ELTS : 8];
+  __shared__ int s_bad[2];                                        // WIDE, not DIRECT: number of the last tile in a buffer whose values are not all finite
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane & 31, hh = lane >> 5;
   const int kvh = blockIdx.x % A.kv.n_kv_heads, part = blockIdx.x / A.kv.n_kv_heads, s = blockIdx.y, g = A.H / A.kv.n_kv_heads, dh = A.kv.head_dim;
   const int cb = A.col_blocks - 1 - part % A.col_blocks, split = part / A.col_blocks;   // (blocks of the last rows see most: first)
@@ -165,29 +178,6 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
   if (R.tree && A.window > 0) for (int i = __popcll(tmask) - A.window; i > 0; --i) tnear &= tnear - 1;
   const float slope = MODS && A.slopes ? A.slopes[head] * 1.44269504088896341f : 0.f;
 
-  bf16x8 qf[NQ][KSN];
-  {
-    const T* qp = (const T*)A.q + row * A.q_row + head * A.q_head;
-#pragma unroll
-    for (int ks = 0; ks < KSN; ++ks) {
-      const int d = 16 * ks + 8 * hh;
-      Raw8<T> x;
-      x.zero();
-      if (live && d < dh) x.load(qp + d);
-      bf16x8 p[3];
-      x.split(p);
-#pragma unroll
-      for (int i = 0; i < NQ; ++i) qf[i][ks] = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, p[i]) ^ A.q_flip);
-    }
-  }
-
-  bf16_t* k_lds = (bf16_t*)smem_c;
-  bf16_t* v_lds = k_lds + P::K_ELTS + (WIDE ? 0 : w * NK * TILE);
-  if constexpr (WIDE) {
-    if (tid < 2) s_bad[tid] = -1;
-    __syncthreads();
-  }
-
   // tile number -> first token
   auto tile_token = [&](int it) { return (it < R.n_prefix ? it : it - R.n_prefix + R.first) * KT; };
   // page of token k0 + lane (KT 32: lane % 32) of a tile, -1: not there or behind the last
@@ -196,12 +186,41 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
     return it < t_end && t < R.keys ? token_page(A.kv, s, t) : -1;
   };
   constexpr int STEP = WIDE ? 1 : 4;
-  Raw8<CT> kr[WIDE ? ITEMS : KSN], vr[ITEMS];
-  const int g_tid = WIDE ? tid : lane;
+  const int g_tid = WIDE ? tid : lane, in_page = (1 << A.kv.page_shift) - 1;
+  const CT *kb = (const CT*)A.kv.k + kvh * A.kv.head_stride, *vb = (const CT*)A.kv.v + kvh * A.kv.head_stride;
+  constexpr int MINE = WIDE ? 0 : NK * TILE;                      // a wave's place in a buffer: w * MINE
+
+  // ---- DIRECT: a load instruction fills 1 KiB of LDS, RPI tokens of DH elements; lane -> (token, place), and the piece of 8 elements that belongs in the place.  What is not there (a page, a
+  // token behind the last, elements from head_dim on) is whatever lies in page 0, or in the head's first piece: finite or not, it is masked like what a column may not see.
+  constexpr int RPI = 512 / DH, INSTS = DIRECT ? KT / RPI / (WIDE ? 4 : 1) : 1;
+  auto dma = [&](lds_ptr kd, lds_ptr vd, int it, int pages) {
+    const int k0 = tile_token(it);
+    const int tr = lane / (DH / 8), place = lane % (DH / 8);
+#pragma unroll
+    for (int u = 0; u < INSTS; ++u) {
+      const int t0 = ((WIDE ? w * INSTS : 0) + u) * RPI, t = t0 + tr;
+      int kc = place ^ (k_place<DH>(t, 0) - t * (DH / 8)), vc = place ^ (v_place<DH>(t, 0) - t * (DH / 8));
+      kc = kc * 8 < dh ? kc : 0; vc = vc * 8 < dh ? vc : 0;
+      long long at;
+      if (A.kv.page_shift >= 3) {                                 // the tokens of an instruction lie in one page: its place is the wave's
+        const int page = max(0, __builtin_amdgcn_readlane(pages, t0));
+        at = page * A.kv.page_stride + ((k0 + t0) & in_page) * A.kv.token_stride;
+        const int off = tr * (int)A.kv.token_stride;
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(kb + at + (off + kc * 8)), (__attribute__((address_space(3))) void*)(kd + t0 * DH), 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(vb + at + (off + vc * 8)), (__attribute__((address_space(3))) void*)(vd + t0 * DH), 16, 0, 0);
+      } else {
+        const int page = max(0, __shfl(pages, t, 64));
+        at = page * A.kv.page_stride + ((k0 + t) & in_page) * A.kv.token_stride;
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(kb + at + kc * 8), (__attribute__((address_space(3))) void*)(kd + t0 * DH), 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(vb + at + vc * 8), (__attribute__((address_space(3))) void*)(vd + t0 * DH), 16, 0, 0);
+      }
+    }
+  };
+
+  // ---- not DIRECT: through registers
+  Raw8<CT> kr[DIRECT ? 1 : WIDE ? ITEMS : KSN], vr[DIRECT ? 1 : ITEMS];
   auto fetch = [&](int it, int pages) {
     const int k0 = tile_token(it);
-    const int in_page = (1 << A.kv.page_shift) - 1;
-    const CT *kb = (const CT*)A.kv.k + kvh * A.kv.head_stride, *vb = (const CT*)A.kv.v + kvh * A.kv.head_stride;
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
       const int item = i * P::GROUP + g_tid, t = item / (DH / 8), c = item % (DH / 8);
@@ -224,7 +243,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
     }
   };
   // the fetched tile to LDS; returns whether a value is not finite (to this thread's knowledge)
-  auto put = [&](int buf) -> bool {
+  auto put = [&](bf16_t* kd, bf16_t* vd) -> bool {
     bool bad = false;
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
@@ -233,15 +252,43 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
       if constexpr (WIDE) {
         kr[i].split(p);
 #pragma unroll
-        for (int j = 0; j < NK; ++j) *(bf16x8*)(k_lds + (buf * NK + j) * TILE + 8 * k_place<DH>(t, c)) = p[j];
+        for (int j = 0; j < NK; ++j) *(bf16x8*)(kd + j * TILE + 8 * k_place<DH>(t, c)) = p[j];
       }
       vr[i].split(p);
       bad = bad || vr[i].bad();
 #pragma unroll
-      for (int j = 0; j < NK; ++j) *(bf16x8*)(v_lds + (buf * NK + j) * TILE + 8 * v_place<DH>(t, c)) = p[j];
+      for (int j = 0; j < NK; ++j) *(bf16x8*)(vd + j * TILE + 8 * v_place<DH>(t, c)) = p[j];
     }
     return bad;
   };
+
+  int it = t_begin + (WIDE ? 0 : w);
+  int pages = pages_of(it), pages_next = pages_of(it + STEP);
+  if constexpr (DIRECT) {
+    if (it < t_end) dma((lds_ptr)k_lds0 + w * MINE, (lds_ptr)v_lds0 + w * MINE, it, pages);
+  } else if (it < t_end) fetch(it, pages);
+
+  bf16x8 qf[NQ][KSN];
+  {
+    const T* qp = (const T*)A.q + row * A.q_row + head * A.q_head;
+#pragma unroll
+    for (int ks = 0; ks < KSN; ++ks) {
+      const int d = 16 * ks + 8 * hh;
+      Raw8<T> x;
+      x.zero();
+      if (live && d < dh) x.load(qp + d);
+      bf16x8 p[3];
+      x.split(p);
+#pragma unroll
+      for (int i = 0; i < NQ; ++i) qf[i][ks] = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, p[i]) ^ A.q_flip);
+    }
+  }
+  if constexpr (WIDE && !DIRECT) {
+    if (tid < 2) s_bad[tid] = -1;
+    __syncthreads();
+    if (it < t_end && __any(put(k_lds0, v_lds0)) && lane == 0) s_bad[0] = it;
+    __syncthreads();
+  }
 
   const float c2 = MODS ? 1.44269504088896341f : A.scale * 1.44269504088896341f;   // scores to powers of two
   const float cap2 = MODS && A.softcap > 0.f ? 2.f * 1.44269504088896341f / A.softcap : 0.f;
@@ -252,53 +299,64 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
 #pragma unroll
     for (int r = 0; r < 16; ++r) oacc[b][r] = 0.f;
 
-  int it = t_begin + (WIDE ? 0 : w);
-  int pages = pages_of(it);
-  bool bad = false;
-  if (it < t_end) fetch(it, pages);
-  int pages_next = pages_of(it + STEP);
-  if constexpr (WIDE) {
-    if (it < t_end && __any(put(0)) && lane == 0) s_bad[0] = it;
-    __syncthreads();
+  // Byte offsets in a buffer of what this lane reads of a tile: the keys' k-steps 0..3 (the others, and the second 32 tokens, lie a constant further on), the values' 32-wide blocks.
+  uint32_t k_at[4], v_at[DB];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) k_at[i] = 16 * k_place<DH>(q, 2 * i + hh);
+#pragma unroll
+  for (int b = 0; b < DB; ++b) {
+    const int t = 4 * hh + ((lane & 15) >> 2), c = 4 * b + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+    v_at[b] = 16 * v_place<DH>(t, c) + 8 * (lane & 1);
   }
-  for (int step = 0; it < t_end; it += STEP, ++step) {
-    const int buf = WIDE ? step & 1 : 0, k0 = tile_token(it);
+  const int wave_last = R.tree ? R.keys : max(R.own0 + min(R.n - 1, (wave_col + 31) / g), R.prefix - 1);   // last token a column of this wave may see
+  const bool wave_live = wave_col < R.n * g;
+
+  // One tile, its keys and values in kt, vt; the next goes to kn, vn.
+  auto tile = [&](bf16_t* kt, bf16_t* vt, bf16_t* kn, bf16_t* vn, int which) {
+    const int k0 = tile_token(it);
     const uint64_t there = __ballot(pages >= 0) & low_ones(KT);
-    bf16x8 kf[NK];
-    f32x16 sacc[KB];
-    if constexpr (WIDE) {
+    const bool full = k0 + KT <= R.full_to && (k0 >= R.full_from || k0 + KT <= R.prefix) && there == low_ones(KT);
+    bool bad = false;
+    if constexpr (DIRECT) {
+      // this tile has landed (for WIDE: everyone's part of it, and everyone is done with the other buffer)
+      __builtin_amdgcn_s_waitcnt(0x0F70);                         // vmcnt(0)
+      if constexpr (WIDE) { asm volatile("" ::: "memory"); __builtin_amdgcn_s_barrier(); asm volatile("" ::: "memory"); }
+      if (it + STEP < t_end) dma((lds_ptr)kn, (lds_ptr)vn, it + STEP, pages_next);
+    } else if constexpr (WIDE) {
       if (it + 1 < t_end) fetch(it + 1, pages_next);
-      bad = s_bad[buf] == it;
+      bad = s_bad[which] == it;
     } else {
-      bad = __any(put(0));
+      bad = __any(put(kt, vt));
     }
+    const bool idle = WIDE && (!wave_live || k0 > wave_last);     // (the wave's part of moving data and the barriers stay)
+    f32x16 sacc[KB];
+    if (!idle) {
 #pragma unroll
-    for (int a = 0; a < KB; ++a) {
+      for (int a = 0; a < KB; ++a) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) sacc[a][r] = 0.f;
+        for (int r = 0; r < 16; ++r) sacc[a][r] = 0.f;
 #pragma unroll
-      for (int ks = 0; ks < KSN; ++ks) {
-        if constexpr (WIDE) {
+        for (int ks = 0; ks < KSN; ++ks) {
+          bf16x8 kf[3];
+          if constexpr (P::KEYS_IN_LDS) {
 #pragma unroll
-          for (int j = 0; j < NK; ++j) kf[j] = *(const bf16x8*)(k_lds + (buf * NK + j) * TILE + 8 * k_place<DH>(32 * a + q, 2 * ks + hh));
-        } else {
-          bf16x8 p[3];
-          kr[ks].split(p);
+            for (int j = 0; j < NK; ++j) kf[j] = *(const bf16x8*)((const char*)kt + k_at[ks & 3] + (2 * j * TILE + 64 * DH * a + 128 * (ks >> 2)));
+          } else kr[ks].split(kf);
 #pragma unroll
-          for (int j = 0; j < NK; ++j) kf[j] = p[j];
+          for (int sum = NP - 1; sum >= 0; --sum)                 // small products first
+#pragma unroll
+            for (int i = 0; i < NQ; ++i)
+              if (sum - i >= 0 && sum - i < NK) sacc[a] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[sum - i], qf[i][ks], sacc[a], 0, 0, 0);
         }
-#pragma unroll
-        for (int sum = NP - 1; sum >= 0; --sum)                   // small products first
-#pragma unroll
-          for (int i = 0; i < NQ; ++i)
-            if (sum - i >= 0 && sum - i < NK) sacc[a] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[sum - i], qf[i][ks], sacc[a], 0, 0, 0);
       }
     }
-    if constexpr (!WIDE) {
+    if constexpr (!WIDE && !DIRECT) {
       if (it + STEP < t_end) fetch(it + STEP, pages_next);        // (the keys' registers are free now)
     }
-    const int pages_now = pages_next;
+    pages = pages_next;
     pages_next = pages_of(it + 2 * STEP);
+    uint64_t vis = ~0ull;                                         // tokens of the tile that the column sees
+    if (!idle) {
     // cap and slopes
     if constexpr (MODS) {
 #pragma unroll
@@ -324,7 +382,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
           }
           sacc[a][r] = x * c2;
         }
-      if (slope != 0.f || __any(slope != 0.f)) {
+      if (__any(slope != 0.f)) {
         const bool nodes = R.tree && k0 + KT > R.base;            // (uniform)
 #pragma unroll
         for (int a = 0; a < KB; ++a)
@@ -338,9 +396,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
       }
     }
     // what the column does not see
-    const bool full = k0 + KT <= R.full_to && (k0 >= R.full_from || k0 + KT <= R.prefix) && there == low_ones(KT);
     if (!full) {
-      uint64_t vis;
       if (R.tree) {
         const int sh = k0 - R.base;                               // bit u of the path is token base + u
         vis = low_ones(-sh) & ~(A.window > 0 ? low_ones(own - A.window + 1 - k0) : 0ull);
@@ -351,11 +407,11 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
       }
       vis |= low_ones(R.prefix - k0);
       vis &= there;
-      vis >>= 4 * hh;
+      const uint64_t mine = vis >> (4 * hh);
 #pragma unroll
       for (int a = 0; a < KB; ++a)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) sacc[a][r] = (uint32_t)(vis >> (32 * a)) >> (8 * (r >> 2) + (r & 3)) & 1u ? sacc[a][r] : -INFINITY;
+        for (int r = 0; r < 16; ++r) sacc[a][r] = (uint32_t)(mine >> (32 * a)) >> (8 * (r >> 2) + (r & 3)) & 1u ? sacc[a][r] : -INFINITY;
     }
     float top = sacc[0][0];
 #pragma unroll
@@ -386,73 +442,93 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
         sum += e;
       }
     l_run += sum;
+    }
+    if (DIRECT && !full) {                                        // is there anything that is not finite among the values?
+      uint32_t any = 0;
+#pragma unroll 4
+      for (int i = 0; i < TILE / 512; ++i) any |= exponents(*(const u32x4*)(vt + i * 512 + lane * 8));
+      bad = __any(any != 0);
+    }
+    if (bad) {
+      // 0 times what is not finite is not 0.  So it is added to the columns that see it, and zeroed for the product.
+      uint64_t spoilt = 0;
+      for (int i = 0; i < TILE / 512; ++i) {
+        const uint64_t b = __ballot(exponents(*(const u32x4*)(vt + i * 512 + lane * 8)) != 0);
+        for (int j = 0; j < RPI; ++j)
+          if (b >> (j * (DH / 8)) & low_ones(DH / 8)) spoilt |= 1ull << (i * RPI + j);
+      }
+      for (uint64_t left = spoilt & there; left && !idle; left &= left - 1) {
+        const int t = __builtin_ctzll(left);
+        const bool seen = vis >> t & 1;
 #pragma unroll
-    for (int jj = 0; jj < KT / 16; ++jj) {
-      bf16x8 pf[3];
-      {
+        for (int b = 0; b < DB; ++b)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int d = 32 * b + 8 * i + 4 * hh;
+            const u32x2 v = *(const u32x2*)(vt + 8 * v_place<DH>(t, d >> 3) + (d & 7));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float x = __builtin_bit_cast(float, e & 1 ? v[e >> 1] & 0xFFFF0000u : v[e >> 1] << 16);
+              oacc[b][4 * i + e] += seen && not_finite(x) ? x : 0.f;
+            }
+          }
+      }
+      if constexpr (WIDE) __syncthreads();
+      for (int i = WIDE ? w : 0; i < TILE / 512; i += WIDE ? 4 : 1) {
+        u32x4 v = *(const u32x4*)(vt + i * 512 + lane * 8);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if ((v[e] & 0x7F80u) == 0x7F80u) v[e] &= 0xFFFF0000u;
+          if ((v[e] & 0x7F800000u) == 0x7F800000u) v[e] &= 0xFFFFu;
+        }
+        *(u32x4*)(vt + i * 512 + lane * 8) = v;
+      }
+      if constexpr (WIDE) __syncthreads();
+    }
+    if (!idle) {
+#pragma unroll
+      for (int jj = 0; jj < KT / 16; ++jj) {
+        bf16x8 pf[3], vf[3];
         float x[8];
 #pragma unroll
         for (int t = 0; t < 8; ++t) x[t] = sacc[jj >> 1][8 * (jj & 1) + t];
         pieces8<NQ>(x, pf);
-      }
 #pragma unroll
-      for (int b = 0; b < DB; ++b) {
-        bf16x8 vf[NK];
-        const int t = 16 * jj + 4 * hh + ((lane & 15) >> 2), c = 4 * b + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+        for (int b = 0; b < DB; ++b) {
 #pragma unroll
-        for (int j = 0; j < NK; ++j) {
-          const bf16_t* vt = v_lds + (buf * NK + j) * TILE + 4 * (lane & 1);
-          const s16x4 lo = read_transposed(vt + 8 * v_place<DH>(t, c)), hi = read_transposed(vt + 8 * v_place<DH>(t + 8, c));
-          typedef short s16x8 __attribute__((ext_vector_type(8)));
-          vf[j] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-        }
-        if (bad) {
-          // 0 times what is not finite is not 0: it goes to the columns that see it by counting (NaN, then the infinities), and out of the product.
-          u32x4 v = __builtin_bit_cast(u32x4, vf[0]);
-#pragma unroll 1
-          for (int kind = 0; kind < 3; ++kind) {
-            u32x4 is;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              is[i] = 0;
-#pragma unroll
-              for (int x = 0; x < 2; ++x) {
-                const uint32_t e = v[i] >> (16 * x) & 0xFFFFu;
-                if (kind == 0 ? (e & 0x7FFFu) > 0x7F80u : e == (kind == 1 ? 0x7F80u : 0xFF80u)) is[i] |= 0x3F80u << (16 * x);
-              }
-            }
-            f32x16 hits;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) hits[r] = 0.f;
-            hits = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, is), pf[0], hits, 0, 0, 0);
-            const float add = kind == 0 ? __builtin_nanf("") : kind == 1 ? INFINITY : -INFINITY;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) oacc[b][r] += hits[r] > 0.f ? add : 0.f;
+          for (int j = 0; j < NK; ++j) {
+            const char* p = (const char*)vt + v_at[b] + (2 * j * TILE + 32 * DH * jj);
+            const s16x4 lo = read_transposed((const bf16_t*)p), hi = read_transposed((const bf16_t*)(p + 16 * DH));
+            typedef short s16x8 __attribute__((ext_vector_type(8)));
+            vf[j] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
           }
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if ((v[i] & 0x7F80u) == 0x7F80u) v[i] &= 0xFFFF0000u;
-            if ((v[i] & 0x7F800000u) == 0x7F800000u) v[i] &= 0xFFFFu;
-          }
-          vf[0] = __builtin_bit_cast(bf16x8, v);
+          for (int sum2 = NP - 1; sum2 >= 0; --sum2)
+#pragma unroll
+            for (int i = 0; i < NQ; ++i)
+              if (sum2 - i >= 0 && sum2 - i < NK) oacc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[sum2 - i], pf[i], oacc[b], 0, 0, 0);
         }
-#pragma unroll
-        for (int sum2 = NP - 1; sum2 >= 0; --sum2)
-#pragma unroll
-          for (int i = 0; i < NQ; ++i)
-            if (sum2 - i >= 0 && sum2 - i < NK) oacc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[sum2 - i], pf[i], oacc[b], 0, 0, 0);
       }
     }
-    pages = pages_now;
-    if constexpr (WIDE) {
-      if (it + 1 < t_end && __any(put(buf ^ 1)) && lane == 0) s_bad[buf ^ 1] = it + 1;
+    if constexpr (WIDE && !DIRECT) {
+      if (it + 1 < t_end && __any(put(kn, vn)) && lane == 0) s_bad[which ^ 1] = it + 1;
       __syncthreads();
     }
+    it += STEP;
+  };
+  if constexpr (P::TWO) {
+    while (it < t_end) {
+      tile(k_lds0 + w * MINE, v_lds0 + w * MINE, k_lds1 + w * MINE, v_lds1 + w * MINE, 0);
+      if (it >= t_end) break;
+      tile(k_lds1 + w * MINE, v_lds1 + w * MINE, k_lds0 + w * MINE, v_lds0 + w * MINE, 1);
+    }
+  } else {
+    while (it < t_end) tile(nullptr, v_lds0 + w * MINE, nullptr, v_lds0 + w * MINE, 0);
   }
   l_run += __shfl_xor(l_run, 32, 64);
   if constexpr (!WIDE) {
     // waves 2 and 3 into 0 and 1, then 1 into 0
-    float* st = (float*)smem_c + lane;
+    float* st = (float*)v_lds0 + lane;
 #pragma unroll
     for (int half = 2; half > 0; half >>= 1) {
       __syncthreads();

@@ -199,8 +199,7 @@ template <typename T, typename CT, int DH, bool WIDE, bool MODS>
 static int launch_attention(const ChunkAttnDev& d, hipStream_t stream) {
   typedef ChunkAttn<T, CT, DH, WIDE, MODS> P;
   auto kernel = k_chunk_attn<P, T, CT>;
-  HIPCHK(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)P::LDS));
-  kernel<<<dim3(d.kv.n_kv_heads * d.col_blocks * d.splits, d.chunk.n_seqs), 256, P::LDS, stream>>>(d);
+  kernel<<<dim3(d.kv.n_kv_heads * d.col_blocks * d.splits, d.chunk.n_seqs), 256, 0, stream>>>(d);
   LAUNCH_CHECK();
   if (d.splits > 1) {
     k_chunk_attn_join<P, T><<<dim3(d.chunk.n_rows, (d.H + 3) / 4), 256, 0, stream>>>(d);
