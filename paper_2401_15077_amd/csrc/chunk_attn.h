@@ -25,6 +25,7 @@ struct ChunkAttnDev {
   const float* slopes; const int* prefix;
   ChunkDev chunk; PagedDev kv;
   int col_blocks, splits, split_tiles;     // parts of the token range at most, tiles of one
+  int lane_pages;                          // pages of fewer than 8 tokens: every lane looks its own up
   float* part_o; float* part_ml;           // [row][head][split][DH], [row][head][split][maximum, sum]
 };
 
@@ -193,26 +194,38 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
   // ---- DIRECT: a load instruction fills 1 KiB of LDS, RPI tokens of DH elements; lane -> (token, place), and the piece of 8 elements that belongs in the place.  What is not there (a page, a
   // token behind the last, elements from head_dim on) is whatever lies in page 0, or in the head's first piece: finite or not, it is masked like what a column may not see.
   constexpr int RPI = 512 / DH, INSTS = DIRECT ? KT / RPI / (WIDE ? 4 : 1) : 1;
-  auto dma = [&](lds_ptr kd, lds_ptr vd, int it, int pages) {
-    const int k0 = tile_token(it);
-    const int tr = lane / (DH / 8), place = lane % (DH / 8);
+  const int tr = lane / (DH / 8), place = lane % (DH / 8);
+  // bytes from an instruction's first token to what this lane loads (the keys' order of pieces repeats every eight tokens, the values' every RPI)
+  uint32_t k_off[8 / RPI], v_off;
+  {
+    const int vc = place ^ (v_place<DH>(tr, 0) - tr * (DH / 8));
 #pragma unroll
-    for (int u = 0; u < INSTS; ++u) {
-      const int t0 = ((WIDE ? w * INSTS : 0) + u) * RPI, t = t0 + tr;
-      int kc = place ^ (k_place<DH>(t, 0) - t * (DH / 8)), vc = place ^ (v_place<DH>(t, 0) - t * (DH / 8));
-      kc = kc * 8 < dh ? kc : 0; vc = vc * 8 < dh ? vc : 0;
-      long long at;
-      if (A.kv.page_shift >= 3) {                                 // the tokens of an instruction lie in one page: its place is the wave's
-        const int page = max(0, __builtin_amdgcn_readlane(pages, t0));
-        at = page * A.kv.page_stride + ((k0 + t0) & in_page) * A.kv.token_stride;
-        const int off = tr * (int)A.kv.token_stride;
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(kb + at + (off + kc * 8)), (__attribute__((address_space(3))) void*)(kd + t0 * DH), 16, 0, 0);
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(vb + at + (off + vc * 8)), (__attribute__((address_space(3))) void*)(vd + t0 * DH), 16, 0, 0);
-      } else {
-        const int page = max(0, __shfl(pages, t, 64));
-        at = page * A.kv.page_stride + ((k0 + t) & in_page) * A.kv.token_stride;
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(kb + at + kc * 8), (__attribute__((address_space(3))) void*)(kd + t0 * DH), 16, 0, 0);
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(vb + at + vc * 8), (__attribute__((address_space(3))) void*)(vd + t0 * DH), 16, 0, 0);
+    for (int i = 0; i < 8 / RPI; ++i) {
+      const int t = i * RPI + tr, kc = place ^ (k_place<DH>(t, 0) - t * (DH / 8));
+      k_off[i] = (uint32_t)(tr * (int)A.kv.token_stride + (kc * 8 < dh ? kc * 8 : 0)) * (uint32_t)sizeof(CT);
+    }
+    v_off = (uint32_t)(tr * (int)A.kv.token_stride + (vc * 8 < dh ? vc * 8 : 0)) * (uint32_t)sizeof(CT);
+  }
+  auto load_lds = [&](const void* from, lds_ptr to) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+  };
+  auto dma = [&](lds_ptr kd, lds_ptr vd, int it, int pages) {
+    const int k0 = tile_token(it), first = WIDE ? w * INSTS : 0;
+    if (!A.lane_pages) {                                          // the tokens of an instruction lie in one page, whose place stays in scalar registers
+#pragma unroll
+      for (int u = 0; u < INSTS; ++u) {
+        const int t0 = (first + u) * RPI, page = max(0, __builtin_amdgcn_readlane(pages, t0));
+        const long long at = page * A.kv.page_stride + ((k0 + t0) & in_page) * A.kv.token_stride;
+        load_lds((const char*)(kb + at) + k_off[u % (8 / RPI)], kd + t0 * DH);
+        load_lds((const char*)(vb + at) + v_off, vd + t0 * DH);
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < INSTS; ++u) {
+        const int t0 = (first + u) * RPI, page = max(0, __shfl(pages, t0 + tr, 64));
+        const long long at = page * A.kv.page_stride + (((k0 + t0 + tr) & in_page) - tr) * A.kv.token_stride;
+        load_lds((const char*)(kb + at) + k_off[u % (8 / RPI)], kd + t0 * DH);
+        load_lds((const char*)(vb + at) + v_off, vd + t0 * DH);
       }
     }
   };
@@ -290,8 +303,8 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
     __syncthreads();
   }
 
-  const float c2 = MODS ? 1.44269504088896341f : A.scale * 1.44269504088896341f;   // scores to powers of two
-  const float cap2 = MODS && A.softcap > 0.f ? 2.f * 1.44269504088896341f / A.softcap : 0.f;
+  const float c2 = A.scale * 1.44269504088896341f;                // scores to powers of two
+  const float cap_in = MODS && A.softcap > 0.f ? 2.f * c2 / A.softcap : 0.f, cap_out = A.softcap * 1.44269504088896341f;
   float m_run = -INFINITY, l_run = 0.f;                           // maximum (in powers of two) of the column, sum of this lane's half of the tokens
   f32x16 oacc[DB];
 #pragma unroll
@@ -359,16 +372,15 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
     if (!idle) {
     // cap and slopes
     if constexpr (MODS) {
+      if (A.softcap > 0.f) {
 #pragma unroll
-      for (int a = 0; a < KB; ++a)
+        for (int a = 0; a < KB; ++a)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          float x = sacc[a][r] * A.scale;
-          if (A.softcap > 0.f) {
-            const float e = __builtin_amdgcn_exp2f(x * cap2);     // e^(2 x / cap); tanh = 1 - 2 / (e + 1)
-            float th = 1.f - 2.f * __builtin_amdgcn_rcpf(e + 1.f);
+          for (int r = 0; r < 16; ++r) {
+            const float e = __builtin_amdgcn_exp2f(sacc[a][r] * cap_in);   // e^(2 x / cap); tanh = 1 - 2 / (e + 1)
+            float x = fmaf(-2.f * cap_out, __builtin_amdgcn_rcpf(e + 1.f), cap_out);
             if constexpr (NQ == 3) {                              // fp32: near 0 that cancels; the Taylor polynomial to y^13 is within 10^-9 below 0.35
-              const float y = x / A.softcap, z = y * y;
+              const float y = sacc[a][r] * (cap_in * 0.34657359027997264f), z = y * y;   // (cap_in = 2 log2(e) scale / cap)
               float t = 3.59212803657248102e-3f;
               t = fmaf(t, z, -8.86323552990219657e-3f);
               t = fmaf(t, z, 2.18694885361552028e-2f);
@@ -376,23 +388,33 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
               t = fmaf(t, z, 0.133333333333333333f);
               t = fmaf(t, z, -0.333333333333333333f);
               t = fmaf(t * z, y, y);
-              th = fabsf(y) < 0.35f ? t : th;
+              x = fabsf(y) < 0.35f ? cap_out * t : x;
             }
-            x = A.softcap * th;
+            sacc[a][r] = x;
           }
-          sacc[a][r] = x * c2;
-        }
-      if (__any(slope != 0.f)) {
-        const bool nodes = R.tree && k0 + KT > R.base;            // (uniform)
+      } else {
 #pragma unroll
         for (int a = 0; a < KB; ++a)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int j = k0 + 32 * a + 8 * (r >> 2) + 4 * hh + (r & 3);
-            int pos = j;
-            if (nodes && j > R.base) pos = R.base + __popcll(tmask & low_ones(j - R.base));
-            sacc[a][r] = fmaf(-slope, (float)abs(own - pos), sacc[a][r]);
-          }
+          for (int r = 0; r < 16; ++r) sacc[a][r] *= c2;
+      }
+      if (A.slopes) {
+        if (R.tree && k0 + KT > R.base) {
+#pragma unroll
+          for (int a = 0; a < KB; ++a)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const int j = k0 + 32 * a + 8 * (r >> 2) + 4 * hh + (r & 3);
+              const int pos = j > R.base ? R.base + __popcll(tmask & low_ones(j - R.base)) : j;
+              sacc[a][r] = fmaf(-slope, (float)abs(own - pos), sacc[a][r]);
+            }
+        } else {
+          const float d = (float)(own - k0 - 4 * hh);
+#pragma unroll
+          for (int a = 0; a < KB; ++a)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sacc[a][r] = fmaf(-slope, fabsf(d - (float)(32 * a + 8 * (r >> 2) + (r & 3))), sacc[a][r]);
+        }
       }
     }
     // what the column does not see

@@ -159,17 +159,19 @@ static int check_attention(const eagle_attention_args* a, const eagle_chunk* chu
   const int elt = elt_of(a->dtype), kelt = elt_of(kv->dtype);
   if (!runs_ok(a->q, a->q_row, a->q_head, elt)) return fail(EAGLE_EINVAL, "attention: q's rows and heads must start on multiples of 16 bytes");
   if (!aligned(a->out, 16) || a->out_row % 8 || a->out_head % 8) return fail(EAGLE_EINVAL, "attention: out's rows and heads must start on multiples of 16 bytes and 8 elements");
+  if (kv->token_stride > 1 << 24) return fail(EAGLE_EINVAL, "attention: the cache's token_stride must be at most 2^24");
   if (!aligned(kv->k, 16) || !aligned(kv->v, 16) || kv->page_stride * kelt % 16 || kv->head_stride * kelt % 16 || kv->token_stride * kelt % 16)
     return fail(EAGLE_EINVAL, "attention: the cache's tokens must start on multiples of 16 bytes");
   d->q = a->q; d->out = a->out; d->q_row = a->q_row; d->q_head = a->q_head; d->out_row = a->out_row; d->out_head = a->out_head;
   d->H = a->n_heads; d->window = std::min(a->window, 1 << 30); d->slopes = a->slopes; d->prefix = a->prefix; d->softcap = a->softcap;
   d->scale = std::fabs(a->scale);
   d->q_flip = std::signbit(a->scale) ? 0x80008000u : 0u;
+  d->lane_pages = kv->page_tokens < 8;
   return EAGLE_OK;
 }
 
 // Work-groups that the token range is split for where sequences, kv heads and column blocks are fewer, and the fewest tiles of a part.
-constexpr int ATTN_TARGET_WGS = 2048, ATTN_MIN_TILES = 4;
+constexpr int ATTN_WIDE_WGS = 512, ATTN_NARROW_WGS = 2048, ATTN_MIN_TILES = 4;
 
 // Columns and parts of a call; returns the bytes of workspace.
 static size_t plan_attention(ChunkAttnDev* d, int elt, int kv_elt, bool* wide) {
@@ -179,7 +181,7 @@ static size_t plan_attention(ChunkAttnDev* d, int elt, int kv_elt, bool* wide) {
   const int KT = *wide && kv_elt == 2 ? 64 : 32;
   d->col_blocks = (int)((cols + (*wide ? 127 : 31)) / (*wide ? 128 : 32));
   const long long units = (long long)d->col_blocks * d->kv.n_kv_heads * d->chunk.n_seqs, tiles = ((long long)d->chunk.max_keys + KT - 1) / KT;
-  const long long parts = std::max(1ll, std::min(ATTN_TARGET_WGS / units, tiles / ATTN_MIN_TILES));
+  const long long parts = std::max(1ll, std::min((*wide ? ATTN_WIDE_WGS : ATTN_NARROW_WGS) / units, tiles / ATTN_MIN_TILES));
   d->split_tiles = (int)((tiles + parts - 1) / parts);
   d->splits = (int)((tiles + d->split_tiles - 1) / d->split_tiles);
   if (d->splits == 1) return 256;
