@@ -140,6 +140,7 @@ struct ChunkAttn {
   static constexpr int JOIN = WIDE ? 0 : 2 * (16 * DB + 2) * 64 * 2;   // elements (of 2 bytes) that joining the waves takes
   static constexpr int V0_ELTS = V_ELTS > JOIN ? V_ELTS : JOIN;
   static constexpr int LDS = 2 * ((TWO ? 2 : 1) * K_ELTS + V0_ELTS + (TWO ? V_ELTS : 0));
+  static constexpr int PRODUCTS = NQ * NK == 9 ? 6 : NQ * NK;     // of pieces that are kept
   static constexpr int WAVES = NK == 3 && DH == 128 ? 1 : 2;      // a SIMD holds (by registers)
   static constexpr int GROUP = WIDE ? 256 : 64;                   // threads that fetch a tile together
   static constexpr int ITEMS = KT * DH / 8 / GROUP;               // runs of 8 elements a thread fetches of the values (and of the keys if they go through LDS)
@@ -181,10 +182,12 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
 
   // tile number -> first token
   auto tile_token = [&](int it) { return (it < R.n_prefix ? it : it - R.n_prefix + R.first) * KT; };
-  // page of token k0 + lane (KT 32: lane % 32) of a tile, -1: not there or behind the last
-  auto pages_of = [&](int it) -> int {
-    const int t = tile_token(it) + (lane & (KT - 1));
-    return it < t_end && t < R.keys ? token_page(A.kv, s, t) : -1;
+  // The table's entry for token k0 + lane (KT 32: lane % 32) of a tile, requested a tile and a half before it is looked at: looked at at once it would wait for every load in flight.
+  const int* table = A.kv.page_table + (size_t)s * A.kv.table_stride;
+  auto entry_of = [&](int it) -> int { return table[max(0, min(tile_token(it) + (lane & (KT - 1)), R.keys - 1)) >> A.kv.page_shift]; };
+  // the page itself, -1: not there, or the token is behind the last
+  auto page_of = [&](int it, int entry) -> int {
+    return (unsigned)entry < (unsigned)A.kv.n_pages && tile_token(it) + (lane & (KT - 1)) < R.keys ? entry : -1;
   };
   constexpr int STEP = WIDE ? 1 : 4;
   const int g_tid = WIDE ? tid : lane, in_page = (1 << A.kv.page_shift) - 1;
@@ -276,7 +279,11 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
   };
 
   int it = t_begin + (WIDE ? 0 : w);
-  int pages = pages_of(it), pages_next = pages_of(it + STEP);
+  int pages = -1, entry_next = 0;
+  if (it < t_end) {
+    pages = page_of(it, entry_of(it));
+    entry_next = entry_of(it + STEP);
+  }
   if constexpr (DIRECT) {
     if (it < t_end) dma((lds_ptr)k_lds0 + w * MINE, (lds_ptr)v_lds0 + w * MINE, it, pages);
   } else if (it < t_end) fetch(it, pages);
@@ -330,6 +337,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
     const uint64_t there = __ballot(pages >= 0) & low_ones(KT);
     const bool full = k0 + KT <= R.full_to && (k0 >= R.full_from || k0 + KT <= R.prefix) && there == low_ones(KT);
     bool bad = false;
+    const int pages_next = page_of(it + STEP, entry_next);
     if constexpr (DIRECT) {
       // this tile has landed (for WIDE: everyone's part of it, and everyone is done with the other buffer)
       __builtin_amdgcn_s_waitcnt(0x0F70);                         // vmcnt(0)
@@ -362,12 +370,22 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
               if (sum - i >= 0 && sum - i < NK) sacc[a] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[sum - i], qf[i][ks], sacc[a], 0, 0, 0);
         }
       }
+      if constexpr (P::KEYS_IN_LDS) {                             // order: four k-steps' reads ahead of their products
+        constexpr int STEPS = KB * KSN, AHEAD = STEPS < 4 ? STEPS : 4;
+        __builtin_amdgcn_sched_group_barrier(0x100, NK * AHEAD, 0);
+#pragma unroll
+        for (int i = 0; i < STEPS - AHEAD; ++i) {
+          __builtin_amdgcn_sched_group_barrier(0x008, P::PRODUCTS, 0);
+          __builtin_amdgcn_sched_group_barrier(0x100, NK, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, P::PRODUCTS * AHEAD, 0);
+      }
     }
     if constexpr (!WIDE && !DIRECT) {
       if (it + STEP < t_end) fetch(it + STEP, pages_next);        // (the keys' registers are free now)
     }
     pages = pages_next;
-    pages_next = pages_of(it + 2 * STEP);
+    entry_next = entry_of(it + 2 * STEP);
     uint64_t vis = ~0ull;                                         // tokens of the tile that the column sees
     if (!idle) {
     // cap and slopes
@@ -453,17 +471,6 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
 #pragma unroll
         for (int r = 0; r < 16; ++r) oacc[b][r] *= f;
     }
-    const float m_sub = m_run == -INFINITY ? 0.f : m_run;
-    float sum = 0.f;
-#pragma unroll
-    for (int a = 0; a < KB; ++a)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const float e = __builtin_amdgcn_exp2f(MODS ? sacc[a][r] - m_sub : fmaf(sacc[a][r], c2, -m_sub));
-        sacc[a][r] = e;
-        sum += e;
-      }
-    l_run += sum;
     }
     if (DIRECT && !full) {                                        // is there anything that is not finite among the values?
       uint32_t any = 0;
@@ -508,6 +515,17 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
       if constexpr (WIDE) __syncthreads();
     }
     if (!idle) {
+    const float m_sub = m_run == -INFINITY ? 0.f : m_run;
+    float sum = 0.f;
+#pragma unroll
+    for (int a = 0; a < KB; ++a)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float e = __builtin_amdgcn_exp2f(MODS ? sacc[a][r] - m_sub : fmaf(sacc[a][r], c2, -m_sub));
+        sacc[a][r] = e;
+        sum += e;
+      }
+    l_run += sum;
 #pragma unroll
       for (int jj = 0; jj < KT / 16; ++jj) {
         bf16x8 pf[3], vf[3];
