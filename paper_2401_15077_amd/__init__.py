@@ -403,10 +403,13 @@ class Eagle:
                  "launches": int(arr[i].launches), "bytes": arr[i].bytes} for i in range(n.value)]
 
 
+_OPERATORS = ("Chunk", "PagedKV", "LogitRules", "rope_plan", "rope", "chunk_attention", "chunk_attention_workspace", "apply_logit_rules")
+
+
 def __getattr__(name):
-    """The operators on the caller's own tensors live in `operators`, which imports torch; their names are this package's too."""
-    if name in ("operators", "Chunk", "PagedKV", "LogitRules", "rope_plan", "rope", "chunk_attention", "chunk_attention_workspace", "apply_logit_rules"):
-        import importlib
-        mod = importlib.import_module(__name__ + ".operators")
-        return mod if name == "operators" else getattr(mod, name)
+    """The operators on the caller's own tensors live in `operators`, which imports torch; their names are this package's too, from their first use on."""
+    if name in _OPERATORS:
+        from . import operators
+        globals().update({n: getattr(operators, n) for n in _OPERATORS})
+        return globals()[name]
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

@@ -6,7 +6,6 @@ require gradients are refused while gradients are enabled."""
 from __future__ import annotations
 
 import ctypes
-import math
 from typing import Optional, Tuple
 
 import torch
@@ -68,17 +67,30 @@ def declare(lib) -> None:
     lib.eagle_apply_logit_rules.argtypes = [P(EagleLogits), P(EagleLogitRules), _vp]
 
 
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device      # (a tensor on the device: the runtime is up)
+_lib = None
+
+
+def _library():
+    global _lib
+    if _lib is None:
+        _lib = load_library()
+    return _lib
+
+
 def _call(fn, device, *args):
     """Calls fn(*args, stream) with the tensors' device current."""
     if device.type != "cuda":
         raise ValueError(f"the tensors are on {device}: libeagle needs a GPU (no CPU fallback exists)")
-    if torch.cuda.current_device() != device.index:
-        with torch.cuda.device(device):
-            rc = fn(*args, torch.cuda.current_stream().cuda_stream)
+    index = device.index
+    if _current_device() != index:
+        with torch.cuda.device(index):
+            rc = fn(*args, _raw_stream(index))
     else:
-        rc = fn(*args, torch.cuda.current_stream().cuda_stream)
+        rc = fn(*args, _raw_stream(index))
     if rc != 0:
-        raise EagleError(rc, load_library().eagle_last_error().decode())
+        raise EagleError(rc, _library().eagle_last_error().decode())
 
 
 def _list(t: Optional[torch.Tensor], name: str, dtype, n: Optional[int], device) -> Optional[int]:
@@ -90,19 +102,22 @@ def _list(t: Optional[torch.Tensor], name: str, dtype, n: Optional[int], device)
     return t.data_ptr()
 
 
-def _heads(t: torch.Tensor, name: str, shape: Tuple, like: Optional[torch.Tensor] = None):
-    """Address, row stride and head stride of a [rows, heads, head_dim] tensor (shape: None where any size will do)."""
-    if t.dim() != 3 or any(w is not None and w != g for w, g in zip(shape, t.shape)):
-        raise ValueError(f"{name} must be [rows, heads, head_dim] = {list(shape)}: got {list(t.shape)}")
-    if t.dtype not in _TYPES:
-        raise ValueError(f"{name} must be float32 or bfloat16: got {t.dtype}")
-    if like is not None and (t.dtype != like.dtype or t.device != like.device):
-        raise ValueError(f"{name} must be {like.dtype} on {like.device}: got {t.dtype} on {t.device}")
-    if t.stride(2) != 1 and t.shape[2] > 1:
+def _heads(t: torch.Tensor, name: str, rows: Optional[int], heads: Optional[int], dim: int, dtype=None, device=None):
+    """Address, row stride and head stride of a [rows, heads, head_dim] tensor (None: any number)."""
+    shape = t.shape
+    if len(shape) != 3 or shape[2] != dim or (rows is not None and shape[0] != rows) or (heads is not None and shape[1] != heads):
+        raise ValueError(f"{name} must be [rows, heads, head_dim] = {[rows, heads, dim]}: got {list(shape)}")
+    if dtype is None:
+        if t.dtype not in _TYPES:
+            raise ValueError(f"{name} must be float32 or bfloat16: got {t.dtype}")
+    elif t.dtype != dtype or t.device != device:
+        raise ValueError(f"{name} must be {dtype} on {device}: got {t.dtype} on {t.device}")
+    stride = t.stride()
+    if stride[2] != 1 and dim > 1:
         raise ValueError(f"the elements of a head of {name} must be consecutive")
     if t.requires_grad and torch.is_grad_enabled():
         raise ValueError(f"{name} requires gradients: libeagle's operators are not recorded by autograd")
-    return t.data_ptr(), t.stride(0), t.stride(1)
+    return t.data_ptr(), stride[0], stride[1]
 
 
 class Chunk:
@@ -146,7 +161,7 @@ def rope_plan(head_dim: int, *, theta: float = 10000.0, rot_dim: Optional[int] =
     """How positions turn a head (see eagle_rope_config); scaling is one of ROPE_SCALINGS.  Host work: make it once."""
     if scaling not in ROPE_SCALINGS:
         raise ValueError(f"scaling must be one of {ROPE_SCALINGS}: got {scaling!r}")
-    lib = load_library()
+    lib = _library()
     cfg = EagleRopeConfig(head_dim, head_dim if rot_dim is None else rot_dim, int(interleaved), ROPE_SCALINGS.index(scaling), theta, factor, low, high, trained_len, mscale)
     plan = EagleRopePlan()
     rc = lib.eagle_rope_plan_init(ctypes.byref(cfg), ctypes.byref(plan))
@@ -163,55 +178,53 @@ def rope(plan: EagleRopePlan, q: Optional[torch.Tensor], k: Optional[torch.Tenso
     x = q if q is not None else k
     if x is None:
         raise ValueError("neither q nor k is given")
-    a = EagleRopeArgs(n_rows=x.shape[0], dtype=_TYPES.get(x.dtype, -1), inverse=int(inverse))
-    D = plan.head_dim
+    R, dtype, device, D = x.shape[0], x.dtype, x.device, plan.head_dim
+    none = (None, 0, 0)
+    qa = qo = ka = ko = va = none
+    H = KVH = 0
     if q is not None:
-        a.q, a.q_row, a.q_head = _heads(q, "q", (None, None, D))
-        a.n_heads = q.shape[1]
-        a.q_out, a.q_out_row, a.q_out_head = (a.q, a.q_row, a.q_head) if q_out is None else _heads(q_out, "q_out", tuple(q.shape), q)
+        H = q.shape[1] if q.dim() > 1 else 0
+        qa = _heads(q, "q", None, None, D)
+        qo = qa if q_out is None else _heads(q_out, "q_out", R, H, D, dtype, device)
     elif q_out is not None:
         raise ValueError("q_out without q")
     if k is not None:
-        a.k, a.k_row, a.k_head = _heads(k, "k", (x.shape[0], None, D), x)
-        a.n_kv_heads = k.shape[1]
+        KVH = k.shape[1] if k.dim() > 1 else 0
+        ka = _heads(k, "k", R, None, D, dtype, device) if q is not None else _heads(k, "k", None, None, D)
         if kv is None:
-            a.k_out, a.k_out_row, a.k_out_head = (a.k, a.k_row, a.k_head) if k_out is None else _heads(k_out, "k_out", tuple(k.shape), k)
+            ko = ka if k_out is None else _heads(k_out, "k_out", R, KVH, D, dtype, device)
         elif k_out is not None:
             raise ValueError("with a cache k goes there: k_out must be None")
+        if v is not None:
+            va = _heads(v, "v", R, KVH, D, dtype, device)
     elif k_out is not None or v is not None:
         raise ValueError("k_out or v without k")
-    if v is not None:
-        a.v, a.v_row, a.v_head = _heads(v, "v", tuple(k.shape), x)
-    a.positions = _list(positions, "positions", torch.int32, x.shape[0], x.device)
+    at = _list(positions, "positions", torch.int32, R, device)
     if kv is not None:
         if chunk is None:
             raise ValueError("a cache needs a chunk")
-        _same_batch(chunk, kv, x.device)
-    elif chunk is not None and chunk.device != x.device:
-        raise ValueError(f"the chunk is on {chunk.device}, the rows on {x.device}")
-    if x.shape[0] == 0:
+        _same_batch(chunk, kv, device)
+    elif chunk is not None and chunk.device != device:
+        raise ValueError(f"the chunk is on {chunk.device}, the rows on {device}")
+    if R == 0:
         return
-    _call(load_library().eagle_rope, x.device, plan, a, chunk.c if chunk is not None else None, kv.c if kv is not None else None)
+    a = EagleRopeArgs(R, H, KVH, _TYPES[dtype], int(inverse), qa[0], ka[0], va[0], qo[0], ko[0], qa[1], qa[2], ka[1], ka[2], va[1], va[2], qo[1], qo[2], ko[1], ko[2], at)
+    _call(_library().eagle_rope, device, plan, a, chunk.c if chunk is not None else None, kv.c if kv is not None else None)
 
 
 def _attention_args(q, kv, chunk, scale, softcap, slopes, window, prefix, out):
-    a = EagleAttentionArgs(dtype=_TYPES.get(q.dtype, -1), window=window, softcap=softcap)
-    a.q, a.q_row, a.q_head = _heads(q, "q", (chunk.n_rows, None, kv.head_dim))
-    a.n_heads = q.shape[1]
-    a.scale = 1.0 / math.sqrt(kv.head_dim) if scale is None else scale
-    if out is None:
-        a.out, a.out_row, a.out_head = a.q, a.q_row, a.q_head
-    else:
-        a.out, a.out_row, a.out_head = _heads(out, "out", tuple(q.shape), q)
-    a.slopes = _list(slopes, "slopes", torch.float32, q.shape[1], q.device)
-    a.prefix = _list(prefix, "prefix", torch.int32, chunk.n_seqs, q.device)
-    _same_batch(chunk, kv, q.device)
-    return a
+    D, device = kv.head_dim, q.device
+    qa = _heads(q, "q", chunk.n_rows, None, D)
+    H = q.shape[1]
+    oa = qa if out is None else _heads(out, "out", chunk.n_rows, H, D, q.dtype, device)
+    _same_batch(chunk, kv, device)
+    return EagleAttentionArgs(H, _TYPES[q.dtype], window, qa[0], oa[0], qa[1], qa[2], oa[1], oa[2], D ** -0.5 if scale is None else scale, softcap,
+                              _list(slopes, "slopes", torch.float32, H, device), _list(prefix, "prefix", torch.int32, chunk.n_seqs, device))
 
 
 def chunk_attention_workspace(q: torch.Tensor, kv: PagedKV, chunk: Chunk) -> int:
     """Bytes of workspace chunk_attention needs for these arguments (whatever the masks)."""
-    lib = load_library()
+    lib = _library()
     a = _attention_args(q, kv, chunk, None, 0.0, None, 0, None, None)
     n = lib.eagle_chunk_attention_workspace(a, chunk.c, kv.c)
     if n == 0:
@@ -226,7 +239,7 @@ def chunk_attention(q: torch.Tensor, kv: PagedKV, chunk: Chunk, *, scale: Option
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     a = _attention_args(q, kv, chunk, scale, softcap, slopes, window, prefix, out)
-    lib = load_library()
+    lib = _library()
     if chunk.n_rows == 0:
         return out
     if workspace is None:
@@ -288,17 +301,16 @@ def apply_logit_rules(logits: torch.Tensor, rules: LogitRules, *, row_start: Opt
         out = logits
     elif out.shape != logits.shape or out.dtype != logits.dtype or out.device != dev or (out.stride(1) != 1 and V > 1):
         raise ValueError(f"out must be {logits.dtype} {list(logits.shape)} on {dev}, its rows consecutive")
-    l = EagleLogits(n_rows=R, vocab=V, dtype=_TYPES[logits.dtype], in_=logits.data_ptr(), out=out.data_ptr(), in_stride=logits.stride(0) if R > 1 else V, out_stride=out.stride(0) if R > 1 else V)
-    l.row_start = _list(row_start, "row_start", torch.int32, rules.n_seqs + 1, dev)
-    l.path_token = _list(path_token, "path_token", torch.int32, R, dev)
-    l.path_mask = _list(path_mask, "path_mask", torch.int64, R, dev)
+    masks = (None, 0, 0)
     if allowed is not None:
         if allowed.dtype != torch.int32 or allowed.dim() != 2 or allowed.device != dev or (allowed.stride(1) != 1 and allowed.shape[1] > 1) or allowed.shape[1] * 32 < V:
             raise ValueError(f"allowed must be an int32 [masks, words] tensor on {dev} of at least {(V + 31) // 32} consecutive words a row")
         if allowed_row is None and allowed.shape[0] != R:
             raise ValueError(f"without allowed_row there is one mask a row ({allowed.shape[0]} masks, {R} rows)")
-        l.allowed, l.n_masks, l.mask_stride = allowed.data_ptr(), allowed.shape[0], max(allowed.stride(0), allowed.shape[1])
-    l.allowed_row = _list(allowed_row, "allowed_row", torch.int32, R, dev)
+        masks = allowed.data_ptr(), allowed.shape[0], max(allowed.stride(0), allowed.shape[1])
+    l = EagleLogits(R, V, _TYPES[logits.dtype], masks[1], logits.data_ptr(), out.data_ptr(), logits.stride(0) if R > 1 else V, out.stride(0) if R > 1 else V, masks[2],
+                    _list(row_start, "row_start", torch.int32, rules.n_seqs + 1, dev), _list(path_token, "path_token", torch.int32, R, dev),
+                    _list(path_mask, "path_mask", torch.int64, R, dev), masks[0], _list(allowed_row, "allowed_row", torch.int32, R, dev))
     if R > 0:
-        _call(load_library().eagle_apply_logit_rules, dev, l, rules.c)
+        _call(_library().eagle_apply_logit_rules, dev, l, rules.c)
     return out
