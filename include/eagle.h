@@ -373,6 +373,35 @@ typedef struct {
 } eagle_logits;
 int eagle_apply_logit_rules(const eagle_logits *logits, const eagle_logit_rules *rules, void *hip_stream);
 
+/* ---- The same three inside a context ------------------------------------------------------------------------------
+ * Positions: how the target's and the head's layers turn queries and keys (null: the default again, pairs (i, i + head_dim / 2) of the whole head by cfg.rope_theta).
+ * theta of the given configuration counts, not cfg's.  Before the first EAGLE_W_Q / _K is loaded (they are laid out by pairs), EAGLE_ESTATE after that.  Keys are read
+ * back (eagle_get_kv_row) in the model's own order of elements. */
+int eagle_set_rope(eagle_ctx *ctx, const eagle_rope_config *rope_host);
+
+/* Scores of every layer of the target and the head: cap, window and slopes as in eagle_attention_args (all of them 0 / null, or rules null: plain again).  slopes is the caller's device
+ * memory and stays theirs: [n_heads], read by every pass.  Only while no slot is active (EAGLE_ESTATE otherwise).  The passes take eagle_chunk_attention's kernels then, which
+ * eagle_get_kernel_stats does not list. */
+typedef struct { float softcap; int32_t window; const float *slopes_dev; } eagle_attention_rules;
+int eagle_set_attention(eagle_ctx *ctx, const eagle_attention_rules *rules_host);
+
+/* Rules that the TARGET's logits pass before a token is chosen or a draft is accepted: the first token of a prompt, eagle_vanilla_step, and every node of eagle_verify
+ * (along the node's path); a slot's prompt counts as n_prompt.  EAGLE_BUF_LOGITS and EAGLE_BUF_VANILLA_LOGITS hold what came out.  The head's own logits are as they were: it drafts
+ * without the rules, acceptance (greedy or Alg. 1) is exact for the ruled target.  Arrays are the caller's device memory, read whenever logits are made, so they may be rewritten between
+ * calls (masks between eagle_draft_tree, which says the tree's tokens, and eagle_verify).  By slot: repetition, presence, frequency [max_batch], bias_start [max_batch + 1].
+ * allowed_row [max_batch][n_nodes]: a node's mask; node 0's serves prompts and vanilla steps too.  Any array may be null.  A mask that leaves a node nothing leaves the token
+ * that follows it unspecified.  rules null: none.  Survives eagle_reset. */
+typedef struct {
+  const float *repetition, *presence, *frequency;
+  const int32_t *bias_start, *bias_token;
+  const float *bias_value;
+  int32_t n_bias, n_masks;
+  const uint32_t *allowed;
+  int64_t mask_stride;
+  const int32_t *allowed_row;
+} eagle_context_rules;
+int eagle_set_logit_rules(eagle_ctx *ctx, const eagle_context_rules *rules_host);
+
 const char *eagle_last_error(void);   /* thread-local text of the last failure */
 const char *eagle_version(void);
 

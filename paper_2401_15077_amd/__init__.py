@@ -31,7 +31,7 @@ EXPORTS = ["eagle_workspace_bytes", "eagle_init", "eagle_free", "eagle_load_weig
            "eagle_set_hint", "eagle_set_page_table", "eagle_set_buffer", "eagle_force_tree", "eagle_expand_level",
            "eagle_force_accept", "eagle_get_buffer", "eagle_get_kv_row", "eagle_set_profiling", "eagle_get_profile", "eagle_get_kernel_stats", "eagle_probe_stream_read",
            "eagle_head_loss", "eagle_feature_noise", "eagle_rope_plan_init", "eagle_rope", "eagle_chunk_attention_workspace", "eagle_chunk_attention",
-           "eagle_apply_logit_rules", "eagle_last_error", "eagle_version"]
+           "eagle_apply_logit_rules", "eagle_set_rope", "eagle_set_attention", "eagle_set_logit_rules", "eagle_last_error", "eagle_version"]
 
 
 class EagleConfig(ctypes.Structure):
@@ -161,6 +161,8 @@ class Eagle:
         if not torch.cuda.is_available():
             raise RuntimeError("libeagle needs a GPU (no CPU fallback exists)")
         self.shape, self.device = shape, torch.device(device)
+        if self.device.type == "cuda" and self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
         self.cfg = make_config(shape, parent, rank, max_batch=max_batch, max_seq=max_seq, page_tokens=page_tokens,
                                temperature=temperature, seed=seed, kv_dtype=kv_dtype, weight_bits=weight_bits,
                                head_loss_rows=head_loss_rows)
@@ -278,6 +280,48 @@ class Eagle:
     def set_hint(self, seq: int, future: Sequence[int], alpha: float, bias: float, seed: int) -> None:
         f = np.ascontiguousarray(future, dtype=np.int32)
         self._chk(self.lib.eagle_set_hint(self.h, seq, _p32(f), len(f), alpha, bias, seed))
+
+    # -- positions, scores and logits other than the default (include/eagle.h: "The same three inside a context")
+    def set_rope(self, **config) -> None:
+        """Keywords of rope_plan (theta: the model's by default); none of them: the default again.  Before the weights are loaded."""
+        from . import operators as ops
+        if not config:
+            self._chk(self.lib.eagle_set_rope(self.h, None))
+            return
+        cfg = ops.rope_config(self.shape.head_dim, **{"theta": self.shape.rope_theta, **config})
+        self._chk(self.lib.eagle_set_rope(self.h, ctypes.byref(cfg)))
+
+    def set_attention(self, *, softcap: float = 0.0, window: int = 0, slopes=None) -> None:
+        """slopes: fp32 tensor [n_heads] on the device; kept until the next call."""
+        from . import operators as ops
+        at = ops._list(slopes, "slopes", self.torch.float32, self.shape.n_heads, self.device)
+        self._chk(self.lib.eagle_set_attention(self.h, ctypes.byref(ops.EagleAttentionRules(softcap, window, at))))
+        self._slopes = slopes
+
+    def set_logit_rules(self, *, repetition=None, presence=None, frequency=None, bias=None, allowed=None, allowed_row=None) -> None:
+        """Tensors on the device, by slot (see eagle_context_rules): fp32 repetition, presence, frequency [max_batch]; bias = (int32 start [max_batch + 1], int32 token, fp32 value);
+        int32 allowed [masks, words] with allowed_row [max_batch * n_nodes].  They are read whenever logits are made, so their contents may change between calls.  No
+        keyword: no rules."""
+        from . import operators as ops
+        t, B, dev = self.torch, self.max_batch, self.device
+        if all(x is None for x in (repetition, presence, frequency, bias, allowed, allowed_row)):
+            self._chk(self.lib.eagle_set_logit_rules(self.h, None))
+            self._rules = None
+            return
+        if (allowed is None) != (allowed_row is None):
+            raise ValueError("allowed and allowed_row belong together")
+        if allowed is not None and (allowed.dtype != t.int32 or allowed.dim() != 2 or allowed.device != dev or (allowed.stride(1) != 1 and allowed.shape[1] > 1) or allowed.shape[1] * 32 < self.shape.vocab):
+            raise ValueError(f"allowed must be an int32 [masks, words] tensor on {dev} of at least {(self.shape.vocab + 31) // 32} consecutive words a row")
+        b = bias if bias is not None else (None, None, None)
+        if bias is not None and b[1].shape != b[2].shape:
+            raise ValueError("bias tokens and values must be equally many")
+        f, i = t.float32, t.int32
+        r = ops.EagleContextRules(ops._list(repetition, "repetition", f, B, dev), ops._list(presence, "presence", f, B, dev), ops._list(frequency, "frequency", f, B, dev),
+                                  ops._list(b[0], "bias start", i, B + 1, dev), ops._list(b[1], "bias token", i, None, dev), ops._list(b[2], "bias value", f, None, dev),
+                                  b[1].shape[0] if bias is not None else 0, allowed.shape[0] if allowed is not None else 0, allowed.data_ptr() if allowed is not None else None,
+                                  max(allowed.stride(0), allowed.shape[1]) if allowed is not None else 0, ops._list(allowed_row, "allowed_row", i, B * self.M, dev))
+        self._chk(self.lib.eagle_set_logit_rules(self.h, ctypes.byref(r)))
+        self._rules = (repetition, presence, frequency, bias, allowed, allowed_row)
 
     def draft_tree(self) -> np.ndarray:
         out = np.zeros((self.n_active, self.M), np.int32)

@@ -1,6 +1,7 @@
 // libeagle: host side -- context, workspace layout, weight loading, and the orchestration of one EAGLE
 // speculative step (drafting: Sec. 3.1 / App. A.1; verification: Sec. 3.3; acceptance: Sec. 2 / App. A.2).
 #include "host.h"
+#include "operators.h"
 #include "kernels.h"
 #include "kernels2.h"
 #include "plans.h"
@@ -114,6 +115,7 @@ struct eagle_ctx {
   ~eagle_ctx() { if (res_host) (void)hipHostFree(res_host); }
   // activations
   float *h, *Q, *PT, *part_o, *part_ml;
+  size_t part_rows = 0;
   bf16_t *xf_d, *xf_2d, *xf_att, *xf_ffn;
   size_t pt_floats;
   // fast path (passes of <= 32 rows)
@@ -129,6 +131,12 @@ struct eagle_ctx {
   int n_cu = 256;                      // compute units of the device (queried by eagle_init; 256 assumed when no device is visible)
   int device = 0;
   void* static_scratch = nullptr;      // this device's address of the library's static scratch array
+  // positions, scores and logit rules other than the default (eagle_set_rope, eagle_set_attention, eagle_set_logit_rules)
+  int rope_mode = PACK_ROPE;           // how rows of q and k are paired
+  bool attn_ruled = false; eagle_attention_rules attn_rules{};
+  bool logits_ruled = false; eagle_context_rules logit_rules{};
+  int *op_start, *op_len, *op_base, *op_prompt, *op_tokens, *op_mask_row, *op_verify_start; unsigned long long *op_mask, *op_path;
+  std::vector<int> h_prompt;           // prompt length by slot
   // training loss of the head (cfg.head_loss_rows > 0): the LM head re-tiled as [d_model rows][vocab columns], the
   // gradient of one pass's logits as a GEMM input, per-row losses of a pass, the running sums of a call
   PackedW lm_head_T; bf16_t* hl_dz = nullptr; float* hl_row_loss = nullptr; double* hl_acc = nullptr; int hl_chunk = 0;
@@ -326,6 +334,8 @@ static size_t layout(eagle_ctx* c) {
   c->xf2_att = a.take<bf16_t>((size_t)c->NXP * 32 * H * dh);
   c->xf2_ffn = a.take<bf16_t>((size_t)c->NXP * 32 * F * (two ? g.n_experts : 1));
   c->facts = a.take<RowFact>(Mm);
+  c->op_start = a.take<int>(B + 1); c->op_len = a.take<int>(B); c->op_base = a.take<int>(B); c->op_prompt = a.take<int>(B); c->op_tokens = a.take<int>(B);
+  c->op_mask_row = a.take<int>(B); c->op_verify_start = a.take<int>(B + 1); c->op_mask = a.take<unsigned long long>(Mm); c->op_path = a.take<unsigned long long>((size_t)B * M);
   c->ssq1 = a.take<float>(PLAN_MAX_NORM_GROUPS * 32); c->ssq2 = a.take<float>(PLAN_MAX_NORM_GROUPS * 32);
   c->trace = a.take<unsigned long long>(1024 * 8);
   c->cnt_gemm = a.take<int>(1024 * COUNTER_STRIDE); c->cnt_attn = a.take<int>((size_t)128 * H * COUNTER_STRIDE);
@@ -372,6 +382,7 @@ static size_t layout(eagle_ctx* c) {
     const int s = std::min(16, c->n_cu / (H * rb));
     if (s > 1) part_rows = std::max(part_rows, (size_t)32 * rb * s);
   }
+  c->part_rows = part_rows;
   c->part_o = a.take<float>(part_rows * H * dh);
   c->part_ml = a.take<float>(part_rows * H * 2);
   return (a.off + 255) & ~(size_t)255;
@@ -448,6 +459,28 @@ extern "C" size_t eagle_workspace_bytes(const eagle_config* cfg) {
 extern "C" const char* eagle_last_error(void) { return g_err; }
 extern "C" const char* eagle_version(void) { return "libeagle 0.1 (gfx950)"; }
 
+// Cosines and sines of every position: plan null: angle = pos * theta^(-2i/dh) formed in fp64, rounded once to fp32; else of the plan's pairs (pairs that
+// do not turn: 1 and 0).  Synchronises.
+static int upload_rope(eagle_ctx* c, const eagle_rope_plan* plan) {
+  const eagle_config& g = c->cfg;
+  const int half = g.head_dim / 2;
+  std::vector<float> cs((size_t)g.max_seq * half), sn((size_t)g.max_seq * half);
+  for (int p = 0; p < g.max_seq; ++p)
+    for (int i = 0; i < half; ++i) {
+      float &x = cs[(size_t)p * half + i], &y = sn[(size_t)p * half + i];
+      if (plan && i >= plan->rot_dim / 2) { x = 1.f; y = 0.f; continue; }
+      const double ang = plan ? (double)(int64_t)((uint64_t)p * plan->turn[i]) * (6.283185307179586477 / 18446744073709551616.0)   // (the product wraps at whole turns)
+                              : (double)p * std::pow((double)g.rope_theta, -2.0 * i / g.head_dim);
+      const double m = plan ? plan->mscale : 1.0;
+      x = (float)(std::cos(ang) * m);
+      y = (float)(std::sin(ang) * m);
+    }
+  if (hipMemcpyAsync(c->rope_cos, cs.data(), cs.size() * 4, hipMemcpyHostToDevice, c->stream) != hipSuccess ||
+      hipMemcpyAsync(c->rope_sin, sn.data(), sn.size() * 4, hipMemcpyHostToDevice, c->stream) != hipSuccess ||
+      hipStreamSynchronize(c->stream) != hipSuccess) return fail(EAGLE_EHIP, "rope table upload failed");
+  return EAGLE_OK;
+}
+
 extern "C" int eagle_init(const eagle_config* cfg, void* workspace_dev, size_t workspace_bytes, void* hip_stream, eagle_ctx** out) {
   if (!out) return fail(EAGLE_EINVAL, "out is null");
   *out = nullptr;
@@ -477,6 +510,7 @@ extern "C" int eagle_init(const eagle_config* cfg, void* workspace_dev, size_t w
   c->cfg.parent = nullptr; c->cfg.rank = nullptr;
   memset(c->loaded, 0, sizeof(c->loaded));
   c->loaded_layer.assign(EAGLE_W_COUNT, std::vector<char>(g.n_layers + 1, 0));
+  c->h_prompt.assign(g.max_batch, 0);
   c->h_ctx.assign(g.max_batch, 0); c->h_ntok.assign(g.max_batch, 0); c->active.assign(g.max_batch, 0); c->head_stale.assign(g.max_batch, 0);
   // zero everything that is not a weight (finite garbage-free caches and padding rows)
   char* z0 = (char*)c->kc;
@@ -488,20 +522,8 @@ extern "C" int eagle_init(const eagle_config* cfg, void* workspace_dev, size_t w
     const size_t span = (size_t)((const char*)(c->len_out + c->cfg.max_batch) - (const char*)c->path);
     if (hipHostMalloc(&c->res_host, span, hipHostMallocDefault) != hipSuccess) { c->res_host = nullptr; delete c; return fail(EAGLE_ENOMEM, "pinned result buffer"); }
   }
-  // RoPE tables: angle = pos * theta^(-2i/dh) formed in fp64, rounded once to fp32
-  {
-    const int half = g.head_dim / 2;
-    std::vector<float> cs((size_t)g.max_seq * half), sn((size_t)g.max_seq * half);
-    for (int p = 0; p < g.max_seq; ++p)
-      for (int i = 0; i < half; ++i) {
-        double ang = (double)p * std::pow((double)g.rope_theta, -2.0 * i / g.head_dim);
-        cs[(size_t)p * half + i] = (float)std::cos(ang);
-        sn[(size_t)p * half + i] = (float)std::sin(ang);
-      }
-    if (hipMemcpyAsync(c->rope_cos, cs.data(), cs.size() * 4, hipMemcpyHostToDevice, c->stream) != hipSuccess ||
-        hipMemcpyAsync(c->rope_sin, sn.data(), sn.size() * 4, hipMemcpyHostToDevice, c->stream) != hipSuccess ||
-        hipStreamSynchronize(c->stream) != hipSuccess) { delete c; return fail(EAGLE_EHIP, "rope table upload failed"); }
-  }
+  rc = upload_rope(c, nullptr);
+  if (rc) { delete c; return rc; }
   {  // static paging: logical page lp of slot s lives in physical page lp*max_batch + s (interleaved on purpose)
     std::vector<int> pt((size_t)g.max_batch * c->pps);
     for (int s = 0; s < g.max_batch; ++s)
@@ -538,9 +560,9 @@ extern "C" void eagle_free(eagle_ctx* c) {
 static int pack_into(eagle_ctx* c, const void* src, PackedW& w, int N, int K, int row_offset, int mode = PACK_PLAIN) {
   if (K != w.K || row_offset % 32) return fail(EAGLE_EINVAL, "internal: pack shape mismatch");
   int last = mode == PACK_PLAIN ? row_offset + (N + 31) / 32 * 32 : row_offset + pack_row_map(mode, N - 1, c->cfg.head_dim) + 1;
-  if (mode == PACK_ROPE) last = row_offset + N;
+  if ((mode & 15) == PACK_ROPE) last = row_offset + N;
   if (last > w.Npad) return fail(EAGLE_EINVAL, "internal: packed rows overflow");
-  if (mode == PACK_ROPE && N % c->cfg.head_dim) return fail(EAGLE_EINVAL, "internal: rope packing needs whole heads");
+  if ((mode & 15) == PACK_ROPE && N % c->cfg.head_dim) return fail(EAGLE_EINVAL, "internal: rope packing needs whole heads");
   if ((mode == PACK_GATE || mode == PACK_UP) && N % 16) return fail(EAGLE_EINVAL, "d_ffn must be a multiple of 16");
   if (w.q4) {
     const size_t items = (size_t)(mode == PACK_PLAIN ? (N + 31) / 32 * 32 : N) * w.NG;
@@ -594,8 +616,8 @@ extern "C" int eagle_load_weight(eagle_ctx* c, int32_t which, int32_t layer, con
   switch (which) {
     case EAGLE_W_ATTN_NORM: HIPCHK(hipMemcpyAsync(w.attn_norm, src, (size_t)d * 4, hipMemcpyDeviceToDevice, c->stream)); break;
     case EAGLE_W_MLP_NORM: HIPCHK(hipMemcpyAsync(w.mlp_norm, src, (size_t)d * 4, hipMemcpyDeviceToDevice, c->stream)); break;
-    case EAGLE_W_Q: rc = pack_into(c, src, w.qkv, H * dh, d, 0, PACK_ROPE); break;
-    case EAGLE_W_K: rc = pack_into(c, src, w.qkv, KVH * dh, d, H * dh, PACK_ROPE); break;
+    case EAGLE_W_Q: rc = pack_into(c, src, w.qkv, H * dh, d, 0, c->rope_mode); break;
+    case EAGLE_W_K: rc = pack_into(c, src, w.qkv, KVH * dh, d, H * dh, c->rope_mode); break;
     case EAGLE_W_V: rc = pack_into(c, src, w.qkv, KVH * dh, d, (H + KVH) * dh); break;
     case EAGLE_W_O: rc = pack_into(c, src, w.o, d, H * dh, 0); break;
     case EAGLE_W_ROUTER:
@@ -817,6 +839,35 @@ static int resnorm(eagle_ctx* c, int M, int MT, const float* h_in, const float* 
   return EAGLE_OK;
 }
 
+// Attention under eagle_set_attention: the pass as a chunk over the layer's cache (pass_chunk), in place over the queries, then re-laid as input of the output projection.
+static int pass_chunk(eagle_ctx* c, const Pass& pass, int n_new) {
+  if (!c->attn_ruled) return EAGLE_OK;
+  k_pass_chunk<<<1, 256, 0, c->stream>>>(c->facts, pass.kind, pass.n_seq, pass.rows_per_seq, n_new, pass.chunk_start + pass.chunk_n, c->op_start, c->op_len, c->op_base, c->op_mask);
+  LAUNCH_CHECK();
+  return EAGLE_OK;
+}
+static int ruled_attention(eagle_ctx* c, const Pass& pass, int M, int MT, const KVCache& kv, int max_keys, bf16_t* xf) {
+  const eagle_config& g = c->cfg;
+  const int H = g.n_heads, dh = g.head_dim;
+  const bool prompt = pass.kind >= PASS_PREFILL_T;
+  eagle_chunk ch{};
+  ch.n_seqs = pass.n_seq; ch.n_rows = M; ch.max_rows = pass.rows_per_seq; ch.max_keys = std::min(max_keys, c->pps << c->page_shift);
+  ch.row_start = c->op_start; ch.key_len = c->op_len;
+  if (!prompt) { ch.tree_base = c->op_base; ch.tree_mask = (const uint64_t*)c->op_mask; }
+  eagle_paged_kv pk{};
+  pk.k = kv.k; pk.v = kv.v; pk.dtype = c->kv_f32 ? EAGLE_F32 : EAGLE_BF16; pk.n_kv_heads = g.n_kv_heads; pk.head_dim = dh; pk.page_tokens = g.page_tokens;
+  pk.n_pages = g.max_batch * c->pps; pk.pages_per_seq = c->pps; pk.token_stride = dh; pk.head_stride = (int64_t)g.page_tokens * dh; pk.page_stride = pk.head_stride * g.n_kv_heads;
+  pk.table_stride = c->pps; pk.page_table = c->page_table + (size_t)pass.seq0 * c->pps;
+  eagle_attention_args aa{};
+  aa.n_heads = H; aa.dtype = EAGLE_F32; aa.window = c->attn_rules.window; aa.q = c->Q; aa.out = c->Q; aa.q_row = aa.out_row = (int64_t)H * dh; aa.q_head = aa.out_head = dh;
+  aa.scale = 1.0f / std::sqrt((float)dh); aa.softcap = c->attn_rules.softcap; aa.slopes = c->attn_rules.slopes_dev;
+  const int rc = chunk_attention(&aa, &ch, &pk, c->part_o, (size_t)((char*)(c->part_ml + c->part_rows * H * 2) - (char*)c->part_o), true, c->stream);
+  if (rc) return rc;
+  k_rows_to_xf<<<dim3(M, (H * dh + 2047) / 2048), 256, 0, c->stream>>>(c->Q, 0, xf, MT, c->NXP, H * dh);
+  LAUNCH_CHECK();
+  return EAGLE_OK;
+}
+
 // One decoder layer on the rows of `pass` (h and xf_d hold the residual stream and its normalised copy).
 // next_gain: the RMSNorm gain applied to the layer's output for whoever consumes it next (nullptr = none).
 static int layer_forward(eagle_ctx* c, const Pass& pass, int M, int MT, int li, int t_max, int n_new, const float* next_gain, float* xout) {
@@ -832,7 +883,8 @@ static int layer_forward(eagle_ctx* c, const Pass& pass, int M, int MT, int li, 
     else k_qkv_rope_store<bf16_t><<<grid, 256, 0, c->stream>>>(c->facts, c->PT, S, w.qkv.N, w.qkv.Npad, MT * 32, c->rope_cos, c->rope_sin, c->Q, kv, H);
     LAUNCH_CHECK();
   }
-  {
+  if (c->attn_ruled) { if ((rc = ruled_attention(c, pass, M, MT, kv, t_max, c->xf_att))) return rc; }
+  else {
     // the MFMA attention kernel of the fast path, one work-group per (KV split, head, sequence x 32-row block)
     int rblocks = (pass.rows_per_seq + 31) / 32;
     int n_splits = attn_splits(c, t_max, H * pass.n_seq * rblocks);
@@ -935,6 +987,7 @@ static int target_forward(eagle_ctx* c, const Pass& pass, int t_max, int n_new, 
   if (c->f32) k_embed<float><<<M, 256, 0, c->stream>>>(pass, c->tree_d, c->st, c->tree_tok, (const float*)c->embed, c->h, g.d_model, g.vocab, kv_for(c, 0), c->facts);
   else k_embed<bf16_t><<<M, 256, 0, c->stream>>>(pass, c->tree_d, c->st, c->tree_tok, (const bf16_t*)c->embed, c->h, g.d_model, g.vocab, kv_for(c, 0), c->facts);
   LAUNCH_CHECK();
+  if ((rc = pass_chunk(c, pass, n_new))) return rc;
   if ((rc = resnorm(c, M, MT, c->h, nullptr, 0, 0, nullptr, c->layers[0].attn_norm, c->xf_d, nullptr))) return rc;
   for (int l = 0; l < g.n_layers; ++l) {
     bool last = l + 1 == g.n_layers;
@@ -976,6 +1029,7 @@ static int head_forward(eagle_ctx* c, const Pass& pass, int t_max, int n_new, bo
   if (c->f32) k_fc_input<float><<<dim3(M, 4), 256, 0, c->stream>>>(pass, c->tree_d, c->st, c->tree_tok, c->pend_f, c->node_f, c->chunk_f, (const float*)c->embed, c->xf_2d, g.d_model, g.vocab, MT, c->NXP, kv_for(c, g.n_layers), c->facts, level_parents(c, pass));
   else k_fc_input<bf16_t><<<dim3(M, 4), 256, 0, c->stream>>>(pass, c->tree_d, c->st, c->tree_tok, c->pend_f, c->node_f, c->chunk_f, (const bf16_t*)c->embed, c->xf_2d, g.d_model, g.vocab, MT, c->NXP, kv_for(c, g.n_layers), c->facts, level_parents(c, pass));
   LAUNCH_CHECK();
+  if ((rc = pass_chunk(c, pass, n_new))) return rc;
   if ((rc = (c->cur_class = KC_FC, gemm(c, c->fc, c->xf_2d, MT, M, &S)))) return rc;
   const float* bias = c->loaded_layer[EAGLE_W_FC_BIAS][0] ? c->fc_bias : nullptr;
   if ((rc = resnorm(c, M, MT, nullptr, c->PT, S, c->fc.Npad, bias, c->layers[g.n_layers].attn_norm, c->xf_d, nullptr))) return rc;
@@ -1211,7 +1265,8 @@ static int layer2(eagle_ctx* c, const Pass& pass, int M, int li, int ctx_max, in
   Gemm2 g = gemm2_base(c, M);
   g.epi = EPI_QKV; g.in_scale = scale_of(c, c->ssq2, c->ssq2_groups); g.kv = kv_for(c, li);
   if ((rc = (c->cur_class = KC_QKV, gemm2(c, w.qkv, c->xf2_d, g, nullptr)))) return rc;
-  {
+  if (c->attn_ruled) { if ((rc = ruled_attention(c, pass, M, 1, kv_for(c, li), ctx_max + n_new, c->xf2_att))) return rc; }
+  else {
     int n_splits = attn_splits(c, ctx_max + 64, H * pass.n_seq);
     unsigned long long* atrace = (c->attn_no++ == c->attn_trace_sel && n_splits * H <= 1024) ? c->trace : nullptr;
     dim3 grid(n_splits, H, pass.n_seq);
@@ -1286,6 +1341,7 @@ static int target_forward2(eagle_ctx* c, const Pass& pass, int ctx_max, int n_ne
   else k2_embed<bf16_t, 2><<<eg, 256, 0, c->stream>>>(pass, c->tree_d, c->st, c->tree_tok, (const bf16_t*)c->embed, cf.vocab, M, c->M, d, c->h2, c->layers[0].attn_norm, c->xf2_d, c->ssq2, kv_for(c, 0), c->facts);
   LAUNCH_CHECK();
   c->ssq2_groups = eg;
+  if ((rc = pass_chunk(c, pass, n_new))) return rc;
   for (int l = 0; l < cf.n_layers; ++l)
     if ((rc = layer2(c, pass, M, l, ctx_max, n_new, l + 1 < cf.n_layers ? c->layers[l + 1].attn_norm : c->final_norm))) return rc;
   k2_features<<<M, 256, 0, c->stream>>>(pass, c->tree_d, c->st, c->h2, scale_of(c, c->ssq2, c->ssq2_groups), c->final_norm, d, c->F, c->pend_f, c->chunk_f);
@@ -1301,6 +1357,7 @@ static int head_forward2(eagle_ctx* c, const Pass& pass, int ctx_max, int n_new,
   if (c->f32) k_fc_input<float><<<dim3(M, 4), 256, 0, c->stream>>>(pass, c->tree_d, c->st, c->tree_tok, c->pend_f, c->node_f, c->chunk_f, (const float*)c->embed, c->xf2_2d, d, cf.vocab, 1, c->NXP, kv_for(c, cf.n_layers), c->facts, level_parents(c, pass));
   else k_fc_input<bf16_t><<<dim3(M, 4), 256, 0, c->stream>>>(pass, c->tree_d, c->st, c->tree_tok, c->pend_f, c->node_f, c->chunk_f, (const bf16_t*)c->embed, c->xf2_2d, d, cf.vocab, 1, c->NXP, kv_for(c, cf.n_layers), c->facts, level_parents(c, pass));
   LAUNCH_CHECK();
+  if ((rc = pass_chunk(c, pass, n_new))) return rc;
   Gemm2 g = gemm2_base(c, M);
   g.epi = EPI_RESID; g.h_in = nullptr; g.h_out = c->h2; g.bias = c->loaded_layer[EAGLE_W_FC_BIAS][0] ? c->fc_bias : nullptr;
   g.gain_next = c->layers[cf.n_layers].attn_norm; g.xf_out = c->xf2_d; g.xf_KS = d / 16; g.ssq_out = c->ssq2;
@@ -1312,6 +1369,33 @@ static int head_forward2(eagle_ctx* c, const Pass& pass, int ctx_max, int n_new,
     LAUNCH_CHECK();
   }
   return lm_head2(c, M, false, c->draft_logits);
+}
+
+// The rules of eagle_set_logit_rules on the logits of slots seq0 .. seq0 + n - 1: a row a slot (vanilla_logits), or a row a tree node (L).
+static int rule_logits(eagle_ctx* c, int seq0, int n, bool nodes, const int* n_tokens) {
+  if (!c->logits_ruled) return EAGLE_OK;
+  const eagle_config& g = c->cfg;
+  const eagle_context_rules& r = c->logit_rules;
+  const int M = c->M;
+  eagle_logits l{};
+  l.n_rows = nodes ? n * M : n; l.vocab = g.vocab; l.dtype = EAGLE_F32; l.in_stride = l.out_stride = g.vocab;
+  l.out = nodes ? c->L : c->vanilla_logits + (size_t)seq0 * g.vocab;
+  l.in = l.out;
+  if (nodes) { l.row_start = c->op_verify_start; l.path_token = c->tree_tok; l.path_mask = (const uint64_t*)c->op_path; }
+  if (r.allowed) {
+    l.allowed = r.allowed; l.n_masks = r.n_masks; l.mask_stride = r.mask_stride;
+    l.allowed_row = r.allowed_row + (size_t)seq0 * M;
+    if (!nodes && n > 1) {                                        // node 0's of every slot, side by side
+      k_node0_rows<<<1, 64, 0, c->stream>>>(l.allowed_row, M, n, c->op_mask_row);
+      LAUNCH_CHECK();
+      l.allowed_row = c->op_mask_row;
+    }
+  }
+  eagle_logit_rules lr{};
+  lr.n_seqs = n; lr.tokens = c->st.tokens + (size_t)seq0 * c->st.tok_stride; lr.token_stride = c->st.tok_stride; lr.n_tokens = n_tokens + seq0; lr.n_prompt = c->op_prompt + seq0;
+  lr.repetition = r.repetition ? r.repetition + seq0 : nullptr; lr.presence = r.presence ? r.presence + seq0 : nullptr; lr.frequency = r.frequency ? r.frequency + seq0 : nullptr;
+  if (r.bias_token) { lr.bias_start = r.bias_start + seq0; lr.bias_token = r.bias_token; lr.bias_value = r.bias_value; lr.n_bias = r.n_bias; }
+  return eagle_apply_logit_rules(&l, &lr, c->stream);
 }
 
 // The next token of n sequences from seq0 on, from their rows of vanilla_logits.
@@ -1365,6 +1449,12 @@ extern "C" int eagle_prefill(eagle_ctx* c, int32_t seq, const int32_t* prompt, i
     if ((rc = fast ? target_forward2(c, pt, start + cn, cn, c->vanilla_logits, last)
                    : target_forward(c, pt, start + cn, cn, last, c->vanilla_logits, 1, 1))) return rc;
     if (last) {
+      if (c->logits_ruled) {
+        k_fill_u32<<<1, 64, 0, c->stream>>>((uint32_t*)c->op_prompt + seq, (uint32_t)n, 1);
+        k_fill_u32<<<1, 64, 0, c->stream>>>((uint32_t*)c->op_tokens + seq, (uint32_t)n, 1);
+        LAUNCH_CHECK();
+        if ((rc = rule_logits(c, seq, 1, false, c->op_tokens))) return rc;
+      }
       if ((rc = choose(c, 1, seq, 1, n))) return rc;
       HIPCHK(hipMemcpyAsync(c->pend_f + (size_t)seq * (c->D + 1) * g.d_model, c->chunk_f + (size_t)(cn - 1) * g.d_model,
                             (size_t)g.d_model * 4, hipMemcpyDeviceToDevice, c->stream));
@@ -1380,6 +1470,7 @@ extern "C" int eagle_prefill(eagle_ctx* c, int32_t seq, const int32_t* prompt, i
   HIPCHK(hipMemcpyAsync(&tok, c->st.tokens + (size_t)seq * c->st.tok_stride + n, 4, hipMemcpyDeviceToHost, c->stream));
   HIPCHK(hipStreamSynchronize(c->stream));
   if (first_token) *first_token = tok;
+  c->h_prompt[seq] = n;
   c->h_ctx[seq] = n; c->h_ntok[seq] = n + 1; c->active[seq] = 1; c->head_stale[seq] = 0;
   c->n_active = seq + 1; c->phase = 0;
   return EAGLE_OK;
@@ -1453,6 +1544,53 @@ extern "C" int eagle_set_hint(eagle_ctx* c, int32_t seq, const int32_t* future, 
   HIPCHK(hipMemcpyAsync(c->hint_bias + seq, &bias, 4, hipMemcpyHostToDevice, c->stream));
   HIPCHK(hipMemcpyAsync(c->hint_seed + seq, &s64, 8, hipMemcpyHostToDevice, c->stream));
   HIPCHK(hipStreamSynchronize(c->stream));
+  return EAGLE_OK;
+}
+
+extern "C" int eagle_set_rope(eagle_ctx* c, const eagle_rope_config* rope) {
+  if (!c) return fail(EAGLE_EINVAL, "null context");
+  for (int w : {(int)EAGLE_W_Q, (int)EAGLE_W_K})
+    for (char loaded : c->loaded_layer[w])
+      if (loaded) return fail(EAGLE_ESTATE, "eagle_set_rope must come before the query and key matrices are loaded (they are laid out by pairs)");
+  if (!rope) {
+    const int rc = upload_rope(c, nullptr);
+    if (!rc) c->rope_mode = PACK_ROPE;
+    return rc;
+  }
+  if (rope->head_dim != c->cfg.head_dim) return fail(EAGLE_EINVAL, "head_dim %d of the positions is not the model's %d", rope->head_dim, c->cfg.head_dim);
+  eagle_rope_plan plan;
+  int rc = eagle_rope_plan_init(rope, &plan);
+  if (rc || (rc = upload_rope(c, &plan))) return rc;
+  c->rope_mode = rope_pack(plan.rot_dim, plan.interleaved);
+  return EAGLE_OK;
+}
+
+extern "C" int eagle_set_attention(eagle_ctx* c, const eagle_attention_rules* r) {
+  if (!c) return fail(EAGLE_EINVAL, "null context");
+  if (c->n_active != 0) return fail(EAGLE_ESTATE, "the attention rules can only change while no sequence is active (after eagle_init / eagle_reset)");
+  if (r && (!(r->softcap >= 0.f) || !std::isfinite(r->softcap) || r->window < 0)) return fail(EAGLE_EINVAL, "softcap must be >= 0 and finite, window >= 0");
+  c->attn_rules = r ? *r : eagle_attention_rules{};
+  c->attn_ruled = r && (r->softcap > 0.f || r->window > 0 || r->slopes_dev);
+  return EAGLE_OK;
+}
+
+extern "C" int eagle_set_logit_rules(eagle_ctx* c, const eagle_context_rules* r) {
+  if (!c) return fail(EAGLE_EINVAL, "null context");
+  if (r) {
+    if (r->bias_token && (!r->bias_start || !r->bias_value || r->n_bias < 0)) return fail(EAGLE_EINVAL, "biases need bias_start, bias_value and n_bias >= 0");
+    if (r->allowed && (!r->allowed_row || r->n_masks < 1 || r->mask_stride < (c->cfg.vocab + 31) / 32)) return fail(EAGLE_EINVAL, "masks need allowed_row, n_masks >= 1 and %d words a row", (c->cfg.vocab + 31) / 32);
+    const int B = c->cfg.max_batch;
+    std::vector<int> start(B + 1);
+    std::vector<unsigned long long> path((size_t)B * c->M);
+    for (int s = 0; s <= B; ++s) start[s] = s * c->M;
+    for (size_t i = 0; i < path.size(); ++i) path[i] = c->tree_h.anc[i % c->M] & ~1ull;   // (the root is the last committed token)
+    HIPCHK(hipMemcpyAsync(c->op_verify_start, start.data(), start.size() * 4, hipMemcpyHostToDevice, c->stream));
+    HIPCHK(hipMemcpyAsync(c->op_path, path.data(), path.size() * 8, hipMemcpyHostToDevice, c->stream));
+    HIPCHK(hipMemcpyAsync(c->op_prompt, c->h_prompt.data(), (size_t)B * 4, hipMemcpyHostToDevice, c->stream));
+    HIPCHK(hipStreamSynchronize(c->stream));
+  }
+  c->logit_rules = r ? *r : eagle_context_rules{};
+  c->logits_ruled = r != nullptr;
   return EAGLE_OK;
 }
 
@@ -1535,6 +1673,7 @@ static int do_verify(eagle_ctx* c) {
     rc = target_forward(c, pv, max_ctx(c) + c->M, c->M, true, c->L, 0, 0);
   }
   if (rc) return rc;
+  if ((rc = rule_logits(c, 0, c->n_active, true, c->st.n_tok))) return rc;
   c->phase = 2;
   return EAGLE_OK;
 }
@@ -1689,6 +1828,7 @@ extern "C" int eagle_vanilla_step(eagle_ctx* c, int32_t* tokens) {
   pass_ctx(c, pv);
   if ((rc = (B <= 32 ? target_forward2(c, pv, max_ctx(c), 1, c->vanilla_logits)
                      : target_forward(c, pv, max_ctx(c) + 1, 1, true, c->vanilla_logits, 1, 0)))) return rc;
+  if ((rc = rule_logits(c, 0, B, false, c->st.n_tok))) return rc;
   if ((rc = choose(c, B, 0, 0, 0))) return rc;
   std::vector<int> tk(B);
   for (int s = 0; s < B; ++s)
@@ -1857,6 +1997,17 @@ extern "C" int eagle_get_kv_row(eagle_ctx* c, int32_t seq, int32_t layer, int32_
   HIPCHK(hipMemcpyAsync(k_host, tmp, (size_t)n * 4, hipMemcpyDeviceToHost, c->stream));
   HIPCHK(hipMemcpyAsync(v_host, tmp + n, (size_t)n * 4, hipMemcpyDeviceToHost, c->stream));
   HIPCHK(hipStreamSynchronize(c->stream));
+  if (c->rope_mode != PACK_ROPE) {                                // the cache holds pair p's members at p and p + head_dim / 2
+    const int dh = g.head_dim;
+    float head[128];
+    for (int h = 0; h < g.n_kv_heads; ++h) {
+      memcpy(head, k_host + (size_t)h * dh, dh * 4);
+      for (int r = 0; r < dh; ++r) {
+        const int at = rope_pair(c->rope_mode, r, dh);
+        k_host[(size_t)h * dh + r] = head[(at >> 1) + (at & 1) * (dh / 2)];
+      }
+    }
+  }
   return EAGLE_OK;
 }
 

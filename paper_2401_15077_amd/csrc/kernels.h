@@ -226,16 +226,21 @@ __device__ inline unsigned long long block_max_key(unsigned long long k, unsigne
 // plane p starts at dst + p*plane_stride.  Source row n lands in packed row row_offset + map(n):
 //   PACK_PLAIN  map(n) = n
 //   PACK_ROPE   rows of a head are interleaved so that the two members of a rotate-half pair (i, i + dh/2) become
-//               neighbours: head*dh + i + half*dh/2  ->  head*dh + 2i + half
+//               neighbours: head*dh + i + half*dh/2  ->  head*dh + 2i + half.  rope_pack() names other pairs: of the first
+//               `rot` rows of a head only, or neighbouring rows; the rest of the head pairs up as it comes
 //   PACK_GATE / PACK_UP  fused gate/up matrix: every 32-row block holds gate rows 16j..16j+15 then up rows
 //               16j..16j+15, so SwiGLU partners sit in the same block
 // One thread builds one 16-byte lane chunk (8 elements along k) of every plane.
 enum { PACK_PLAIN = 0, PACK_ROPE = 1, PACK_GATE = 2, PACK_UP = 3 };
+__host__ __device__ inline int rope_pack(int rot, int interleaved) { return PACK_ROPE | interleaved << 4 | rot << 8; }
+// Member (0 or 1) and number of the pair that row r of a head belongs to, as 2 * number + member.
+__host__ __device__ inline int rope_pair(int mode, int r, int dh) {
+  const int rot = mode >> 8 ? mode >> 8 : dh, half = rot >> 1;
+  if (mode >> 4 & 1 || r >= rot) return r;
+  return 2 * (r % half) + r / half;
+}
 __host__ __device__ inline int pack_row_map(int mode, int n, int dh) {
-  if (mode == PACK_ROPE) {
-    int head = n / dh, r = n % dh, half = dh >> 1;
-    return head * dh + 2 * (r % half) + r / half;
-  }
+  if ((mode & 15) == PACK_ROPE) return n / dh * dh + rope_pair(mode, n % dh, dh);
   if (mode == PACK_GATE) return (n >> 4) * 32 + (n & 15);
   if (mode == PACK_UP) return (n >> 4) * 32 + 16 + (n & 15);
   return n;
@@ -1194,6 +1199,28 @@ __global__ __launch_bounds__(256) void k_qkv_rope_store(const RowFact* __restric
 }
 
 // (Tree-masked paged attention for both paths is k2_attn, in kernels2.h.)
+
+// The pass in flight as a chunk over the cache (for the attention of eagle_set_attention): decoding passes as trees -- the pending rows' masks are all rows up to
+// their own -- and prompts as consecutive tokens.  One block.
+__global__ __launch_bounds__(256) void k_pass_chunk(const RowFact* __restrict__ facts, int kind, int n_seq, int rows_per_seq, int n_new, int prompt_keys,
+                                                    int* row_start, int* key_len, int* base, unsigned long long* mask) {
+  const bool prompt = kind >= PASS_PREFILL_T;
+  for (int s = threadIdx.x; s <= n_seq; s += blockDim.x) {
+    row_start[s] = s * rows_per_seq;
+    if (s == n_seq) break;
+    const int b = facts[s * rows_per_seq].base;
+    base[s] = b;
+    key_len[s] = prompt ? prompt_keys : b + n_new;
+  }
+  if (!prompt)
+    for (int r = threadIdx.x; r < n_seq * rows_per_seq; r += blockDim.x) {
+      const RowFact f = facts[r];
+      mask[r] = kind == PASS_DRAFT_PENDING ? (2ull << f.rel) - 1ull : (unsigned long long)f.mask_hi << 32 | f.mask_lo;
+    }
+}
+__global__ void k_node0_rows(const int* __restrict__ allowed_row, int M, int B, int* out) {
+  for (int s = threadIdx.x; s < B; s += blockDim.x) out[s] = allowed_row[s * M];
+}
 
 // ============================================================================ SwiGLU and logits epilogues
 // act[r][k] = silu(gate) * up with the fused matrix's row order (PACK_GATE / PACK_UP)   (F = d_ffn)

@@ -1,5 +1,5 @@
 // libeagle: operators on the caller's own tensors (host side): argument checks, launch shapes.
-#include "host.h"
+#include "operators.h"
 #include "rope.h"
 #include "chunk_attn.h"
 #include "logit_rules.h"
@@ -173,28 +173,30 @@ static int check_attention(const eagle_attention_args* a, const eagle_chunk* chu
 // Work-groups that the token range is split for where sequences, kv heads and column blocks are fewer, and the fewest tiles of a part.
 constexpr int ATTN_WIDE_WGS = 512, ATTN_NARROW_WGS = 2048, ATTN_MIN_TILES = 4;
 
-// Columns and parts of a call; returns the bytes of workspace.
-static size_t plan_attention(ChunkAttnDev* d, int elt, int kv_elt, bool* wide) {
+// Columns and parts of a call; returns the bytes of workspace, at most `limit` of them if that is possible.
+static size_t plan_attention(ChunkAttnDev* d, int kv_dtype, size_t limit, bool* wide) {
   const int g = d->H / d->kv.n_kv_heads;
   const long long cols = (long long)d->chunk.max_rows * g;
   *wide = cols > 32;
-  const int KT = *wide && kv_elt == 2 ? 64 : 32;
+  const int KT = *wide && kv_dtype == EAGLE_BF16 ? 64 : 32;
   d->col_blocks = (int)((cols + (*wide ? 127 : 31)) / (*wide ? 128 : 32));
   const long long units = (long long)d->col_blocks * d->kv.n_kv_heads * d->chunk.n_seqs, tiles = ((long long)d->chunk.max_keys + KT - 1) / KT;
-  const long long parts = std::max(1ll, std::min((*wide ? ATTN_WIDE_WGS : ATTN_NARROW_WGS) / units, tiles / ATTN_MIN_TILES));
-  d->split_tiles = (int)((tiles + parts - 1) / parts);
-  d->splits = (int)((tiles + d->split_tiles - 1) / d->split_tiles);
-  if (d->splits == 1) return 256;
-  const size_t pairs = (size_t)d->chunk.n_rows * d->H * d->splits, DH = d->kv.head_dim <= 64 ? 64 : 128;
-  (void)elt;
-  return (pairs * 8 + 255) / 256 * 256 + pairs * DH * 4 + 256;
+  long long parts = std::max(1ll, std::min((*wide ? ATTN_WIDE_WGS : ATTN_NARROW_WGS) / units, tiles / ATTN_MIN_TILES));
+  const size_t pairs = (size_t)d->chunk.n_rows * d->H, DH = d->kv.head_dim <= 64 ? 64 : 128;
+  for (;; --parts) {
+    d->split_tiles = (int)((tiles + parts - 1) / parts);
+    d->splits = (int)((tiles + d->split_tiles - 1) / d->split_tiles);
+    if (d->splits == 1) return 256;
+    const size_t bytes = (pairs * d->splits * 8 + 255) / 256 * 256 + pairs * d->splits * DH * 4;
+    if (bytes <= limit) return bytes;
+  }
 }
 
 extern "C" size_t eagle_chunk_attention_workspace(const eagle_attention_args* a, const eagle_chunk* chunk, const eagle_paged_kv* kv) {
   ChunkAttnDev d;
   bool wide;
   if (check_attention(a, chunk, kv, &d)) return 0;
-  return plan_attention(&d, elt_of(a->dtype), elt_of(kv->dtype), &wide);
+  return plan_attention(&d, kv->dtype, SIZE_MAX, &wide);
 }
 
 template <typename T, typename CT, int DH, bool WIDE, bool MODS>
@@ -218,13 +220,12 @@ static int launch_attention(const ChunkAttnDev& d, bool wide, bool mods, hipStre
 #undef ATTEND
 }
 
-extern "C" int eagle_chunk_attention(const eagle_attention_args* a, const eagle_chunk* chunk, const eagle_paged_kv* kv, void* workspace, size_t workspace_bytes,
-                                     void* hip_stream) {
+int chunk_attention(const eagle_attention_args* a, const eagle_chunk* chunk, const eagle_paged_kv* kv, void* workspace, size_t workspace_bytes, bool fit, hipStream_t stream) {
   ChunkAttnDev d;
   int rc = check_attention(a, chunk, kv, &d);
   if (rc) return rc;
   bool wide;
-  const size_t need = plan_attention(&d, elt_of(a->dtype), elt_of(kv->dtype), &wide);
+  const size_t need = plan_attention(&d, kv->dtype, fit ? workspace_bytes : SIZE_MAX, &wide);
   if (!workspace || !aligned(workspace, 256)) return fail(EAGLE_EINVAL, "attention: workspace must be a 256-byte aligned device pointer");
   if (workspace_bytes < need) return fail(EAGLE_ENOMEM, "attention: workspace of %zu bytes is smaller than the %zu needed", workspace_bytes, need);
   if (chunk->n_rows == 0) return EAGLE_OK;
@@ -233,10 +234,14 @@ extern "C" int eagle_chunk_attention(const eagle_attention_args* a, const eagle_
   d.part_ml = (float*)workspace;
   d.part_o = (float*)((char*)workspace + (pairs * 8 + 255) / 256 * 256);
   const bool mods = d.softcap > 0.f || d.slopes || d.scale == 0.f;   // (a scale of 0 times a masked score)
-  const hipStream_t stream = (hipStream_t)hip_stream;
   if (a->dtype == EAGLE_BF16) return launch_attention<bf16_t, bf16_t>(d, wide, mods, stream);
   if (kv->dtype == EAGLE_BF16) return launch_attention<float, bf16_t>(d, wide, mods, stream);
   return launch_attention<float, float>(d, wide, mods, stream);
+}
+
+extern "C" int eagle_chunk_attention(const eagle_attention_args* a, const eagle_chunk* chunk, const eagle_paged_kv* kv, void* workspace, size_t workspace_bytes,
+                                     void* hip_stream) {
+  return chunk_attention(a, chunk, kv, workspace, workspace_bytes, false, (hipStream_t)hip_stream);
 }
 
 // ---------------------------------------------------------------------------- logit rules

@@ -56,6 +56,15 @@ class EagleLogits(ctypes.Structure):
                 ("row_start", _vp), ("path_token", _vp), ("path_mask", _vp), ("allowed", _vp), ("allowed_row", _vp)]
 
 
+class EagleAttentionRules(ctypes.Structure):
+    _fields_ = [("softcap", _f32), ("window", _i32), ("slopes_dev", _vp)]
+
+
+class EagleContextRules(ctypes.Structure):
+    _fields_ = [("repetition", _vp), ("presence", _vp), ("frequency", _vp), ("bias_start", _vp), ("bias_token", _vp), ("bias_value", _vp), ("n_bias", _i32), ("n_masks", _i32),
+                ("allowed", _vp), ("mask_stride", _i64), ("allowed_row", _vp)]
+
+
 def declare(lib) -> None:
     """Argument types of the entry points."""
     P = ctypes.POINTER
@@ -64,6 +73,9 @@ def declare(lib) -> None:
     lib.eagle_chunk_attention_workspace.argtypes = [P(EagleAttentionArgs), P(EagleChunk), P(EaglePagedKV)]
     lib.eagle_chunk_attention_workspace.restype = ctypes.c_size_t
     lib.eagle_chunk_attention.argtypes = [P(EagleAttentionArgs), P(EagleChunk), P(EaglePagedKV), _vp, ctypes.c_size_t, _vp]
+    lib.eagle_set_rope.argtypes = [_vp, P(EagleRopeConfig)]
+    lib.eagle_set_attention.argtypes = [_vp, P(EagleAttentionRules)]
+    lib.eagle_set_logit_rules.argtypes = [_vp, P(EagleContextRules)]
     lib.eagle_apply_logit_rules.argtypes = [P(EagleLogits), P(EagleLogitRules), _vp]
 
 
@@ -156,13 +168,18 @@ def _same_batch(chunk: Chunk, kv: PagedKV, device) -> None:
         raise ValueError(f"the page table has {kv.n_seqs} sequences, the chunk {chunk.n_seqs}")
 
 
+def rope_config(head_dim: int, *, theta: float = 10000.0, rot_dim: Optional[int] = None, interleaved: bool = False, scaling: str = "none", factor: float = 1.0, low: float = 1.0,
+                high: float = 4.0, trained_len: int = 4096, mscale: float = 1.0) -> EagleRopeConfig:
+    if scaling not in ROPE_SCALINGS:
+        raise ValueError(f"scaling must be one of {ROPE_SCALINGS}: got {scaling!r}")
+    return EagleRopeConfig(head_dim, head_dim if rot_dim is None else rot_dim, int(interleaved), ROPE_SCALINGS.index(scaling), theta, factor, low, high, trained_len, mscale)
+
+
 def rope_plan(head_dim: int, *, theta: float = 10000.0, rot_dim: Optional[int] = None, interleaved: bool = False, scaling: str = "none", factor: float = 1.0, low: float = 1.0,
               high: float = 4.0, trained_len: int = 4096, mscale: float = 1.0) -> EagleRopePlan:
     """How positions turn a head (see eagle_rope_config); scaling is one of ROPE_SCALINGS.  Host work: make it once."""
-    if scaling not in ROPE_SCALINGS:
-        raise ValueError(f"scaling must be one of {ROPE_SCALINGS}: got {scaling!r}")
     lib = _library()
-    cfg = EagleRopeConfig(head_dim, head_dim if rot_dim is None else rot_dim, int(interleaved), ROPE_SCALINGS.index(scaling), theta, factor, low, high, trained_len, mscale)
+    cfg = rope_config(head_dim, theta=theta, rot_dim=rot_dim, interleaved=interleaved, scaling=scaling, factor=factor, low=low, high=high, trained_len=trained_len, mscale=mscale)
     plan = EagleRopePlan()
     rc = lib.eagle_rope_plan_init(ctypes.byref(cfg), ctypes.byref(plan))
     if rc != 0:
