@@ -13,6 +13,7 @@
 #pragma once
 #include "rows.h"
 #include "rope.h"
+#include <type_traits>
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
@@ -136,7 +137,7 @@ struct ChunkAttn {
   static constexpr int TILE = KT * DH;                            // elements of a piece of a tile
   static constexpr int OWNERS = WIDE ? 1 : 4;                     // waves with a tile of their own
   static constexpr int K_ELTS = KEYS_IN_LDS ? OWNERS * NK * TILE : 8, V_ELTS = OWNERS * NK * TILE;   // of one buffer
-  static constexpr bool TWO = WIDE || DIRECT;                     // buffers
+  static constexpr bool TWO = WIDE;                               // buffers
   static constexpr int JOIN = WIDE ? 0 : 2 * (16 * DB + 2) * 64 * 2;   // elements (of 2 bytes) that joining the waves takes
   static constexpr int V0_ELTS = V_ELTS > JOIN ? V_ELTS : JOIN;
   static constexpr int LDS = 2 * ((TWO ? 2 : 1) * K_ELTS + V0_ELTS + (TWO ? V_ELTS : 0));
@@ -147,6 +148,17 @@ struct ChunkAttn {
 };
 
 typedef __attribute__((address_space(3))) bf16_t* lds_ptr;
+// At most N vector-memory operations of this wave under way; all of its LDS operations done.  No access to memory moves across.
+template <int N> __device__ __forceinline__ void wait_loads() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | (N >> 4) << 14);
+  asm volatile("" ::: "memory");
+}
+__device__ __forceinline__ void wait_lds() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xC07F);
+  asm volatile("" ::: "memory");
+}
 
 template <typename P, typename T, typename CT>
 __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev A) {
@@ -192,6 +204,8 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
   constexpr int STEP = WIDE ? 1 : 4;
   const int g_tid = WIDE ? tid : lane, in_page = (1 << A.kv.page_shift) - 1;
   const CT *kb = (const CT*)A.kv.k + kvh * A.kv.head_stride, *vb = (const CT*)A.kv.v + kvh * A.kv.head_stride;
+  // Narrow and DIRECT: a wave has one buffer for keys and one for values; the next keys are on their way from the end of the scores on, the next values from the end of the products on.
+  constexpr bool STAGGERED = !WIDE && DIRECT;
   constexpr int MINE = WIDE ? 0 : NK * TILE;                      // a wave's place in a buffer: w * MINE
 
   // ---- DIRECT: a load instruction fills 1 KiB of LDS, RPI tokens of DH elements; lane -> (token, place), and the piece of 8 elements that belongs in the place.  What is not there (a page, a
@@ -209,26 +223,30 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
     }
     v_off = (uint32_t)(tr * (int)A.kv.token_stride + (vc * 8 < dh ? vc * 8 : 0)) * (uint32_t)sizeof(CT);
   }
+  typedef std::integral_constant<int, 1> KEYS;
+  typedef std::integral_constant<int, 2> VALUES;
+  typedef std::integral_constant<int, 3> BOTH;
   auto load_lds = [&](const void* from, lds_ptr to) {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
   };
-  auto dma = [&](lds_ptr kd, lds_ptr vd, int it, int pages) {
+  auto dma = [&](lds_ptr kd, lds_ptr vd, int it, int pages, auto what) {
+    constexpr bool K = decltype(what)::value & 1, V = decltype(what)::value & 2;
     const int k0 = tile_token(it), first = WIDE ? w * INSTS : 0;
     if (!A.lane_pages) {                                          // the tokens of an instruction lie in one page, whose place stays in scalar registers
 #pragma unroll
       for (int u = 0; u < INSTS; ++u) {
         const int t0 = (first + u) * RPI, page = max(0, __builtin_amdgcn_readlane(pages, t0));
         const long long at = page * A.kv.page_stride + ((k0 + t0) & in_page) * A.kv.token_stride;
-        load_lds((const char*)(kb + at) + k_off[u % (8 / RPI)], kd + t0 * DH);
-        load_lds((const char*)(vb + at) + v_off, vd + t0 * DH);
+        if constexpr (K) load_lds((const char*)(kb + at) + k_off[u % (8 / RPI)], kd + t0 * DH);
+        if constexpr (V) load_lds((const char*)(vb + at) + v_off, vd + t0 * DH);
       }
     } else {
 #pragma unroll
       for (int u = 0; u < INSTS; ++u) {
         const int t0 = (first + u) * RPI, page = max(0, __shfl(pages, t0 + tr, 64));
         const long long at = page * A.kv.page_stride + (((k0 + t0 + tr) & in_page) - tr) * A.kv.token_stride;
-        load_lds((const char*)(kb + at) + k_off[u % (8 / RPI)], kd + t0 * DH);
-        load_lds((const char*)(vb + at) + v_off, vd + t0 * DH);
+        if constexpr (K) load_lds((const char*)(kb + at) + k_off[u % (8 / RPI)], kd + t0 * DH);
+        if constexpr (V) load_lds((const char*)(vb + at) + v_off, vd + t0 * DH);
       }
     }
   };
@@ -284,8 +302,13 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
     pages = page_of(it, entry_of(it));
     entry_next = entry_of(it + STEP);
   }
-  if constexpr (DIRECT) {
-    if (it < t_end) dma((lds_ptr)k_lds0 + w * MINE, (lds_ptr)v_lds0 + w * MINE, it, pages);
+  if constexpr (STAGGERED) {
+    if (it < t_end) {
+      dma((lds_ptr)k_lds0 + w * MINE, (lds_ptr)v_lds0, it, pages, KEYS());
+      dma((lds_ptr)k_lds0, (lds_ptr)v_lds0 + w * MINE, it, pages, VALUES());
+    }
+  } else if constexpr (DIRECT) {
+    if (it < t_end) dma((lds_ptr)k_lds0, (lds_ptr)v_lds0, it, pages, BOTH());
   } else if (it < t_end) fetch(it, pages);
 
   bf16x8 qf[NQ][KSN];
@@ -332,17 +355,20 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
   const bool wave_live = wave_col < R.n * g;
 
   // One tile, its keys and values in kt, vt; the next goes to kn, vn.
-  auto tile = [&](bf16_t* kt, bf16_t* vt, bf16_t* kn, bf16_t* vn, int which) {
+  auto tile = [&](bf16_t* kt, bf16_t* vt, bf16_t* kn, bf16_t* vn, int which, auto last) {
+    constexpr bool LAST = decltype(last)::value;                  // STAGGERED: nothing follows (known ahead, so that the loads in flight can be counted)
     const int k0 = tile_token(it);
     const uint64_t there = __ballot(pages >= 0) & low_ones(KT);
     const bool full = k0 + KT <= R.full_to && (k0 >= R.full_from || k0 + KT <= R.prefix) && there == low_ones(KT);
     bool bad = false;
     const int pages_next = page_of(it + STEP, entry_next);
-    if constexpr (DIRECT) {
+    if constexpr (STAGGERED) {
+      wait_loads<INSTS>();                   // the keys have landed (the values are behind them)
+    } else if constexpr (DIRECT) {
       // this tile has landed (for WIDE: everyone's part of it, and everyone is done with the other buffer)
-      __builtin_amdgcn_s_waitcnt(0x0F70);                         // vmcnt(0)
-      if constexpr (WIDE) { asm volatile("" ::: "memory"); __builtin_amdgcn_s_barrier(); asm volatile("" ::: "memory"); }
-      if (it + STEP < t_end) dma((lds_ptr)kn, (lds_ptr)vn, it + STEP, pages_next);
+      wait_loads<0>();
+      if constexpr (WIDE) { __builtin_amdgcn_s_barrier(); asm volatile("" ::: "memory"); }
+      if (it + STEP < t_end) dma((lds_ptr)kn, (lds_ptr)vn, it + STEP, pages_next, BOTH());
     } else if constexpr (WIDE) {
       if (it + 1 < t_end) fetch(it + 1, pages_next);
       bad = s_bad[which] == it;
@@ -384,8 +410,12 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
     if constexpr (!WIDE && !DIRECT) {
       if (it + STEP < t_end) fetch(it + STEP, pages_next);        // (the keys' registers are free now)
     }
+    if constexpr (STAGGERED && !LAST) {
+      wait_lds();                                                 // the keys have been read
+      dma((lds_ptr)kt, (lds_ptr)vt, it + STEP, pages_next, KEYS());
+    }
     pages = pages_next;
-    entry_next = entry_of(it + 2 * STEP);
+    if constexpr (!STAGGERED) entry_next = entry_of(it + 2 * STEP);
     uint64_t vis = ~0ull;                                         // tokens of the tile that the column sees
     if (!idle) {
     // cap and slopes
@@ -472,6 +502,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
         for (int r = 0; r < 16; ++r) oacc[b][r] *= f;
     }
     }
+    if constexpr (STAGGERED) wait_loads<LAST ? 0 : INSTS>();   // the values have landed
     if (DIRECT && !full) {                                        // is there anything that is not finite among the values?
       uint32_t any = 0;
 #pragma unroll 4
@@ -550,6 +581,11 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
         }
       }
     }
+    if constexpr (STAGGERED && !LAST) {
+      entry_next = entry_of(it + 2 * STEP);
+      wait_lds();                                                 // the values have been read
+      dma((lds_ptr)kt, (lds_ptr)vt, it + STEP, pages, VALUES());
+    }
     if constexpr (WIDE && !DIRECT) {
       if (it + 1 < t_end && __any(put(kn, vn)) && lane == 0) s_bad[which ^ 1] = it + 1;
       __syncthreads();
@@ -558,12 +594,17 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
   };
   if constexpr (P::TWO) {
     while (it < t_end) {
-      tile(k_lds0 + w * MINE, v_lds0 + w * MINE, k_lds1 + w * MINE, v_lds1 + w * MINE, 0);
+      tile(k_lds0, v_lds0, k_lds1, v_lds1, 0, std::false_type());
       if (it >= t_end) break;
-      tile(k_lds1 + w * MINE, v_lds1 + w * MINE, k_lds0 + w * MINE, v_lds0 + w * MINE, 1);
+      tile(k_lds1, v_lds1, k_lds0, v_lds0, 1, std::false_type());
     }
   } else {
-    while (it < t_end) tile(nullptr, v_lds0 + w * MINE, nullptr, v_lds0 + w * MINE, 0);
+    bf16_t *kt = k_lds0 + w * (P::KEYS_IN_LDS ? MINE : 0), *vt = v_lds0 + w * MINE;
+    if constexpr (STAGGERED) {
+      while (it + STEP < t_end) tile(kt, vt, kt, vt, 0, std::false_type());
+      if (it < t_end) tile(kt, vt, kt, vt, 0, std::true_type());
+    } else
+      while (it < t_end) tile(kt, vt, kt, vt, 0, std::false_type());
   }
   l_run += __shfl_xor(l_run, 32, 64);
   if constexpr (!WIDE) {
