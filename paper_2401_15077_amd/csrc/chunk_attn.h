@@ -64,7 +64,7 @@ __device__ inline ColumnRange column_range(const ChunkAttnDev& A, int s, int col
 
 __device__ __forceinline__ uint64_t low_ones(int n) { return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1ull; }
 
-// x as an exact sum of bf16 pieces; what is not finite stays in the first.
+// x as an exact sum of bf16 pieces.  (Of what is not finite the first is the same, the others NaN.)
 template <int NP> __device__ __forceinline__ void pieces8(const float* x, bf16x8* p) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
@@ -85,35 +85,28 @@ __device__ __forceinline__ uint32_t exponents(u32x4 v) {
   for (int e = 0; e < 4; ++e) any |= (v[e] & 0x7F807F80u) + 0x00800080u;
   return any & 0x80008000u;
 }
-__device__ __forceinline__ bool pair_not_finite(uint32_t w) { return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u; }
-
 // Eight elements of a token in flight, and their pieces.
 template <typename CT> struct Raw8;
 template <> struct Raw8<bf16_t> {
   u32x4 v;
   __device__ __forceinline__ void load(const bf16_t* p) { v = *(const u32x4*)p; }
   __device__ __forceinline__ void zero() { v = u32x4{0, 0, 0, 0}; }
-  __device__ __forceinline__ bool bad() const { return pair_not_finite(v.x) || pair_not_finite(v.y) || pair_not_finite(v.z) || pair_not_finite(v.w); }
   __device__ __forceinline__ void split(bf16x8* p) const { p[0] = __builtin_bit_cast(bf16x8, v); }
 };
 template <> struct Raw8<float> {
   f32x4 a, b;
   __device__ __forceinline__ void load(const float* p) { a = *(const f32x4*)p; b = *(const f32x4*)(p + 4); }
   __device__ __forceinline__ void zero() { a = b = f32x4{0.f, 0.f, 0.f, 0.f}; }
-  __device__ __forceinline__ bool bad() const {
-    bool r = false;
+  __device__ __forceinline__ uint32_t bad() const {               // (see exponents())
+    const u32x4 u = __builtin_bit_cast(u32x4, a), v = __builtin_bit_cast(u32x4, b);
+    uint32_t any = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) r = r || not_finite(a[i]) || not_finite(b[i]);
-    return r;
+    for (int i = 0; i < 4; ++i) any |= ((u[i] & 0x7F800000u) + 0x00800000u) | ((v[i] & 0x7F800000u) + 0x00800000u);
+    return any & 0x80000000u;
   }
   __device__ __forceinline__ void split(bf16x8* p) const {
     const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
     pieces8<3>(x, p);
-    if (bad()) {                                                  // (inf - inf in the later pieces)
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (not_finite(x[i])) { p[1][i] = (__bf16)0.f; p[2][i] = (__bf16)0.f; }
-    }
   }
 };
 
@@ -278,7 +271,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
   };
   // the fetched tile to LDS; returns whether a value is not finite (to this thread's knowledge)
   auto put = [&](bf16_t* kd, bf16_t* vd) -> bool {
-    bool bad = false;
+    uint32_t bad = 0;
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
       const int item = i * P::GROUP + g_tid, t = item / (DH / 8), c = item % (DH / 8);
@@ -289,11 +282,11 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
         for (int j = 0; j < NK; ++j) *(bf16x8*)(kd + j * TILE + 8 * k_place<DH>(t, c)) = p[j];
       }
       vr[i].split(p);
-      bad = bad || vr[i].bad();
+      if constexpr (!DIRECT) bad |= vr[i].bad();
 #pragma unroll
       for (int j = 0; j < NK; ++j) *(bf16x8*)(vd + j * TILE + 8 * v_place<DH>(t, c)) = p[j];
     }
-    return bad;
+    return bad != 0;
   };
 
   int it = t_begin + (WIDE ? 0 : w);
@@ -534,7 +527,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
           }
       }
       if constexpr (WIDE) __syncthreads();
-      for (int i = WIDE ? w : 0; i < TILE / 512; i += WIDE ? 4 : 1) {
+      for (int i = WIDE ? w : 0; i < NK * TILE / 512; i += WIDE ? 4 : 1) {   // (all pieces)
         u32x4 v = *(const u32x4*)(vt + i * 512 + lane * 8);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
