@@ -655,30 +655,46 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
   }
 }
 
-// Adds up the parts of the (row, head) pairs whose tokens were split; a wave a pair.
+// Adds up the parts (at most 64) of the (row, head) pairs whose tokens were split; a wave a pair.  Its time is one chain of loads, so the first parts are requested before it is known how many
+// there are: they lie in the workspace whatever they hold.
 template <typename P, typename T>
 __global__ __launch_bounds__(256) void k_chunk_attn_join(const ChunkAttnDev A) {
-  constexpr int DH = P::DH, E = DH / 64;
+  constexpr int DH = P::DH, E = DH / 64, AHEAD = 8;
   const int row = blockIdx.x, head = blockIdx.y * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63, dh = A.kv.head_dim;
   if (head >= A.H) return;
+  const size_t at = ((size_t)row * A.H + head) * A.splits;
+  const float* po = A.part_o + at * DH + lane * E;
+  float ov[AHEAD][E];
+  auto request = [&](int k0) {
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+      for (int e = 0; e < E; ++e) ov[u][e] = po[(size_t)min(k0 + u, A.splits - 1) * DH + e];
+  };
+  const float2 ml = *(const float2*)(A.part_ml + 2 * (at + min(lane, A.splits - 1)));
+  request(0);
   const int s = wave_row_seq(A.chunk.row_start, A.chunk.n_seqs, row);
   if (s < 0) return;
   const int g = A.H / A.kv.n_kv_heads, i = row - max(0, A.chunk.row_start[s]), col = i * g + head % g;
   const ColumnRange R = column_range<P::KT>(A, s, col / P::COLS * P::COLS, P::COLS, g);
   if (i >= R.n || R.n_tiles <= A.split_tiles) return;
   const int n = (R.n_tiles + A.split_tiles - 1) / A.split_tiles;   // at most A.splits
-  const size_t at = ((size_t)row * A.H + head) * A.splits;
-  float m = -INFINITY;
-  for (int k = lane; k < n; k += 64) m = fmaxf(m, A.part_ml[2 * (at + k)]);
+  const float mine = lane < n ? ml.x : -INFINITY;
+  float m = mine;
   for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-  float l = 0.f, x[E];
+  const float f = mine == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mine - m);
+  float l = f == 0.f ? 0.f : f * ml.y, x[E];
+  for (int o = 32; o; o >>= 1) l += __shfl_xor(l, o, 64);
 #pragma unroll
   for (int e = 0; e < E; ++e) x[e] = 0.f;
-  for (int k = 0; k < n; ++k) {
-    const float mk = A.part_ml[2 * (at + k)], f = mk == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mk - m);
-    l = fmaf(f, A.part_ml[2 * (at + k) + 1], l);
+  for (int k0 = 0; k0 < n; k0 += AHEAD) {
+    if (k0 > 0) request(k0);
 #pragma unroll
-    for (int e = 0; e < E; ++e) x[e] = mk == -INFINITY ? x[e] : fmaf(f, A.part_o[(at + k) * DH + lane * E + e], x[e]);
+    for (int u = 0; u < AHEAD; ++u) {
+      const float fk = k0 + u < n ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), k0 + u)) : 0.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[e] = fk == 0.f ? x[e] : fmaf(fk, ov[u][e], x[e]);
+    }
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
   T* o = (T*)A.out + row * A.out_row + head * A.out_head;

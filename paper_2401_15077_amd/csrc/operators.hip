@@ -170,21 +170,26 @@ static int check_attention(const eagle_attention_args* a, const eagle_chunk* chu
   return EAGLE_OK;
 }
 
-// Work-groups that the token range is split for where sequences, kv heads and column blocks are fewer, and the fewest tiles of a part.
-constexpr int ATTN_WIDE_WGS = 512, ATTN_NARROW_WGS = 2048, ATTN_MIN_TILES = 4;
+// Where sequences, kv heads and column blocks make fewer work-groups than these, the tokens are split; a part has a few tiles at least (the narrow shape: whole rounds of its four waves),
+// and there are at most as many parts as k_chunk_attn_join has lanes.
+// Narrow, 64 sequences of 1k to 16k tokens, 64 / 8 heads, bf16, us with 1, 2, 3, 4, 6, 8 parts at most: 433 (2), 419 (3), 451 (4), 406 (6), 417 (8).  One token over 701 keys, 32 heads, fp32,
+// 22 tiles: parts of 4 tiles 17.6, of 5 23.0, of 3 29.4.  Wide: one a CU (four trees of 26 nodes on 8 kv heads, fp32 queries, 37 tiles: 8 parts 27, 10 parts 32 to 38; 2011 fp32 rows on 32 heads, 512 work-groups: whole
+// 327, in two 339 and 26 more for joining).
+constexpr int ATTN_WIDE_WGS = 256, ATTN_NARROW_WGS = 3072, ATTN_MIN_TILES = 4, ATTN_MAX_PARTS = 64;
 
 // Columns and parts of a call; returns the bytes of workspace, at most `limit` of them if that is possible.
 static size_t plan_attention(ChunkAttnDev* d, int kv_dtype, size_t limit, bool* wide) {
   const int g = d->H / d->kv.n_kv_heads;
   const long long cols = (long long)d->chunk.max_rows * g;
   *wide = cols > 32;
-  const int KT = *wide && kv_dtype == EAGLE_BF16 ? 64 : 32;
+  const int KT = *wide && kv_dtype == EAGLE_BF16 ? 64 : 32, round = *wide ? 1 : 4;
   d->col_blocks = (int)((cols + (*wide ? 127 : 31)) / (*wide ? 128 : 32));
   const long long units = (long long)d->col_blocks * d->kv.n_kv_heads * d->chunk.n_seqs, tiles = ((long long)d->chunk.max_keys + KT - 1) / KT;
-  long long parts = std::max(1ll, std::min((*wide ? ATTN_WIDE_WGS : ATTN_NARROW_WGS) / units, tiles / ATTN_MIN_TILES));
+  long long parts = std::min((*wide ? ATTN_WIDE_WGS : ATTN_NARROW_WGS) / units, (tiles + ATTN_MIN_TILES - 1) / ATTN_MIN_TILES);
+  parts = std::max(1ll, std::min(parts, (long long)ATTN_MAX_PARTS));
   const size_t pairs = (size_t)d->chunk.n_rows * d->H, DH = d->kv.head_dim <= 64 ? 64 : 128;
   for (;; --parts) {
-    d->split_tiles = (int)((tiles + parts - 1) / parts);
+    d->split_tiles = (int)((tiles + parts * round - 1) / (parts * round) * round);
     d->splits = (int)((tiles + d->split_tiles - 1) / d->split_tiles);
     if (d->splits == 1) return 256;
     const size_t bytes = (pairs * d->splits * 8 + 255) / 256 * 256 + pairs * d->splits * DH * 4;
