@@ -348,9 +348,10 @@ int eagle_chunk_attention(const eagle_attention_args *args, const eagle_chunk *c
  * counts.  A repetition that is not above 0 counts as 1.  A mask may leave a row empty: all of it is -inf. */
 typedef struct {
   int32_t n_seqs;
-  const int32_t *tokens;              /* dev [n_seqs][token_stride] */
+  const int32_t *tokens;              /* dev, sequence s at s * token_stride; stride 0: one text for all */
   int64_t token_stride;
-  const int32_t *n_tokens, *n_prompt; /* dev [n_seqs]; n_tokens at most token_stride (more is not read); n_prompt null: 0 */
+  int32_t max_tokens;                 /* of a sequence, at most 2^29; where n_tokens says more, the rest is not read */
+  const int32_t *n_tokens, *n_prompt; /* dev [n_seqs]; n_prompt null: 0 */
   const float *repetition, *presence, *frequency;   /* dev [n_seqs] */
   const int32_t *bias_start, *bias_token;           /* dev [n_seqs + 1], [bias_start[n_seqs]]; entries beyond n_bias are not read */
   const float *bias_value;

@@ -1392,7 +1392,7 @@ static int rule_logits(eagle_ctx* c, int seq0, int n, bool nodes, const int* n_t
     }
   }
   eagle_logit_rules lr{};
-  lr.n_seqs = n; lr.tokens = c->st.tokens + (size_t)seq0 * c->st.tok_stride; lr.token_stride = c->st.tok_stride; lr.n_tokens = n_tokens + seq0; lr.n_prompt = c->op_prompt + seq0;
+  lr.n_seqs = n; lr.tokens = c->st.tokens + (size_t)seq0 * c->st.tok_stride; lr.token_stride = c->st.tok_stride; lr.max_tokens = (int32_t)c->st.tok_stride; lr.n_tokens = n_tokens + seq0; lr.n_prompt = c->op_prompt + seq0;
   lr.repetition = r.repetition ? r.repetition + seq0 : nullptr; lr.presence = r.presence ? r.presence + seq0 : nullptr; lr.frequency = r.frequency ? r.frequency + seq0 : nullptr;
   if (r.bias_token) { lr.bias_start = r.bias_start + seq0; lr.bias_token = r.bias_token; lr.bias_value = r.bias_value; lr.n_bias = r.n_bias; }
   return eagle_apply_logit_rules(&l, &lr, c->stream);

@@ -175,7 +175,7 @@ static int check_attention(const eagle_attention_args* a, const eagle_chunk* chu
 // Narrow, 64 sequences of 1k to 16k tokens, 64 / 8 heads, bf16, us with 1, 2, 3, 4, 6, 8 parts at most: 433 (2), 419 (3), 451 (4), 406 (6), 417 (8).  One token over 701 keys, 32 heads, fp32,
 // 22 tiles: parts of 4 tiles 17.6, of 5 23.0, of 3 29.4.  Wide: one a CU (four trees of 26 nodes on 8 kv heads, fp32 queries, 37 tiles: 8 parts 27, 10 parts 32 to 38; 2011 fp32 rows on 32 heads, 512 work-groups: whole
 // 327, in two 339 and 26 more for joining).
-constexpr int ATTN_WIDE_WGS = 256, ATTN_NARROW_WGS = 3072, ATTN_MIN_TILES = 4, ATTN_MAX_PARTS = 64;
+constexpr int ATTN_WIDE_WGS = 256, ATTN_NARROW_WGS = 3000, ATTN_MIN_TILES = 4, ATTN_MAX_PARTS = 64;
 
 // Columns and parts of a call; returns the bytes of workspace, at most `limit` of them if that is possible.
 static size_t plan_attention(ChunkAttnDev* d, int kv_dtype, size_t limit, bool* wide) {
@@ -252,18 +252,18 @@ extern "C" int eagle_chunk_attention(const eagle_attention_args* a, const eagle_
 // ---------------------------------------------------------------------------- logit rules
 template <typename T>
 static int launch_rules(RulesDev d, bool runs, hipStream_t stream) {
-  // A slice costs its work-group a walk over the row's text and a word of LDS a token (two with biases), so slices are as long as leaves about a thousand work-groups.
-  int slice = d.bias_token ? 8192 : 16384;
-  while (slice > 1024 && (long long)d.n_rows * ((d.vocab + slice - 1) / slice) < 1024) slice >>= 1;
-  d.slice = slice;
-  constexpr int VE = 16 / sizeof(T);
+  // A slice costs its work-group a walk over the row's text and a word of LDS a token, so a row is cut into no more slices than 512 threads need, or than make 1024 work-groups, four a CU;
+  // and into slices of one length, so that no short one walks the text for little.  160 rows of 100003 bf16 logits: 26.2 us with 512 threads, 27.7 with 256, 31.0 with 1024 (two work-groups a CU,
+  // a third round nearly empty); 104 rows of 32000 fp32 logits: 10.5 us at 1024 work-groups, 11.0 at 512.
+  constexpr int VE = 16 / sizeof(T), PIECES = 2;
+  auto pieces = [&](int t) { return (d.vocab + t * VE * PIECES - 1) / (t * VE * PIECES); };
+  const int parts = std::max(pieces(512), std::min((1024 + d.n_rows - 1) / d.n_rows, pieces(128)));
+  const int threads = (pieces(64) + parts - 1) / parts * 64;
+  const int slice = threads * VE * PIECES;
   const int reach = d.vocab + (runs ? VE - 1 : 0);              // (the first piece of a row may begin up to VE - 1 elements in front of it)
   const dim3 grid((reach + slice - 1) / slice, d.n_rows);
-  const int threads = slice >= 8192 ? 512 : 256;
-  const size_t lds = (size_t)slice * (d.bias_token ? 8 : 4);
-  auto kernel = runs ? k_logit_rules<T, VE> : k_logit_rules<T, 1>;
-  HIPCHK(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 65536));
-  kernel<<<grid, threads, lds, stream>>>(d);
+  auto kernel = runs ? k_logit_rules<T, VE, PIECES> : k_logit_rules<T, 1, VE * PIECES>;
+  kernel<<<grid, threads, (size_t)slice * 4 + 16, stream>>>(d);      // (at most 32 KB)
   LAUNCH_CHECK();
   return EAGLE_OK;
 }
@@ -271,16 +271,17 @@ static int launch_rules(RulesDev d, bool runs, hipStream_t stream) {
 extern "C" int eagle_apply_logit_rules(const eagle_logits* l, const eagle_logit_rules* rules, void* hip_stream) {
   if (!l || !rules) return fail(EAGLE_EINVAL, "null argument");
   if (!is_type(l->dtype)) return fail(EAGLE_EINVAL, "logits: dtype must be EAGLE_F32 or EAGLE_BF16");
-  if (l->n_rows < 0 || l->n_rows > 65535 || l->vocab < 1 || rules->n_seqs < 1) return fail(EAGLE_EINVAL, "logits: n_rows must be 0..65535, vocab and n_seqs >= 1");
+  if (l->n_rows < 0 || l->n_rows > 65535 || l->vocab < 1 || l->vocab > 1 << 30 || rules->n_seqs < 1) return fail(EAGLE_EINVAL, "logits: n_rows must be 0..65535, vocab 1..2^30, n_seqs >= 1");
   if (l->n_rows == 0) return EAGLE_OK;
   if (!l->in || !l->out) return fail(EAGLE_EINVAL, "logits: in or out is null");
   if (l->in_stride < l->vocab || l->out_stride < l->vocab) return fail(EAGLE_EINVAL, "logits: rows of %d entries need strides of at least that", l->vocab);
   if (!l->row_start && l->n_rows != rules->n_seqs) return fail(EAGLE_EINVAL, "logits: without row_start there is one row a sequence (%d rows, %d sequences)", l->n_rows, rules->n_seqs);
   if (!l->path_token != !l->path_mask) return fail(EAGLE_EINVAL, "logits: path_token and path_mask belong together");
   if (l->allowed && (l->n_masks < 1 || l->mask_stride < (l->vocab + 31) / 32)) return fail(EAGLE_EINVAL, "logits: masks need n_masks >= 1 and %d words a row", (l->vocab + 31) / 32);
-  if (rules->tokens && (!rules->n_tokens || rules->token_stride < 0)) return fail(EAGLE_EINVAL, "logits: tokens need n_tokens and token_stride >= 0");
+  if (rules->tokens && (!rules->n_tokens || rules->token_stride < 0 || rules->max_tokens < 0 || rules->max_tokens > 1 << 29))
+    return fail(EAGLE_EINVAL, "logits: tokens need n_tokens, token_stride >= 0 and max_tokens 0..2^29");
   if (rules->bias_token && (!rules->bias_start || !rules->bias_value || rules->n_bias < 0)) return fail(EAGLE_EINVAL, "logits: biases need bias_start, bias_value and n_bias >= 0");
-  RulesDev d{l->n_rows, l->vocab, l->n_masks, rules->n_seqs, rules->n_bias, 0, l->in, l->out, l->in_stride, l->out_stride, l->mask_stride, rules->token_stride,
+  RulesDev d{l->n_rows, l->vocab, l->n_masks, rules->n_seqs, rules->n_bias, rules->max_tokens, l->in, l->out, l->in_stride, l->out_stride, l->mask_stride, rules->token_stride,
              l->row_start, l->path_token, l->allowed_row, rules->tokens, rules->n_tokens, rules->n_prompt, rules->bias_start, rules->n_bias > 0 ? rules->bias_token : nullptr,
              (const unsigned long long*)l->path_mask, l->allowed, rules->repetition, rules->presence, rules->frequency, rules->bias_value};
   const int elt = elt_of(l->dtype);

@@ -47,7 +47,7 @@ class EagleAttentionArgs(ctypes.Structure):
 
 
 class EagleLogitRules(ctypes.Structure):
-    _fields_ = [("n_seqs", _i32), ("tokens", _vp), ("token_stride", _i64), ("n_tokens", _vp), ("n_prompt", _vp), ("repetition", _vp), ("presence", _vp), ("frequency", _vp),
+    _fields_ = [("n_seqs", _i32), ("tokens", _vp), ("token_stride", _i64), ("max_tokens", _i32), ("n_tokens", _vp), ("n_prompt", _vp), ("repetition", _vp), ("presence", _vp), ("frequency", _vp),
                 ("bias_start", _vp), ("bias_token", _vp), ("bias_value", _vp), ("n_bias", _i32)]
 
 
@@ -153,8 +153,9 @@ class PagedKV:
             raise ValueError("k and v must be [n_pages, n_kv_heads, page_tokens, head_dim], float32 or bfloat16, of the same type, shape and strides on one device")
         if k.stride(3) != 1 and k.shape[3] > 1:
             raise ValueError("the elements of a token of k and v must be consecutive")
-        if page_table.dtype != torch.int32 or page_table.dim() != 2 or page_table.device != k.device or (page_table.stride(1) != 1 and page_table.shape[1] > 1):
-            raise ValueError(f"page_table must be an int32 [n_seqs, pages] tensor on {k.device}, its rows consecutive")
+        if page_table.dtype != torch.int32 or page_table.dim() != 2 or page_table.device != k.device or (page_table.stride(1) != 1 and page_table.shape[1] > 1) \
+                or (page_table.shape[0] > 1 and page_table.stride(0) < page_table.shape[1]):
+            raise ValueError(f"page_table must be an int32 [n_seqs, pages] tensor on {k.device}, its rows consecutive and apart")
         self.device, self.dtype, self.n_seqs, self.n_kv_heads, self.head_dim = k.device, k.dtype, page_table.shape[0], k.shape[1], k.shape[3]
         self._keep = (k, v, page_table)
         self.c = EaglePagedKV(k.data_ptr(), v.data_ptr(), _TYPES[k.dtype], k.shape[1], k.shape[3], k.shape[2], k.shape[0], page_table.shape[1], k.stride(0), k.stride(1), k.stride(2),
@@ -295,7 +296,7 @@ class LogitRules:
         self._keep = (tokens, n_tokens, n_prompt, repetition, presence, frequency, b)
         self.longest = tokens.shape[1] if tokens is not None else 0
         f, i = torch.float32, torch.int32
-        self.c = EagleLogitRules(self.n_seqs, tokens.data_ptr() if tokens is not None else None, tokens.stride(0) if tokens is not None and S > 1 else self.longest,
+        self.c = EagleLogitRules(self.n_seqs, tokens.data_ptr() if tokens is not None else None, tokens.stride(0) if tokens is not None else 0, self.longest,
                                  _list(n_tokens, "n_tokens", i, S, dev), _list(n_prompt, "n_prompt", i, S, dev), _list(repetition, "repetition", f, S, dev),
                                  _list(presence, "presence", f, S, dev), _list(frequency, "frequency", f, S, dev), _list(b[0], "bias start", i, S + 1, dev),
                                  _list(b[1], "bias token", i, None, dev), _list(b[2], "bias value", f, None, dev), b[1].shape[0] if bias is not None else 0)
@@ -320,8 +321,9 @@ def apply_logit_rules(logits: torch.Tensor, rules: LogitRules, *, row_start: Opt
         raise ValueError(f"out must be {logits.dtype} {list(logits.shape)} on {dev}, its rows consecutive")
     masks = (None, 0, 0)
     if allowed is not None:
-        if allowed.dtype != torch.int32 or allowed.dim() != 2 or allowed.device != dev or (allowed.stride(1) != 1 and allowed.shape[1] > 1) or allowed.shape[1] * 32 < V:
-            raise ValueError(f"allowed must be an int32 [masks, words] tensor on {dev} of at least {(V + 31) // 32} consecutive words a row")
+        if allowed.dtype != torch.int32 or allowed.dim() != 2 or allowed.device != dev or (allowed.stride(1) != 1 and allowed.shape[1] > 1) or allowed.shape[1] * 32 < V \
+                or (allowed.shape[0] > 1 and allowed.stride(0) < allowed.shape[1]):
+            raise ValueError(f"allowed must be an int32 [masks, words] tensor on {dev} of at least {(V + 31) // 32} consecutive words a row, its rows apart")
         if allowed_row is None and allowed.shape[0] != R:
             raise ValueError(f"without allowed_row there is one mask a row ({allowed.shape[0]} masks, {R} rows)")
         masks = allowed.data_ptr(), allowed.shape[0], max(allowed.stride(0), allowed.shape[1])

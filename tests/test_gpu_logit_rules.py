@@ -128,6 +128,49 @@ def test_one_row_a_sequence_and_rows_of_none():
     p.apply_logit_rules(y[:0], r2, row_start=i32([0, 0, 0, 0]))
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("repeated", [False, True])
+def test_long_lists(dtype, repeated):
+    """More entries and more text than a work-group has threads, from lists that start anywhere; entries for a token again, thousands later."""
+    p = pkg()
+    rng = np.random.default_rng(5 + repeated)
+    S, V, longest = 3, 5003, 9001
+    tokens = rng.integers(0, V, (S, longest))
+    n_tokens, n_prompt = [longest, 8193, 4099], [17, 8200, 0]
+    counts = [4000, 1, 2500]
+    bstart = np.cumsum([0] + counts)
+    btoken = np.concatenate([rng.integers(0, V, n) if repeated else rng.permutation(V)[:n] for n in counts])
+    bvalue = rng.standard_normal(bstart[-1]).astype(np.float32)
+    pres, freq, rep = np.float32([0.5, 0.0, -0.3]), np.float32([0.2, 0.7, 0.0]), np.float32([1.3, 3.0, 0.7])
+    x = torch.randn(S, V, device=DEV, generator=torch.Generator(device=DEV).manual_seed(3)).mul_(3).to(TYPES[dtype])
+    f32 = lambda a: torch.tensor(a, device=DEV)
+    wide = i32(np.concatenate([np.zeros((S, 1)), tokens, np.zeros((S, 1))], 1))
+    rules = p.LogitRules(wide[:, 1:-1], i32(n_tokens), n_prompt=i32(n_prompt), repetition=f32(rep), presence=f32(pres), frequency=f32(freq),
+                         bias=(i32(bstart), i32(btoken), f32(bvalue)))
+    want, size = ref.logit_rules(x.double().cpu().numpy(), np.arange(S + 1), tokens=tokens, n_tokens=n_tokens, n_prompt=n_prompt, repetition=rep, presence=pres, frequency=freq,
+                                 bias=(bstart, btoken, bvalue))
+    check(p.apply_logit_rules(x, rules, out=torch.empty_like(x)), want, size, x.dtype)
+
+
+def test_texts_that_are_views():
+    """What a sequence says beyond its columns is not read, and one text may stand for all sequences."""
+    p = pkg()
+    V = 64
+    wide = i32(np.arange(60).reshape(3, 20))
+    x = torch.zeros(3, V, device=DEV)
+    ones = torch.ones(3, device=DEV)
+    y = p.apply_logit_rules(x.clone(), p.LogitRules(wide[:, 2:7], i32([3, 50, 2 ** 31 - 1]), frequency=ones))
+    want = torch.zeros_like(x)
+    for s, n in enumerate([3, 5, 5]):
+        want[s, 20 * s + 2:20 * s + 2 + n] = -1
+    assert torch.equal(y, want)
+    y = p.apply_logit_rules(x.clone(), p.LogitRules(wide[1:2, :6].expand(3, 6), i32([1, -4, 6]), frequency=ones))
+    want.zero_()
+    want[0, 20] = -1
+    want[2, 20:26] = -1
+    assert torch.equal(y, want)
+
+
 def test_a_long_text_of_one_token_counts_exactly():
     p = pkg()
     n = 200000

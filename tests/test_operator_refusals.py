@@ -176,3 +176,21 @@ def test_binding_checks():
         pkg.apply_logit_rules(x.double(), r)
     with pytest.raises(ValueError, match="GPU"):
         pkg.apply_logit_rules(x, r, row_start=i32(0, 2, 4))
+
+
+def test_rows_that_lie_on_each_other():
+    k = torch.zeros(9, 2, 32, 64)
+    table = torch.zeros(1, 4, dtype=torch.int32)
+    pkg.PagedKV(k, k, table)
+    with pytest.raises(ValueError, match="page_table"):
+        pkg.PagedKV(k, k, table.expand(3, 4))
+    x, r = torch.zeros(4, 50), pkg.LogitRules(n_seqs=4)
+    with pytest.raises(ValueError, match="allowed"):
+        pkg.apply_logit_rules(x, r, allowed=torch.zeros(1, 2, dtype=torch.int32).expand(4, 2))
+
+
+def test_the_most_tokens(lib):
+    for r in (dict(max_tokens=-1), dict(max_tokens=2 ** 29 + 1)):
+        call = ops.EagleLogits(n_rows=4, vocab=100, in_=A, out=A, in_stride=100, out_stride=100), ops.EagleLogitRules(n_seqs=4, tokens=A, n_tokens=A, token_stride=8, **r)
+        assert lib.eagle_apply_logit_rules(*call, None) == EINVAL, r
+    assert lib.eagle_apply_logit_rules(ops.EagleLogits(n_rows=1, vocab=2 ** 30 + 1, in_=A, out=A, in_stride=2 ** 31, out_stride=2 ** 31), ops.EagleLogitRules(n_seqs=1), None) == EINVAL
