@@ -26,6 +26,7 @@ struct ChunkAttnDev {
   const float* slopes; const int* prefix;
   ChunkDev chunk; PagedDev kv;
   int col_blocks, splits, split_tiles;     // parts of the token range at most, tiles of one
+  int turn;                                // column blocks in descending order before the others ascend
   int lane_pages;                          // pages of fewer than 8 tokens: every lane looks its own up
   float* part_o; float* part_ml;           // [row][head][split][DH], [row][head][split][maximum, sum]
 };
@@ -111,9 +112,10 @@ template <> struct Raw8<float> {
 };
 
 // Where 16 bytes (8 elements, piece c) of token t lie in a tile in LDS, in units of 8 elements.  Keys are read a token a lane: eight consecutive tokens' pieces lie in eight different
-// 16-byte columns.  Values are read transposed, four tokens by 64 bytes at a time: those lie in four different 64-byte columns.
-template <int DH> __device__ __forceinline__ int k_place(int t, int c) { return t * (DH / 8) + (c ^ (t & 7)); }
-template <int DH> __device__ __forceinline__ int v_place(int t, int c) { return t * (DH / 8) + (c ^ (DH == 128 ? (t & 3) << 2 : (t & 2) << 1)); }
+// 16-byte columns.  Values are read transposed, four tokens by 64 bytes at a time: those lie in four different 64-byte columns.  (Rows of 96 elements, 3/4 of the banks, put four tokens into
+// four different 64-byte columns by themselves.)
+template <int ROW> __device__ __forceinline__ int k_place(int t, int c) { return t * (ROW / 8) + (c ^ (ROW == 96 ? t >> 2 & 3 : t & 7)); }
+template <int ROW> __device__ __forceinline__ int v_place(int t, int c) { return t * (ROW / 8) + (c ^ (ROW == 128 ? (t & 3) << 2 : ROW == 64 ? (t & 2) << 1 : 0)); }
 
 __device__ __forceinline__ s16x4 read_transposed(const bf16_t* p) {   // lane l of 16 gets element l of the four 16-element rows whose l / 4-th this address is in
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p);
@@ -127,7 +129,9 @@ struct ChunkAttn {
   static constexpr bool DIRECT = NK == 1, KEYS_IN_LDS = WIDE || DIRECT;
   static constexpr int KT = WIDE && NK == 1 ? 64 : 32, KB = KT / 32, KSN = DH / 16, DB = DH / 32;
   static constexpr int COLS = WIDE ? 128 : 32;
-  static constexpr int TILE = KT * DH;                            // elements of a piece of a tile
+  static constexpr int ROW = DIRECT && DH == 96 ? 128 : DH;       // elements of a token in LDS (a DIRECT load fills 1 KiB: whole tokens)
+  static constexpr int PART = DH <= 64 ? 64 : 128;                // and in the workspace
+  static constexpr int TILE = KT * ROW;                           // elements of a piece of a tile
   static constexpr int OWNERS = WIDE ? 1 : 4;                     // waves with a tile of their own
   static constexpr int K_ELTS = KEYS_IN_LDS ? OWNERS * NK * TILE : 8, V_ELTS = OWNERS * NK * TILE;   // of one buffer
   static constexpr bool TWO = WIDE;                               // buffers
@@ -135,9 +139,9 @@ struct ChunkAttn {
   static constexpr int V0_ELTS = V_ELTS > JOIN ? V_ELTS : JOIN;
   static constexpr int LDS = 2 * ((TWO ? 2 : 1) * K_ELTS + V0_ELTS + (TWO ? V_ELTS : 0));
   static constexpr int PRODUCTS = NQ * NK == 9 ? 6 : NQ * NK;     // of pieces that are kept
-  static constexpr int WAVES = NK == 3 && DH == 128 ? 1 : 2;      // a SIMD holds (by registers)
+  static constexpr int WAVES = NK == 3 && (DH == 128 || (DH == 96 && !WIDE)) ? 1 : 2;      // a SIMD holds (by registers)
   static constexpr int GROUP = WIDE ? 256 : 64;                   // threads that fetch a tile together
-  static constexpr int ITEMS = KT * DH / 8 / GROUP;               // runs of 8 elements a thread fetches of the values (and of the keys if they go through LDS)
+  static constexpr int RUNS = KT * DH / 8, ITEMS = (RUNS + GROUP - 1) / GROUP;   // runs of 8 elements in a tile; runs of 8 elements a thread fetches of the values (and of the keys if they go through LDS)
 };
 
 typedef __attribute__((address_space(3))) bf16_t* lds_ptr;
@@ -155,14 +159,15 @@ __device__ __forceinline__ void wait_lds() {
 
 template <typename P, typename T, typename CT>
 __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev A) {
-  constexpr int DH = P::DH, NQ = P::NQ, NK = P::NK, NP = P::NP, KT = P::KT, KB = P::KB, KSN = P::KSN, DB = P::DB, COLS = P::COLS, TILE = P::TILE, ITEMS = P::ITEMS;
+  constexpr int DH = P::DH, ROW = P::ROW, NQ = P::NQ, NK = P::NK, NP = P::NP, KT = P::KT, KB = P::KB, KSN = P::KSN, DB = P::DB, COLS = P::COLS, TILE = P::TILE, ITEMS = P::ITEMS;
   constexpr bool WIDE = P::WIDE, MODS = P::MODS, DIRECT = P::DIRECT;
   // (arrays of their own: the compiler tells reads of one from loads on their way into another)
   __shared__ __attribute__((aligned(16))) bf16_t k_lds0[P::K_ELTS], k_lds1[P::TWO ? P::K_ELTS : 8], v_lds0[P::V0_ELTS], v_lds1[P::TWO ? P::V_ELTS : 8];
   __shared__ int s_bad[2];                                        // WIDE, not DIRECT: number of the last tile in a buffer whose values are not all finite
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane & 31, hh = lane >> 5;
   const int kvh = blockIdx.x % A.kv.n_kv_heads, part = blockIdx.x / A.kv.n_kv_heads, s = blockIdx.y, g = A.H / A.kv.n_kv_heads, dh = A.kv.head_dim;
-  const int cb = A.col_blocks - 1 - part % A.col_blocks, split = part / A.col_blocks;   // (blocks of the last rows see most: first)
+  // Blocks of the last rows see most and go first.  Where all work-groups are resident at once, two a CU, the second half ascends, so that a CU's two see as much as another's.
+  const int nth = part % A.col_blocks, split = part / A.col_blocks, cb = nth < A.turn ? A.col_blocks - 1 - nth : nth - A.turn;
   const int col0 = cb * COLS;
   const ColumnRange R = column_range<KT>(A, s, col0, COLS, g);
   if (col0 >= R.n * g) return;
@@ -203,15 +208,15 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
 
   // ---- DIRECT: a load instruction fills 1 KiB of LDS, RPI tokens of DH elements; lane -> (token, place), and the piece of 8 elements that belongs in the place.  What is not there (a page, a
   // token behind the last, elements from head_dim on) is whatever lies in page 0, or in the head's first piece: finite or not, it is masked like what a column may not see.
-  constexpr int RPI = 512 / DH, INSTS = DIRECT ? KT / RPI / (WIDE ? 4 : 1) : 1;
-  const int tr = lane / (DH / 8), place = lane % (DH / 8);
+  constexpr int RPI = 512 / ROW, INSTS = DIRECT ? KT / RPI / (WIDE ? 4 : 1) : 1;
+  const int tr = lane / (ROW / 8), place = lane % (ROW / 8);
   // bytes from an instruction's first token to what this lane loads (the keys' order of pieces repeats every eight tokens, the values' every RPI)
   uint32_t k_off[8 / RPI], v_off;
   {
-    const int vc = place ^ (v_place<DH>(tr, 0) - tr * (DH / 8));
+    const int vc = place ^ (v_place<ROW>(tr, 0) - tr * (ROW / 8));
 #pragma unroll
     for (int i = 0; i < 8 / RPI; ++i) {
-      const int t = i * RPI + tr, kc = place ^ (k_place<DH>(t, 0) - t * (DH / 8));
+      const int t = i * RPI + tr, kc = place ^ (k_place<ROW>(t, 0) - t * (ROW / 8));
       k_off[i] = (uint32_t)(tr * (int)A.kv.token_stride + (kc * 8 < dh ? kc * 8 : 0)) * (uint32_t)sizeof(CT);
     }
     v_off = (uint32_t)(tr * (int)A.kv.token_stride + (vc * 8 < dh ? vc * 8 : 0)) * (uint32_t)sizeof(CT);
@@ -230,16 +235,16 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
       for (int u = 0; u < INSTS; ++u) {
         const int t0 = (first + u) * RPI, page = max(0, __builtin_amdgcn_readlane(pages, t0));
         const long long at = page * A.kv.page_stride + ((k0 + t0) & in_page) * A.kv.token_stride;
-        if constexpr (K) load_lds((const char*)(kb + at) + k_off[u % (8 / RPI)], kd + t0 * DH);
-        if constexpr (V) load_lds((const char*)(vb + at) + v_off, vd + t0 * DH);
+        if constexpr (K) load_lds((const char*)(kb + at) + k_off[u % (8 / RPI)], kd + t0 * ROW);
+        if constexpr (V) load_lds((const char*)(vb + at) + v_off, vd + t0 * ROW);
       }
     } else {
 #pragma unroll
       for (int u = 0; u < INSTS; ++u) {
         const int t0 = (first + u) * RPI, page = max(0, __shfl(pages, t0 + tr, 64));
         const long long at = page * A.kv.page_stride + (((k0 + t0 + tr) & in_page) - tr) * A.kv.token_stride;
-        if constexpr (K) load_lds((const char*)(kb + at) + k_off[u % (8 / RPI)], kd + t0 * DH);
-        if constexpr (V) load_lds((const char*)(vb + at) + v_off, vd + t0 * DH);
+        if constexpr (K) load_lds((const char*)(kb + at) + k_off[u % (8 / RPI)], kd + t0 * ROW);
+        if constexpr (V) load_lds((const char*)(vb + at) + v_off, vd + t0 * ROW);
       }
     }
   };
@@ -252,7 +257,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
     for (int i = 0; i < ITEMS; ++i) {
       const int item = i * P::GROUP + g_tid, t = item / (DH / 8), c = item % (DH / 8);
       const int page = __shfl(pages, t, 64);
-      const bool ok = page >= 0 && c * 8 < dh;
+      const bool ok = page >= 0 && c * 8 < dh && (P::RUNS % P::GROUP == 0 || item < P::RUNS);
       const long long at = page * A.kv.page_stride + ((k0 + t) & in_page) * A.kv.token_stride + c * 8;
       if constexpr (WIDE) { kr[i].zero(); if (ok) kr[i].load(kb + at); }
       vr[i].zero();
@@ -275,16 +280,17 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
       const int item = i * P::GROUP + g_tid, t = item / (DH / 8), c = item % (DH / 8);
+      if (P::RUNS % P::GROUP != 0 && item >= P::RUNS) continue;
       bf16x8 p[3];
       if constexpr (WIDE) {
         kr[i].split(p);
 #pragma unroll
-        for (int j = 0; j < NK; ++j) *(bf16x8*)(kd + j * TILE + 8 * k_place<DH>(t, c)) = p[j];
+        for (int j = 0; j < NK; ++j) *(bf16x8*)(kd + j * TILE + 8 * k_place<ROW>(t, c)) = p[j];
       }
       vr[i].split(p);
       if constexpr (!DIRECT) bad |= vr[i].bad();
 #pragma unroll
-      for (int j = 0; j < NK; ++j) *(bf16x8*)(vd + j * TILE + 8 * v_place<DH>(t, c)) = p[j];
+      for (int j = 0; j < NK; ++j) *(bf16x8*)(vd + j * TILE + 8 * v_place<ROW>(t, c)) = p[j];
     }
     return bad != 0;
   };
@@ -338,11 +344,11 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
   // Byte offsets in a buffer of what this lane reads of a tile: the keys' k-steps 0..3 (the others, and the second 32 tokens, lie a constant further on), the values' 32-wide blocks.
   uint32_t k_at[4], v_at[DB];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) k_at[i] = 16 * k_place<DH>(q, 2 * i + hh);
+  for (int i = 0; i < 4; ++i) k_at[i] = 16 * k_place<ROW>(q, 2 * i + hh);
 #pragma unroll
   for (int b = 0; b < DB; ++b) {
     const int t = 4 * hh + ((lane & 15) >> 2), c = 4 * b + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-    v_at[b] = 16 * v_place<DH>(t, c) + 8 * (lane & 1);
+    v_at[b] = 16 * v_place<ROW>(t, c) + 8 * (lane & 1);
   }
   const int wave_last = R.tree ? R.keys : max(R.own0 + min(R.n - 1, (wave_col + 31) / g), R.prefix - 1);   // last token a column of this wave may see
   const bool wave_live = wave_col < R.n * g;
@@ -380,7 +386,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
           bf16x8 kf[3];
           if constexpr (P::KEYS_IN_LDS) {
 #pragma unroll
-            for (int j = 0; j < NK; ++j) kf[j] = *(const bf16x8*)((const char*)kt + k_at[ks & 3] + (2 * j * TILE + 64 * DH * a + 128 * (ks >> 2)));
+            for (int j = 0; j < NK; ++j) kf[j] = *(const bf16x8*)((const char*)kt + k_at[ks & 3] + (2 * j * TILE + 64 * ROW * a + 128 * (ks >> 2)));
           } else kr[ks].split(kf);
 #pragma unroll
           for (int sum = NP - 1; sum >= 0; --sum)                 // small products first
@@ -506,10 +512,9 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
       // 0 times what is not finite is not 0.  So it is added to the columns that see it, and zeroed for the product.
       uint64_t spoilt = 0;
       for (int i = 0; i < TILE / 512; ++i) {
-        const uint64_t b = __ballot(exponents(*(const u32x4*)(vt + i * 512 + lane * 8)) != 0);
-        for (int j = 0; j < RPI; ++j)
-          if (b >> (j * (DH / 8)) & low_ones(DH / 8)) spoilt |= 1ull << (i * RPI + j);
+        if (exponents(*(const u32x4*)(vt + i * 512 + lane * 8)) != 0) spoilt |= 1ull << ((i * 64 + lane) / (ROW / 8));
       }
+      for (int o = 32; o; o >>= 1) spoilt |= __shfl_xor((unsigned long long)spoilt, o, 64);
       for (uint64_t left = spoilt & there; left && !idle; left &= left - 1) {
         const int t = __builtin_ctzll(left);
         const bool seen = vis >> t & 1;
@@ -518,7 +523,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int d = 32 * b + 8 * i + 4 * hh;
-            const u32x2 v = *(const u32x2*)(vt + 8 * v_place<DH>(t, d >> 3) + (d & 7));
+            const u32x2 v = *(const u32x2*)(vt + 8 * v_place<ROW>(t, d >> 3) + (d & 7));
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const float x = __builtin_bit_cast(float, e & 1 ? v[e >> 1] & 0xFFFF0000u : v[e >> 1] << 16);
@@ -561,8 +566,8 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
         for (int b = 0; b < DB; ++b) {
 #pragma unroll
           for (int j = 0; j < NK; ++j) {
-            const char* p = (const char*)vt + v_at[b] + (2 * j * TILE + 32 * DH * jj);
-            const s16x4 lo = read_transposed((const bf16_t*)p), hi = read_transposed((const bf16_t*)(p + 16 * DH));
+            const char* p = (const char*)vt + v_at[b] + (2 * j * TILE + 32 * ROW * jj);
+            const s16x4 lo = read_transposed((const bf16_t*)p), hi = read_transposed((const bf16_t*)(p + 16 * ROW));
             typedef short s16x8 __attribute__((ext_vector_type(8)));
             vf[j] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
           }
@@ -644,7 +649,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
   } else {
     const size_t at = ((size_t)row * A.H + head) * A.splits + split;
     if (hh == 0) { A.part_ml[2 * at] = m_run; A.part_ml[2 * at + 1] = l_run; }
-    float* o = A.part_o + at * DH;
+    float* o = A.part_o + at * P::PART;
 #pragma unroll
     for (int b = 0; b < DB; ++b)
 #pragma unroll
@@ -659,17 +664,17 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
 // there are: they lie in the workspace whatever they hold.
 template <typename P, typename T>
 __global__ __launch_bounds__(256) void k_chunk_attn_join(const ChunkAttnDev A) {
-  constexpr int DH = P::DH, E = DH / 64, AHEAD = 8;
+  constexpr int PART = P::PART, E = PART / 64, AHEAD = 8;
   const int row = blockIdx.x, head = blockIdx.y * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63, dh = A.kv.head_dim;
   if (head >= A.H) return;
   const size_t at = ((size_t)row * A.H + head) * A.splits;
-  const float* po = A.part_o + at * DH + lane * E;
+  const float* po = A.part_o + at * PART + lane * E;
   float ov[AHEAD][E];
   auto request = [&](int k0) {
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u)
 #pragma unroll
-      for (int e = 0; e < E; ++e) ov[u][e] = po[(size_t)min(k0 + u, A.splits - 1) * DH + e];
+      for (int e = 0; e < E; ++e) ov[u][e] = po[(size_t)min(k0 + u, A.splits - 1) * PART + e];
   };
   const float2 ml = *(const float2*)(A.part_ml + 2 * (at + min(lane, A.splits - 1)));
   request(0);

@@ -175,7 +175,7 @@ static int check_attention(const eagle_attention_args* a, const eagle_chunk* chu
 // Narrow, 64 sequences of 1k to 16k tokens, 64 / 8 heads, bf16, us with 1, 2, 3, 4, 6, 8 parts at most: 433 (2), 419 (3), 451 (4), 406 (6), 417 (8).  One token over 701 keys, 32 heads, fp32,
 // 22 tiles: parts of 4 tiles 17.6, of 5 23.0, of 3 29.4.  Wide: one a CU (four trees of 26 nodes on 8 kv heads, fp32 queries, 37 tiles: 8 parts 27, 10 parts 32 to 38; 2011 fp32 rows on 32 heads, 512 work-groups: whole
 // 327, in two 339 and 26 more for joining).
-constexpr int ATTN_WIDE_WGS = 256, ATTN_NARROW_WGS = 3000, ATTN_MIN_TILES = 4, ATTN_MAX_PARTS = 64;
+constexpr int ATTN_WIDE_WGS = 256, ATTN_NARROW_WGS = 3200, ATTN_MIN_TILES = 4, ATTN_MAX_PARTS = 64;
 
 // Columns and parts of a call; returns the bytes of workspace, at most `limit` of them if that is possible.
 static size_t plan_attention(ChunkAttnDev* d, int kv_dtype, size_t limit, bool* wide) {
@@ -187,12 +187,12 @@ static size_t plan_attention(ChunkAttnDev* d, int kv_dtype, size_t limit, bool* 
   const long long units = (long long)d->col_blocks * d->kv.n_kv_heads * d->chunk.n_seqs, tiles = ((long long)d->chunk.max_keys + KT - 1) / KT;
   long long parts = std::min((*wide ? ATTN_WIDE_WGS : ATTN_NARROW_WGS) / units, (tiles + ATTN_MIN_TILES - 1) / ATTN_MIN_TILES);
   parts = std::max(1ll, std::min(parts, (long long)ATTN_MAX_PARTS));
-  const size_t pairs = (size_t)d->chunk.n_rows * d->H, DH = d->kv.head_dim <= 64 ? 64 : 128;
+  const size_t pairs = (size_t)d->chunk.n_rows * d->H, PART = d->kv.head_dim <= 64 ? 64 : 128;
   for (;; --parts) {
     d->split_tiles = (int)((tiles + parts * round - 1) / (parts * round) * round);
     d->splits = (int)((tiles + d->split_tiles - 1) / d->split_tiles);
     if (d->splits == 1) return 256;
-    const size_t bytes = (pairs * d->splits * 8 + 255) / 256 * 256 + pairs * d->splits * DH * 4;
+    const size_t bytes = (pairs * d->splits * 8 + 255) / 256 * 256 + pairs * d->splits * PART * 4;
     if (bytes <= limit) return bytes;
   }
 }
@@ -205,9 +205,11 @@ extern "C" size_t eagle_chunk_attention_workspace(const eagle_attention_args* a,
 }
 
 template <typename T, typename CT, int DH, bool WIDE, bool MODS>
-static int launch_attention(const ChunkAttnDev& d, hipStream_t stream) {
+static int launch_attention(ChunkAttnDev d, hipStream_t stream) {
   typedef ChunkAttn<T, CT, DH, WIDE, MODS> P;
   auto kernel = k_chunk_attn<P, T, CT>;
+  const int blocks = d.kv.n_kv_heads * d.col_blocks;
+  d.turn = P::WAVES == 2 && d.chunk.n_seqs == 1 && d.splits == 1 && blocks <= 512 ? std::max(1, 256 / d.kv.n_kv_heads) : d.col_blocks;
   kernel<<<dim3(d.kv.n_kv_heads * d.col_blocks * d.splits, d.chunk.n_seqs), 256, 0, stream>>>(d);
   LAUNCH_CHECK();
   if (d.splits > 1) {
@@ -218,9 +220,9 @@ static int launch_attention(const ChunkAttnDev& d, hipStream_t stream) {
 }
 template <typename T, typename CT>
 static int launch_attention(const ChunkAttnDev& d, bool wide, bool mods, hipStream_t stream) {
-  const bool big = d.kv.head_dim > 64;
 #define ATTEND(DH, WIDE) return mods ? launch_attention<T, CT, DH, WIDE, true>(d, stream) : launch_attention<T, CT, DH, WIDE, false>(d, stream)
-  if (big) { if (wide) ATTEND(128, true); else ATTEND(128, false); }
+  if (d.kv.head_dim > 96) { if (wide) ATTEND(128, true); else ATTEND(128, false); }
+  if (d.kv.head_dim > 64) { if (wide) ATTEND(96, true); else ATTEND(96, false); }
   if (wide) ATTEND(64, true); else ATTEND(64, false);
 #undef ATTEND
 }

@@ -167,6 +167,23 @@ def test_what_a_row_does_not_see_does_not_reach_it(rows, keys, H, value, types):
         c.copy_(old)
 
 
+@pytest.mark.parametrize("types", ALL)
+@pytest.mark.parametrize("D", [72, 80, 88, 96, 104, 112, 120])
+@pytest.mark.parametrize("rows,keys", [([1, 2], [150, 40]), ([70, 30], [200, 90])])
+def test_head_sizes_between(rows, keys, D, types):
+    """Between 64 and 128, where a token's elements and what a tile holds of them differ: masks, pages that are not there, values that are not finite."""
+    p = pkg()
+    run(rows, keys, 4, 2, D, types, 16, gap=[(0, 1)], window=60, prefix=[7, 3], slopes=True, poison=True)
+    q, kv, chunk, out, (kc, vc, table) = run(rows, keys, 4, 4, D, types, 32)
+    t = keys[1] - 1                                               # what only the last row sees
+    for at in (3, D - 1):
+        vc[table[1, t // 32], :, t % 32, at] = float("inf")
+    got = p.chunk_attention(q, kv, chunk)
+    assert torch.equal(got[:-1], out[:-1])
+    rest = [e for e in range(D) if e not in (3, D - 1)]
+    assert torch.equal(got[-1][:, rest], out[-1][:, rest]) and torch.all(got[-1][:, [3, D - 1]] == float("inf"))
+
+
 def test_strides_orders_and_rows_of_no_sequence():
     p = pkg()
     q, kv, chunk, out, (kc, vc, table) = run([3, 9], [50, 70], 4, 2, 64, "bf16/bf16", 16)
