@@ -66,9 +66,10 @@ __device__ inline ColumnRange column_range(const ChunkAttnDev& A, int s, int col
 __device__ __forceinline__ uint64_t low_ones(int n) { return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1ull; }
 
 // x as an exact sum of bf16 pieces.  (Of what is not finite the first is the same, the others NaN.)
-template <int NP> __device__ __forceinline__ void pieces8(const float* x, bf16x8* p) {
+typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+template <int NP, int N, typename V> __device__ __forceinline__ void pieces(const float* x, V* p) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < N; ++i) {
     p[0][i] = (__bf16)x[i];
     if constexpr (NP == 3) {
       float r = x[i] - (float)p[0][i];
@@ -86,6 +87,13 @@ __device__ __forceinline__ uint32_t exponents(u32x4 v) {
   for (int e = 0; e < 4; ++e) any |= (v[e] & 0x7F807F80u) + 0x00800080u;
   return any & 0x80008000u;
 }
+__device__ __forceinline__ uint32_t not_finite_any(f32x4 x) {
+  const u32x4 u = __builtin_bit_cast(u32x4, x);
+  uint32_t any = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) any |= (u[i] & 0x7F800000u) + 0x00800000u;
+  return any & 0x80000000u;
+}
 // Eight elements of a token in flight, and their pieces.
 template <typename CT> struct Raw8;
 template <> struct Raw8<bf16_t> {
@@ -98,16 +106,10 @@ template <> struct Raw8<float> {
   f32x4 a, b;
   __device__ __forceinline__ void load(const float* p) { a = *(const f32x4*)p; b = *(const f32x4*)(p + 4); }
   __device__ __forceinline__ void zero() { a = b = f32x4{0.f, 0.f, 0.f, 0.f}; }
-  __device__ __forceinline__ uint32_t bad() const {               // (see exponents())
-    const u32x4 u = __builtin_bit_cast(u32x4, a), v = __builtin_bit_cast(u32x4, b);
-    uint32_t any = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) any |= ((u[i] & 0x7F800000u) + 0x00800000u) | ((v[i] & 0x7F800000u) + 0x00800000u);
-    return any & 0x80000000u;
-  }
+  __device__ __forceinline__ uint32_t bad() const { return not_finite_any(a) | not_finite_any(b); }
   __device__ __forceinline__ void split(bf16x8* p) const {
     const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-    pieces8<3>(x, p);
+    pieces<3, 8>(x, p);
   }
 };
 
@@ -138,10 +140,15 @@ struct ChunkAttn {
   static constexpr int JOIN = WIDE ? 0 : 2 * (16 * DB + 2) * 64 * 2;   // elements (of 2 bytes) that joining the waves takes
   static constexpr int V0_ELTS = V_ELTS > JOIN ? V_ELTS : JOIN;
   static constexpr int LDS = 2 * ((TWO ? 2 : 1) * K_ELTS + V0_ELTS + (TWO ? V_ELTS : 0));
-  static constexpr int PRODUCTS = NQ * NK == 9 ? 6 : NQ * NK;     // of pieces that are kept
+  // The products of pieces that are kept, n-th of them: a piece of the cache, one of the columns (queries, weights).  Small ones come first, and of three cache pieces each is done with as soon
+  // as can be, so that the next one's can take its registers.
+  static constexpr int PRODUCTS = NQ * NK == 9 ? 6 : NQ * NK;
+  static constexpr int cache_piece(int n) { return NK == 1 ? 0 : n == 0 ? 2 : n < 3 ? 1 : 0; }
+  static constexpr int column_piece(int n) { return NQ == 1 ? 0 : NK == 1 ? 2 - n : n == 0 ? 0 : n < 3 ? 2 - n : 5 - n; }
+  static constexpr bool done_with(int n) { return NK == 3 && (n == 0 || n == 2 || n == 5); }   // the cache piece of product n
   static constexpr int WAVES = NK == 3 && (DH == 128 || (DH == 96 && !WIDE)) ? 1 : 2;      // a SIMD holds (by registers)
-  static constexpr int GROUP = WIDE ? 256 : 64;                   // threads that fetch a tile together
-  static constexpr int RUNS = KT * DH / 8, ITEMS = (RUNS + GROUP - 1) / GROUP;   // runs of 8 elements in a tile; runs of 8 elements a thread fetches of the values (and of the keys if they go through LDS)
+  static constexpr bool SPLIT = WIDE && !DIRECT;                  // fp32 keys and values go through LDS in pieces
+  static constexpr int ITEMS = SPLIT ? KT * DH / 4 / 256 : KT * DH / 8 / 64;   // runs of 4 (SPLIT) or 8 elements a thread fetches of the values, and of the keys if they go through LDS
 };
 
 typedef __attribute__((address_space(3))) bf16_t* lds_ptr;
@@ -159,7 +166,7 @@ __device__ __forceinline__ void wait_lds() {
 
 template <typename P, typename T, typename CT>
 __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev A) {
-  constexpr int DH = P::DH, ROW = P::ROW, NQ = P::NQ, NK = P::NK, NP = P::NP, KT = P::KT, KB = P::KB, KSN = P::KSN, DB = P::DB, COLS = P::COLS, TILE = P::TILE, ITEMS = P::ITEMS;
+  constexpr int DH = P::DH, ROW = P::ROW, NQ = P::NQ, NK = P::NK, KT = P::KT, KB = P::KB, KSN = P::KSN, DB = P::DB, COLS = P::COLS, TILE = P::TILE, ITEMS = P::ITEMS;
   constexpr bool WIDE = P::WIDE, MODS = P::MODS, DIRECT = P::DIRECT;
   // (arrays of their own: the compiler tells reads of one from loads on their way into another)
   __shared__ __attribute__((aligned(16))) bf16_t k_lds0[P::K_ELTS], k_lds1[P::TWO ? P::K_ELTS : 8], v_lds0[P::V0_ELTS], v_lds1[P::TWO ? P::V_ELTS : 8];
@@ -250,18 +257,26 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
   };
 
   // ---- not DIRECT: through registers
-  Raw8<CT> kr[DIRECT ? 1 : WIDE ? ITEMS : KSN], vr[DIRECT ? 1 : ITEMS];
+  f32x4 k4[P::SPLIT ? ITEMS : 1], v4[P::SPLIT ? ITEMS : 1];
+  Raw8<CT> kr[DIRECT || WIDE ? 1 : KSN], vr[DIRECT || WIDE ? 1 : ITEMS];
   auto fetch = [&](int it, int pages) {
     const int k0 = tile_token(it);
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-      const int item = i * P::GROUP + g_tid, t = item / (DH / 8), c = item % (DH / 8);
+      constexpr int RUN = P::SPLIT ? 4 : 8;
+      int item = i * (WIDE ? 256 : 64) + g_tid;
+      if constexpr (P::SPLIT) asm volatile("" : "+v"(item));      // (see put_step)
+      const int t = item / (DH / RUN), c = item % (DH / RUN);
       const int page = __shfl(pages, t, 64);
-      const bool ok = page >= 0 && c * 8 < dh && (P::RUNS % P::GROUP == 0 || item < P::RUNS);
-      const long long at = page * A.kv.page_stride + ((k0 + t) & in_page) * A.kv.token_stride + c * 8;
-      if constexpr (WIDE) { kr[i].zero(); if (ok) kr[i].load(kb + at); }
-      vr[i].zero();
-      if (ok) vr[i].load(vb + at);
+      const bool ok = page >= 0 && c * RUN < dh;
+      const long long at = page * A.kv.page_stride + ((k0 + t) & in_page) * A.kv.token_stride + c * RUN;
+      if constexpr (P::SPLIT) {
+        k4[i] = v4[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (ok) { k4[i] = *(const f32x4*)(kb + at); v4[i] = *(const f32x4*)(vb + at); }
+      } else {
+        vr[i].zero();
+        if (ok) vr[i].load(vb + at);
+      }
     }
     if constexpr (!WIDE) {
       const int page = pages;                                     // (KT = 32: the lane's own token)
@@ -274,32 +289,57 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
       }
     }
   };
-  // the fetched tile to LDS; returns whether a value is not finite (to this thread's knowledge)
-  auto put = [&](bf16_t* kd, bf16_t* vd) -> bool {
-    uint32_t bad = 0;
+  // SPLIT: a step of bringing the fetched tile to LDS, of as many as there are products of a tile's scores: three for two elements, six for a run.
+  auto put_step = [&](bf16_t* kd, bf16_t* vd, int n, u32x2* pk) -> uint32_t {
+    const int run = n / 6, i = run >> 1, pair = n % 6 / 3, j = n % 3;
+    const bool values = run & 1;
+    f32x4& x = values ? v4[i] : k4[i];
+    const uint32_t bad = values && pair == 0 && j == 0 ? not_finite_any(x) : 0;
+    const uint32_t h = bf16_pair(x[2 * pair], x[2 * pair + 1]);
+    pk[j][pair] = h;
+    if (j < 2) {
+      x[2 * pair] -= __builtin_bit_cast(float, h << 16);
+      x[2 * pair + 1] -= __builtin_bit_cast(float, h & 0xFFFF0000u);
+    } else if (pair == 1) {
+      int item = i * 256 + tid;
+      asm volatile("" : "+v"(item));                             // (worked out anew for every tile: kept, the places cost more registers than there are)
+      const int t = item / (DH / 4), c = item % (DH / 4);
+      bf16_t* d = (values ? vd + 8 * v_place<ROW>(t, c >> 1) : kd + 8 * k_place<ROW>(t, c >> 1)) + 4 * (c & 1);
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
-      const int item = i * P::GROUP + g_tid, t = item / (DH / 8), c = item % (DH / 8);
-      if (P::RUNS % P::GROUP != 0 && item >= P::RUNS) continue;
-      bf16x8 p[3];
-      if constexpr (WIDE) {
-        kr[i].split(p);
-#pragma unroll
-        for (int j = 0; j < NK; ++j) *(bf16x8*)(kd + j * TILE + 8 * k_place<ROW>(t, c)) = p[j];
-      }
-      vr[i].split(p);
-      if constexpr (!DIRECT) bad |= vr[i].bad();
-#pragma unroll
-      for (int j = 0; j < NK; ++j) *(bf16x8*)(vd + j * TILE + 8 * v_place<ROW>(t, c)) = p[j];
+      for (int u = 0; u < 3; ++u) *(u32x2*)(d + u * TILE) = pk[u];
     }
-    return bad != 0;
+    return bad;
+  };
+  // the fetched tile to LDS; returns not 0 if a value is not finite (to this thread's knowledge)
+  auto put = [&](bf16_t* kd, bf16_t* vd) -> uint32_t {
+    uint32_t bad = 0;
+    if constexpr (P::SPLIT) {
+      u32x2 pk[3];
+#pragma unroll
+      for (int n = 0; n < 12 * ITEMS; ++n) bad |= put_step(kd, vd, n, pk);
+    } else {
+#pragma unroll
+      for (int i = 0; i < ITEMS; ++i) {
+        const int item = i * 64 + lane, t = item / (DH / 8), c = item % (DH / 8);
+        bf16x8 p[3];
+        vr[i].split(p);
+        if constexpr (!DIRECT) bad |= vr[i].bad();
+#pragma unroll
+        for (int j = 0; j < NK; ++j) *(bf16x8*)(vd + j * TILE + 8 * v_place<ROW>(t, c)) = p[j];
+      }
+    }
+    return bad;
   };
 
   int it = t_begin + (WIDE ? 0 : w);
-  int pages = -1, entry_next = 0;
+  int pages = -1, entry_next = 0, pages1 = -1;                    // (SPLIT: pages1 are the next tile's, entry_next is the one's behind it)
   if (it < t_end) {
     pages = page_of(it, entry_of(it));
     entry_next = entry_of(it + STEP);
+    if constexpr (P::SPLIT) {
+      if (it + 1 < t_end) pages1 = page_of(it + 1, entry_next);
+      entry_next = entry_of(it + 2);
+    }
   }
   if constexpr (STAGGERED) {
     if (it < t_end) {
@@ -325,11 +365,12 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
       for (int i = 0; i < NQ; ++i) qf[i][ks] = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, p[i]) ^ A.q_flip);
     }
   }
-  if constexpr (WIDE && !DIRECT) {
+  if constexpr (P::SPLIT) {
     if (tid < 2) s_bad[tid] = -1;
     __syncthreads();
-    if (it < t_end && __any(put(k_lds0, v_lds0)) && lane == 0) s_bad[0] = it;
+    if (it < t_end && __any(put(k_lds0, v_lds0) != 0) && lane == 0) s_bad[0] = it;
     __syncthreads();
+    fetch(it + 1, pages1);
   }
 
   const float c2 = A.scale * 1.44269504088896341f;                // scores to powers of two
@@ -360,7 +401,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
     const uint64_t there = __ballot(pages >= 0) & low_ones(KT);
     const bool full = k0 + KT <= R.full_to && (k0 >= R.full_from || k0 + KT <= R.prefix) && there == low_ones(KT);
     bool bad = false;
-    const int pages_next = page_of(it + STEP, entry_next);
+    const int pages_next = P::SPLIT ? pages1 : page_of(it + STEP, entry_next);
     if constexpr (STAGGERED) {
       wait_loads<INSTS>();                   // the keys have landed (the values are behind them)
     } else if constexpr (DIRECT) {
@@ -369,33 +410,50 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
       if constexpr (WIDE) { __builtin_amdgcn_s_barrier(); asm volatile("" ::: "memory"); }
       if (it + STEP < t_end) dma((lds_ptr)kn, (lds_ptr)vn, it + STEP, pages_next, BOTH());
     } else if constexpr (WIDE) {
-      if (it + 1 < t_end) fetch(it + 1, pages_next);
       bad = s_bad[which] == it;
     } else {
-      bad = __any(put(kt, vt));
+      bad = __any(put(kt, vt) != 0);
     }
     const bool idle = WIDE && (!wave_live || k0 > wave_last);     // (the wave's part of moving data and the barriers stay)
     f32x16 sacc[KB];
-    if (!idle) {
+    uint32_t next_bad = 0;
+    if (idle) {
+      if constexpr (P::SPLIT) next_bad = put(kn, vn);
+    } else {
+      auto key = [&](int a, int ks, int j) -> bf16x8 { return *(const bf16x8*)((const char*)kt + k_at[ks & 3] + (2 * j * TILE + 64 * ROW * a + 128 * (ks >> 2))); };
 #pragma unroll
-      for (int a = 0; a < KB; ++a) {
+      for (int a = 0; a < KB; ++a)
 #pragma unroll
         for (int r = 0; r < 16; ++r) sacc[a][r] = 0.f;
+      if constexpr (P::SPLIT) {
+        // The next tile's pieces are made between this one's products (behind the last tile they are zeros): a step of it while the matrix unit works, in this order.
+        bf16x8 kf[NK];
+        u32x2 pk[3];
 #pragma unroll
-        for (int ks = 0; ks < KSN; ++ks) {
-          bf16x8 kf[3];
-          if constexpr (P::KEYS_IN_LDS) {
+        for (int j = NK - 1; j >= 0; --j) kf[j] = key(0, 0, j);
 #pragma unroll
-            for (int j = 0; j < NK; ++j) kf[j] = *(const bf16x8*)((const char*)kt + k_at[ks & 3] + (2 * j * TILE + 64 * ROW * a + 128 * (ks >> 2)));
-          } else kr[ks].split(kf);
-#pragma unroll
-          for (int sum = NP - 1; sum >= 0; --sum)                 // small products first
-#pragma unroll
-            for (int i = 0; i < NQ; ++i)
-              if (sum - i >= 0 && sum - i < NK) sacc[a] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[sum - i], qf[i][ks], sacc[a], 0, 0, 0);
+        for (int n = 0; n < KSN * P::PRODUCTS; ++n) {
+          const int ks = n / P::PRODUCTS, u = n % P::PRODUCTS, j = P::cache_piece(u);
+          sacc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[j], qf[P::column_piece(u)][ks], sacc[0], 0, 0, 0);
+          if (P::done_with(u) && ks + 1 < KSN) kf[j] = key(0, ks + 1, j);
+          next_bad |= put_step(kn, vn, n, pk);
+          __builtin_amdgcn_sched_barrier(0);
         }
+      } else {
+#pragma unroll
+        for (int a = 0; a < KB; ++a)
+#pragma unroll
+          for (int ks = 0; ks < KSN; ++ks) {
+            bf16x8 kf[3];
+            if constexpr (P::KEYS_IN_LDS) {
+#pragma unroll
+              for (int j = 0; j < NK; ++j) kf[j] = key(a, ks, j);
+            } else kr[ks].split(kf);
+#pragma unroll
+            for (int u = 0; u < P::PRODUCTS; ++u) sacc[a] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[P::cache_piece(u)], qf[P::column_piece(u)][ks], sacc[a], 0, 0, 0);
+          }
       }
-      if constexpr (P::KEYS_IN_LDS) {                             // order: four k-steps' reads ahead of their products
+      if constexpr (P::KEYS_IN_LDS && !P::SPLIT) {                // order: four k-steps' reads ahead of their products
         constexpr int STEPS = KB * KSN, AHEAD = STEPS < 4 ? STEPS : 4;
         __builtin_amdgcn_sched_group_barrier(0x100, NK * AHEAD, 0);
 #pragma unroll
@@ -414,7 +472,12 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
       dma((lds_ptr)kt, (lds_ptr)vt, it + STEP, pages_next, KEYS());
     }
     pages = pages_next;
-    if constexpr (!STAGGERED) entry_next = entry_of(it + 2 * STEP);
+    if constexpr (P::SPLIT) {
+      if (__any(next_bad != 0) && lane == 0) s_bad[which ^ 1] = it + 1;
+      pages1 = it + 2 < t_end ? page_of(it + 2, entry_next) : -1;
+      fetch(it + 2, pages1);
+      entry_next = entry_of(it + 3);
+    } else if constexpr (!STAGGERED) entry_next = entry_of(it + 2 * STEP);
     uint64_t vis = ~0ull;                                         // tokens of the tile that the column sees
     if (!idle) {
     // cap and slopes
@@ -511,6 +574,9 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
     if (bad) {
       // 0 times what is not finite is not 0.  So it is added to the columns that see it, and zeroed for the product.
       uint64_t spoilt = 0;
+      int h4 = 4 * hh;
+      asm volatile("" : "+v"(h4));                                // (nothing of this is worked out ahead of the loop and kept)
+#pragma unroll 1
       for (int i = 0; i < TILE / 512; ++i) {
         if (exponents(*(const u32x4*)(vt + i * 512 + lane * 8)) != 0) spoilt |= 1ull << ((i * 64 + lane) / (ROW / 8));
       }
@@ -522,7 +588,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
         for (int b = 0; b < DB; ++b)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const int d = 32 * b + 8 * i + 4 * hh;
+            const int d = 32 * b + 8 * i + h4;
             const u32x2 v = *(const u32x2*)(vt + 8 * v_place<ROW>(t, d >> 3) + (d & 7));
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -532,6 +598,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
           }
       }
       if constexpr (WIDE) __syncthreads();
+#pragma unroll 1
       for (int i = WIDE ? w : 0; i < NK * TILE / 512; i += WIDE ? 4 : 1) {   // (all pieces)
         u32x4 v = *(const u32x4*)(vt + i * 512 + lane * 8);
 #pragma unroll
@@ -545,49 +612,59 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
     }
     if (!idle) {
     const float m_sub = m_run == -INFINITY ? 0.f : m_run;
+    // 16 tokens at a time: their values are read a block ahead, and the weights of the next 16 are made between the products, in this order.
+    constexpr int GROUPS = KT / 16 * DB, SLOTS = DB * P::PRODUCTS, WORK = NQ == 3 ? 12 : 4;
+    u32x4 pf[2][NQ];
+    bf16x8 vf[NK == 1 ? 2 : 1][NK];
     float sum = 0.f;
-#pragma unroll
-    for (int a = 0; a < KB; ++a)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const float e = __builtin_amdgcn_exp2f(MODS ? sacc[a][r] - m_sub : fmaf(sacc[a][r], c2, -m_sub));
-        sacc[a][r] = e;
-        sum += e;
+    auto weights = [&](int jj, int n) {                           // n of WORK steps: a pair's weights and their first piece, its second, its third
+      const int pair = NQ == 3 ? n / 3 : n, j = NQ == 3 ? n % 3 : 0, a = jj >> 1, r = 8 * (jj & 1) + 2 * pair;
+      float x = sacc[a][r], y = sacc[a][r + 1];
+      if (j == 0) {
+        x = __builtin_amdgcn_exp2f(MODS ? x - m_sub : fmaf(x, c2, -m_sub));
+        y = __builtin_amdgcn_exp2f(MODS ? y - m_sub : fmaf(y, c2, -m_sub));
+        sum += x;
+        sum += y;
       }
+      const uint32_t h = bf16_pair(x, y);
+      pf[jj & 1][j][pair] = h;
+      if (j + 1 < NQ) {
+        sacc[a][r] = x - __builtin_bit_cast(float, h << 16);
+        sacc[a][r + 1] = y - __builtin_bit_cast(float, h & 0xFFFF0000u);
+      }
+    };
+    auto value = [&](int i, int j) {                              // piece j of block i % DB of 16 tokens
+      const char* p = (const char*)vt + v_at[i % DB] + (2 * j * TILE + 32 * ROW * (i / DB));
+      const s16x4 lo = read_transposed((const bf16_t*)p), hi = read_transposed((const bf16_t*)(p + 16 * ROW));
+      vf[NK == 1 ? i & 1 : 0][j] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+#pragma unroll
+    for (int j = NK - 1; j >= 0; --j) value(0, j);
+#pragma unroll
+    for (int n = 0; n < WORK; ++n) weights(0, n);
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i) {
+      const int jj = i / DB, b = i % DB;
+      if (NK == 1 && i + 1 < GROUPS) value(i + 1, 0);
+#pragma unroll
+      for (int u = 0; u < P::PRODUCTS; ++u) {
+        const int j = P::cache_piece(u), slot = b * P::PRODUCTS + u;
+        oacc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[NK == 1 ? i & 1 : 0][j], __builtin_bit_cast(bf16x8, pf[jj & 1][P::column_piece(u)]), oacc[b], 0, 0, 0);
+        if (P::done_with(u) && i + 1 < GROUPS) value(i + 1, j);
+        if (jj + 1 < KT / 16)
+#pragma unroll
+          for (int n = slot * WORK / SLOTS; n < (slot + 1) * WORK / SLOTS; ++n) weights(jj + 1, n);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
     l_run += sum;
-#pragma unroll
-      for (int jj = 0; jj < KT / 16; ++jj) {
-        bf16x8 pf[3], vf[3];
-        float x[8];
-#pragma unroll
-        for (int t = 0; t < 8; ++t) x[t] = sacc[jj >> 1][8 * (jj & 1) + t];
-        pieces8<NQ>(x, pf);
-#pragma unroll
-        for (int b = 0; b < DB; ++b) {
-#pragma unroll
-          for (int j = 0; j < NK; ++j) {
-            const char* p = (const char*)vt + v_at[b] + (2 * j * TILE + 32 * ROW * jj);
-            const s16x4 lo = read_transposed((const bf16_t*)p), hi = read_transposed((const bf16_t*)(p + 16 * ROW));
-            typedef short s16x8 __attribute__((ext_vector_type(8)));
-            vf[j] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-          }
-#pragma unroll
-          for (int sum2 = NP - 1; sum2 >= 0; --sum2)
-#pragma unroll
-            for (int i = 0; i < NQ; ++i)
-              if (sum2 - i >= 0 && sum2 - i < NK) oacc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[sum2 - i], pf[i], oacc[b], 0, 0, 0);
-        }
-      }
     }
     if constexpr (STAGGERED && !LAST) {
       entry_next = entry_of(it + 2 * STEP);
       wait_lds();                                                 // the values have been read
       dma((lds_ptr)kt, (lds_ptr)vt, it + STEP, pages, VALUES());
     }
-    if constexpr (WIDE && !DIRECT) {
-      if (it + 1 < t_end && __any(put(kn, vn)) && lane == 0) s_bad[which ^ 1] = it + 1;
-      __syncthreads();
-    }
+    if constexpr (P::SPLIT) __syncthreads();
     it += STEP;
   };
   if constexpr (P::TWO) {
