@@ -145,7 +145,7 @@ struct ChunkAttn {
   static constexpr int PRODUCTS = NQ * NK == 9 ? 6 : NQ * NK;
   static constexpr int cache_piece(int n) { return NK == 1 ? 0 : n == 0 ? 2 : n < 3 ? 1 : 0; }
   static constexpr int column_piece(int n) { return NQ == 1 ? 0 : NK == 1 ? 2 - n : n == 0 ? 0 : n < 3 ? 2 - n : 5 - n; }
-  static constexpr bool done_with(int n) { return NK == 3 && (n == 0 || n == 2 || n == 5); }   // the cache piece of product n
+  static constexpr bool done_with(int n) { return NK == 3 ? n == 0 || n == 2 || n == 5 : n == PRODUCTS - 1; }   // the cache piece of product n
   static constexpr int WAVES = NK == 3 && (DH == 128 || (DH == 96 && !WIDE)) ? 1 : 2;      // a SIMD holds (by registers)
   static constexpr bool SPLIT = WIDE && !DIRECT;                  // fp32 keys and values go through LDS in pieces
   static constexpr int ITEMS = SPLIT ? KT * DH / 4 / 256 : KT * DH / 8 / 64;   // runs of 4 (SPLIT) or 8 elements a thread fetches of the values, and of the keys if they go through LDS
@@ -184,18 +184,26 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
 
   // this lane's column
   const int wave_col = col0 + (WIDE ? 32 * w : 0);
-  const int col = wave_col + q, tok_i = min(col / g, R.n - 1), head = kvh * g + col % g;
-  const bool live = col < R.n * g;
-  const int row = R.row0 + tok_i;
-  unsigned long long tmask = 0;
-  int own = R.own0 + tok_i;                                       // position (and, for consecutive tokens, index)
-  if (R.tree) {
-    tmask = A.chunk.tree_mask[row];
-    own = R.base + __popcll(tmask) - 1;
+  struct Column { int tok, head, row; bool live; };
+  auto column = [&]() -> Column {                                 // (asked for again where it is needed: kept, it costs registers of the loop)
+    int col = wave_col + q;
+    asm volatile("" : "+v"(col));
+    const int tok = min(col / g, R.n - 1);
+    return Column{tok, kvh * g + col % g, R.row0 + tok, col < R.n * g};
+  };
+  unsigned long long tnear = 0;                                   // nodes of the path inside the window
+  int own;                                                        // position (and, for consecutive tokens, index)
+  float slope;
+  {
+    const Column c = column();
+    own = R.own0 + c.tok;
+    if (R.tree) {
+      tnear = A.chunk.tree_mask[c.row];
+      own = R.base + __popcll(tnear) - 1;
+      if (A.window > 0) for (int i = __popcll(tnear) - A.window; i > 0; --i) tnear &= tnear - 1;
+    }
+    slope = MODS && A.slopes ? A.slopes[c.head] * 1.44269504088896341f : 0.f;
   }
-  unsigned long long tnear = tmask;                               // nodes of the path inside the window
-  if (R.tree && A.window > 0) for (int i = __popcll(tmask) - A.window; i > 0; --i) tnear &= tnear - 1;
-  const float slope = MODS && A.slopes ? A.slopes[head] * 1.44269504088896341f : 0.f;
 
   // tile number -> first token
   auto tile_token = [&](int it) { return (it < R.n_prefix ? it : it - R.n_prefix + R.first) * KT; };
@@ -238,12 +246,23 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
     constexpr bool K = decltype(what)::value & 1, V = decltype(what)::value & 2;
     const int k0 = tile_token(it), first = WIDE ? w * INSTS : 0;
     if (!A.lane_pages) {                                          // the tokens of an instruction lie in one page, whose place stays in scalar registers
+      long long at[INSTS];
+      if (in_page >= KT - 1) {                                    // (and those of the tile: one product does)
+        at[0] = max(0, __builtin_amdgcn_readfirstlane(pages)) * A.kv.page_stride + ((k0 & in_page) + first * RPI) * A.kv.token_stride;
+#pragma unroll
+        for (int u = 1; u < INSTS; ++u) at[u] = at[u - 1] + RPI * A.kv.token_stride;
+      } else {
+#pragma unroll
+        for (int u = 0; u < INSTS; ++u) {
+          const int t0 = (first + u) * RPI;
+          at[u] = max(0, __builtin_amdgcn_readlane(pages, t0)) * A.kv.page_stride + ((k0 + t0) & in_page) * A.kv.token_stride;
+        }
+      }
 #pragma unroll
       for (int u = 0; u < INSTS; ++u) {
-        const int t0 = (first + u) * RPI, page = max(0, __builtin_amdgcn_readlane(pages, t0));
-        const long long at = page * A.kv.page_stride + ((k0 + t0) & in_page) * A.kv.token_stride;
-        if constexpr (K) load_lds((const char*)(kb + at) + k_off[u % (8 / RPI)], kd + t0 * ROW);
-        if constexpr (V) load_lds((const char*)(vb + at) + v_off, vd + t0 * ROW);
+        const int t0 = (first + u) * RPI;
+        if constexpr (K) load_lds((const char*)(kb + at[u]) + k_off[u % (8 / RPI)], kd + t0 * ROW);
+        if constexpr (V) load_lds((const char*)(vb + at[u]) + v_off, vd + t0 * ROW);
       }
     } else {
 #pragma unroll
@@ -271,8 +290,10 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
       const bool ok = page >= 0 && c * RUN < dh;
       const long long at = page * A.kv.page_stride + ((k0 + t) & in_page) * A.kv.token_stride + c * RUN;
       if constexpr (P::SPLIT) {
-        k4[i] = v4[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (ok) { k4[i] = *(const f32x4*)(kb + at); v4[i] = *(const f32x4*)(vb + at); }
+        f32x4 k = {0.f, 0.f, 0.f, 0.f}, v = k;
+        if (ok) { k = *(const f32x4*)(kb + at); v = *(const f32x4*)(vb + at); }
+        k4[i] = k;
+        v4[i] = v;
       } else {
         vr[i].zero();
         if (ok) vr[i].load(vb + at);
@@ -352,13 +373,14 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
 
   bf16x8 qf[NQ][KSN];
   {
-    const T* qp = (const T*)A.q + row * A.q_row + head * A.q_head;
+    const Column c = column();
+    const T* qp = (const T*)A.q + c.row * A.q_row + c.head * A.q_head;
 #pragma unroll
     for (int ks = 0; ks < KSN; ++ks) {
       const int d = 16 * ks + 8 * hh;
       Raw8<T> x;
       x.zero();
-      if (live && d < dh) x.load(qp + d);
+      if (c.live && d < dh) x.load(qp + d);
       bf16x8 p[3];
       x.split(p);
 #pragma unroll
@@ -373,8 +395,10 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
     fetch(it + 1, pages1);
   }
 
-  const float c2 = A.scale * 1.44269504088896341f;                // scores to powers of two
-  const float cap_in = MODS && A.softcap > 0.f ? 2.f * c2 / A.softcap : 0.f, cap_out = A.softcap * 1.44269504088896341f;
+  auto uniform = [](float x) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x))); };
+  const float c2 = uniform(A.scale * 1.44269504088896341f);       // scores to powers of two
+  const float cap_in = uniform(MODS && A.softcap > 0.f ? 2.f * c2 / A.softcap : 0.f), cap_out = uniform(A.softcap * 1.44269504088896341f);
+  const float cap_y = uniform(cap_in * 0.34657359027997264f);     // scale / cap
   float m_run = -INFINITY, l_run = 0.f;                           // maximum (in powers of two) of the column, sum of this lane's half of the tokens
   f32x16 oacc[DB];
 #pragma unroll
@@ -383,9 +407,9 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
     for (int r = 0; r < 16; ++r) oacc[b][r] = 0.f;
 
   // Byte offsets in a buffer of what this lane reads of a tile: the keys' k-steps 0..3 (the others, and the second 32 tokens, lie a constant further on), the values' 32-wide blocks.
-  uint32_t k_at[4], v_at[DB];
+  uint32_t k_at[4], v_at[DB];                                     // (rows of 96 elements: pieces 4 to 7 lie behind 0 to 3 in the same order)
 #pragma unroll
-  for (int i = 0; i < 4; ++i) k_at[i] = 16 * k_place<ROW>(q, 2 * i + hh);
+  for (int i = 0; i < 4; ++i) k_at[i] = ROW == 96 && i > 1 ? k_at[i - 2] + 64 : 16 * k_place<ROW>(q, 2 * i + hh);
 #pragma unroll
   for (int b = 0; b < DB; ++b) {
     const int t = 4 * hh + ((lane & 15) >> 2), c = 4 * b + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
@@ -439,29 +463,27 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
           next_bad |= put_step(kn, vn, n, pk);
           __builtin_amdgcn_sched_barrier(0);
         }
+      } else if constexpr (P::KEYS_IN_LDS) {                      // reads some k-steps ahead of their products: LDS answers in the time of about four products
+        constexpr int STEPS = KB * KSN, AHEAD = NQ == 3 ? 2 : 4;
+        bf16x8 kf[AHEAD];
+#pragma unroll
+        for (int n = 0; n < AHEAD; ++n) kf[n] = key(n / KSN, n % KSN, 0);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int n = 0; n < STEPS; ++n) {
+#pragma unroll
+          for (int u = 0; u < P::PRODUCTS; ++u) sacc[n / KSN] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[n % AHEAD], qf[P::column_piece(u)][n % KSN], sacc[n / KSN], 0, 0, 0);
+          if (n + AHEAD < STEPS) kf[n % AHEAD] = key((n + AHEAD) / KSN, (n + AHEAD) % KSN, 0);
+          __builtin_amdgcn_sched_barrier(0);
+        }
       } else {
 #pragma unroll
-        for (int a = 0; a < KB; ++a)
+        for (int ks = 0; ks < KSN; ++ks) {
+          bf16x8 kf[3];
+          kr[ks].split(kf);
 #pragma unroll
-          for (int ks = 0; ks < KSN; ++ks) {
-            bf16x8 kf[3];
-            if constexpr (P::KEYS_IN_LDS) {
-#pragma unroll
-              for (int j = 0; j < NK; ++j) kf[j] = key(a, ks, j);
-            } else kr[ks].split(kf);
-#pragma unroll
-            for (int u = 0; u < P::PRODUCTS; ++u) sacc[a] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[P::cache_piece(u)], qf[P::column_piece(u)][ks], sacc[a], 0, 0, 0);
-          }
-      }
-      if constexpr (P::KEYS_IN_LDS && !P::SPLIT) {                // order: four k-steps' reads ahead of their products
-        constexpr int STEPS = KB * KSN, AHEAD = STEPS < 4 ? STEPS : 4;
-        __builtin_amdgcn_sched_group_barrier(0x100, NK * AHEAD, 0);
-#pragma unroll
-        for (int i = 0; i < STEPS - AHEAD; ++i) {
-          __builtin_amdgcn_sched_group_barrier(0x008, P::PRODUCTS, 0);
-          __builtin_amdgcn_sched_group_barrier(0x100, NK, 0);
+          for (int u = 0; u < P::PRODUCTS; ++u) sacc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[P::cache_piece(u)], qf[P::column_piece(u)][ks], sacc[0], 0, 0, 0);
         }
-        __builtin_amdgcn_sched_group_barrier(0x008, P::PRODUCTS * AHEAD, 0);
       }
     }
     if constexpr (!WIDE && !DIRECT) {
@@ -482,7 +504,30 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
     if (!idle) {
     // cap and slopes
     if constexpr (MODS) {
-      if (A.softcap > 0.f) {
+      bool small = false;                                         // the cap bends no score of this wave much
+      if (NQ == 1 && A.softcap > 0.f) {
+        float far = 0.f;
+#pragma unroll
+        for (int a = 0; a < KB; ++a)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) far = fmaxf(far, fabsf(sacc[a][r]));
+        small = !__any(far * cap_y > 0.7f);
+      }
+      if (small) {
+        // tanh(y) = y (1 + z (a1 + z (a2 + z (a3 + z a4)))), z = y^2: the coefficients of the least largest error up to 0.7, which is 9.7 * 10^-8.  Seven operations at the full rate for five of
+        // which two take four times as long.
+        const float k = cap_out * cap_y, y2 = cap_y * cap_y;
+#pragma unroll
+        for (int a = 0; a < KB; ++a)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const float x = sacc[a][r], z = x * (x * y2);
+            float t = fmaf(k * 0.01346275f, z, k * -0.05054204f);
+            t = fmaf(t, z, k * 0.13272971f);
+            t = fmaf(t, z, k * -0.33329716f);
+            sacc[a][r] = x * fmaf(t, z, k);
+          }
+      } else if (A.softcap > 0.f) {
 #pragma unroll
         for (int a = 0; a < KB; ++a)
 #pragma unroll
@@ -490,7 +535,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
             const float e = __builtin_amdgcn_exp2f(sacc[a][r] * cap_in);   // e^(2 x / cap); tanh = 1 - 2 / (e + 1)
             float x = fmaf(-2.f * cap_out, __builtin_amdgcn_rcpf(e + 1.f), cap_out);
             if constexpr (NQ == 3) {                              // fp32: near 0 that cancels; the Taylor polynomial to y^13 is within 10^-9 below 0.35
-              const float y = sacc[a][r] * (cap_in * 0.34657359027997264f), z = y * y;   // (cap_in = 2 log2(e) scale / cap)
+              const float y = sacc[a][r] * cap_y, z = y * y;
               float t = 3.59212803657248102e-3f;
               t = fmaf(t, z, -8.86323552990219657e-3f);
               t = fmaf(t, z, 2.18694885361552028e-2f);
@@ -510,6 +555,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
       }
       if (A.slopes) {
         if (R.tree && k0 + KT > R.base) {
+          const unsigned long long tmask = A.chunk.tree_mask[column().row];
 #pragma unroll
           for (int a = 0; a < KB; ++a)
 #pragma unroll
@@ -615,7 +661,8 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
     // 16 tokens at a time: their values are read a block ahead, and the weights of the next 16 are made between the products, in this order.
     constexpr int GROUPS = KT / 16 * DB, SLOTS = DB * P::PRODUCTS, WORK = NQ == 3 ? 12 : 4;
     u32x4 pf[2][NQ];
-    bf16x8 vf[NK == 1 ? 2 : 1][NK];
+    constexpr int AHEAD = NK == 3 ? 1 : NQ == 3 ? 2 : 4;          // (of three pieces each is read again as soon as it is done with)
+    bf16x8 vf[AHEAD][NK];
     float sum = 0.f;
     auto weights = [&](int jj, int n) {                           // n of WORK steps: a pair's weights and their first piece, its second, its third
       const int pair = NQ == 3 ? n / 3 : n, j = NQ == 3 ? n % 3 : 0, a = jj >> 1, r = 8 * (jj & 1) + 2 * pair;
@@ -636,21 +683,22 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
     auto value = [&](int i, int j) {                              // piece j of block i % DB of 16 tokens
       const char* p = (const char*)vt + v_at[i % DB] + (2 * j * TILE + 32 * ROW * (i / DB));
       const s16x4 lo = read_transposed((const bf16_t*)p), hi = read_transposed((const bf16_t*)(p + 16 * ROW));
-      vf[NK == 1 ? i & 1 : 0][j] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+      vf[i % AHEAD][j] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     };
 #pragma unroll
-    for (int j = NK - 1; j >= 0; --j) value(0, j);
+    for (int i = 0; i < AHEAD; ++i)
+#pragma unroll
+      for (int j = NK - 1; j >= 0; --j) value(i, j);
 #pragma unroll
     for (int n = 0; n < WORK; ++n) weights(0, n);
 #pragma unroll
     for (int i = 0; i < GROUPS; ++i) {
       const int jj = i / DB, b = i % DB;
-      if (NK == 1 && i + 1 < GROUPS) value(i + 1, 0);
 #pragma unroll
       for (int u = 0; u < P::PRODUCTS; ++u) {
         const int j = P::cache_piece(u), slot = b * P::PRODUCTS + u;
-        oacc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[NK == 1 ? i & 1 : 0][j], __builtin_bit_cast(bf16x8, pf[jj & 1][P::column_piece(u)]), oacc[b], 0, 0, 0);
-        if (P::done_with(u) && i + 1 < GROUPS) value(i + 1, j);
+        oacc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i % AHEAD][j], __builtin_bit_cast(bf16x8, pf[jj & 1][P::column_piece(u)]), oacc[b], 0, 0, 0);
+        if (P::done_with(u) && i + AHEAD < GROUPS) value(i + AHEAD, j);
         if (jj + 1 < KT / 16)
 #pragma unroll
           for (int n = slot * WORK / SLOTS; n < (slot + 1) * WORK / SLOTS; ++n) weights(jj + 1, n);
@@ -710,10 +758,11 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
     }
     if (w > 0) return;
   }
-  if (!live) return;
+  const Column c = column();
+  if (!c.live) return;
   if (whole) {
     const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
-    T* o = (T*)A.out + row * A.out_row + head * A.out_head;
+    T* o = (T*)A.out + c.row * A.out_row + c.head * A.out_head;
 #pragma unroll
     for (int b = 0; b < DB; ++b)
 #pragma unroll
@@ -724,7 +773,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
         store_run<4>(o + d, x);
       }
   } else {
-    const size_t at = ((size_t)row * A.H + head) * A.splits + split;
+    const size_t at = ((size_t)c.row * A.H + c.head) * A.splits + split;
     if (hh == 0) { A.part_ml[2 * at] = m_run; A.part_ml[2 * at + 1] = l_run; }
     float* o = A.part_o + at * P::PART;
 #pragma unroll
