@@ -305,7 +305,7 @@ int eagle_rope_plan_init(const eagle_rope_config *cfg, eagle_rope_plan *out);
 /* Rotates q [n_rows][n_heads][head_dim] into q_out and k [n_rows][n_kv_heads][head_dim] into the cache, together with v -- or, without a cache (kv null), k into
  * k_out.  Row and head strides in elements, elements of a head consecutive; outputs may be the inputs.  With a cache `chunk` is needed; v null leaves the
  * cache's values alone.  positions (dev int32 [n_rows]) overrides the positions that `chunk` gives; without a chunk (null: n_rows is the field here) it
- * is needed.  q (with q_out) or k may be null.  Rows that no sequence owns are left as they are, in the outputs too (without a chunk there are none), and
+ * is needed.  q (with q_out) or k may be null.  Rows that no sequence owns, and those from a sequence's max_rows on, are left as they are, in the outputs too (without a chunk there are none), and
  * a token at or behind max_keys, or on a page that is not there, is not stored.
  * inverse: the transposed map (angles negated, the same mscale): the gradient of the rotation with respect to its input; without a cache only.
  * Two rows of one call must not be the same token of the cache. */
@@ -325,7 +325,7 @@ int eagle_rope(const eagle_rope_plan *plan, const eagle_rope_args *args, const e
  *   - j < prefix[s] (tree: at most the tokens in front of the tree): a prefix every row of the sequence sees, in front of the window and ahead of the row.
  * A row that sees nothing gets zeros.  q, out: EAGLE_F32 over a cache of either type, or EAGLE_BF16 over EAGLE_BF16; out is of q's type and may be q.
  * head_dim: a multiple of 8, 8..128.  q's rows and the cache's tokens start on multiples of 16 bytes, out's of 8 elements.  NaN and infinities in a token stay with
- * the rows that see it.  Rows that no sequence owns are left as they are.
+ * the rows that see it (a key that is not finite may make NaN of a score).  Rows that no sequence owns are left as they are.
  * workspace (dev, 256-byte aligned): eagle_chunk_attention_workspace() bytes, for the same arguments; its contents need not be kept or cleared. */
 typedef struct {
   int32_t n_heads, dtype, window;

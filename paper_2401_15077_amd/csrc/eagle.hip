@@ -1547,7 +1547,7 @@ extern "C" int eagle_set_hint(eagle_ctx* c, int32_t seq, const int32_t* future, 
   return EAGLE_OK;
 }
 
-extern "C" int eagle_set_rope(eagle_ctx* c, const eagle_rope_config* rope) {
+extern "C" int eagle_set_rope(eagle_ctx* c, const eagle_rope_config* rope) try {
   if (!c) return fail(EAGLE_EINVAL, "null context");
   for (int w : {(int)EAGLE_W_Q, (int)EAGLE_W_K})
     for (char loaded : c->loaded_layer[w])
@@ -1563,18 +1563,20 @@ extern "C" int eagle_set_rope(eagle_ctx* c, const eagle_rope_config* rope) {
   if (rc || (rc = upload_rope(c, &plan))) return rc;
   c->rope_mode = rope_pack(plan.rot_dim, plan.interleaved);
   return EAGLE_OK;
+} catch (const std::exception&) {
+  return fail(EAGLE_ENOMEM, "out of host memory");
 }
 
 extern "C" int eagle_set_attention(eagle_ctx* c, const eagle_attention_rules* r) {
   if (!c) return fail(EAGLE_EINVAL, "null context");
   if (c->n_active != 0) return fail(EAGLE_ESTATE, "the attention rules can only change while no sequence is active (after eagle_init / eagle_reset)");
-  if (r && (!(r->softcap >= 0.f) || !std::isfinite(r->softcap) || r->window < 0)) return fail(EAGLE_EINVAL, "softcap must be >= 0 and finite, window >= 0");
+  if (r && (!(r->softcap >= 0.f) || !std::isfinite(r->softcap) || (r->softcap > 0.f && r->softcap < 1e-30f) || r->window < 0)) return fail(EAGLE_EINVAL, "softcap must be 0 or 10^-30 and more and finite, window >= 0");
   c->attn_rules = r ? *r : eagle_attention_rules{};
   c->attn_ruled = r && (r->softcap > 0.f || r->window > 0 || r->slopes_dev);
   return EAGLE_OK;
 }
 
-extern "C" int eagle_set_logit_rules(eagle_ctx* c, const eagle_context_rules* r) {
+extern "C" int eagle_set_logit_rules(eagle_ctx* c, const eagle_context_rules* r) try {
   if (!c) return fail(EAGLE_EINVAL, "null context");
   if (r) {
     if (r->bias_token && (!r->bias_start || !r->bias_value || r->n_bias < 0)) return fail(EAGLE_EINVAL, "biases need bias_start, bias_value and n_bias >= 0");
@@ -1592,6 +1594,8 @@ extern "C" int eagle_set_logit_rules(eagle_ctx* c, const eagle_context_rules* r)
   c->logit_rules = r ? *r : eagle_context_rules{};
   c->logits_ruled = r != nullptr;
   return EAGLE_OK;
+} catch (const std::exception&) {
+  return fail(EAGLE_ENOMEM, "out of host memory");
 }
 
 static int step_ready(eagle_ctx* c) {

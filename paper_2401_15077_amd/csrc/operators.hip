@@ -4,6 +4,7 @@
 #include "chunk_attn.h"
 #include "logit_rules.h"
 
+#include <cfloat>
 #include <cmath>
 #include <cstring>
 #include <algorithm>
@@ -113,6 +114,8 @@ extern "C" int eagle_rope(const eagle_rope_plan* plan, const eagle_rope_args* a,
     if (a->k && !a->k_out) return fail(EAGLE_EINVAL, "rope: without a cache k needs k_out");
     if (a->v) return fail(EAGLE_EINVAL, "rope: v goes to a cache only");
   }
+  if ((a->q && ((a->n_rows > 1 && a->q_out_row == 0) || (a->n_heads > 1 && a->q_out_head == 0))) ||
+      (a->k && !kv && ((a->n_rows > 1 && a->k_out_row == 0) || (a->n_kv_heads > 1 && a->k_out_head == 0)))) return fail(EAGLE_EINVAL, "rope: rows or heads of an output lie on each other");
   const int elt = elt_of(a->dtype);
   if (a->q) runs = runs && runs_ok(a->q, a->q_row, a->q_head, elt) && runs_ok(a->q_out, a->q_out_row, a->q_out_head, elt);
   if (a->k) runs = runs && runs_ok(a->k, a->k_row, a->k_head, elt);
@@ -154,8 +157,15 @@ static int check_attention(const eagle_attention_args* a, const eagle_chunk* chu
   if (a->n_heads < 1 || a->n_heads > 65535 || a->n_heads % kv->n_kv_heads) return fail(EAGLE_EINVAL, "attention: n_heads must be a multiple of the cache's heads");
   if (kv->head_dim % 8 || kv->head_dim > 128) return fail(EAGLE_EINVAL, "attention: head_dim must be a multiple of 8, at most 128");
   if (!std::isfinite(a->scale) || !(a->softcap >= 0.f) || !std::isfinite(a->softcap)) return fail(EAGLE_EINVAL, "attention: scale must be finite, softcap >= 0 and finite");
+  if (!std::isfinite(a->scale * 2.885390f) || (a->softcap > 0.f && (a->softcap < FLT_MIN || !std::isfinite(a->scale * 2.885390f / a->softcap))))
+    return fail(EAGLE_EINVAL, "attention: scale, or scale / softcap, is too large");
   if (a->window < 0) return fail(EAGLE_EINVAL, "attention: window must be >= 0");
   if (chunk->n_rows > 0 && (!a->q || !a->out)) return fail(EAGLE_EINVAL, "attention: q or out is null");
+  if ((chunk->n_rows > 1 && a->out_row == 0) || (a->n_heads > 1 && a->out_head == 0)) return fail(EAGLE_EINVAL, "attention: rows or heads of out lie on each other");
+  // (bounds that a caller leaves wide are drawn in, so that they cost no work-groups and no number overflows)
+  d->chunk.max_rows = std::min(chunk->max_rows, std::max(1, chunk->n_rows));
+  d->chunk.max_keys = (int)std::min((long long)chunk->max_keys, (long long)kv->pages_per_seq * kv->page_tokens);
+  if ((long long)d->chunk.max_rows * (a->n_heads / kv->n_kv_heads) > 1 << 30) return fail(EAGLE_EINVAL, "attention: too many rows a kv head");
   const int elt = elt_of(a->dtype), kelt = elt_of(kv->dtype);
   if (!runs_ok(a->q, a->q_row, a->q_head, elt)) return fail(EAGLE_EINVAL, "attention: q's rows and heads must start on multiples of 16 bytes");
   if (!aligned(a->out, 16) || a->out_row % 8 || a->out_head % 8) return fail(EAGLE_EINVAL, "attention: out's rows and heads must start on multiples of 16 bytes and 8 elements");

@@ -79,7 +79,7 @@ __global__ __launch_bounds__(256) void k_rope(const RopeDev A) {
     long long cell = -1;
     if (A.has_chunk) {
       const int s = wave_row_seq(A.chunk.row_start, A.chunk.n_seqs, r);
-      if (s < 0) cell = -2;
+      if (s < 0 || r - max(0, A.chunk.row_start[s]) >= A.chunk.max_rows) cell = -2;
       else {
         int token, p;
         if (A.chunk.tree_mask) {

@@ -232,3 +232,17 @@ def test_lengths_beyond_what_the_host_said_are_not_read():
     assert float(p.chunk_attention(q, kv, none).abs().sum()) == 0.0
     minus = p.Chunk(i32([0, 4]), i32([-5]), 4, 4, 64)
     assert float(p.chunk_attention(q, kv, minus).abs().sum()) == 0.0
+
+
+@pytest.mark.parametrize("types", ALL)
+def test_wide_bounds_and_a_cap_of_almost_nothing(types):
+    p = pkg()
+    q, kv, chunk, out, (kc, vc, table) = run([40, 1, 7], [96, 40, 64], 8, 2, 128, types, 32)
+    loose = p.Chunk(i32([0, 40, 41, 48]), i32([96, 40, 64]), 48, 2 ** 30, 2 ** 30)
+    tight = p.Chunk(i32([0, 40, 41, 48]), i32([96, 40, 64]), 48, 48, table.shape[1] * 32)
+    assert torch.equal(p.chunk_attention(q, kv, loose), p.chunk_attention(q, kv, tight))
+    # no score but 0: the mean of what a row sees
+    plain = p.chunk_attention(torch.zeros_like(q), kv, chunk)
+    for cap in (1e-25, 1.0, 1e25):
+        assert torch.equal(p.chunk_attention(torch.zeros_like(q), kv, chunk, softcap=cap), plain)
+    assert torch.isfinite(p.chunk_attention(q, kv, chunk, softcap=1e-25)).all()

@@ -24,6 +24,18 @@ def i32(a):
     return torch.tensor(a, dtype=torch.int32, device=DEV)
 
 
+def test_rows_beyond_the_bound_are_left():
+    """As in the attention: max_rows bounds the rows of a sequence that are processed."""
+    p = pkg()
+    k = torch.randn(5, 1, 8, device=DEV)
+    q, before = k.clone(), k.clone()
+    cache = torch.zeros(1, 1, 8, 8, device=DEV)
+    kv = p.PagedKV(cache, cache.clone(), i32([[0], [0]]))
+    p.rope(p.rope_plan(8), q, k, chunk=p.Chunk(i32([0, 3, 5]), i32([3, 5]), 5, 2, 8), kv=kv)
+    assert torch.equal(q[2], before[2]) and not torch.equal(q[1], before[1]) and not torch.equal(q[4], before[4])
+    assert float(cache[0, 0, 2].abs().sum()) == 0.0 and all(float(cache[0, 0, t].abs().sum()) > 0 for t in (0, 1, 3, 4))
+
+
 def near(got, want, size, dtype, mscale=1.0):
     got = got.double().cpu().numpy()
     tol = 8 * U * size + (2.0 ** -8 * np.abs(want) * 1.001 if dtype == torch.bfloat16 else 0.0)

@@ -194,3 +194,17 @@ def test_the_most_tokens(lib):
         call = ops.EagleLogits(n_rows=4, vocab=100, in_=A, out=A, in_stride=100, out_stride=100), ops.EagleLogitRules(n_seqs=4, tokens=A, n_tokens=A, token_stride=8, **r)
         assert lib.eagle_apply_logit_rules(*call, None) == EINVAL, r
     assert lib.eagle_apply_logit_rules(ops.EagleLogits(n_rows=1, vocab=2 ** 30 + 1, in_=A, out=A, in_stride=2 ** 31, out_stride=2 ** 31), ops.EagleLogitRules(n_seqs=1), None) == EINVAL
+
+
+def test_outputs_that_lie_on_each_other_and_scores_out_of_range(lib):
+    good = dict(n_rows=4, n_heads=4, dtype=0, q=A, q_out=A, q_row=256, q_head=64, q_out_row=256, q_out_head=64, positions=A)
+    for bad in (dict(q_out_row=0), dict(q_out_head=0)):
+        assert lib.eagle_rope(plan(), ops.EagleRopeArgs(**{**good, **bad}), None, None, None) == EINVAL, bad
+    att = dict(n_heads=4, dtype=0, q=A, out=A, q_row=256, q_head=64, out_row=256, out_head=64, scale=0.1)
+    size = lambda **kw: lib.eagle_chunk_attention_workspace(ops.EagleAttentionArgs(**{**att, **kw}), chunk(), paged())
+    assert size() > 0 and size(softcap=1e-30) > 0
+    for bad in (dict(out_row=0), dict(out_head=0), dict(softcap=1e-39), dict(scale=3e38), dict(scale=1e20, softcap=1e-20)):
+        assert size(**bad) == 0, bad
+    # bounds left wide need what tight ones need
+    a = ops.EagleAttentionArgs(**att)
+    assert lib.eagle_chunk_attention_workspace(a, chunk(max_rows=2 ** 30, max_keys=2 ** 30), paged()) == lib.eagle_chunk_attention_workspace(a, chunk(max_rows=4, max_keys=128), paged())
