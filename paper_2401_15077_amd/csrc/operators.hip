@@ -266,8 +266,8 @@ template <typename T>
 static int launch_rules(RulesDev d, bool runs, hipStream_t stream) {
   // A slice costs its work-group a walk over the row's text and a word of LDS a token, so a row is cut into no more slices than 512 threads need, or than make 1024 work-groups, four a CU;
   // and into slices of one length, so that no short one walks the text for little.  160 rows of 100003 bf16 logits: 26.2 us with 512 threads, 27.7 with 256, 31.0 with 1024 (two work-groups a CU,
-  // a third round nearly empty); 104 rows of 32000 fp32 logits: 10.5 us at 1024 work-groups, 11.0 at 512.
-  constexpr int VE = 16 / sizeof(T), PIECES = 2;
+  // a third round nearly empty); 104 rows of 32000 fp32 logits: 10.5 us at 1024 work-groups, 11.0 at 512.  Runs a thread: bf16 26.0 with two, 27.4 with three; fp32 10.5 with two, 9.9 with three.
+  constexpr int VE = 16 / sizeof(T), PIECES = sizeof(T) == 4 ? 3 : 2;
   auto pieces = [&](int t) { return (d.vocab + t * VE * PIECES - 1) / (t * VE * PIECES); };
   const int parts = std::max(pieces(512), std::min((1024 + d.n_rows - 1) / d.n_rows, pieces(128)));
   const int threads = (pieces(64) + parts - 1) / parts * 64;
