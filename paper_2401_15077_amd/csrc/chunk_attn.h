@@ -181,6 +181,8 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
   __shared__ __attribute__((aligned(16))) bf16_t k_lds0[P::K_ELTS], k_lds1[P::TWO ? P::K_ELTS : 8], v_lds0[P::V0_ELTS], v_lds1[P::TWO ? P::V_ELTS : 8];
   __shared__ int s_bad[2];                                        // WIDE, not DIRECT: number of the last tile in a buffer whose values are not all finite
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane & 31, hh = lane >> 5;
+  // The lane, worked out anew: inside the loop, what can be had from the thread's number in an instruction or two is not kept (the widest shapes hold 240 of 256 registers).
+  auto lane_now = []() -> int { int l = threadIdx.x; asm volatile("" : "+v"(l)); return l & 63; };
   const int kvh = blockIdx.x % A.kv.n_kv_heads, part = blockIdx.x / A.kv.n_kv_heads, s = blockIdx.y, g = A.H / A.kv.n_kv_heads, dh = A.kv.head_dim;
   // Blocks of the last rows see most and go first.  Where all work-groups are resident at once, two a CU, the second half ascends, so that a CU's two see as much as another's.
   const int nth = part % A.col_blocks, split = part / A.col_blocks, cb = nth < A.turn ? A.col_blocks - 1 - nth : nth - A.turn;
@@ -195,22 +197,23 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
   const int wave_col = col0 + (WIDE ? 32 * w : 0);
   struct Column { int tok, head, row; bool live; };
   auto column = [&]() -> Column {                                 // (asked for again where it is needed: kept, it costs registers of the loop)
-    int col = wave_col + q;
-    asm volatile("" : "+v"(col));
+    const int col = wave_col + (lane_now() & 31);
     const int tok = min(col / g, R.n - 1);
     return Column{tok, kvh * g + col % g, R.row0 + tok, col < R.n * g};
   };
-  unsigned long long tnear = 0;                                   // nodes of the path inside the window
+  auto near_path = [&](int row) -> unsigned long long {           // nodes of the row's path inside the window
+    unsigned long long m = A.chunk.tree_mask[row];
+    if (A.window > 0) for (int i = __popcll(m) - A.window; i > 0; --i) m &= m - 1;
+    return m;
+  };
+  unsigned long long kept_path = 0;                               // (SPLIT has no registers for it)
   int own;                                                        // position (and, for consecutive tokens, index)
   float slope;
   {
     const Column c = column();
     own = R.own0 + c.tok;
-    if (R.tree) {
-      tnear = A.chunk.tree_mask[c.row];
-      own = R.base + __popcll(tnear) - 1;
-      if (A.window > 0) for (int i = __popcll(tnear) - A.window; i > 0; --i) tnear &= tnear - 1;
-    }
+    if (R.tree) own = R.base + __popcll(A.chunk.tree_mask[c.row]) - 1;
+    if (R.tree && !P::SPLIT) kept_path = near_path(c.row);
     slope = MODS && A.slopes ? A.slopes[c.head] * 1.44269504088896341f : 0.f;
   }
 
@@ -218,13 +221,13 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
   auto tile_token = [&](int it) { return (it < R.n_prefix ? it : it - R.n_prefix + R.first) * KT; };
   // The table's entry for token k0 + lane (KT 32: lane % 32) of a tile, requested a tile and a half before it is looked at: looked at at once it would wait for every load in flight.
   const int* table = A.kv.page_table + (size_t)s * A.kv.table_stride;
-  auto entry_of = [&](int it) -> int { return table[max(0, min(tile_token(it) + (lane & (KT - 1)), R.keys - 1)) >> A.kv.page_shift]; };
+  auto entry_of = [&](int it) -> int { return table[max(0, min(tile_token(it) + (lane_now() & (KT - 1)), R.keys - 1)) >> A.kv.page_shift]; };
   // the page itself, -1: not there, or the token is behind the last
   auto page_of = [&](int it, int entry) -> int {
-    return (unsigned)entry < (unsigned)A.kv.n_pages && tile_token(it) + (lane & (KT - 1)) < R.keys ? entry : -1;
+    return (unsigned)entry < (unsigned)A.kv.n_pages && tile_token(it) + (lane_now() & (KT - 1)) < R.keys ? entry : -1;
   };
   constexpr int STEP = WIDE ? 1 : 4;
-  const int g_tid = WIDE ? tid : lane, in_page = (1 << A.kv.page_shift) - 1;
+  const int in_page = (1 << A.kv.page_shift) - 1;
   const CT *kb = (const CT*)A.kv.k + kvh * A.kv.head_stride, *vb = (const CT*)A.kv.v + kvh * A.kv.head_stride;
   // Narrow and DIRECT: a wave has one buffer for keys and one for values; the next keys are on their way from the end of the scores on, the next values from the end of the products on.
   constexpr bool STAGGERED = !WIDE && DIRECT;
@@ -289,23 +292,24 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
   Raw8<CT> kr[DIRECT || WIDE ? 1 : KSN], vr[DIRECT || WIDE ? 1 : ITEMS];
   auto fetch = [&](int it, int pages) {
     const int k0 = tile_token(it);
+    if constexpr (P::SPLIT) {                                     // a token is eight threads': every eighth run of 4 elements
+      const int l = lane_now(), t = 8 * w + (l >> 3), c = l & 7, page = __shfl(pages, t, 64);
+      const long long at = page * A.kv.page_stride + ((k0 + t) & in_page) * A.kv.token_stride + 4 * c;
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
-      constexpr int RUN = P::SPLIT ? 4 : 8;
-      int item = i * (WIDE ? 256 : 64) + g_tid;
-      if constexpr (P::SPLIT) asm volatile("" : "+v"(item));      // (see put_step)
-      const int t = item / (DH / RUN), c = item % (DH / RUN);
-      const int page = __shfl(pages, t, 64);
-      const bool ok = page >= 0 && c * RUN < dh;
-      const long long at = page * A.kv.page_stride + ((k0 + t) & in_page) * A.kv.token_stride + c * RUN;
-      if constexpr (P::SPLIT) {
+      for (int i = 0; i < ITEMS; ++i) {
         f32x4 k = {0.f, 0.f, 0.f, 0.f}, v = k;
-        if (ok) { k = *(const f32x4*)(kb + at); v = *(const f32x4*)(vb + at); }
+        if (page >= 0 && 4 * c + 32 * i < dh) { k = *(const f32x4*)(kb + at + 32 * i); v = *(const f32x4*)(vb + at + 32 * i); }
         k4[i] = k;
         v4[i] = v;
-      } else {
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < ITEMS; ++i) {
+        const int item = i * 64 + lane, t = item / (DH / 8), c = item % (DH / 8);
+        const int page = __shfl(pages, t, 64);
+        const long long at = page * A.kv.page_stride + ((k0 + t) & in_page) * A.kv.token_stride + c * 8;
         vr[i].zero();
-        if (ok) vr[i].load(vb + at);
+        if (page >= 0 && c * 8 < dh) vr[i].load(vb + at);
       }
     }
     if constexpr (!WIDE) {
@@ -331,9 +335,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
       x[2 * pair] -= __builtin_bit_cast(float, h << 16);
       x[2 * pair + 1] -= __builtin_bit_cast(float, h & 0xFFFF0000u);
     } else if (pair == 1) {
-      int item = i * 256 + tid;
-      asm volatile("" : "+v"(item));                             // (worked out anew for every tile: kept, the places cost more registers than there are)
-      const int t = item / (DH / 4), c = item % (DH / 4);
+      const int t = tid >> 3, c = (tid & 7) + 8 * i;
       bf16_t* d = (values ? vd + 8 * v_place<ROW>(t, c >> 1) : kd + 8 * k_place<ROW>(t, c >> 1)) + 4 * (c & 1);
 #pragma unroll
       for (int u = 0; u < 3; ++u) *(u32x2*)(d + u * TILE) = pk[u];
@@ -504,11 +506,12 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
     }
     pages = pages_next;
     if constexpr (P::SPLIT) {
-      if (__any(next_bad != 0) && lane == 0) s_bad[which ^ 1] = it + 1;
+      if (__any(next_bad != 0) && lane_now() == 0) s_bad[which ^ 1] = it + 1;
       pages1 = it + 2 < t_end ? page_of(it + 2, entry_next) : -1;
       fetch(it + 2, pages1);
       entry_next = entry_of(it + 3);
     } else if constexpr (!STAGGERED) entry_next = entry_of(it + 2 * STEP);
+    const int lane = lane_now(), hh = lane >> 5;
     uint64_t vis = ~0ull;                                         // tokens of the tile that the column sees
     if (!idle) {
     // cap and slopes
@@ -587,6 +590,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
       if (R.tree) {
         const int sh = k0 - R.base;                               // bit u of the path is token base + u
         vis = low_ones(-sh) & ~(A.window > 0 ? low_ones(own - A.window + 1 - k0) : 0ull);
+        const unsigned long long tnear = P::SPLIT ? near_path(column().row) : kept_path;
         vis |= sh >= 64 || sh <= -64 ? 0ull : sh >= 0 ? tnear >> sh : tnear << -sh;
       } else {
         vis = low_ones(own + 1 - k0);
@@ -629,8 +633,6 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
     if (bad) {
       // 0 times what is not finite is not 0.  So it is added to the columns that see it, and zeroed for the product.
       uint64_t spoilt = 0;
-      int h4 = 4 * hh;
-      asm volatile("" : "+v"(h4));                                // (nothing of this is worked out ahead of the loop and kept)
 #pragma unroll 1
       for (int i = 0; i < TILE / 512; ++i) {
         if (exponents(*(const u32x4*)(vt + i * 512 + lane * 8)) != 0) spoilt |= 1ull << ((i * 64 + lane) / (ROW / 8));
@@ -643,13 +645,14 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
         for (int b = 0; b < DB; ++b)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const int d = 32 * b + 8 * i + h4;
+            const int d = 32 * b + 8 * i + 4 * hh;
             const u32x2 v = *(const u32x2*)(vt + 8 * v_place<ROW>(t, d >> 3) + (d & 7));
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const float x = __builtin_bit_cast(float, e & 1 ? v[e >> 1] & 0xFFFF0000u : v[e >> 1] << 16);
               oacc[b][4 * i + e] += seen && not_finite(x) ? x : 0.f;
             }
+            __builtin_amdgcn_sched_barrier(0);                    // (one read at a time: all of them at once would take registers that the loop keeps)
           }
       }
       if constexpr (WIDE) __syncthreads();
@@ -741,7 +744,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
   l_run += __shfl_xor(l_run, 32, 64);
   if constexpr (!WIDE) {
     // waves 2 and 3 into 0 and 1, then 1 into 0
-    float* st = (float*)v_lds0 + lane;
+    float* st = (float*)v_lds0 + lane_now();
 #pragma unroll
     for (int half = 2; half > 0; half >>= 1) {
       __syncthreads();
@@ -769,6 +772,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
   }
   const Column c = column();
   if (!c.live) return;
+  const int half = lane_now() >> 5;
   if (whole) {
     const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
     T* o = (T*)A.out + c.row * A.out_row + c.head * A.out_head;
@@ -776,21 +780,21 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
     for (int b = 0; b < DB; ++b)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int d = 32 * b + 8 * i + 4 * hh;
+        const int d = 32 * b + 8 * i + 4 * half;
         if (d >= dh) continue;
         const float x[4] = {oacc[b][4 * i] * inv, oacc[b][4 * i + 1] * inv, oacc[b][4 * i + 2] * inv, oacc[b][4 * i + 3] * inv};
         store_run<4>(o + d, x);
       }
   } else {
     const size_t at = ((size_t)c.row * A.H + c.head) * A.splits + split;
-    if (hh == 0) { A.part_ml[2 * at] = m_run; A.part_ml[2 * at + 1] = l_run; }
+    if (half == 0) { A.part_ml[2 * at] = m_run; A.part_ml[2 * at + 1] = l_run; }
     float* o = A.part_o + at * P::PART;
 #pragma unroll
     for (int b = 0; b < DB; ++b)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float x[4] = {oacc[b][4 * i], oacc[b][4 * i + 1], oacc[b][4 * i + 2], oacc[b][4 * i + 3]};
-        store_run<4>(o + 32 * b + 8 * i + 4 * hh, x);
+        store_run<4>(o + 32 * b + 8 * i + 4 * half, x);
       }
   }
 }
