@@ -132,12 +132,11 @@ extern "C" int eagle_rope(const eagle_rope_plan* plan, const eagle_rope_args* a,
   d.q_row = a->q_row; d.q_head = a->q_head; d.k_row = a->k_row; d.k_head = a->k_head; d.v_row = a->v_row; d.v_head = a->v_head;
   d.q_out_row = a->q_out_row; d.q_out_head = a->q_out_head; d.k_out_row = a->k_out_row; d.k_out_head = a->k_out_head;
   d.positions = a->positions; d.has_chunk = chunk != nullptr; d.has_kv = kv != nullptr;
-  d.rows_per_wg = a->n_rows >= 1024 ? 4 : 1;
-  const int groups = (a->n_rows + d.rows_per_wg - 1) / d.rows_per_wg, VE = runs ? 16 / elt : 1;
+  const int VE = runs ? 16 / elt : 1;
   const int units = (plan->head_dim + 2 * VE - 1) / (2 * VE), least = std::max(1, 256 / units);
-  const int parts = std::max(1, std::min(1024 / groups, (d.n_heads_all + least - 1) / least));
+  const int parts = std::max(1, std::min(1024 / a->n_rows, (d.n_heads_all + least - 1) / least));   // (few rows: their heads in parts, of at least a unit a thread)
   d.heads_per_wg = (d.n_heads_all + parts - 1) / parts;
-  const dim3 grid(groups, (d.n_heads_all + d.heads_per_wg - 1) / d.heads_per_wg);
+  const dim3 grid(a->n_rows, (d.n_heads_all + d.heads_per_wg - 1) / d.heads_per_wg);
   const hipStream_t stream = (hipStream_t)hip_stream;
   const bool cf = kv && kv->dtype == EAGLE_F32;
   if (a->dtype == EAGLE_F32) { if (cf) launch_rope<float, float>(d, runs, grid, stream); else launch_rope<float, bf16_t>(d, runs, grid, stream); }
@@ -180,6 +179,7 @@ static int check_attention(const eagle_attention_args* a, const eagle_chunk* chu
   return EAGLE_OK;
 }
 
+// WIDE beyond 32 columns (64 sequences of 1k to 16k tokens, 8 heads a kv head, bf16, with joining: 32 columns narrow 459, wide 486; 40 columns 516, 525; 64 columns 548, 532).
 // Where sequences, kv heads and column blocks make fewer work-groups than these, the tokens are split; a part has a few tiles at least (the narrow shape: whole rounds of its four waves),
 // and there are at most as many parts as k_chunk_attn_join has lanes.
 // Narrow, 64 sequences of 1k to 16k tokens, 64 / 8 heads, bf16, us with 1, 2, 3, 4, 6, 8 parts at most: 433 (2), 419 (3), 451 (4), 406 (6), 417 (8).  One token over 701 keys, 32 heads, fp32,

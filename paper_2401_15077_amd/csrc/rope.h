@@ -6,7 +6,7 @@ struct RopeDev {
   unsigned long long turn[128];            // pair p: fraction of a turn a position, times 2^64
   float mscale, sign;                      // sign -1: the transposed map
   int rot_dim, interleaved, head_dim;
-  int n_rows, H, KVH, rows_per_wg, heads_per_wg, n_heads_all;   // n_heads_all: H query heads, KVH key heads, and KVH value heads if v is given
+  int n_rows, H, KVH, heads_per_wg, n_heads_all;   // n_heads_all: H query heads, KVH key heads, and KVH value heads if v is given
   const void *q, *k, *v;
   void *q_out, *k_out;
   long long q_row, q_head, k_row, k_head, v_row, v_head, q_out_row, q_out_head, k_out_row, k_out_head;
@@ -63,18 +63,19 @@ template <int VE> __device__ inline void store_run(bf16_t* p, const float* x) {
   else *(u32x4*)p = u32x4{bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]), bf16_pair(x[4], x[5]), bf16_pair(x[6], x[7])};
 }
 
-// A work-group takes rows_per_wg rows and heads_per_wg of their heads.  First a wave finds out about each row, then the threads work out the cosines and
-// sines of the rows' pairs, once for all heads (in LDS), then every thread moves runs of VE elements, two at a time: the two members of VE pairs (half
+// A work-group takes a row and heads_per_wg of its heads.  First a wave finds out about the row, then the threads work out the cosines and
+// sines of the row's pairs, once for all heads (in LDS), then every thread moves runs of VE elements, two at a time: the two members of VE pairs (half
 // layout), or VE pairs side by side (interleaved), or what is not rotated.  VE = 16 bytes' worth where strides and sizes allow, else 1.
+// Bound by HBM, and by latency for a few rows: 8191 rows of 64 + 8 + 8 heads of 128 in bf16 take 63 us, 5.3 TB/s read and written (four rows a work-group 78: fewer, longer chains of loads;
+// elements instead of runs 190); 2011 fp32 rows of 64 + 8 heads in a loop over the same tensors 25; 104 rows of 32 + 8 + 8 heads 5.6 (four a work-group 8.1).
 template <typename T, typename CT, int VE>
 __global__ __launch_bounds__(256) void k_rope(const RopeDev A) {
-  __shared__ float2 cs[4][128];
-  __shared__ int s_pos[4];
-  __shared__ long long s_cell[4];                                 // the row's place in the cache: element offset of kv head 0, -1 none, -2: not a row of any sequence
+  __shared__ float2 cs[128];
+  __shared__ int s_pos;
+  __shared__ long long s_cell;                                    // the row's place in the cache: element offset of kv head 0, -1 none, -2: not a row of any sequence
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  const int row0 = blockIdx.x * A.rows_per_wg, rows = min(A.rows_per_wg, A.n_rows - row0);
-  if (wave < rows) {
-    const int r = row0 + wave;
+  const int r = blockIdx.x;
+  if (wave == 0) {
     int pos = A.positions ? A.positions[r] : 0;
     long long cell = -1;
     if (A.has_chunk) {
@@ -94,23 +95,22 @@ __global__ __launch_bounds__(256) void k_rope(const RopeDev A) {
         }
       }
     }
-    if (lane == 0) { s_pos[wave] = pos; s_cell[wave] = cell; }
+    if (lane == 0) { s_pos = pos; s_cell = cell; }
   }
   __syncthreads();
   const int half = A.rot_dim >> 1;
-  for (int i = tid; i < rows * half; i += 256) {
-    const int r = i / half, p = i - r * half;
-    float2 c = cos_sin_turn(A.turn[p], s_pos[r]);
+  const long long cell = s_cell;
+  if (cell == -2) return;
+  for (int p = tid; p < half; p += 256) {
+    float2 c = cos_sin_turn(A.turn[p], s_pos);
     c.x *= A.mscale; c.y *= A.mscale * A.sign;
-    cs[r][p] = c;
+    cs[p] = c;
   }
   __syncthreads();
   const int rot_units = half / VE, units = rot_units + (A.head_dim - A.rot_dim + 2 * VE - 1) / (2 * VE);   // (VE > 1: half is a multiple of VE)
   const int h0 = blockIdx.y * A.heads_per_wg, nh = min(A.heads_per_wg, A.n_heads_all - h0);
-  for (int i = tid; i < rows * nh * units; i += 256) {
-    const int rh = i / units, u = i - rh * units, rl = rh / nh, h = h0 + rh - rl * nh, r = row0 + rl;
-    const long long cell = s_cell[rl];
-    if (cell == -2) continue;
+  for (int i = tid; i < nh * units; i += 256) {
+    const int h = h0 + i / units, u = i % units;
     const bool is_q = h < A.H, is_k = !is_q && h < A.H + A.KVH;
     const int kh = is_q ? h : h - A.H - (is_k ? 0 : A.KVH);       // head within q, k or v
     if (!is_q && A.has_kv && cell < 0) continue;
@@ -126,7 +126,7 @@ __global__ __launch_bounds__(256) void k_rope(const RopeDev A) {
     load_run<VE>(src + e0, a);
     if (two) load_run<VE>(src + e1, b);
     if (rotated) {
-      const float2* c = cs[rl] + u * VE;
+      const float2* c = cs + u * VE;
       if (A.interleaved && VE > 1) {
 #pragma unroll
         for (int j = 0; j < VE; j += 2) {
