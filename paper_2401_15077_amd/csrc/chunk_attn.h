@@ -11,11 +11,11 @@
 // Two shapes.  WIDE (more than 32 columns a sequence and kv head): four waves of 32 columns share tiles of tokens in LDS.  Narrow: one block of 32 columns, the four waves take every
 // fourth tile and join at the end.  Where sequences, kv heads and column blocks do not fill the chip, the token range is split over work-groups and k_chunk_attn_join adds the parts up.
 //
-// What bounds it, and what it reaches (us, kernel with join; MI355X).  A batch of 64 tokens over 1k to 16k tokens each, 64 / 8 heads of 128, bf16: 406, the cache once at 5.6 TB/s (a bare read in
+// What bounds it, and what it reaches (us a call, joining with it).  A batch of 64 tokens over 1k to 16k tokens each, 64 / 8 heads of 128, bf16: 406, the cache once at 5.6 TB/s (a bare read in
 // the same order reaches 6.0); tiles go to LDS without registers, a wave's next keys under way while it works on the values.  1536 and 509 rows behind a window of 4096 and a cap, 32 / 8 heads, bf16:
-// 201, 0.61 PFLOP/s of visible products: per tile 32 matrix instructions beside 460 vector ones (mask, cap, exponent, sums), which share a SIMD's two waves.  2011 fp32 rows, 32 heads of 80:
-// 190: 72 matrix and 600 vector instructions a tile (making the pieces: a third), and the last rows' blocks, which see 63 tiles, alone on their CU at the end.  Four trees of 26 nodes, fp32
-// over bf16, about 2000 tokens: 28, five tiles of 3.4 one after the other, 6 until the first tile is there, 6 for joining.  One token over 701, fp32: 19, all of it latency.
+// 194, 0.63 PFLOP/s of visible products: per tile 32 matrix instructions beside 460 vector ones (mask, cap, exponent, sums), which share a SIMD's two waves.  2011 fp32 rows, 32 heads of 80:
+// 169: 72 matrix and 500 vector instructions a tile (making the pieces: a third), and the last rows' blocks, which see 63 tiles, alone on their CU at the end.  Four trees of 26 nodes, fp32
+// over bf16, about 2000 tokens: 29, five tiles of 3.4 one after the other, 6 until the first tile is there, 6 for joining.  One token over 701, fp32: 19, all of it latency.
 //
 // A wave issues a vector instruction every 4.75 cycles and a matrix instruction takes the matrix unit 33, in whose shadow seven vector instructions fit if they stand between the matrix
 // instructions: the compiler does not put them there, so the order in which pieces and weights are made is written out, a step a product.

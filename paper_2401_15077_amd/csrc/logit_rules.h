@@ -19,6 +19,8 @@ struct RulesDev {
 // bias leaves its penalised value in its word instead, in fp32, and is finished from there by the thread that holds the entry.
 // Of several entries for a token the last counts.  That a token has several shows when BIASED is set twice; only then the list is taken from its end, one entry a thread at a time, and of those
 // at hand the largest index wins.
+// Bound by HBM and, where texts are long, by the vector unit: 160 rows of 100003 bf16 logits with texts of 4500 tokens, masks and 150 entries 25.5 us, of which logits and masks alone take 15 to
+// 16, the text's walk and the penalties of whole runs 8, entries 2; 104 rows of 32000 fp32 logits along trees 9.9 (kernel; without runs 40 and 13.4).
 // VE elements at a time where a row of `in` and of `out` start at the same place of a 16-byte piece; the first and last pieces may be partly outside the row.
 typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 constexpr uint32_t RULES_SEEN = 0x80000000u, RULES_BIASED = 0x40000000u, RULES_TAKEN = 0xFFFFFFFFu;
