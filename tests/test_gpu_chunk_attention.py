@@ -121,6 +121,15 @@ def test_tree_level_rows_of_some_nodes(types):
 
 
 @pytest.mark.parametrize("types", ALL)
+@pytest.mark.parametrize("D", [64, 80, 128])
+@pytest.mark.parametrize("window", [3, 40])
+def test_trees_of_many_columns_behind_a_window(window, D, types):
+    rng = np.random.default_rng(7)
+    t = [tree(40, rng), tree(30, rng)]
+    run([40, 30], [200, 61], 8, 2, D, types, 32, masks=t[0] + t[1], base=[160, 31], window=window, slopes=True, softcap=30.0, prefix=[5, 200])
+
+
+@pytest.mark.parametrize("types", ALL)
 @pytest.mark.parametrize("mods", [dict(softcap=3.0), dict(slopes=True), dict(window=1), dict(window=17), dict(window=100), dict(prefix=[40, 0]), dict(prefix=[300, 2]),
                                   dict(window=33, prefix=[5, 70], softcap=20.0, slopes=True), dict(scale=0.3), dict(scale=-0.2), dict(scale=0.0), dict(window=400)], ids=str)
 @pytest.mark.parametrize("rows,keys", [([1, 1], [300, 77]), ([50, 9], [300, 77]), ([150, 64], [260, 64])])
