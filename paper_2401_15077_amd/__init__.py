@@ -310,16 +310,14 @@ class Eagle:
             return
         if (allowed is None) != (allowed_row is None):
             raise ValueError("allowed and allowed_row belong together")
-        if allowed is not None and (allowed.dtype != t.int32 or allowed.dim() != 2 or allowed.device != dev or (allowed.stride(1) != 1 and allowed.shape[1] > 1) or allowed.shape[1] * 32 < self.shape.vocab):
-            raise ValueError(f"allowed must be an int32 [masks, words] tensor on {dev} of at least {(self.shape.vocab + 31) // 32} consecutive words a row")
+        masks = ops._masks(allowed, self.shape.vocab, dev) if allowed is not None else (None, 0, 0)
         b = bias if bias is not None else (None, None, None)
         if bias is not None and b[1].shape != b[2].shape:
             raise ValueError("bias tokens and values must be equally many")
         f, i = t.float32, t.int32
         r = ops.EagleContextRules(ops._list(repetition, "repetition", f, B, dev), ops._list(presence, "presence", f, B, dev), ops._list(frequency, "frequency", f, B, dev),
                                   ops._list(b[0], "bias start", i, B + 1, dev), ops._list(b[1], "bias token", i, None, dev), ops._list(b[2], "bias value", f, None, dev),
-                                  b[1].shape[0] if bias is not None else 0, allowed.shape[0] if allowed is not None else 0, allowed.data_ptr() if allowed is not None else None,
-                                  max(allowed.stride(0), allowed.shape[1]) if allowed is not None else 0, ops._list(allowed_row, "allowed_row", i, B * self.M, dev))
+                                  b[1].shape[0] if bias is not None else 0, masks[1], masks[0], masks[2], ops._list(allowed_row, "allowed_row", i, B * self.M, dev))
         self._chk(self.lib.eagle_set_logit_rules(self.h, ctypes.byref(r)))
         self._rules = (repetition, presence, frequency, bias, allowed, allowed_row)
 

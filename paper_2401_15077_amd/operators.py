@@ -132,6 +132,14 @@ def _heads(t: torch.Tensor, name: str, rows: Optional[int], heads: Optional[int]
     return t.data_ptr(), stride[0], stride[1]
 
 
+def _masks(allowed: torch.Tensor, vocab: int, device):
+    """Address, number and row stride (in words) of the masks `allowed`."""
+    if allowed.dtype != torch.int32 or allowed.dim() != 2 or allowed.device != device or (allowed.stride(1) != 1 and allowed.shape[1] > 1) or allowed.shape[1] * 32 < vocab \
+            or (allowed.shape[0] > 1 and allowed.stride(0) < allowed.shape[1]):
+        raise ValueError(f"allowed must be an int32 [masks, words] tensor on {device} of at least {(vocab + 31) // 32} consecutive words a row, its rows apart")
+    return allowed.data_ptr(), allowed.shape[0], max(allowed.stride(0), allowed.shape[1])
+
+
 class Chunk:
     """New tokens of a batch: int32 row_start [n_seqs + 1], key_len [n_seqs]; for draft trees int32 tree_base [n_seqs] and int64 tree_mask [n_rows].
     max_rows / max_keys bound the rows of a sequence and key_len."""
@@ -321,12 +329,9 @@ def apply_logit_rules(logits: torch.Tensor, rules: LogitRules, *, row_start: Opt
         raise ValueError(f"out must be {logits.dtype} {list(logits.shape)} on {dev}, its rows consecutive")
     masks = (None, 0, 0)
     if allowed is not None:
-        if allowed.dtype != torch.int32 or allowed.dim() != 2 or allowed.device != dev or (allowed.stride(1) != 1 and allowed.shape[1] > 1) or allowed.shape[1] * 32 < V \
-                or (allowed.shape[0] > 1 and allowed.stride(0) < allowed.shape[1]):
-            raise ValueError(f"allowed must be an int32 [masks, words] tensor on {dev} of at least {(V + 31) // 32} consecutive words a row, its rows apart")
+        masks = _masks(allowed, V, dev)
         if allowed_row is None and allowed.shape[0] != R:
             raise ValueError(f"without allowed_row there is one mask a row ({allowed.shape[0]} masks, {R} rows)")
-        masks = allowed.data_ptr(), allowed.shape[0], max(allowed.stride(0), allowed.shape[1])
     l = EagleLogits(R, V, _TYPES[logits.dtype], masks[1], logits.data_ptr(), out.data_ptr(), logits.stride(0) if R > 1 else V, out.stride(0) if R > 1 else V, masks[2],
                     _list(row_start, "row_start", torch.int32, rules.n_seqs + 1, dev), _list(path_token, "path_token", torch.int32, R, dev),
                     _list(path_mask, "path_mask", torch.int64, R, dev), masks[0], _list(allowed_row, "allowed_row", torch.int32, R, dev))
