@@ -65,12 +65,15 @@ class EagleError(RuntimeError):
 
 
 _lib = None
+_operators_declared = False
 
 
 def load_library(need_gpu_runtime: bool = True):
     """dlopen libeagle.so.  torch is imported first so that the HIP runtime it ships is the one in the process."""
     global _lib
     if _lib is not None:
+        if need_gpu_runtime:
+            _declare_operators(_lib)
         return _lib
     if not os.path.exists(LIB_PATH):
         raise RuntimeError(f"{LIB_PATH} is missing: run `python -c 'import __graft_entry__ as g; g.build()'` "
@@ -110,12 +113,20 @@ def load_library(need_gpu_runtime: bool = True):
     lib.eagle_head_loss.argtypes = [vp, vp, vp, i32, ctypes.c_float, vp, ctypes.POINTER(ctypes.c_float)]
     lib.eagle_feature_noise.argtypes = [vp, vp, vp, i32, ctypes.c_float, ctypes.c_uint64, ctypes.c_uint64]
     if need_gpu_runtime:
-        from . import operators
-        operators.declare(lib)
+        _declare_operators(lib)
     lib.eagle_last_error.restype = ctypes.c_char_p
     lib.eagle_version.restype = ctypes.c_char_p
     _lib = lib
     return lib
+
+
+def _declare_operators(lib) -> None:
+    """The argument types of the operators, whose module imports torch: not when the library is loaded without it, but at the latest when it is asked for again."""
+    global _operators_declared
+    if not _operators_declared:
+        from . import operators
+        operators.declare(lib)
+        _operators_declared = True
 
 
 def _p32(a: Optional[np.ndarray]):
