@@ -826,8 +826,9 @@ __global__ __launch_bounds__(256) void k_chunk_attn_join(const ChunkAttnDev A) {
   const float mine = lane < n ? ml.x : -INFINITY;
   float m = mine;
   for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-  const float f = mine == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mine - m);
-  float l = f == 0.f ? 0.f : f * ml.y, x[E];
+  // A part without a maximum saw nothing (its sum is 0), or nothing but scores that are NaN: then its sum is NaN, and so is the row.
+  const float sum = lane < n ? ml.y : 0.f, f = mine == -INFINITY ? (sum == 0.f ? 0.f : sum) : __builtin_amdgcn_exp2f(mine - m);
+  float l = f == 0.f ? 0.f : f * sum, x[E];
   for (int o = 32; o; o >>= 1) l += __shfl_xor(l, o, 64);
 #pragma unroll
   for (int e = 0; e < E; ++e) x[e] = 0.f;

@@ -1,0 +1,88 @@
+"""Numbers at the ends of the range in the attention of a chunk: what is not finite stays with the rows that see it and stays what it is, whatever the launch shape; bits of a row that depend on
+nothing the row does not see."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import operators as ref
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = {"fp32": torch.float32, "bf16": torch.bfloat16}
+ALL = ["fp32/fp32", "fp32/bf16", "bf16/bf16"]
+
+
+def pkg():
+    import paper_2401_15077_amd
+    return paper_2401_15077_amd
+
+
+def i32(a):
+    return torch.tensor(np.asarray(a), dtype=torch.int32, device=DEV)
+
+
+class Call:
+    """Queries, a cache (pages in order) and the chunk of a batch."""
+
+    def __init__(self, rows, keys, H, KVH, D, types, page, *, seed=0, max_keys=None, base=None, masks=None):
+        p = pkg()
+        self.rows, self.keys, self.page = rows, keys, page
+        dtype, cdtype = (TYPES[t] for t in types.split("/"))
+        gen = torch.Generator(device=DEV).manual_seed(seed + 11)
+        per = [-(-k // page) for k in keys]
+        n_pages = sum(per)
+        self.table = np.full((len(keys), max(per)), -1, np.int32)
+        at = 0
+        for s, n in enumerate(per):
+            self.table[s, :n] = np.arange(at, at + n)
+            at += n
+        self.k, self.v = (torch.randn(n_pages, KVH, page, D, device=DEV, generator=gen).to(cdtype) for _ in range(2))
+        self.q = torch.randn(sum(rows), H, D, device=DEV, generator=gen).to(dtype)
+        self.start = np.cumsum([0] + list(rows))
+        self.base, self.masks = base, masks
+        self.chunk = p.Chunk(i32(self.start), i32(keys), sum(rows), max(rows), max_keys or max(keys), tree_base=None if base is None else i32(base),
+                             tree_mask=None if masks is None else torch.tensor(masks, dtype=torch.int64, device=DEV))
+
+    def at(self, s, t):
+        """Page and slot of token t of sequence s."""
+        return int(self.table[s, t // self.page]), t % self.page
+
+    def __call__(self, **kw):
+        p = pkg()
+        out = p.chunk_attention(self.q, p.PagedKV(self.k, self.v, i32(self.table)), self.chunk, **kw)
+        torch.cuda.synchronize()
+        return out
+
+
+SHAPES = [([1], [701], 4, 64), ([1], [40], 4, 64), ([1, 2], [2100, 300], 4, 128), ([26], [900], 8, 128), ([40], [60], 4, 64), ([70], [1100], 2, 96)]
+
+
+@pytest.mark.parametrize("types", ALL)
+@pytest.mark.parametrize("rows,keys,H,D", SHAPES)
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), float("-inf")])
+def test_a_query_that_is_not_finite(rows, keys, H, D, value, types):
+    """Its scores are NaN or infinite: the row and head are NaN, all others what they were.  (An infinite element makes scores of both signs, and inf - inf in the softmax.)"""
+    c = Call(rows, keys, H, H, D, types, 32)
+    plain = c()
+    assert torch.isfinite(plain).all()
+    r, h = sum(rows) - 1, H - 1
+    c.q[r, h, 5] = value
+    got = c()
+    assert torch.isnan(got[r, h]).all()
+    got[r, h] = plain[r, h]
+    assert torch.equal(got, plain)
+
+
+@pytest.mark.parametrize("types", ALL)
+@pytest.mark.parametrize("D", [64, 96, 128])
+@pytest.mark.parametrize("rows", [1, 40])
+def test_a_range_of_tokens_in_which_only_a_nan_key_is_visible(rows, D, types):
+    """Pages of one token: of tokens 64 to 639 only number 300 is there, and its key is NaN.  A part of a split token range may hold that token and nothing else that is visible."""
+    c = Call([rows], [701], 2, 2, D, types, 1)
+    c.table[0, 64:640] = -1
+    c.table[0, 300] = 300
+    plain = c()
+    assert torch.isfinite(plain).all()
+    c.k[300, 1, 0, 0] = float("nan")
+    got = c()
+    assert torch.isnan(got[:, 1]).all() and torch.equal(got[:, 0], plain[:, 0])
