@@ -5,8 +5,9 @@
 // maximum and sum and the rescaling are lane-local, and a score's place in the accumulator is where the second product wants its weight.  One pass over the keys with the running
 // maximum and sum of the softmax; everything but the operands of the matrix instructions is fp32.
 //
-// fp32 operands are exact sums of three bf16 pieces (8 bits each of the 24), and of the nine products of two such sums the six of at least 2^-16 of the largest are kept: what is
-// left out is 2^-24 of a product.  bf16 operands are one piece.  Weights are one piece for bf16 queries (the output rounds by as much) and three for fp32.
+// fp32 operands are exact sums of three bf16 pieces (8 bits each of the 24), and of the nine products of two such sums the six of at least 2^-15 of the largest are kept: what is
+// left out is 2^-22 of a product at most.  The cache's first pieces are cut off and not rounded, since the largest numbers would round to infinity (and their other pieces to NaN).  bf16
+// operands are one piece.  Weights are one piece for bf16 queries (the output rounds by as much) and three for fp32.
 //
 // Two shapes.  WIDE (more than 32 columns a sequence and kv head): four waves of 32 columns share tiles of tokens in LDS.  Narrow: one block of 32 columns, the four waves take every
 // fourth tile and join at the end.  Where sequences, kv heads and column blocks do not fill the chip, the token range is split over work-groups and k_chunk_attn_join adds the parts up.
@@ -74,19 +75,30 @@ __device__ inline ColumnRange column_range(const ChunkAttnDev& A, int s, int col
 
 __device__ __forceinline__ uint64_t low_ones(int n) { return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1ull; }
 
-// x as an exact sum of bf16 pieces.  (Of what is not finite the first is the same, the others NaN.)
-typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
-template <int NP, int N, typename V> __device__ __forceinline__ void pieces(const float* x, V* p) {
+// The upper halves of two fp32 numbers: their first pieces.
+__device__ __forceinline__ uint32_t upper_pair(float a, float b) { return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, a), 0x07060302u); }
+// Eight numbers as exact sums of three bf16 pieces, the first of which is cut off (NEAREST: rounded, but where that is infinite).  (Of what is not finite the first is the same, but for a signalling
+// NaN, which may become infinite; the others are NaN.)
+template <bool NEAREST> __device__ __forceinline__ void pieces(const float* x, bf16x8* p) {
+  u32x4 h[3];
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    p[0][i] = (__bf16)x[i];
-    if constexpr (NP == 3) {
-      float r = x[i] - (float)p[0][i];
-      p[1][i] = (__bf16)r;
-      r -= (float)p[1][i];
-      p[2][i] = (__bf16)r;
+  for (int i = 0; i < 4; ++i) {
+    float a = x[2 * i], b = x[2 * i + 1];
+    h[0][i] = upper_pair(a, b);
+    if constexpr (NEAREST) {
+      const uint32_t n = bf16_pair(a, b);
+      if ((n & 0x7F80u) != 0x7F80u) h[0][i] = (h[0][i] & 0xFFFF0000u) | (n & 0xFFFFu);
+      if ((n & 0x7F800000u) != 0x7F800000u) h[0][i] = (h[0][i] & 0xFFFFu) | (n & 0xFFFF0000u);
+    }
+#pragma unroll
+    for (int j = 1; j < 3; ++j) {
+      a -= __builtin_bit_cast(float, h[j - 1][i] << 16);
+      b -= __builtin_bit_cast(float, h[j - 1][i] & 0xFFFF0000u);
+      h[j][i] = bf16_pair(a, b);
     }
   }
+#pragma unroll
+  for (int j = 0; j < 3; ++j) p[j] = __builtin_bit_cast(bf16x8, h[j]);
 }
 __device__ __forceinline__ bool not_finite(float x) { return (__builtin_bit_cast(uint32_t, x) & 0x7F800000u) == 0x7F800000u; }
 // Not 0 if one of the eight bf16 numbers is not finite: an exponent of ones carries into the sign's place.
@@ -109,16 +121,16 @@ template <> struct Raw8<bf16_t> {
   u32x4 v;
   __device__ __forceinline__ void load(const bf16_t* p) { v = *(const u32x4*)p; }
   __device__ __forceinline__ void zero() { v = u32x4{0, 0, 0, 0}; }
-  __device__ __forceinline__ void split(bf16x8* p) const { p[0] = __builtin_bit_cast(bf16x8, v); }
+  template <bool NEAREST = false> __device__ __forceinline__ void split(bf16x8* p) const { p[0] = __builtin_bit_cast(bf16x8, v); }
 };
 template <> struct Raw8<float> {
   f32x4 a, b;
   __device__ __forceinline__ void load(const float* p) { a = *(const f32x4*)p; b = *(const f32x4*)(p + 4); }
   __device__ __forceinline__ void zero() { a = b = f32x4{0.f, 0.f, 0.f, 0.f}; }
   __device__ __forceinline__ uint32_t bad() const { return not_finite_any(a) | not_finite_any(b); }
-  __device__ __forceinline__ void split(bf16x8* p) const {
+  template <bool NEAREST = false> __device__ __forceinline__ void split(bf16x8* p) const {
     const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-    pieces<3, 8>(x, p);
+    pieces<NEAREST>(x, p);
   }
 };
 
@@ -329,7 +341,8 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
     const bool values = run & 1;
     f32x4& x = values ? v4[i] : k4[i];
     const uint32_t bad = values && pair == 0 && j == 0 ? not_finite_any(x) : 0;
-    const uint32_t h = bf16_pair(x[2 * pair], x[2 * pair + 1]);
+    uint32_t h = j == 0 ? upper_pair(x[2 * pair], x[2 * pair + 1]) : bf16_pair(x[2 * pair], x[2 * pair + 1]);
+    if (j == 0) asm volatile("" : "+v"(h));                       // (the remainders come from it: the compiler would take them from the numbers, in more registers than there are)
     pk[j][pair] = h;
     if (j < 2) {
       x[2 * pair] -= __builtin_bit_cast(float, h << 16);
@@ -393,7 +406,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
       x.zero();
       if (c.live && d < dh) x.load(qp + d);
       bf16x8 p[3];
-      x.split(p);
+      x.template split<true>(p);
 #pragma unroll
       for (int i = 0; i < NQ; ++i) qf[i][ks] = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, p[i]) ^ A.q_flip);
     }

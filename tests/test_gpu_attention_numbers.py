@@ -86,3 +86,61 @@ def test_a_range_of_tokens_in_which_only_a_nan_key_is_visible(rows, D, types):
     c.k[300, 1, 0, 0] = float("nan")
     got = c()
     assert torch.isnan(got[:, 1]).all() and torch.equal(got[:, 0], plain[:, 0])
+
+
+BIG = 3.4028234663852886e38                                       # the largest fp32 number: as bf16 it would round to infinity
+
+
+@pytest.mark.parametrize("rows,keys,H,D", SHAPES)
+@pytest.mark.parametrize("value", [BIG, -BIG, 3.3962e38])
+def test_the_largest_values_of_an_fp32_cache(rows, keys, H, D, value):
+    """They are finite: 0 times one is 0 for the rows that do not see it, and the row that sees only it gets it.  (Rows that see others too add up products of weights that may reach 2^8: beyond the
+    range that is infinite.)"""
+    rows, keys = [max(2, n) for n in rows], [max(2, n) for n in rows]
+    c = Call(rows, keys, H, H, D, "fp32/fp32", 32)
+    plain = c()
+    for s, n in enumerate(keys):
+        page, slot = c.at(s, n - 1)                               # what only the last row sees
+        c.v[page, :, slot, 3] = value
+    got = c()
+    unlike = (got != plain).nonzero()
+    last = {int(x) - 1 for x in c.start[1:]}
+    assert all(int(r) in last and int(d) == 3 for r, _, d in unlike)
+    assert not torch.isnan(got).any()
+    c = Call(rows, keys, H, H, D, "fp32/fp32", 32)
+    page, slot = c.at(0, 0)
+    c.v[page, :, slot, 3] = value
+    got = c()
+    assert torch.equal(got[0, :, 3], torch.full_like(got[0, :, 3], value))
+    assert not torch.isnan(got).any()
+
+
+@pytest.mark.parametrize("types", ["fp32/fp32", "fp32/bf16"])
+@pytest.mark.parametrize("rows,keys,H,D", SHAPES)
+def test_the_largest_keys_and_queries_against_zeros(rows, keys, H, D, types):
+    """0 times the largest number is 0: element 3 adds nothing to a score, whichever side holds it, and bits are those of a 0 there."""
+    c = Call(rows, keys, H, H, D, types, 32)
+    c.q[:, :, 3] = 0.0
+    c.k[:, :, :, 3] = 0.0
+    plain = c()
+    c.q[:, :, 3] = BIG
+    assert torch.equal(c(), plain)
+    c.q[:, :, 3] = 0.0
+    c.k[:, :, :, 3] = BIG if types == "fp32/fp32" else float(torch.finfo(torch.bfloat16).max)
+    assert torch.equal(c(), plain)
+
+
+@pytest.mark.parametrize("rows,keys,H,D", SHAPES)
+def test_products_of_the_largest_keys_and_small_queries(rows, keys, H, D):
+    """A score that one product decides: key element 3 is near the end of the range, query element 3 brings it back.  Every product of pieces is exact in fp32 or rounds by 2^-24, six of nine are
+    kept: the score is off by 2^-22 (left out) and 16 * 2^-24 (roundings) of |q k| <= 12, so a weight by 2 * 12 * 20 * 2^-24 = 2^-15.1 of itself, the others' 64 roundings included: 2^-14."""
+    c = Call(rows, keys, H, H, D, "fp32/fp32", 32)
+    gen = torch.Generator(device=DEV).manual_seed(5)
+    c.k.zero_()
+    c.q.zero_()
+    c.k[..., 3] = BIG * (1.0 - 2.0 ** -6 * torch.rand(c.k.shape[:-1], device=DEV, generator=gen))
+    c.q[..., 3] = 2.0 ** -122 * (1.0 + torch.rand(c.q.shape[:-1], device=DEV, generator=gen))
+    got = c(scale=0.1).double().cpu().numpy()
+    want, mean, _, _ = ref.attention(c.q.double().cpu().numpy(), c.k.double().cpu().numpy(), c.v.double().cpu().numpy(), c.table, ref.chunk_rows(c.start, keys), sum(rows), keys, page=32,
+                                     scale=0.1)
+    assert (np.abs(got - want) <= 2.0 ** -14 * mean).all()
