@@ -529,7 +529,19 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
     if (!idle) {
     // cap and slopes
     if constexpr (MODS) {
-      bool small = false;                                         // the cap bends no score of this wave much
+      // bf16 queries: a score up to 0.7 of the cap takes a polynomial, one beyond it the exponential, each by its own size alone; where no score of the wave is beyond (of those that no row sees
+      // neither), the exponential is left out.
+      const float k = cap_out * cap_y;
+      auto bent = [&](float x) -> float {
+        // tanh(y) = y (1 + z (a1 + z (a2 + z (a3 + z a4)))), z = y^2: the coefficients of the least largest error up to 0.7, which is 9.7 * 10^-8.  Seven operations at the full rate for five of
+        // which two take four times as long.
+        const float y = x * cap_y, z = y * y;
+        float t = fmaf(k * 0.01346275f, z, k * -0.05054204f);
+        t = fmaf(t, z, k * 0.13272971f);
+        t = fmaf(t, z, k * -0.33329716f);
+        return x * fmaf(t, z, k);
+      };
+      bool small = false;
       if (NQ == 1 && A.softcap > 0.f) {
         float far = 0.f;
 #pragma unroll
@@ -539,19 +551,10 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
         small = !__any(far * cap_y > 0.7f);
       }
       if (small) {
-        // tanh(y) = y (1 + z (a1 + z (a2 + z (a3 + z a4)))), z = y^2: the coefficients of the least largest error up to 0.7, which is 9.7 * 10^-8.  Seven operations at the full rate for five of
-        // which two take four times as long.
-        const float k = cap_out * cap_y;
 #pragma unroll
         for (int a = 0; a < KB; ++a)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const float x = sacc[a][r], y = x * cap_y, z = y * y;
-            float t = fmaf(k * 0.01346275f, z, k * -0.05054204f);
-            t = fmaf(t, z, k * 0.13272971f);
-            t = fmaf(t, z, k * -0.33329716f);
-            sacc[a][r] = x * fmaf(t, z, k);
-          }
+          for (int r = 0; r < 16; ++r) sacc[a][r] = bent(sacc[a][r]);
       } else if (A.softcap > 0.f) {
 #pragma unroll
         for (int a = 0; a < KB; ++a)
@@ -569,6 +572,8 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
               t = fmaf(t, z, -0.333333333333333333f);
               t = fmaf(t * z, y, y);
               x = fabsf(y) < 0.35f ? cap_out * t : x;
+            } else {
+              x = fabsf(sacc[a][r]) * cap_y > 0.7f ? x : bent(sacc[a][r]);
             }
             sacc[a][r] = x;
           }

@@ -144,3 +144,51 @@ def test_products_of_the_largest_keys_and_small_queries(rows, keys, H, D):
     want, mean, _, _ = ref.attention(c.q.double().cpu().numpy(), c.k.double().cpu().numpy(), c.v.double().cpu().numpy(), c.table, ref.chunk_rows(c.start, keys), sum(rows), keys, page=32,
                                      scale=0.1)
     assert (np.abs(got - want) <= 2.0 ** -14 * mean).all()
+
+
+@pytest.mark.parametrize("types", ALL)
+@pytest.mark.parametrize("rows,keys,H", [([40], [100], 4), ([6], [50], 4), ([200], [230], 2), ([1], [701], 4)])
+@pytest.mark.parametrize("cap", [4.0, 50.0, 3000.0])
+def test_capped_scores_depend_on_nothing_that_is_not_seen(rows, keys, H, cap, types):
+    """Newer tokens, what lies behind the last token, and the queries of other rows and heads: a row's bits are its own."""
+    c = Call(rows, keys, H, H, 64, types, 32)
+    n, K = rows[0], keys[0]
+    plain = c(softcap=cap)
+    queries, cached = c.q.clone(), c.k.clone()
+    for value in (1e5, float("inf"), float("nan")):
+        first = n // 2 if n > 1 else n                            # rows in front of it see none of what changes
+        for t in range(K - n + first, c.k.shape[0] * 32):
+            page, slot = c.at(0, t)
+            c.k[page, :, slot] = value
+        assert torch.equal(c(softcap=cap)[:first], plain[:first]), value
+        c.k.copy_(cached)
+    c.q[:, 1:] *= 4000.0                                          # all heads but the first, and all rows but the first
+    c.q[1:] *= 4000.0
+    got = c(softcap=cap)
+    assert torch.equal(got[0, 0], plain[0, 0])
+    c.q.copy_(queries)
+    c.q[:, 0] *= 4000.0
+    assert torch.equal(c(softcap=cap)[:, 1:], plain[:, 1:])
+
+
+@pytest.mark.parametrize("types", ALL)
+@pytest.mark.parametrize("rows", [1, 20, 50])
+def test_a_score_beyond_a_large_cap_beside_small_ones(rows, types):
+    """One key is far below -0.7 of a cap of 10^6; it has no weight, and the others' scores, of a few units, are hardly bent.  They are off by relative errors of their own size: 64 roundings of the
+    product and 16 of the cap's polynomial, of at most B = scale * sum |q k| without that key: 2 * 80 u B of a weight, u = 2^-24; sums 64 u; bf16 queries round weights and result by 2^-8."""
+    H, K = 4, 60
+    c = Call([rows], [K], H, H, 64, types, 32)
+    q = c.q[:1].expand(rows, H, 64).contiguous()                  # one query for all rows, so that one key is far from all of them
+    c.q.copy_(q)
+    c.k[0, :, 0] = (q[0].float() * -2e5).to(c.k.dtype)
+    got = c(softcap=1e6).double().cpu().numpy()
+    args = c.q.double().cpu().numpy(), c.k.double().cpu().numpy(), c.v.double().cpu().numpy()
+    facts = ref.chunk_rows(c.start, [K])
+    want, mean, _, _ = ref.attention(*args, c.table, facts, rows, [K], page=32, scale=0.125, softcap=1e6)
+    args[1][0, :, 0] = 0.0
+    _, _, big, _ = ref.attention(*args, c.table, facts, rows, [K], page=32, scale=0.125, softcap=1e6)
+    u = 2.0 ** -24
+    tol = (160 * u * big + 64 * u)[:, :, None] * mean
+    if types.startswith("bf16"):
+        tol = tol + 2.0 ** -8 * 1.001 * (mean + np.abs(want))
+    assert (np.abs(got - want) <= tol).all()
