@@ -57,7 +57,7 @@ __device__ inline ColumnRange column_range(const ChunkAttnDev& A, int s, int col
   c.n = min(n_all, A.chunk.max_rows);
   c.keys = chunk_keys(A.chunk, A.kv, s);
   c.tree = A.chunk.tree_mask != nullptr;
-  c.base = c.tree ? max(0, min(A.chunk.tree_base[s], c.keys)) : 0;
+  c.base = c.tree ? min(max(0, A.chunk.tree_base[s]), 1 << 30) : 0;   // (positions count from it, also where fewer tokens may be read)
   c.own0 = c.tree ? c.base : min(max(0, A.chunk.key_len[s]), 1 << 30) - n_all;
   c.prefix = A.prefix ? min(A.prefix[s], c.tree ? c.base : c.keys) : 0;
   c.prefix = max(0, c.prefix);

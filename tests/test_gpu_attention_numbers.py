@@ -192,3 +192,28 @@ def test_a_score_beyond_a_large_cap_beside_small_ones(rows, types):
     if types.startswith("bf16"):
         tol = tol + 2.0 ** -8 * 1.001 * (mean + np.abs(want))
     assert (np.abs(got - want) <= tol).all()
+
+
+@pytest.mark.parametrize("types", ALL)
+@pytest.mark.parametrize("nodes,max_keys", [(26, 64), (26, 96), (3, 32), (40, 128), (26, 512)])
+@pytest.mark.parametrize("kw", [dict(window=70), dict(window=120, slopes=True), dict(slopes=True), dict(window=5), dict(window=90, prefix=20)], ids=str)
+def test_trees_whose_tokens_are_more_than_max_keys(nodes, max_keys, types, kw):
+    """Tokens from max_keys on are not there; positions, hence windows and distances, are still those of the whole text.  (Largest term of a score: 8 for q k, 160 / 2 for a distance.)"""
+    base, H = 100, 8
+    masks = [1]
+    for v in range(1, nodes):
+        masks.append(masks[(v - 1) // 3] | 1 << v)
+    c = Call([nodes], [base + nodes], H, 2, 64, types, 32, base=[base], masks=masks, max_keys=max_keys)
+    sl = (2.0 ** (-torch.arange(1, H + 1, dtype=torch.float32))).to(DEV) if kw.get("slopes") else None
+    prefix = [kw["prefix"]] if "prefix" in kw else None
+    got = c(window=kw.get("window", 0), slopes=sl, prefix=None if prefix is None else i32(prefix)).double().cpu().numpy()
+    table = c.table.copy()
+    table[0, max_keys // 32:] = -1
+    want, mean, big, count = ref.attention(c.q.double().cpu().numpy(), c.k.double().cpu().numpy(), c.v.double().cpu().numpy(), table, ref.chunk_rows(c.start, c.keys, [base], masks), nodes,
+                                           c.keys, page=32, scale=0.125, slopes=None if sl is None else sl.double().cpu().numpy(), window=kw.get("window", 0), prefix=prefix, tree_base=[base])
+    u = 2.0 ** -24
+    tol = (2 * (64 * u * big + 4 * u * (big + 80)) + 64 * u)[:, :, None] * mean
+    if types.startswith("bf16"):
+        tol = tol + 2.0 ** -8 * 1.001 * (mean + np.abs(want))
+    assert (np.abs(got - want) <= tol).all()
+    assert (got[count == 0] == 0.0).all()
