@@ -325,7 +325,7 @@ int eagle_rope(const eagle_rope_plan *plan, const eagle_rope_args *args, const e
  *   - j < prefix[s] (tree: at most the tokens in front of the tree): a prefix every row of the sequence sees, in front of the window and ahead of the row.
  * A row that sees nothing gets zeros.  q, out: EAGLE_F32 over a cache of either type, or EAGLE_BF16 over EAGLE_BF16; out is of q's type and may be q.
  * head_dim: a multiple of 8, 8..128.  q's rows and the cache's tokens start on multiples of 16 bytes, out's of 8 elements.  NaN and infinities in a token stay with
- * the rows that see it (a key that is not finite may make NaN of a score).  Rows that no sequence owns are left as they are.
+ * the rows that see it: a key that is not finite may make NaN of a score; a value that is infinite makes its element of the row's result infinite or NaN, never finite.  Rows that no sequence owns are left as they are.
  * workspace (dev, 256-byte aligned): eagle_chunk_attention_workspace() bytes, for the same arguments; its contents need not be kept or cleared. */
 typedef struct {
   int32_t n_heads, dtype, window;

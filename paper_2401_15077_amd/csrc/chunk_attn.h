@@ -846,7 +846,7 @@ __global__ __launch_bounds__(256) void k_chunk_attn_join(const ChunkAttnDev A) {
   for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
   // A part without a maximum saw nothing (its sum is 0), or nothing but scores that are NaN: then its sum is NaN, and so is the row.
   const float sum = lane < n ? ml.y : 0.f, f = mine == -INFINITY ? (sum == 0.f ? 0.f : sum) : __builtin_amdgcn_exp2f(mine - m);
-  float l = f == 0.f ? 0.f : f * sum, x[E];
+  float l = f * sum, x[E];
   for (int o = 32; o; o >>= 1) l += __shfl_xor(l, o, 64);
 #pragma unroll
   for (int e = 0; e < E; ++e) x[e] = 0.f;
@@ -854,9 +854,10 @@ __global__ __launch_bounds__(256) void k_chunk_attn_join(const ChunkAttnDev A) {
     if (k0 > 0) request(k0);
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
-      const float fk = k0 + u < n ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), k0 + u)) : 0.f;
+      const bool there = k0 + u < n;                              // (what lies behind the parts may be anything)
+      const float fk = there ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), k0 + u)) : 0.f;
 #pragma unroll
-      for (int e = 0; e < E; ++e) x[e] = fk == 0.f ? x[e] : fmaf(fk, ov[u][e], x[e]);
+      for (int e = 0; e < E; ++e) x[e] = there ? fmaf(fk, ov[u][e], x[e]) : x[e];   // (0 times an infinity that a row sees is NaN, as it is within a part)
     }
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;

@@ -217,3 +217,24 @@ def test_trees_whose_tokens_are_more_than_max_keys(nodes, max_keys, types, kw):
         tol = tol + 2.0 ** -8 * 1.001 * (mean + np.abs(want))
     assert (np.abs(got - want) <= tol).all()
     assert (got[count == 0] == 0.0).all()
+
+
+@pytest.mark.parametrize("types", ALL)
+@pytest.mark.parametrize("rows,keys,H,D", SHAPES)
+@pytest.mark.parametrize("steep", [False, True])
+def test_an_infinite_value_deep_in_the_context(rows, keys, H, D, steep, types):
+    """In a tile that every row sees whole, far from the rows, with a weight or (steep) one that is 0 in fp32: its element is never finite, all others are what they were."""
+    c = Call(rows, keys, H, H, D, types, 32)
+    kw = dict(slopes=torch.full((H,), 2.0, device=DEV)) if steep else {}
+    plain = c(**kw)
+    assert torch.isfinite(plain).all()
+    for s in range(len(rows)):
+        page, slot = c.at(s, 1)
+        c.v[page, :, slot, 5] = float("inf")
+    got = c(**kw)
+    sees = torch.ones(sum(rows), dtype=torch.bool, device=DEV)
+    for s, (n, K) in enumerate(zip(rows, keys)):
+        sees[c.start[s]:c.start[s] + max(0, 1 - (K - n))] = False
+    assert not torch.isfinite(got[sees][..., 5]).any()
+    got[..., 5] = plain[..., 5]
+    assert torch.equal(got, plain)
