@@ -1,8 +1,8 @@
 """Operators on the caller's own tensors: rotary positions with the append to a paged cache, attention of a chunk of new tokens over it, and the
 rules that logits pass before a token is chosen (argument marshalling only; include/eagle.h has the definitions).
 
-Every call is enqueued on torch's current stream of the tensors' device and does not synchronise.  Outputs are not recorded by autograd: inputs that
-require gradients are refused while gradients are enabled."""
+Every call is enqueued on torch's current stream of the tensors' device and does not synchronise.  Outputs are not recorded by autograd: tensors that
+require gradients (inputs, caches, slopes, rules, outputs) are refused while gradients are enabled."""
 from __future__ import annotations
 
 import ctypes
@@ -105,12 +105,18 @@ def _call(fn, device, *args):
         raise EagleError(rc, _library().eagle_last_error().decode())
 
 
+def _plain(t: torch.Tensor, name: str) -> None:
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name} requires gradients: libeagle's operators are not recorded by autograd")
+
+
 def _list(t: Optional[torch.Tensor], name: str, dtype, n: Optional[int], device) -> Optional[int]:
     """Address of a contiguous 1-D tensor of n entries (None: any number) on `device`; None for None."""
     if t is None:
         return None
     if t.dtype != dtype or t.dim() != 1 or (n is not None and t.shape[0] != n) or t.device != device or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of {'any number of' if n is None else n} entries on {device}: got {t.dtype} {tuple(t.shape)} on {t.device}")
+    _plain(t, name)
     return t.data_ptr()
 
 
@@ -127,8 +133,7 @@ def _heads(t: torch.Tensor, name: str, rows: Optional[int], heads: Optional[int]
     stride = t.stride()
     if stride[2] != 1 and dim > 1:
         raise ValueError(f"the elements of a head of {name} must be consecutive")
-    if t.requires_grad and torch.is_grad_enabled():
-        raise ValueError(f"{name} requires gradients: libeagle's operators are not recorded by autograd")
+    _plain(t, name)
     return t.data_ptr(), stride[0], stride[1]
 
 
@@ -175,6 +180,8 @@ def _same_batch(chunk: Chunk, kv: PagedKV, device) -> None:
         raise ValueError(f"the chunk is on {chunk.device}, the cache on {kv.device}, the rows on {device}")
     if kv.n_seqs != chunk.n_seqs:
         raise ValueError(f"the page table has {kv.n_seqs} sequences, the chunk {chunk.n_seqs}")
+    _plain(kv._keep[0], "k of the cache")
+    _plain(kv._keep[1], "v of the cache")
 
 
 def rope_config(head_dim: int, *, theta: float = 10000.0, rot_dim: Optional[int] = None, interleaved: bool = False, scaling: str = "none", factor: float = 1.0, low: float = 1.0,
@@ -302,6 +309,7 @@ class LogitRules:
         if bias is not None and b[1].shape != b[2].shape:
             raise ValueError("bias tokens and values must be equally many")
         self._keep = (tokens, n_tokens, n_prompt, repetition, presence, frequency, b)
+        self._values = [(t, name) for t, name in ((repetition, "repetition"), (presence, "presence"), (frequency, "frequency"), (b[2], "bias value")) if t is not None]
         self.longest = tokens.shape[1] if tokens is not None else 0
         f, i = torch.float32, torch.int32
         self.c = EagleLogitRules(self.n_seqs, tokens.data_ptr() if tokens is not None else None, tokens.stride(0) if tokens is not None else 0, self.longest,
@@ -317,8 +325,9 @@ def apply_logit_rules(logits: torch.Tensor, rules: LogitRules, *, row_start: Opt
     [rows]: tokens along a draft tree.  allowed: int32 [masks, words >= vocab / 32], a bit a token; allowed_row: int32 [rows], the row's mask (-1: none; None: row r's is mask r)."""
     if logits.dim() != 2 or logits.dtype not in _TYPES or (logits.stride(1) != 1 and logits.shape[1] > 1):
         raise ValueError("logits must be a float32 or bfloat16 [rows, vocab] tensor, its rows consecutive")
-    if logits.requires_grad and torch.is_grad_enabled():
-        raise ValueError("logits require gradients: libeagle's operators are not recorded by autograd")
+    _plain(logits, "logits")
+    for t, name in rules._values:                                 # (they may have been made while gradients were off)
+        _plain(t, name)
     R, V = logits.shape
     dev = logits.device
     if rules.device is not None and rules.device != dev:
@@ -327,6 +336,8 @@ def apply_logit_rules(logits: torch.Tensor, rules: LogitRules, *, row_start: Opt
         out = logits
     elif out.shape != logits.shape or out.dtype != logits.dtype or out.device != dev or (out.stride(1) != 1 and V > 1):
         raise ValueError(f"out must be {logits.dtype} {list(logits.shape)} on {dev}, its rows consecutive")
+    else:
+        _plain(out, "out")
     masks = (None, 0, 0)
     if allowed is not None:
         masks = _masks(allowed, V, dev)
