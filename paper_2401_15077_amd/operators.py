@@ -79,6 +79,7 @@ def declare(lib) -> None:
     lib.eagle_apply_logit_rules.argtypes = [P(EagleLogits), P(EagleLogitRules), _vp]
 
 
+_written = torch.autograd.graph.increment_version                 # tells autograd that a tensor it may have saved is no longer what it was
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device      # (a tensor on the device: the runtime is up)
 _lib = None
@@ -243,6 +244,8 @@ def rope(plan: EagleRopePlan, q: Optional[torch.Tensor], k: Optional[torch.Tenso
         return
     a = EagleRopeArgs(R, H, KVH, _TYPES[dtype], int(inverse), qa[0], ka[0], va[0], qo[0], ko[0], qa[1], qa[2], ka[1], ka[2], va[1], va[2], qo[1], qo[2], ko[1], ko[2], at)
     _call(_library().eagle_rope, device, plan, a, chunk.c if chunk is not None else None, kv.c if kv is not None else None)
+    k_to = () if k is None else (k_out if k_out is not None else k,) if kv is None else kv._keep[:2] if v is not None else kv._keep[:1]
+    _written(k_to if q is None else (q_out if q_out is not None else q, *k_to))
 
 
 def _attention_args(q, kv, chunk, scale, softcap, slopes, window, prefix, out):
@@ -283,6 +286,7 @@ def chunk_attention(q: torch.Tensor, kv: PagedKV, chunk: Chunk, *, scale: Option
     elif workspace.dtype != torch.uint8 or not workspace.is_contiguous() or workspace.device != q.device:
         raise ValueError(f"workspace must be a contiguous uint8 tensor on {q.device}")
     _call(lib.eagle_chunk_attention, q.device, a, chunk.c, kv.c, workspace.data_ptr(), workspace.numel())
+    _written(out)
     return out
 
 
@@ -348,4 +352,5 @@ def apply_logit_rules(logits: torch.Tensor, rules: LogitRules, *, row_start: Opt
                     _list(path_mask, "path_mask", torch.int64, R, dev), masks[0], _list(allowed_row, "allowed_row", torch.int32, R, dev))
     if R > 0:
         _call(_library().eagle_apply_logit_rules, dev, l, rules.c)
+        _written(out)
     return out

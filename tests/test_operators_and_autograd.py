@@ -88,3 +88,42 @@ def test_context_setters():
         pkg.Eagle.set_attention(c, slopes=leaf(H))
     with pytest.raises(ValueError, match="frequency requires gradients"):
         pkg.Eagle.set_logit_rules(c, frequency=leaf(2))
+
+
+def test_what_a_call_writes_counts_as_written():
+    """And nothing else does."""
+    def versions(call, **named):
+        before = {n: t._version for n, t in named.items()}
+        call()
+        return {n for n, t in named.items() if t._version != before[n]}
+
+    q, k, v, q2, k2, kc, vc, x, y = f32(R, H, D), f32(R, KVH, D), f32(R, KVH, D), f32(R, H, D), f32(R, KVH, D), f32(9, KVH, 32, D), f32(9, KVH, 32, D), f32(R, V), f32(R, V)
+    plan, c, kv = pkg.rope_plan(D), chunk(), cache(kc, vc)
+    every = dict(q=q, k=k, v=v, q2=q2, k2=k2, kc=kc, vc=vc, x=x, y=y)
+    assert versions(lambda: pkg.rope(plan, q, k, v, chunk=c, kv=kv), **every) == {"q", "kc", "vc"}
+    assert versions(lambda: pkg.rope(plan, q, k, chunk=c, kv=kv, q_out=q2), **every) == {"q2", "kc"}
+    assert versions(lambda: pkg.rope(plan, None, k, v, chunk=c, kv=kv), **every) == {"kc", "vc"}
+    assert versions(lambda: pkg.rope(plan, q, k, chunk=c, q_out=q2, k_out=k2), **every) == {"q2", "k2"}
+    assert versions(lambda: pkg.rope(plan, None, k, chunk=c), **every) == {"k"}
+    assert versions(lambda: pkg.rope(plan, q, None, chunk=c), **every) == {"q"}
+    assert versions(lambda: attend(kv, q=q, out=q2), **every) == {"q2"}
+    assert versions(lambda: attend(kv, q=q, out=q), **every) == {"q"}
+    assert versions(lambda: rule(logits=x, out=y), **every) == {"y"}
+    assert versions(lambda: rule(logits=x), **every) == {"x"}
+
+
+def test_a_saved_tensor_that_a_call_overwrites_is_noticed():
+    w = leaf(R, V)
+    x = w * 2.0
+    loss = (x * x).sum()                                          # saves x
+    rule(logits=x.detach())
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+
+
+def test_tensors_of_inference_mode():
+    with torch.inference_mode():
+        x = f32(R, V)
+        rule(logits=x)
+        attend(q=f32(R, H, D))
+        turn(cache())
