@@ -303,7 +303,8 @@ typedef struct {
 int eagle_rope_plan_init(const eagle_rope_config *cfg, eagle_rope_plan *out);
 
 /* Rotates q [n_rows][n_heads][head_dim] into q_out and k [n_rows][n_kv_heads][head_dim] into the cache, together with v -- or, without a cache (kv null), k into
- * k_out.  Row and head strides in elements, elements of a head consecutive; outputs may be the inputs.  With a cache `chunk` is needed; v null leaves the
+ * k_out.  Row and head strides in elements, elements of a head consecutive; an output may be its input (the same strides), else outputs lie apart from
+ * all other tensors of the call.  With a cache `chunk` is needed; v null leaves the
  * cache's values alone.  positions (dev int32 [n_rows]) overrides the positions that `chunk` gives; without a chunk (null: n_rows is the field here) it
  * is needed.  q (with q_out) or k may be null.  Rows that no sequence owns, and those from a sequence's max_rows on, are left as they are, in the outputs too (without a chunk there are none), and
  * a token at or behind max_keys, or on a page that is not there, is not stored.
@@ -323,7 +324,8 @@ int eagle_rope(const eagle_rope_plan *plan, const eagle_rope_args *args, const e
  * distance = the row's position - token j's (a token in front of the chunk lies at its index).  Token j is visible to a row if j < key_len[s], its page is there, and
  *   - j comes before the row or is the row itself (tree: is in front of the tree, or the row's node or an ancestor), and distance < window if window > 0, or
  *   - j < prefix[s] (tree: at most the tokens in front of the tree): a prefix every row of the sequence sees, in front of the window and ahead of the row.
- * A row that sees nothing gets zeros.  q, out: EAGLE_F32 over a cache of either type, or EAGLE_BF16 over EAGLE_BF16; out is of q's type and may be q.
+ * A row that sees nothing gets zeros.  q, out: EAGLE_F32 over a cache of either type, or EAGLE_BF16 over EAGLE_BF16; out is of q's type and is q
+ * (the same strides) or lies apart from it.
  * head_dim: a multiple of 8, 8..128.  q's rows and the cache's tokens start on multiples of 16 bytes, out's of 8 elements.  NaN and infinities in a token stay with
  * the rows that see it: a key that is not finite may make NaN of a score; a value that is infinite makes its element of the row's result infinite or NaN, never finite.  Rows that no sequence owns are left as they are.
  * workspace (dev, 256-byte aligned): eagle_chunk_attention_workspace() bytes, for the same arguments; its contents need not be kept or cleared. */
@@ -357,7 +359,7 @@ typedef struct {
   const float *bias_value;
   int32_t n_bias;
 } eagle_logit_rules;
-/* in, out: [n_rows][vocab] of `dtype`, row strides in elements; out may be in.  Sequence s has the rows row_start[s] .. row_start[s+1]-1 (null: row r is
+/* in, out: [n_rows][vocab] of `dtype`, row strides in elements; out is in (the same stride) or lies apart from it.  Sequence s has the rows row_start[s] .. row_start[s+1]-1 (null: row r is
  * sequence r's, and n_rows = n_seqs); rows that no sequence owns are left as they are.  path_token (dev [n_rows]) and path_mask (dev uint64 [n_rows]), or both
  * null: bit u of a row's mask adds the token of its sequence's row u to its text (u < 64).  allowed: bit t % 32 of word t / 32 of row allowed_row[r] of
  * [n_masks][mask_stride] words (allowed_row null: row r); a row number outside 0..n_masks-1 (-1, say): no mask. */

@@ -39,6 +39,38 @@ static int check_kv(const eagle_paged_kv* k, PagedDev* d) {
 // Whether runs of 16 bytes (of an element of `elt` bytes) may be moved at every (row, head).
 static bool runs_ok(const void* p, int64_t row, int64_t head, int elt) { return aligned(p, 16) && row * elt % 16 == 0 && head * elt % 16 == 0; }
 
+// Rows of heads of consecutive elements: (row, head) begins at p + (row * row_stride + head * head_stride) * elt.
+struct Heads { const void* p; int64_t rows, row, heads, head; int dim, elt; };
+static bool same_place(const Heads& a, const Heads& b) { return a.p == b.p && (a.rows == 1 || a.row == b.row) && (a.heads == 1 || a.head == b.head); }
+// Whether a and b share an element, as far as that is easily seen: strides that differ say nothing (callers keep such tensors apart).  At most two divisions a head, where the ranges overlap.
+static bool share_elements(Heads a, Heads b) {
+  if (!a.p || !b.p) return false;
+  auto range = [](const Heads& x, int64_t* lo, int64_t* hi) {
+    const int64_t r = (x.rows - 1) * x.row, h = (x.heads - 1) * x.head;
+    *lo = (int64_t)(uintptr_t)x.p + (std::min<int64_t>(r, 0) + std::min<int64_t>(h, 0)) * x.elt;
+    *hi = (int64_t)(uintptr_t)x.p + (std::max<int64_t>(r, 0) + std::max<int64_t>(h, 0) + x.dim) * x.elt;
+  };
+  int64_t alo, ahi, blo, bhi;
+  range(a, &alo, &ahi);
+  range(b, &blo, &bhi);
+  if (ahi <= blo || bhi <= alo) return false;
+  if (a.heads == 1) a.head = b.head;
+  if (b.heads == 1) b.head = a.head;
+  if (a.rows == 1) a.row = b.rows == 1 ? 0 : b.row;
+  if (b.rows == 1) b.row = a.row;
+  if (a.row != b.row || a.head != b.head || a.elt != b.elt) return false;
+  // a's (i, h) and b's (i', h') lie (i' - i) * row + (h' - h) * head + (b - a) elements apart: closer than a head's length?
+  const int64_t apart = (int64_t)(uintptr_t)b.p - (int64_t)(uintptr_t)a.p, row = a.row * a.elt, len = (int64_t)a.dim * a.elt;
+  for (int64_t h = 1 - a.heads; h < b.heads; ++h) {
+    const int64_t d = apart + h * a.head * a.elt, near = row ? -d / row : 0;
+    for (int64_t i = near - 1; i <= near + 1; ++i)
+      if (std::abs(d + std::max(1 - a.rows, std::min(i, b.rows - 1)) * row) < len) return true;
+  }
+  return false;
+}
+// An output and what is read: the same tensor, or apart.
+static bool torn(const Heads& out, const Heads& in) { return !same_place(out, in) && share_elements(out, in); }
+
 // ---------------------------------------------------------------------------- rotary positions
 extern "C" int eagle_rope_plan_init(const eagle_rope_config* c, eagle_rope_plan* out) {
   if (!c || !out) return fail(EAGLE_EINVAL, "null argument");
@@ -127,6 +159,13 @@ extern "C" int eagle_rope(const eagle_rope_plan* plan, const eagle_rope_args* a,
   d.n_rows = a->n_rows; d.H = a->q ? a->n_heads : 0; d.KVH = a->k ? a->n_kv_heads : 0;
   const long long heads = (long long)d.H + d.KVH + (a->v ? d.KVH : 0);
   if (heads > 65535) return fail(EAGLE_EINVAL, "rope: too many heads");
+  {
+    const Heads q{a->q, a->n_rows, a->q_row, a->n_heads, a->q_head, plan->head_dim, elt}, k{a->k, a->n_rows, a->k_row, a->n_kv_heads, a->k_head, plan->head_dim, elt};
+    const Heads v{a->v, a->n_rows, a->v_row, a->n_kv_heads, a->v_head, plan->head_dim, elt}, q_out{a->q ? a->q_out : nullptr, a->n_rows, a->q_out_row, a->n_heads, a->q_out_head, plan->head_dim, elt};
+    const Heads k_out{a->k && !kv ? a->k_out : nullptr, a->n_rows, a->k_out_row, a->n_kv_heads, a->k_out_head, plan->head_dim, elt};
+    if (torn(q_out, q) || torn(k_out, k)) return fail(EAGLE_EINVAL, "rope: an output lies on part of its input: it must be the input or apart from it");
+    if (share_elements(q_out, k) || share_elements(q_out, v) || share_elements(k_out, q) || share_elements(q_out, k_out)) return fail(EAGLE_EINVAL, "rope: an output lies on another tensor of the call");
+  }
   d.n_heads_all = (int)heads;
   d.q = a->q; d.k = a->k; d.v = a->v; d.q_out = a->q_out; d.k_out = a->k_out;
   d.q_row = a->q_row; d.q_head = a->q_head; d.k_row = a->k_row; d.k_head = a->k_head; d.v_row = a->v_row; d.v_head = a->v_head;
@@ -166,6 +205,8 @@ static int check_attention(const eagle_attention_args* a, const eagle_chunk* chu
   d->chunk.max_keys = (int)std::min((long long)chunk->max_keys, (long long)kv->pages_per_seq * kv->page_tokens);
   if ((long long)d->chunk.max_rows * (a->n_heads / kv->n_kv_heads) > 1 << 30) return fail(EAGLE_EINVAL, "attention: too many rows a kv head");
   const int elt = elt_of(a->dtype), kelt = elt_of(kv->dtype);
+  if (chunk->n_rows > 0 && torn(Heads{a->out, chunk->n_rows, a->out_row, a->n_heads, a->out_head, kv->head_dim, elt}, Heads{a->q, chunk->n_rows, a->q_row, a->n_heads, a->q_head, kv->head_dim, elt}))
+    return fail(EAGLE_EINVAL, "attention: out lies on part of q: it must be q or apart from it");
   if (!runs_ok(a->q, a->q_row, a->q_head, elt)) return fail(EAGLE_EINVAL, "attention: q's rows and heads must start on multiples of 16 bytes");
   if (!aligned(a->out, 16) || a->out_row % 8 || a->out_head % 8) return fail(EAGLE_EINVAL, "attention: out's rows and heads must start on multiples of 16 bytes and 8 elements");
   if (kv->token_stride > 1 << 24) return fail(EAGLE_EINVAL, "attention: the cache's token_stride must be at most 2^24");
@@ -297,6 +338,8 @@ extern "C" int eagle_apply_logit_rules(const eagle_logits* l, const eagle_logit_
              l->row_start, l->path_token, l->allowed_row, rules->tokens, rules->n_tokens, rules->n_prompt, rules->bias_start, rules->n_bias > 0 ? rules->bias_token : nullptr,
              (const unsigned long long*)l->path_mask, l->allowed, rules->repetition, rules->presence, rules->frequency, rules->bias_value};
   const int elt = elt_of(l->dtype);
+  if (torn(Heads{l->out, l->n_rows, l->out_stride, 1, 0, l->vocab, elt}, Heads{l->in, l->n_rows, l->in_stride, 1, 0, l->vocab, elt}))
+    return fail(EAGLE_EINVAL, "logits: out lies on part of in: it must be in or apart from it");
   const bool runs = aligned(l->in, elt) && ((uintptr_t)l->in - (uintptr_t)l->out) % 16 == 0 && (l->in_stride - l->out_stride) * elt % 16 == 0;
   return l->dtype == EAGLE_F32 ? launch_rules<float>(d, runs, (hipStream_t)hip_stream) : launch_rules<bf16_t>(d, runs, (hipStream_t)hip_stream);
 }
