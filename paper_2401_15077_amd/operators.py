@@ -2,7 +2,7 @@
 rules that logits pass before a token is chosen (argument marshalling only; include/eagle.h has the definitions).
 
 Every call is enqueued on torch's current stream of the tensors' device and does not synchronise.  Outputs are not recorded by autograd: tensors that
-require gradients (inputs, caches, slopes, rules, outputs) are refused while gradients are enabled."""
+require gradients (inputs, outputs, slopes, and what a cache's or rules' handle was made from) are refused while gradients are enabled."""
 from __future__ import annotations
 
 import ctypes
@@ -79,7 +79,8 @@ def declare(lib) -> None:
     lib.eagle_apply_logit_rules.argtypes = [P(EagleLogits), P(EagleLogitRules), _vp]
 
 
-_written = torch.autograd.graph.increment_version                 # tells autograd that a tensor it may have saved is no longer what it was
+# tells autograd that tensors it may have saved are no longer what they were
+_written = getattr(torch._C, "_increment_version", None) or torch.autograd.graph.increment_version
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device      # (a tensor on the device: the runtime is up)
 _lib = None
@@ -117,7 +118,8 @@ def _list(t: Optional[torch.Tensor], name: str, dtype, n: Optional[int], device)
         return None
     if t.dtype != dtype or t.dim() != 1 or (n is not None and t.shape[0] != n) or t.device != device or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of {'any number of' if n is None else n} entries on {device}: got {t.dtype} {tuple(t.shape)} on {t.device}")
-    _plain(t, name)
+    if t.requires_grad:
+        _plain(t, name)
     return t.data_ptr()
 
 
@@ -134,7 +136,8 @@ def _heads(t: torch.Tensor, name: str, rows: Optional[int], heads: Optional[int]
     stride = t.stride()
     if stride[2] != 1 and dim > 1:
         raise ValueError(f"the elements of a head of {name} must be consecutive")
-    _plain(t, name)
+    if t.requires_grad:
+        _plain(t, name)
     return t.data_ptr(), stride[0], stride[1]
 
 
@@ -171,7 +174,7 @@ class PagedKV:
                 or (page_table.shape[0] > 1 and page_table.stride(0) < page_table.shape[1]):
             raise ValueError(f"page_table must be an int32 [n_seqs, pages] tensor on {k.device}, its rows consecutive and apart")
         self.device, self.dtype, self.n_seqs, self.n_kv_heads, self.head_dim = k.device, k.dtype, page_table.shape[0], k.shape[1], k.shape[3]
-        self._keep = (k, v, page_table)
+        self.both, self._table, self.grads = (k, v), page_table, k.requires_grad or v.requires_grad
         self.c = EaglePagedKV(k.data_ptr(), v.data_ptr(), _TYPES[k.dtype], k.shape[1], k.shape[3], k.shape[2], k.shape[0], page_table.shape[1], k.stride(0), k.stride(1), k.stride(2),
                               max(page_table.stride(0), page_table.shape[1]), page_table.data_ptr())
 
@@ -181,8 +184,9 @@ def _same_batch(chunk: Chunk, kv: PagedKV, device) -> None:
         raise ValueError(f"the chunk is on {chunk.device}, the cache on {kv.device}, the rows on {device}")
     if kv.n_seqs != chunk.n_seqs:
         raise ValueError(f"the page table has {kv.n_seqs} sequences, the chunk {chunk.n_seqs}")
-    _plain(kv._keep[0], "k of the cache")
-    _plain(kv._keep[1], "v of the cache")
+    if kv.grads:
+        _plain(kv.both[0], "k of the cache")
+        _plain(kv.both[1], "v of the cache")
 
 
 def rope_config(head_dim: int, *, theta: float = 10000.0, rot_dim: Optional[int] = None, interleaved: bool = False, scaling: str = "none", factor: float = 1.0, low: float = 1.0,
@@ -244,8 +248,10 @@ def rope(plan: EagleRopePlan, q: Optional[torch.Tensor], k: Optional[torch.Tenso
         return
     a = EagleRopeArgs(R, H, KVH, _TYPES[dtype], int(inverse), qa[0], ka[0], va[0], qo[0], ko[0], qa[1], qa[2], ka[1], ka[2], va[1], va[2], qo[1], qo[2], ko[1], ko[2], at)
     _call(_library().eagle_rope, device, plan, a, chunk.c if chunk is not None else None, kv.c if kv is not None else None)
-    k_to = () if k is None else (k_out if k_out is not None else k,) if kv is None else kv._keep[:2] if v is not None else kv._keep[:1]
-    _written(k_to if q is None else (q_out if q_out is not None else q, *k_to))
+    if q is not None:
+        _written((q if q_out is None else q_out,))
+    if k is not None:
+        _written((k if k_out is None else k_out,) if kv is None else kv.both if v is not None else (kv.both[0],))
 
 
 def _attention_args(q, kv, chunk, scale, softcap, slopes, window, prefix, out):
@@ -286,7 +292,7 @@ def chunk_attention(q: torch.Tensor, kv: PagedKV, chunk: Chunk, *, scale: Option
     elif workspace.dtype != torch.uint8 or not workspace.is_contiguous() or workspace.device != q.device:
         raise ValueError(f"workspace must be a contiguous uint8 tensor on {q.device}")
     _call(lib.eagle_chunk_attention, q.device, a, chunk.c, kv.c, workspace.data_ptr(), workspace.numel())
-    _written(out)
+    _written((out,))
     return out
 
 
@@ -313,7 +319,7 @@ class LogitRules:
         if bias is not None and b[1].shape != b[2].shape:
             raise ValueError("bias tokens and values must be equally many")
         self._keep = (tokens, n_tokens, n_prompt, repetition, presence, frequency, b)
-        self._values = [(t, name) for t, name in ((repetition, "repetition"), (presence, "presence"), (frequency, "frequency"), (b[2], "bias value")) if t is not None]
+        self.grads = [(t, name) for t, name in ((repetition, "repetition"), (presence, "presence"), (frequency, "frequency"), (b[2], "bias value")) if t is not None and t.requires_grad]
         self.longest = tokens.shape[1] if tokens is not None else 0
         f, i = torch.float32, torch.int32
         self.c = EagleLogitRules(self.n_seqs, tokens.data_ptr() if tokens is not None else None, tokens.stride(0) if tokens is not None else 0, self.longest,
@@ -329,8 +335,9 @@ def apply_logit_rules(logits: torch.Tensor, rules: LogitRules, *, row_start: Opt
     [rows]: tokens along a draft tree.  allowed: int32 [masks, words >= vocab / 32], a bit a token; allowed_row: int32 [rows], the row's mask (-1: none; None: row r's is mask r)."""
     if logits.dim() != 2 or logits.dtype not in _TYPES or (logits.stride(1) != 1 and logits.shape[1] > 1):
         raise ValueError("logits must be a float32 or bfloat16 [rows, vocab] tensor, its rows consecutive")
-    _plain(logits, "logits")
-    for t, name in rules._values:                                 # (they may have been made while gradients were off)
+    if logits.requires_grad:
+        _plain(logits, "logits")
+    for t, name in rules.grads:                                   # (where they were made while gradients were off)
         _plain(t, name)
     R, V = logits.shape
     dev = logits.device
@@ -340,7 +347,7 @@ def apply_logit_rules(logits: torch.Tensor, rules: LogitRules, *, row_start: Opt
         out = logits
     elif out.shape != logits.shape or out.dtype != logits.dtype or out.device != dev or (out.stride(1) != 1 and V > 1):
         raise ValueError(f"out must be {logits.dtype} {list(logits.shape)} on {dev}, its rows consecutive")
-    else:
+    elif out.requires_grad:
         _plain(out, "out")
     masks = (None, 0, 0)
     if allowed is not None:
@@ -352,5 +359,5 @@ def apply_logit_rules(logits: torch.Tensor, rules: LogitRules, *, row_start: Opt
                     _list(path_mask, "path_mask", torch.int64, R, dev), masks[0], _list(allowed_row, "allowed_row", torch.int32, R, dev))
     if R > 0:
         _call(_library().eagle_apply_logit_rules, dev, l, rules.c)
-        _written(out)
+        _written((out,))
     return out
