@@ -347,7 +347,7 @@ int eagle_chunk_attention(const eagle_attention_args *args, const eagle_chunk *c
  *   x = logit;  t anywhere in the text: x / repetition if x > 0, else x * repetition;  c > 0: x - presence - frequency * c;  x + bias[t];
  *   t not allowed: -inf
  * Every array may be null (no such rule).  Token ids outside the vocabulary count for nothing.  A token may stand in a bias list more than once: the last entry
- * counts.  A repetition that is not above 0 counts as 1.  A mask may leave a row empty: all of it is -inf. */
+ * counts.  A repetition that is not above 0 counts as 1, one below 2^-126 as 2^-126.  A mask may leave a row empty: all of it is -inf. */
 typedef struct {
   int32_t n_seqs;
   const int32_t *tokens;              /* dev, sequence s at s * token_stride; stride 0: one text for all */

@@ -47,7 +47,7 @@ __global__ __launch_bounds__(512) void k_logit_rules(const RulesDev A) {
   const int first = A.row_start ? A.row_start[seq] : seq, last = A.row_start ? A.row_start[seq + 1] : seq + 1;
   const int n = A.tokens ? max(0, min(A.n_tokens[seq], A.max_tokens)) : 0, prompt = A.n_prompt ? A.n_prompt[seq] : 0;
   float rep = A.repetition ? A.repetition[seq] : 1.f;
-  if (!(rep > 0.f)) rep = 1.f;
+  rep = rep > 0.f ? fmaxf(rep, 1.17549435e-38f) : 1.f;             // (a subnormal one's reciprocal may be infinite)
   const float pres = A.presence ? A.presence[seq] : 0.f, freq = A.frequency ? A.frequency[seq] : 0.f;
   const uint32_t* mask = nullptr;
   if (A.allowed) {
