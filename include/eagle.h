@@ -253,7 +253,8 @@ int eagle_probe_stream_read(const void *buf_dev, size_t bytes, int32_t iters, vo
  *     workspace must not run at the same time).
  *   - Arguments the host holds are checked: EAGLE_EINVAL, nothing launched.  What lies in device memory (lengths, page numbers, token ids) cannot
  *     be; the kernels bound every access instead, as said at each field.
- *   - Types are EAGLE_F32 and EAGLE_BF16; sums and statistics are kept in 32 bits. */
+ *   - Types are EAGLE_F32 and EAGLE_BF16; sums and statistics are kept in 32 bits.  Attention of EAGLE_BF16 queries rounds each softmax weight to bf16 (by 2^-8 of it at most) before it is
+ *     multiplied with its value, as the result is rounded; with EAGLE_F32 queries nothing is, and a product is off by 2^-22 of itself at most. */
 
 /* New tokens of a batch of sequences: sequence s has the rows row_start[s] .. row_start[s+1]-1 of the row tensors, and with them key_len[s] tokens in
  * the cache (row i of n is token key_len[s] - n + i).  A draft tree instead of consecutive tokens: tree_base[s] tokens are in front of the tree, node u lies

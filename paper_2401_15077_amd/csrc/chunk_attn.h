@@ -7,16 +7,21 @@
 //
 // fp32 operands are exact sums of three bf16 pieces (8 bits each of the 24), and of the nine products of two such sums the six of at least 2^-15 of the largest are kept: what is
 // left out is 2^-22 of a product at most.  The cache's first pieces are cut off and not rounded, since the largest numbers would round to infinity (and their other pieces to NaN).  bf16
-// operands are one piece.  Weights are one piece for bf16 queries (the output rounds by as much) and three for fp32.
+// operands are one piece.  Weights are three pieces for fp32 queries and one for bf16: that rounds a weight by at most 2^-8 of itself, as the output rounds (their sum takes them unrounded).  The
+// error against 64 bits is 0.0022 to 0.0023 of the result's norm, 0.0017 of which is the output's rounding alone; a second piece would be half as many products again.
 //
 // Two shapes.  WIDE (more than 32 columns a sequence and kv head): four waves of 32 columns share tiles of tokens in LDS.  Narrow: one block of 32 columns, the four waves take every
 // fourth tile and join at the end.  Where sequences, kv heads and column blocks do not fill the chip, the token range is split over work-groups and k_chunk_attn_join adds the parts up.
 //
 // What bounds it, and what it reaches (us a call, joining with it).  A batch of 64 tokens over 1k to 16k tokens each, 64 / 8 heads of 128, bf16: 406, the cache once at 5.6 TB/s (a bare read in
 // the same order reaches 6.0); tiles go to LDS without registers, a wave's next keys under way while it works on the values.  1536 and 509 rows behind a window of 4096 and a cap, 32 / 8 heads, bf16:
-// 194, 0.63 PFLOP/s of visible products: per tile 32 matrix instructions beside 460 vector ones (mask, cap, exponent, sums), which share a SIMD's two waves.  2011 fp32 rows, 32 heads of 80:
-// 169: 72 matrix and 500 vector instructions a tile (making the pieces: a third), and the last rows' blocks, which see 63 tiles, alone on their CU at the end.  Four trees of 26 nodes, fp32
-// over bf16, about 2000 tokens: 29, five tiles of 3.4 one after the other, 6 until the first tile is there, 6 for joining.  One token over 701, fp32: 19, all of it latency.
+// 191, 0.63 PFLOP/s of visible products: per tile 32 matrix instructions beside 460 vector ones (mask, cap, exponent, sums), which share a SIMD's two waves; the matrix unit is busy a quarter of the
+// time.  2011 fp32 rows, 32 heads of 80: 171: 72 matrix and 630 vector instructions a tile (making the pieces, also in waves that have nothing to multiply: a third), the matrix unit busy a third of the
+// time, and the last rows' blocks, which see 63 tiles, alone on their CU at the end.  Four trees of 26 nodes, fp32 over bf16, about 2000 tokens: 29, five tiles of 3.4 one after the other, 6 until the
+// first tile is there, 6 for joining.  One token over 701, fp32: 19, all of it latency.
+//
+// Registers: fp32 queries over a bf16 cache of 128 hold all 256 and spill (3 and, with cap or slopes, 17 of the wide shape, 7 and 6 of the narrow), which is a few of their loads a tile; no other shape
+// spills vector registers.
 //
 // A wave issues a vector instruction every 4.75 cycles and a matrix instruction takes the matrix unit 33, in whose shadow seven vector instructions fit if they stand between the matrix
 // instructions: the compiler does not put them there, so the order in which pieces and weights are made is written out, a step a product.
@@ -193,7 +198,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
   __shared__ __attribute__((aligned(16))) bf16_t k_lds0[P::K_ELTS], k_lds1[P::TWO ? P::K_ELTS : 8], v_lds0[P::V0_ELTS], v_lds1[P::TWO ? P::V_ELTS : 8];
   __shared__ int s_bad[2];                                        // WIDE, not DIRECT: number of the last tile in a buffer whose values are not all finite
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane & 31, hh = lane >> 5;
-  // The lane, worked out anew: inside the loop, what can be had from the thread's number in an instruction or two is not kept (the widest shapes hold 240 of 256 registers).
+  // The lane, worked out anew: inside the loop, what can be had from the thread's number in an instruction or two is not kept (the widest shapes hold all 256 registers).
   auto lane_now = []() -> int { int l = threadIdx.x; asm volatile("" : "+v"(l)); return l & 63; };
   const int kvh = blockIdx.x % A.kv.n_kv_heads, part = blockIdx.x / A.kv.n_kv_heads, s = blockIdx.y, g = A.H / A.kv.n_kv_heads, dh = A.kv.head_dim;
   // Blocks of the last rows see most and go first.  Where all work-groups are resident at once, two a CU, the second half ascends, so that a CU's two see as much as another's.

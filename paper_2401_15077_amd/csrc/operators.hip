@@ -220,11 +220,14 @@ static int check_attention(const eagle_attention_args* a, const eagle_chunk* chu
   return EAGLE_OK;
 }
 
-// WIDE beyond 32 columns (64 sequences of 1k to 16k tokens, 8 heads a kv head, bf16, with joining: 32 columns narrow 459, wide 486; 40 columns 516, 525; 64 columns 548, 532).
+// WIDE beyond 32 columns, where a narrow block would read the cache a second time (64 sequences of 1k to 16k tokens, 8 heads a kv head, with joining, narrow / wide.  bf16: 32 columns 451 / 464,
+// 40 486 / 485, 48 496 / 487, 64 511 / 489.  fp32 queries would stay narrow a little longer where there are as many sequences: 32 columns 533 / 624 over bf16, 1035 / 2109 over fp32; 64 columns
+// 705 / 805, 1679 / 2196.)
 // Where sequences, kv heads and column blocks make fewer work-groups than these, the tokens are split; a part has a few tiles at least (the narrow shape: whole rounds of its four waves),
 // and there are at most as many parts as k_chunk_attn_join has lanes.
-// Narrow, 64 sequences of 1k to 16k tokens, 64 / 8 heads, bf16, us with 1, 2, 3, 4, 6, 8 parts at most: 433 (2), 419 (3), 451 (4), 406 (6), 417 (8).  One token over 701 keys, 32 heads, fp32,
-// 22 tiles: parts of 4 tiles 17.6, of 5 23.0, of 3 29.4.  Wide: one a CU (four trees of 26 nodes on 8 kv heads, fp32 queries, 37 tiles: 8 parts 27, 10 parts 32 to 38; 2011 fp32 rows on 32 heads, 512 work-groups: whole
+// Narrow, 64 sequences of 1k to 16k tokens, 64 / 8 heads, us with 1 to 8 parts at most.  bf16: 434, 417, 414, 439, 407, 407, 408, 414; fp32 over bf16 with 1, 2, 4, 6, 8: 531, 578, 613, 489, 537; over
+// fp32 993, 1173, 1309, 986, 1124.  (Not in order: the sequences' own numbers of parts, hence the rounds of work-groups, change with the bound; six is the least of all three.)  Sixteen of those
+// sequences, bf16, with 1, 2, 4, 6, 8, 12, 16, 25: 215, 173, 172, 180, 171, 179, 177, 181; this bound makes it 25.  One token over 701 keys, 32 heads, fp32, 22 tiles: parts of 4 tiles 17.6, of 5 23.0, of 3 29.4.  Wide: one a CU (four trees of 26 nodes on 8 kv heads, fp32 queries, 37 tiles: 8 parts 27, 10 parts 32 to 38; 2011 fp32 rows on 32 heads, 512 work-groups: whole
 // 327, in two 339 and 26 more for joining).
 constexpr int ATTN_WIDE_WGS = 256, ATTN_NARROW_WGS = 3200, ATTN_MIN_TILES = 4, ATTN_MAX_PARTS = 64;
 
