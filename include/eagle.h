@@ -40,7 +40,7 @@ extern "C" {
 typedef struct eagle_ctx eagle_ctx;
 
 enum { EAGLE_OK = 0, EAGLE_EINVAL = -1, EAGLE_ENOMEM = -2, EAGLE_ESEQ_FULL = -3, EAGLE_ESTATE = -4, EAGLE_EHIP = -5 };
-enum { EAGLE_F32 = 0, EAGLE_BF16 = 1 };
+enum { EAGLE_F32 = 0, EAGLE_BF16 = 1, EAGLE_E4M3 = 2, EAGLE_INT8 = 3 };   /* the last two: codes of a cache (eagle_coded_kv) only */
 
 typedef struct {
   int32_t dtype;                      /* EAGLE_F32 | EAGLE_BF16: type of the weight matrices (and of the embedding) */
@@ -342,6 +342,33 @@ typedef struct {
 size_t eagle_chunk_attention_workspace(const eagle_attention_args *args, const eagle_chunk *chunk, const eagle_paged_kv *kv);
 int eagle_chunk_attention(const eagle_attention_args *args, const eagle_chunk *chunk, const eagle_paged_kv *kv, void *workspace_dev, size_t workspace_bytes,
                           void *hip_stream);
+
+/* Paged keys and values in 8 bits: codes, a byte each, at the places that eagle_paged_kv's fields say (strides in codes), and a scale (fp32) for every block of block_tokens tokens
+ * of a page's kv head: that of the block that holds token t of a page at page * scale_page + head * scale_head + t / block_tokens (strides in floats).  An element is code * scale.
+ * EAGLE_E4M3: a sign, four bits of exponent, three of mantissa, up to 448, NaN and no infinity; EAGLE_INT8: -127..127 (-128 is read as itself).  A scale's sign is not looked at. */
+typedef struct {
+  void *k, *v;
+  float *k_scale, *v_scale;
+  int32_t dtype, n_kv_heads, head_dim, page_tokens /* power of two */, block_tokens /* 16, 32, 64 or 128, at most page_tokens */, n_pages, pages_per_seq;
+  int64_t page_stride, head_stride, token_stride, table_stride, scale_page, scale_head;
+  const int32_t *page_table;          /* dev int32 [n_seqs][table_stride >= pages_per_seq] */
+} eagle_coded_kv;
+
+/* eagle_rope with the append to a cache of codes (chunk, kv and k are needed, k_out is null).  With M the largest code (448 or 127), for every block that new tokens go to, keys and values
+ * each for themselves, a = the largest absolute value of the new tokens' finite elements (keys as they are after the rotation):
+ *   - the block holds no other token of the sequence (one below key_len that this call does not write), or its scale is not positive and finite: scale = 2^e, e the least whole number in
+ *     -100..100 with a <= M 2^e; codes of other tokens become 0
+ *   - else scale = its scale times 2^n, n the least whole number >= 0 with a <= M scale 2^n, which stays within 2^100; codes of other tokens are rounded again where n > 0
+ *   - code = element / scale, to nearest, ties to even, within -M..M (an infinity is M); NaN stays NaN in EAGLE_E4M3 and becomes 0 in EAGLE_INT8
+ * with everything from the position to the code worked out in 64 bits.  Codes at or behind key_len, of pages that are not there and of blocks without new tokens stay as they are.
+ * Two sequences of one call must not append to the same block. */
+int eagle_rope_coded(const eagle_rope_plan *plan, const eagle_rope_args *args, const eagle_chunk *chunk, const eagle_coded_kv *kv, void *hip_stream);
+
+/* eagle_chunk_attention over a cache of codes: k_j and v_j are code * scale, q and out EAGLE_F32 or EAGLE_BF16; codes and their products with the queries are exact as those of a bf16 cache are.
+ * head_dim: a multiple of 16, 16..128; the cache's tokens start on multiples of 16 bytes.  What a scale that is not finite makes of scores and results stays with the rows that see a
+ * token of its block: a value scale makes all of their result NaN, a key scale their scores infinite or NaN. */
+size_t eagle_chunk_attention_coded_workspace(const eagle_attention_args *args, const eagle_chunk *chunk, const eagle_coded_kv *kv);
+int eagle_chunk_attention_coded(const eagle_attention_args *args, const eagle_chunk *chunk, const eagle_coded_kv *kv, void *workspace_dev, size_t workspace_bytes, void *hip_stream);
 
 /* What logits pass before a token is chosen.  The text of row r is its sequence's tokens and, along a draft tree, the tokens of the nodes on its path; with
  * c = how often token t occurs in it behind the sequence's first n_prompt tokens:

@@ -152,3 +152,59 @@ def logit_rules(x, row_start, *, tokens=None, n_tokens=None, n_prompt=None, repe
                     if not int(allowed[m][t // 32]) >> (t % 32) & 1:
                         y[r, t] = -math.inf
     return y, size
+
+
+def code_value(codes, e4m3):
+    """Numbers that uint8 codes stand for."""
+    c = np.asarray(codes, dtype=np.uint8).astype(np.int64)
+    if not e4m3:
+        return np.where(c >= 128, c - 256, c).astype(np.float64)
+    e, m = c >> 3 & 15, c & 7
+    x = np.where(e == 0, m * 2.0 ** -9, (8 + m) * 2.0 ** (e.astype(np.float64) - 10))
+    x = np.where(c & 127 == 127, np.nan, x)
+    return np.where(c & 128, -x, x)
+
+
+def nearest_code(x, e4m3):
+    """Numbers that the codes of the numbers x stand for: to nearest, ties to even, within the largest; NaN stays NaN (e4m3) or is 0."""
+    x = np.asarray(x, dtype=np.float64)
+    if not e4m3:
+        return np.rint(np.clip(np.where(np.isnan(x), 0.0, x), -127.0, 127.0))
+    y = np.clip(x, -448.0, 448.0)
+    step = 2.0 ** (np.maximum(np.frexp(np.where(np.isnan(y), 1.0, y))[1] - 1, -6) - 3.0)
+    return np.rint(y / step) * step
+
+
+def append_codes(x, values, scale, facts, table, key_len, *, page, block, e4m3, max_rows, max_keys, row_start):
+    """x [rows, heads, dim] into a cache of codes: values [pages, heads, page, dim] (what the codes stand for), scale [pages, heads, blocks] -> both anew, and the elements x / scale of what was
+    written, NaN elsewhere."""
+    x = np.asarray(x, dtype=np.float64)
+    values, scale = values.copy(), scale.astype(np.float64)
+    exact = np.full(values.shape, np.nan)
+    M = 448.0 if e4m3 else 127.0
+    blocks = {}
+    for r, s, t, _, _ in facts:
+        if r - int(row_start[s]) < max_rows and 0 <= t < max_keys and t // page < len(table[s]) and 0 <= table[s][t // page] < len(values):
+            blocks.setdefault((s, t // block), []).append((r, t))
+    for (s, b), new in blocks.items():
+        pg, first = int(table[s][b * block // page]), b * block
+        cell, at = first % page, first % page // block
+        written = {t for _, t in new}
+        stay = [t for t in range(first, min(first + block, int(key_len[s]))) if t not in written]
+        for h in range(x.shape[1]):
+            el = np.concatenate([np.abs(x[r, h]) for r, _ in new])
+            a = el[np.isfinite(el)].max(initial=0.0)
+            old = scale[pg, h, at]
+            keep = bool(stay) and old > 0 and np.isfinite(old)
+            u = old if keep else 2.0 ** -100
+            limit = max(old, 2.0 ** 100) if keep else 2.0 ** 100
+            while a > M * u and 2 * u <= limit:
+                u *= 2
+            for t in stay:
+                c = values[pg, h, t % page]
+                values[pg, h, t % page] = 0.0 if not keep else c if u == old else nearest_code(c * (old / u), e4m3)
+            scale[pg, h, at] = u
+            for r, t in new:
+                values[pg, h, t % page] = nearest_code(x[r, h] / u, e4m3)
+                exact[pg, h, t % page] = x[r, h] / u
+    return values, scale, exact

@@ -28,6 +28,7 @@
 #pragma once
 #include "rows.h"
 #include "rope.h"
+#include "codes.h"
 #include <type_traits>
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -44,7 +45,13 @@ struct ChunkAttnDev {
   int turn;                                // column blocks in descending order before the others ascend
   int lane_pages;                          // pages of fewer than 8 tokens: every lane looks its own up
   float* part_o; float* part_ml;           // [row][head][split][DH], [row][head][split][maximum, sum]
+  const float *k_scale, *v_scale;          // a cache of codes: scale of block b of a page's kv head at page * scale_page + head * scale_head + b
+  long long scale_page, scale_head;
+  int block_shift;
 };
+// Types of a cache of 8-bit codes.
+struct e4m3_t { uint8_t bits; };
+struct int8_code_t { int8_t bits; };
 
 // What a column block of a sequence has to visit: tiles [0, n_prefix) and from first on, n_tiles in all; and what its rows have in common.
 struct ColumnRange {
@@ -139,6 +146,27 @@ template <> struct Raw8<float> {
   }
 };
 
+// Eight codes as bf16 numbers: exact (at most four or seven significant bits).
+__device__ __forceinline__ bf16x8 coded8(u32x2 u, e4m3_t) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  u32x4 h;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    h[2 * i] = __builtin_bit_cast(uint32_t, (bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u[i], 1.f, false));
+    h[2 * i + 1] = __builtin_bit_cast(uint32_t, (bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u[i], 1.f, true));
+  }
+  return __builtin_bit_cast(bf16x8, h);
+}
+__device__ __forceinline__ bf16x8 coded8(u32x2 u, int8_code_t) {
+  u32x4 h;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t w = u[i >> 1] >> (i & 1 ? 16 : 0);
+    h[i] = upper_pair((float)(int)(int8_t)w, (float)(int)(int8_t)(w >> 8));
+  }
+  return __builtin_bit_cast(bf16x8, h);
+}
+
 // Where 16 bytes (8 elements, piece c) of token t lie in a tile in LDS, in units of 8 elements.  Keys are read a token a lane: eight consecutive tokens' pieces lie in eight different
 // 16-byte columns.  Values are read transposed, four tokens by 64 bytes at a time: those lie in four different 64-byte columns.  (Rows of 96 elements, 3/4 of the banks, put four tokens into
 // four different 64-byte columns by themselves.)
@@ -149,13 +177,16 @@ __device__ __forceinline__ s16x4 read_transposed(const bf16_t* p) {   // lane l 
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p);
 }
 
+// Tokens of a tile, by shape, whether queries are fp32, and bytes of an element of the cache.
+constexpr int tile_tokens(bool wide, bool fp32, int bytes) { return wide && (bytes == 2 || (bytes == 1 && !fp32)) ? 64 : 32; }
+
 template <typename T, typename CT, int DH_, bool WIDE_, bool MODS_>
 struct ChunkAttn {
   static constexpr int DH = DH_, NQ = sizeof(T) == 4 ? 3 : 1, NK = sizeof(CT) == 4 ? 3 : 1, NP = NQ > NK ? NQ : NK;
-  static constexpr bool WIDE = WIDE_, MODS = MODS_;
+  static constexpr bool WIDE = WIDE_, MODS = MODS_, CODED = sizeof(CT) == 1;
   // bf16 caches go from memory to LDS without passing through registers (DIRECT); fp32 ones are split into their pieces on the way.  The narrow shape has fp32 keys in registers.
-  static constexpr bool DIRECT = NK == 1, KEYS_IN_LDS = WIDE || DIRECT;
-  static constexpr int KT = WIDE && NK == 1 ? 64 : 32, KB = KT / 32, KSN = DH / 16, DB = DH / 32;
+  static constexpr bool DIRECT = sizeof(CT) == 2, KEYS_IN_LDS = WIDE || NK == 1;
+  static constexpr int KT = tile_tokens(WIDE, NQ == 3, sizeof(CT)), KB = KT / 32, KSN = DH / 16, DB = DH / 32;
   static constexpr int COLS = WIDE ? 128 : 32;
   static constexpr int ROW = DIRECT && DH == 96 ? 128 : DH;       // elements of a token in LDS (a DIRECT load fills 1 KiB: whole tokens)
   static constexpr int PART = DH <= 64 ? 64 : 128;                // and in the workspace
@@ -173,8 +204,9 @@ struct ChunkAttn {
   static constexpr int column_piece(int n) { return NQ == 1 ? 0 : NK == 1 ? 2 - n : n == 0 ? 0 : n < 3 ? 2 - n : 5 - n; }
   static constexpr bool done_with(int n) { return NK == 3 ? n == 0 || n == 2 || n == 5 : n == PRODUCTS - 1; }   // the cache piece of product n
   static constexpr int WAVES = NK == 3 && (DH == 128 || (DH == 96 && !WIDE)) ? 1 : 2;      // a SIMD holds (by registers)
-  static constexpr bool SPLIT = WIDE && !DIRECT;                  // fp32 keys and values go through LDS in pieces
-  static constexpr int ITEMS = SPLIT ? KT * DH / 4 / 256 : KT * DH / 8 / 64;   // runs of 4 (SPLIT) or 8 elements a thread fetches of the values, and of the keys if they go through LDS
+  static constexpr bool SPLIT = WIDE && NK == 3;                   // fp32 keys and values go through LDS in pieces
+  static constexpr int RUNS = DH == 64 ? 4 : 8, THREADS = WIDE ? 256 : 64;   // CODED: runs of 16 codes of a token, threads that fetch a tile
+  static constexpr int ITEMS = SPLIT ? KT * DH / 4 / 256 : CODED ? (KT * RUNS + THREADS - 1) / THREADS : KT * DH / 8 / 64;   // runs of 4 (SPLIT) or 8 elements a thread fetches of the values, and of the keys if they go through LDS
 };
 
 typedef __attribute__((address_space(3))) bf16_t* lds_ptr;
@@ -193,7 +225,7 @@ __device__ __forceinline__ void wait_lds() {
 template <typename P, typename T, typename CT>
 __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev A) {
   constexpr int DH = P::DH, ROW = P::ROW, NQ = P::NQ, NK = P::NK, KT = P::KT, KB = P::KB, KSN = P::KSN, DB = P::DB, COLS = P::COLS, TILE = P::TILE, ITEMS = P::ITEMS;
-  constexpr bool WIDE = P::WIDE, MODS = P::MODS, DIRECT = P::DIRECT;
+  constexpr bool WIDE = P::WIDE, MODS = P::MODS, DIRECT = P::DIRECT, CODED = P::CODED;
   // (arrays of their own: the compiler tells reads of one from loads on their way into another)
   __shared__ __attribute__((aligned(16))) bf16_t k_lds0[P::K_ELTS], k_lds1[P::TWO ? P::K_ELTS : 8], v_lds0[P::V0_ELTS], v_lds1[P::TWO ? P::V_ELTS : 8];
   __shared__ int s_bad[2];                                        // WIDE, not DIRECT: number of the last tile in a buffer whose values are not all finite
@@ -306,10 +338,27 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
 
   // ---- not DIRECT: through registers
   f32x4 k4[P::SPLIT ? ITEMS : 1], v4[P::SPLIT ? ITEMS : 1];
-  Raw8<CT> kr[DIRECT || WIDE ? 1 : KSN], vr[DIRECT || WIDE ? 1 : ITEMS];
+  typedef Raw8<std::conditional_t<CODED, bf16_t, CT>> Raw;
+  Raw kr[DIRECT || CODED || WIDE ? 1 : KSN], vr[DIRECT || CODED || WIDE ? 1 : ITEMS];
+  u32x4 k16[CODED ? ITEMS : 1], v16[CODED ? ITEMS : 1];
+  float2 sc_fetched = {1.f, 1.f}, sc_next = {1.f, 1.f};           // CODED: scales of the keys and values of the lane's token of the fetched tile, of the one in LDS
   auto fetch = [&](int it, int pages) {
     const int k0 = tile_token(it);
-    if constexpr (P::SPLIT) {                                     // a token is eight threads': every eighth run of 4 elements
+    if constexpr (CODED) {
+      const int mine = WIDE ? tid : lane_now();
+#pragma unroll
+      for (int i = 0; i < ITEMS; ++i) {
+        const int item = i * P::THREADS + mine, t = item / P::RUNS, c = item % P::RUNS, page = __shfl(pages, t & (KT - 1), 64);
+        const long long at = page * A.kv.page_stride + ((k0 + t) & in_page) * A.kv.token_stride + c * 16;
+        k16[i] = v16[i] = u32x4{0, 0, 0, 0};
+        if (t < KT && page >= 0 && c * 16 < dh) { k16[i] = *(const u32x4*)(kb + at); v16[i] = *(const u32x4*)(vb + at); }
+      }
+      sc_fetched = float2{1.f, 1.f};
+      if (pages >= 0) {
+        const long long at = pages * A.scale_page + kvh * A.scale_head + (((k0 + (mine & (KT - 1))) & in_page) >> A.block_shift);
+        sc_fetched = float2{fabsf(A.k_scale[at]), fabsf(A.v_scale[at])};
+      }
+    } else if constexpr (P::SPLIT) {                              // a token is eight threads': every eighth run of 4 elements
       const int l = lane_now(), t = 8 * w + (l >> 3), c = l & 7, page = __shfl(pages, t, 64);
       const long long at = page * A.kv.page_stride + ((k0 + t) & in_page) * A.kv.token_stride + 4 * c;
 #pragma unroll
@@ -319,7 +368,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
         k4[i] = k;
         v4[i] = v;
       }
-    } else {
+    } else if constexpr (!WIDE) {
 #pragma unroll
       for (int i = 0; i < ITEMS; ++i) {
         const int item = i * 64 + lane, t = item / (DH / 8), c = item % (DH / 8);
@@ -329,7 +378,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
         if (page >= 0 && c * 8 < dh) vr[i].load(vb + at);
       }
     }
-    if constexpr (!WIDE) {
+    if constexpr (!WIDE && !CODED) {
       const int page = pages;                                     // (KT = 32: the lane's own token)
       const long long at = page * A.kv.page_stride + ((k0 + q) & in_page) * A.kv.token_stride;
 #pragma unroll
@@ -367,6 +416,18 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
       u32x2 pk[3];
 #pragma unroll
       for (int n = 0; n < 12 * ITEMS; ++n) bad |= put_step(kd, vd, n, pk);
+    } else if constexpr (CODED) {
+      const int mine = WIDE ? tid : lane_now();
+#pragma unroll
+      for (int i = 0; i < ITEMS; ++i) {
+        const int item = i * P::THREADS + mine, t = item / P::RUNS, c = item % P::RUNS;
+        if (t >= KT || c * 16 >= DH) continue;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          *(bf16x8*)(kd + 8 * k_place<ROW>(t, 2 * c + h)) = coded8(u32x2{k16[i][2 * h], k16[i][2 * h + 1]}, CT());
+          *(bf16x8*)(vd + 8 * v_place<ROW>(t, 2 * c + h)) = coded8(u32x2{v16[i][2 * h], v16[i][2 * h + 1]}, CT());
+        }
+      }
     } else {
 #pragma unroll
       for (int i = 0; i < ITEMS; ++i) {
@@ -381,12 +442,13 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
     return bad;
   };
 
+  constexpr bool AHEAD2 = P::SPLIT || (CODED && WIDE);           // through registers into the other of two buffers: fetched two tiles ahead
   int it = t_begin + (WIDE ? 0 : w);
-  int pages = -1, entry_next = 0, pages1 = -1;                    // (SPLIT: pages1 are the next tile's, entry_next is the one's behind it)
+  int pages = -1, entry_next = 0, pages1 = -1;                    // (AHEAD2: pages1 are the next tile's, entry_next is the one's behind it)
   if (it < t_end) {
     pages = page_of(it, entry_of(it));
     entry_next = entry_of(it + STEP);
-    if constexpr (P::SPLIT) {
+    if constexpr (AHEAD2) {
       if (it + 1 < t_end) pages1 = page_of(it + 1, entry_next);
       entry_next = entry_of(it + 2);
     }
@@ -423,6 +485,12 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
     __syncthreads();
     fetch(it + 1, pages1);
   }
+  if constexpr (CODED && WIDE) {
+    put(k_lds0, v_lds0);
+    sc_next = sc_fetched;
+    __syncthreads();
+    fetch(it + 1, pages1);
+  }
 
   auto uniform = [](float x) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x))); };
   const float c2 = uniform(A.scale * 1.44269504088896341f);       // scores to powers of two
@@ -454,7 +522,8 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
     const uint64_t there = __ballot(pages >= 0) & low_ones(KT);
     const bool full = k0 + KT <= R.full_to && (k0 >= R.full_from || k0 + KT <= R.prefix) && there == low_ones(KT);
     bool bad = false;
-    const int pages_next = P::SPLIT ? pages1 : page_of(it + STEP, entry_next);
+    const int pages_next = AHEAD2 ? pages1 : page_of(it + STEP, entry_next);
+    float2 sc = sc_next;                                          // CODED: scales of the lane's token of this tile
     if constexpr (STAGGERED) {
       wait_loads<INSTS>();                   // the keys have landed (the values are behind them)
     } else if constexpr (DIRECT) {
@@ -462,6 +531,11 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
       wait_loads<0>();
       if constexpr (WIDE) { __builtin_amdgcn_s_barrier(); asm volatile("" ::: "memory"); }
       if (it + STEP < t_end) dma((lds_ptr)kn, (lds_ptr)vn, it + STEP, pages_next, BOTH());
+    } else if constexpr (CODED) {
+      if constexpr (!WIDE) sc = sc_fetched;
+      put(WIDE ? kn : kt, WIDE ? vn : vt);
+      if constexpr (WIDE) sc_next = sc_fetched;
+      else if (it + STEP < t_end) fetch(it + STEP, pages_next);
     } else if constexpr (WIDE) {
       bad = s_bad[which] == it;
     } else {
@@ -515,7 +589,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
         }
       }
     }
-    if constexpr (!WIDE && !DIRECT) {
+    if constexpr (!WIDE && !DIRECT && !CODED) {
       if (it + STEP < t_end) fetch(it + STEP, pages_next);        // (the keys' registers are free now)
     }
     if constexpr (STAGGERED && !LAST) {
@@ -523,14 +597,34 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
       dma((lds_ptr)kt, (lds_ptr)vt, it + STEP, pages_next, KEYS());
     }
     pages = pages_next;
-    if constexpr (P::SPLIT) {
-      if (__any(next_bad != 0) && lane_now() == 0) s_bad[which ^ 1] = it + 1;
+    if constexpr (AHEAD2) {
+      if (P::SPLIT && __any(next_bad != 0) && lane_now() == 0) s_bad[which ^ 1] = it + 1;
       pages1 = it + 2 < t_end ? page_of(it + 2, entry_next) : -1;
       fetch(it + 2, pages1);
       entry_next = entry_of(it + 3);
     } else if constexpr (!STAGGERED) entry_next = entry_of(it + 2 * STEP);
     const int lane = lane_now(), hh = lane >> 5;
     uint64_t vis = ~0ull;                                         // tokens of the tile that the column sees
+    // CODED: a block is at least 16 tokens and begins at a multiple of 16, so each 16 tokens of a tile have one scale: the first one's.  k_by: to powers of two (MODS: of the score as it is).
+    constexpr int GROUPS16 = CODED ? KT / 16 : 1;
+    float k_by[GROUPS16], v_by[GROUPS16];
+    if constexpr (CODED) {
+      const float x = MODS ? sc.x : sc.x * c2;
+#pragma unroll
+      for (int i = 0; i < GROUPS16; ++i) {
+        k_by[i] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 16 * i));
+        v_by[i] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, sc.y), 16 * i));
+      }
+      // a score of -inf must not meet a scale that is 0 or not finite: such a tile takes its scales before the mask
+      if (!idle && (MODS || __any(!(x > 0.f && x < INFINITY)))) {
+#pragma unroll
+        for (int a = 0; a < KB; ++a)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) sacc[a][r] *= k_by[2 * a + (r >> 3)];
+#pragma unroll
+        for (int i = 0; i < GROUPS16; ++i) k_by[i] = 1.f;
+      }
+    }
     if (!idle) {
     // cap and slopes
     if constexpr (MODS) {
@@ -628,12 +722,25 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
         for (int r = 0; r < 16; ++r) sacc[a][r] = (uint32_t)(mine >> (32 * a)) >> (8 * (r >> 2) + (r & 3)) & 1u ? sacc[a][r] : -INFINITY;
     }
     float top = sacc[0][0];
+    if constexpr (CODED && !MODS) {
+      top = -INFINITY;
 #pragma unroll
-    for (int a = 0; a < KB; ++a)
+      for (int a = 0; a < KB; ++a)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) top = fmaxf(top, sacc[a][r]);
+        for (int h = 0; h < 2; ++h) {
+          float x = sacc[a][8 * h];
+#pragma unroll
+          for (int r = 1; r < 8; ++r) x = fmaxf(x, sacc[a][8 * h + r]);
+          top = fmaxf(top, x * k_by[2 * a + h]);
+        }
+    } else {
+#pragma unroll
+      for (int a = 0; a < KB; ++a)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, sacc[a][r]);
+    }
     top = fmaxf(top, __shfl_xor(top, 32, 64));
-    if constexpr (!MODS) top *= c2;
+    if constexpr (!MODS && !CODED) top *= c2;
     // The maximum moves only when it grows by more than 8 (weights up to 2^8 lose nothing in fp32 or bf16), and lane by lane, so that a column's bits are its own.
     const bool moved = top > m_run + 8.f || (m_run == -INFINITY && top > -INFINITY);
     if (__any(moved)) {
@@ -647,7 +754,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
     }
     }
     if constexpr (STAGGERED) wait_loads<LAST ? 0 : INSTS>();   // the values have landed
-    if (DIRECT && !full) {                                        // is there anything that is not finite among the values?
+    if (NK == 1 && !full) {                                       // is there anything that is not finite among the values?
       uint32_t any = 0;
 #pragma unroll 4
       for (int i = 0; i < TILE / 512; ++i) any |= exponents(*(const u32x4*)(vt + i * 512 + lane * 8));
@@ -691,6 +798,20 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
       }
       if constexpr (WIDE) __syncthreads();
     }
+    if constexpr (CODED) {                                        // a block of values whose scale is not finite: nothing finite for the columns that see one of them
+      if (__any(not_finite(sc.y)) && !idle) {
+#pragma unroll
+        for (int i = 0; i < GROUPS16; ++i) {
+          const bool odd = not_finite(v_by[i]);
+          const float add = odd && (vis & there) >> (16 * i) & 0xFFFFu ? NAN : 0.f;
+#pragma unroll
+          for (int b = 0; b < DB; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) oacc[b][r] += add;
+          if (odd) v_by[i] = 0.f;
+        }
+      }
+    }
     if (!idle) {
     const float m_sub = m_run == -INFINITY ? 0.f : m_run;
     // 16 tokens at a time: their values are read a block ahead, and the weights of the next 16 are made between the products, in this order.
@@ -703,10 +824,12 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
       const int pair = NQ == 3 ? n / 3 : n, j = NQ == 3 ? n % 3 : 0, a = jj >> 1, r = 8 * (jj & 1) + 2 * pair;
       float x = sacc[a][r], y = sacc[a][r + 1];
       if (j == 0) {
-        x = __builtin_amdgcn_exp2f(MODS ? x - m_sub : fmaf(x, c2, -m_sub));
-        y = __builtin_amdgcn_exp2f(MODS ? y - m_sub : fmaf(y, c2, -m_sub));
+        const float by = CODED ? k_by[CODED ? jj : 0] : c2;
+        x = __builtin_amdgcn_exp2f(MODS ? x - m_sub : fmaf(x, by, -m_sub));
+        y = __builtin_amdgcn_exp2f(MODS ? y - m_sub : fmaf(y, by, -m_sub));
         sum += x;
         sum += y;
+        if constexpr (CODED) { x *= v_by[jj]; y *= v_by[jj]; }
       }
       const uint32_t h = bf16_pair(x, y);
       pf[jj & 1][j][pair] = h;
@@ -747,7 +870,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
       wait_lds();                                                 // the values have been read
       dma((lds_ptr)kt, (lds_ptr)vt, it + STEP, pages, VALUES());
     }
-    if constexpr (P::SPLIT) __syncthreads();
+    if constexpr (AHEAD2) __syncthreads();
     it += STEP;
   };
   if constexpr (P::TWO) {

@@ -69,12 +69,11 @@ template <int VE> __device__ inline void store_run(bf16_t* p, const float* x) {
 // Bound by HBM, and by latency for a few rows: 8191 rows of 64 + 8 + 8 heads of 128 in bf16 take 63 us, 5.3 TB/s read and written (four rows a work-group 78: fewer, longer chains of loads;
 // elements instead of runs 190); 2011 fp32 rows of 64 + 8 heads in a loop over the same tensors 25; 104 rows of 32 + 8 + 8 heads 5.6 (four a work-group 8.1).
 template <typename T, typename CT, int VE>
-__global__ __launch_bounds__(256) void k_rope(const RopeDev A) {
+__device__ __forceinline__ void rope_row(const RopeDev& A, int r, int part) {
   __shared__ float2 cs[128];
   __shared__ int s_pos;
   __shared__ long long s_cell;                                    // the row's place in the cache: element offset of kv head 0, -1 none, -2: not a row of any sequence
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  const int r = blockIdx.x;
   if (wave == 0) {
     int pos = A.positions ? A.positions[r] : 0;
     long long cell = -1;
@@ -108,7 +107,7 @@ __global__ __launch_bounds__(256) void k_rope(const RopeDev A) {
   }
   __syncthreads();
   const int rot_units = half / VE, units = rot_units + (A.head_dim - A.rot_dim + 2 * VE - 1) / (2 * VE);   // (VE > 1: half is a multiple of VE)
-  const int h0 = blockIdx.y * A.heads_per_wg, nh = min(A.heads_per_wg, A.n_heads_all - h0);
+  const int h0 = part * A.heads_per_wg, nh = min(A.heads_per_wg, A.n_heads_all - h0);
   for (int i = tid; i < nh * units; i += 256) {
     const int h = h0 + i / units, u = i % units;
     const bool is_q = h < A.H, is_k = !is_q && h < A.H + A.KVH;
@@ -154,3 +153,5 @@ __global__ __launch_bounds__(256) void k_rope(const RopeDev A) {
     }
   }
 }
+template <typename T, typename CT, int VE>
+__global__ __launch_bounds__(256) void k_rope(const RopeDev A) { rope_row<T, CT, VE>(A, blockIdx.x, blockIdx.y); }

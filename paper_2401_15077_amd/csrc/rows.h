@@ -33,7 +33,7 @@ __device__ inline int chunk_keys(const ChunkDev& c, const PagedDev& kv, int s) {
 }
 
 // Page of token t (0 <= t < chunk_keys) of sequence s, -1 where it is not there.
-__device__ inline int token_page(const PagedDev& kv, int s, int t) {
+template <typename Cache> __device__ inline int token_page(const Cache& kv, int s, int t) {
   const int p = kv.page_table[(size_t)s * kv.table_stride + (t >> kv.page_shift)];
   return (unsigned)p < (unsigned)kv.n_pages ? p : -1;
 }

@@ -6,14 +6,15 @@ require gradients (inputs, outputs, slopes, and what a cache's or rules' handle 
 from __future__ import annotations
 
 import ctypes
-from typing import Optional, Tuple
+from typing import Optional, Tuple, Union
 
 import torch
 
-from . import EAGLE_BF16, EAGLE_F32, EagleError, load_library
+from . import EAGLE_BF16, EAGLE_E4M3, EAGLE_F32, EAGLE_INT8, EagleError, load_library
 
 _i32, _i64, _vp, _f32, _f64 = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p, ctypes.c_float, ctypes.c_double
 _TYPES = {torch.float32: EAGLE_F32, torch.bfloat16: EAGLE_BF16}
+_CODES = {torch.float8_e4m3fn: EAGLE_E4M3, torch.int8: EAGLE_INT8}
 ROPE_SCALINGS = ("none", "linear", "base", "bands", "ramp")
 
 
@@ -24,6 +25,12 @@ class EagleChunk(ctypes.Structure):
 class EaglePagedKV(ctypes.Structure):
     _fields_ = [("k", _vp), ("v", _vp), ("dtype", _i32), ("n_kv_heads", _i32), ("head_dim", _i32), ("page_tokens", _i32), ("n_pages", _i32), ("pages_per_seq", _i32),
                 ("page_stride", _i64), ("head_stride", _i64), ("token_stride", _i64), ("table_stride", _i64), ("page_table", _vp)]
+
+
+class EagleCodedKV(ctypes.Structure):
+    _fields_ = [("k", _vp), ("v", _vp), ("k_scale", _vp), ("v_scale", _vp), ("dtype", _i32), ("n_kv_heads", _i32), ("head_dim", _i32), ("page_tokens", _i32), ("block_tokens", _i32),
+                ("n_pages", _i32), ("pages_per_seq", _i32), ("page_stride", _i64), ("head_stride", _i64), ("token_stride", _i64), ("table_stride", _i64), ("scale_page", _i64),
+                ("scale_head", _i64), ("page_table", _vp)]
 
 
 class EagleRopeConfig(ctypes.Structure):
@@ -73,6 +80,10 @@ def declare(lib) -> None:
     lib.eagle_chunk_attention_workspace.argtypes = [P(EagleAttentionArgs), P(EagleChunk), P(EaglePagedKV)]
     lib.eagle_chunk_attention_workspace.restype = ctypes.c_size_t
     lib.eagle_chunk_attention.argtypes = [P(EagleAttentionArgs), P(EagleChunk), P(EaglePagedKV), _vp, ctypes.c_size_t, _vp]
+    lib.eagle_rope_coded.argtypes = [P(EagleRopePlan), P(EagleRopeArgs), P(EagleChunk), P(EagleCodedKV), _vp]
+    lib.eagle_chunk_attention_coded_workspace.argtypes = [P(EagleAttentionArgs), P(EagleChunk), P(EagleCodedKV)]
+    lib.eagle_chunk_attention_coded_workspace.restype = ctypes.c_size_t
+    lib.eagle_chunk_attention_coded.argtypes = [P(EagleAttentionArgs), P(EagleChunk), P(EagleCodedKV), _vp, ctypes.c_size_t, _vp]
     lib.eagle_set_rope.argtypes = [_vp, P(EagleRopeConfig)]
     lib.eagle_set_attention.argtypes = [_vp, P(EagleAttentionRules)]
     lib.eagle_set_logit_rules.argtypes = [_vp, P(EagleContextRules)]
@@ -162,6 +173,12 @@ class Chunk:
                             _list(tree_mask, "tree_mask", torch.int64, self.n_rows, self.device))
 
 
+def _page_table(page_table: torch.Tensor, device) -> None:
+    if page_table.dtype != torch.int32 or page_table.dim() != 2 or page_table.device != device or (page_table.stride(1) != 1 and page_table.shape[1] > 1) \
+            or (page_table.shape[0] > 1 and page_table.stride(0) < page_table.shape[1]):
+        raise ValueError(f"page_table must be an int32 [n_seqs, pages] tensor on {device}, its rows consecutive and apart")
+
+
 class PagedKV:
     """A paged cache: k, v [n_pages, n_kv_heads, page_tokens, head_dim] of the same type and strides, int32 page_table [n_seqs, pages]."""
 
@@ -170,13 +187,35 @@ class PagedKV:
             raise ValueError("k and v must be [n_pages, n_kv_heads, page_tokens, head_dim], float32 or bfloat16, of the same type, shape and strides on one device")
         if k.stride(3) != 1 and k.shape[3] > 1:
             raise ValueError("the elements of a token of k and v must be consecutive")
-        if page_table.dtype != torch.int32 or page_table.dim() != 2 or page_table.device != k.device or (page_table.stride(1) != 1 and page_table.shape[1] > 1) \
-                or (page_table.shape[0] > 1 and page_table.stride(0) < page_table.shape[1]):
-            raise ValueError(f"page_table must be an int32 [n_seqs, pages] tensor on {k.device}, its rows consecutive and apart")
+        _page_table(page_table, k.device)
         self.device, self.dtype, self.n_seqs, self.n_kv_heads, self.head_dim = k.device, k.dtype, page_table.shape[0], k.shape[1], k.shape[3]
         self.both, self._table, self.grads = (k, v), page_table, k.requires_grad or v.requires_grad
+        self.of_k = (k,)                                          # what an append of keys alone writes
         self.c = EaglePagedKV(k.data_ptr(), v.data_ptr(), _TYPES[k.dtype], k.shape[1], k.shape[3], k.shape[2], k.shape[0], page_table.shape[1], k.stride(0), k.stride(1), k.stride(2),
                               max(page_table.stride(0), page_table.shape[1]), page_table.data_ptr())
+
+
+class PagedKV8:
+    """A paged cache of 8-bit codes: k, v [n_pages, n_kv_heads, page_tokens, head_dim], float8_e4m3fn or int8, of the same type and strides, with float32 k_scale, v_scale [n_pages, n_kv_heads,
+    blocks] of the same strides, a scale for each page_tokens / blocks tokens; int32 page_table [n_seqs, pages].  An element is code * scale."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor):
+        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.stride() != v.stride() or k.device != v.device or k.dtype not in _CODES:
+            raise ValueError("k and v must be [n_pages, n_kv_heads, page_tokens, head_dim], float8_e4m3fn or int8, of the same type, shape and strides on one device")
+        if k.stride(3) != 1 and k.shape[3] > 1:
+            raise ValueError("the elements of a token of k and v must be consecutive")
+        _page_table(page_table, k.device)
+        for t, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+            if t.dtype != torch.float32 or t.device != k.device or t.dim() != 3 or t.shape[:2] != k.shape[:2] or t.shape[2] < 1 or k.shape[2] % t.shape[2] or t.shape != k_scale.shape \
+                    or t.stride() != k_scale.stride() or (t.stride(2) != 1 and t.shape[2] > 1):
+                raise ValueError(f"{name} must be a float32 [n_pages, n_kv_heads, blocks of a page] tensor on {k.device}, a page's scales of a head consecutive, both of the same shape and strides")
+        self.device, self.dtype, self.n_seqs, self.n_kv_heads, self.head_dim = k.device, k.dtype, page_table.shape[0], k.shape[1], k.shape[3]
+        self.both, self._table = (k, v, k_scale, v_scale), page_table
+        self.grads = any(t.requires_grad for t in self.both)
+        self.of_k = (k, k_scale)
+        self.c = EagleCodedKV(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), _CODES[k.dtype], k.shape[1], k.shape[3], k.shape[2], k.shape[2] // k_scale.shape[2], k.shape[0],
+                              page_table.shape[1], k.stride(0), k.stride(1), k.stride(2), max(page_table.stride(0), page_table.shape[1]), k_scale.stride(0), k_scale.stride(1),
+                              page_table.data_ptr())
 
 
 def _same_batch(chunk: Chunk, kv: PagedKV, device) -> None:
@@ -185,8 +224,8 @@ def _same_batch(chunk: Chunk, kv: PagedKV, device) -> None:
     if kv.n_seqs != chunk.n_seqs:
         raise ValueError(f"the page table has {kv.n_seqs} sequences, the chunk {chunk.n_seqs}")
     if kv.grads:
-        _plain(kv.both[0], "k of the cache")
-        _plain(kv.both[1], "v of the cache")
+        for t, name in zip(kv.both, ("k of the cache", "v of the cache", "k_scale", "v_scale")):
+            _plain(t, name)
 
 
 def rope_config(head_dim: int, *, theta: float = 10000.0, rot_dim: Optional[int] = None, interleaved: bool = False, scaling: str = "none", factor: float = 1.0, low: float = 1.0,
@@ -209,10 +248,10 @@ def rope_plan(head_dim: int, *, theta: float = 10000.0, rot_dim: Optional[int] =
 
 
 def rope(plan: EagleRopePlan, q: Optional[torch.Tensor], k: Optional[torch.Tensor], v: Optional[torch.Tensor] = None, *, chunk: Optional[Chunk] = None,
-         kv: Optional[PagedKV] = None, positions: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None,
+         kv: Union[PagedKV, PagedKV8, None] = None, positions: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None,
          inverse: bool = False) -> None:
     """Rotates q [rows, heads, head_dim] into q_out (None: in place) and k [rows, kv heads, head_dim] into the cache `kv`, with v, or without a cache into
-    k_out (None: in place)."""
+    k_out (None: in place).  Over a PagedKV8 keys and values are rounded to codes of their blocks' scales (eagle_rope_coded)."""
     x = q if q is not None else k
     if x is None:
         raise ValueError("neither q nor k is given")
@@ -247,11 +286,12 @@ def rope(plan: EagleRopePlan, q: Optional[torch.Tensor], k: Optional[torch.Tenso
     if R == 0:
         return
     a = EagleRopeArgs(R, H, KVH, _TYPES[dtype], int(inverse), qa[0], ka[0], va[0], qo[0], ko[0], qa[1], qa[2], ka[1], ka[2], va[1], va[2], qo[1], qo[2], ko[1], ko[2], at)
-    _call(_library().eagle_rope, device, plan, a, chunk.c if chunk is not None else None, kv.c if kv is not None else None)
+    lib = _library()
+    _call(lib.eagle_rope_coded if type(kv) is PagedKV8 else lib.eagle_rope, device, plan, a, chunk.c if chunk is not None else None, kv.c if kv is not None else None)
     if q is not None:
         _written((q if q_out is None else q_out,))
     if k is not None:
-        _written((k if k_out is None else k_out,) if kv is None else kv.both if v is not None else (kv.both[0],))
+        _written((k if k_out is None else k_out,) if kv is None else kv.both if v is not None else kv.of_k)
 
 
 def _attention_args(q, kv, chunk, scale, softcap, slopes, window, prefix, out):
@@ -264,17 +304,23 @@ def _attention_args(q, kv, chunk, scale, softcap, slopes, window, prefix, out):
                               _list(slopes, "slopes", torch.float32, H, device), _list(prefix, "prefix", torch.int32, chunk.n_seqs, device))
 
 
-def chunk_attention_workspace(q: torch.Tensor, kv: PagedKV, chunk: Chunk) -> int:
+def _attention_calls(lib, kv):
+    if type(kv) is PagedKV8:
+        return lib.eagle_chunk_attention_coded_workspace, lib.eagle_chunk_attention_coded
+    return lib.eagle_chunk_attention_workspace, lib.eagle_chunk_attention
+
+
+def chunk_attention_workspace(q: torch.Tensor, kv: Union[PagedKV, PagedKV8], chunk: Chunk) -> int:
     """Bytes of workspace chunk_attention needs for these arguments (whatever the masks)."""
     lib = _library()
     a = _attention_args(q, kv, chunk, None, 0.0, None, 0, None, None)
-    n = lib.eagle_chunk_attention_workspace(a, chunk.c, kv.c)
+    n = _attention_calls(lib, kv)[0](a, chunk.c, kv.c)
     if n == 0:
         raise EagleError(-1, lib.eagle_last_error().decode())
     return n
 
 
-def chunk_attention(q: torch.Tensor, kv: PagedKV, chunk: Chunk, *, scale: Optional[float] = None, softcap: float = 0.0, slopes: Optional[torch.Tensor] = None, window: int = 0,
+def chunk_attention(q: torch.Tensor, kv: Union[PagedKV, PagedKV8], chunk: Chunk, *, scale: Optional[float] = None, softcap: float = 0.0, slopes: Optional[torch.Tensor] = None, window: int = 0,
                     prefix: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """softmax(score) v of every row of q [rows, heads, head_dim] over the visible tokens of `kv` -> out (None: a new tensor).  scale: None = head_dim ** -0.5.
     workspace: a uint8 tensor of chunk_attention_workspace() bytes (None: one from torch's allocator for this call)."""
@@ -284,14 +330,15 @@ def chunk_attention(q: torch.Tensor, kv: PagedKV, chunk: Chunk, *, scale: Option
     lib = _library()
     if chunk.n_rows == 0:
         return out
+    size_of, attend = _attention_calls(lib, kv)
     if workspace is None:
-        n = lib.eagle_chunk_attention_workspace(a, chunk.c, kv.c)
+        n = size_of(a, chunk.c, kv.c)
         if n == 0:
             raise EagleError(-1, lib.eagle_last_error().decode())
         workspace = torch.empty(n, dtype=torch.uint8, device=q.device)
     elif workspace.dtype != torch.uint8 or not workspace.is_contiguous() or workspace.device != q.device:
         raise ValueError(f"workspace must be a contiguous uint8 tensor on {q.device}")
-    _call(lib.eagle_chunk_attention, q.device, a, chunk.c, kv.c, workspace.data_ptr(), workspace.numel())
+    _call(attend, q.device, a, chunk.c, kv.c, workspace.data_ptr(), workspace.numel())
     _written((out,))
     return out
 

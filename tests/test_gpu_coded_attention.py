@@ -1,0 +1,264 @@
+"""Attention of a chunk of new tokens over a paged cache of 8-bit codes against the oracle in 64 bits.
+
+Tolerances.  u = 2^-24.  Codes are exact bf16 numbers, so a score over 128 elements is three products of pieces (fp32 queries) in eight blocks of 16: at most 64 roundings of partial sums of at most
+B = scale * k_scale * sum |q code|, and 5 u of itself from scale, block scale, cap and slopes.  A weight takes its block's value scale by one more rounding.  So, with the sums over T tokens, the
+output is off by (2 * (64 u B + 5 u (B + C)) + (T / 8 + 33) u) * A: A the weighted mean of |v|, C the largest cap or slope term.  bf16 queries: every weight rounds to bf16 (2^-8 A), and the result
+once more (2^-8 of itself)."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import operators as ref
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U = 2.0 ** -24
+TYPES = {"fp32": torch.float32, "bf16": torch.bfloat16}
+CODES = {"e4m3": torch.float8_e4m3fn, "int8": torch.int8}
+ALL = ["fp32/e4m3", "fp32/int8", "bf16/e4m3", "bf16/int8"]
+
+
+def pkg():
+    import paper_2401_15077_amd
+    return paper_2401_15077_amd
+
+
+def i32(a):
+    return torch.tensor(np.asarray(a), dtype=torch.int32, device=DEV)
+
+
+def tree(n, rng):
+    masks, depth = [1], [0]
+    for v in range(1, n):
+        p = int(rng.choice([u for u in range(v) if depth[u] < 15]))
+        masks.append(masks[p] | 1 << v)
+        depth.append(depth[p] + 1)
+    return masks
+
+
+def held(x, cache, block, gen):
+    """Codes and scales of x [pages, heads, tokens, dim], the scales spread a little beyond what the largest element needs."""
+    P, H, N, D = x.shape
+    M = 448.0 if cache == "e4m3" else 127.0
+    x = x.view(P, H, N // block, block * D)
+    scale = x.abs().amax(-1) / M * (1.0 + torch.rand(P, H, N // block, device=DEV, generator=gen))
+    y = x / scale[..., None]
+    return (y.to(CODES[cache]) if cache == "e4m3" else y.round().to(torch.int8)).view(P, H, N, D), scale
+
+
+def values(codes, scale, block):
+    v = ref.code_value(codes.contiguous().view(torch.uint8).cpu().numpy(), codes.dtype == torch.float8_e4m3fn)
+    with np.errstate(invalid="ignore"):
+        return v * np.repeat(np.abs(scale.double().cpu().numpy()), block, axis=2)[..., None]
+
+
+def case(rows, keys, H, KVH, D, types, page, block, *, masks=None, base=None, seed=0, poison=False, gap=(), pad=0, room=5):
+    p = pkg()
+    dtype, cache = types.split("/")
+    gen = torch.Generator(device=DEV).manual_seed(seed + 3)
+    R, S = sum(rows), len(rows)
+    need = [max(1, -(-k // page)) for k in keys]
+    n_pages = sum(need) + 2
+    order = np.random.default_rng(seed).permutation(n_pages).tolist()
+    table = np.full((S, max(need) + 1), -7, np.int32)
+    for s, n in enumerate(need):
+        table[s, :n] = [order.pop() for _ in range(n)]
+    for s, g in gap:
+        table[s, g] = n_pages + g if g % 2 else -1
+    (kc, ks), (vc, vs) = (held(torch.randn(n_pages, KVH, page, D, device=DEV, generator=gen), cache, block, gen) for _ in range(2))
+    if pad:
+        kc, vc = (torch.cat([c.view(torch.uint8), torch.full((n_pages, KVH, page, pad), 127, dtype=torch.uint8, device=DEV)], 3).view(CODES[cache])[..., :D] for c in (kc, vc))
+    if poison:                                                    # what no sequence owns: NaN codes, and scales that are no numbers
+        owned = torch.zeros(n_pages, page, dtype=torch.bool, device=DEV)
+        for s, k in enumerate(keys):
+            for t in range(k):
+                if 0 <= table[s, t // page] < n_pages:
+                    owned[table[s, t // page], t % page] = True
+        for c, sc in ((kc, ks), (vc, vs)):
+            c.view(torch.uint8).masked_fill_(~owned[:, None, :, None], 0xFF)
+            sc.masked_fill_(~owned.view(n_pages, 1, page // block, block).any(-1), float("nan"))
+    q = (torch.randn(R, H, D, device=DEV, generator=gen) * 1.5).to(TYPES[dtype])
+    start = np.cumsum([0] + list(rows))
+    tm = None if masks is None else torch.tensor([m - (1 << 64) if m >> 63 else m for m in masks], dtype=torch.int64, device=DEV)
+    chunk = p.Chunk(i32(start), i32(keys), R, max(max(rows), 1), max(keys) + room, tree_base=None if base is None else i32(base), tree_mask=tm)
+    return q, p.PagedKV8(kc, vc, i32(table), ks, vs), chunk, ref.chunk_rows(start, keys, base, masks), table
+
+
+def check(q, kv, chunk, facts, table, keys, page, block, *, softcap=0.0, window=0, slopes=False, prefix=None, base=None, scale=None, out=None):
+    p = pkg()
+    R, H, D = q.shape
+    sl = torch.tensor(2.0 ** (-8.0 * np.arange(1, H + 1) / H), dtype=torch.float32, device=DEV) if slopes else None
+    out = torch.full(q.shape, 5.0, dtype=q.dtype, device=DEV) if out is None else out
+    before = q.clone()
+    p.chunk_attention(q, kv, chunk, scale=scale, softcap=softcap, slopes=sl, window=window, prefix=None if prefix is None else i32(prefix), out=out)
+    torch.cuda.synchronize()
+    kc, vc, ks, vs = kv.both
+    want, mean, big, count = ref.attention(before.double().cpu().numpy(), values(kc, ks, block), values(vc, vs, block), table, facts, R, keys, page=page, scale=D ** -0.5 if scale is None else scale,
+                                           softcap=softcap, slopes=None if sl is None else sl.double().cpu().numpy(), window=window, prefix=prefix, tree_base=base)
+    extra = softcap + (max(keys) * float(sl.max()) if slopes else 0.0)
+    tol = (2 * (64 * U * big + 5 * U * (big + extra)) + (count[:, None] / 8 + 33) * U)[:, :, None] * mean + 1e-30
+    if q.dtype == torch.bfloat16:
+        tol = tol + 2.0 ** -8 * 1.001 * (mean + np.abs(want))
+    got = out.double().cpu().numpy()
+    err = np.abs(got - want) / tol
+    print(f"rows {R} keys {keys[:4]} worst {err.max():.3f} of the bound, rel {np.linalg.norm(got - want) / max(np.linalg.norm(want), 1e-30):.2e}", flush=True)
+    assert err.max() <= 1.0
+    assert (got[count == 0] == 0.0).all()
+    return out
+
+
+def run(rows, keys, H, KVH, D, types, page, block, *, masks=None, base=None, seed=0, poison=False, gap=(), pad=0, room=5, **mods):
+    q, kv, chunk, facts, table = case(rows, keys, H, KVH, D, types, page, block, masks=masks, base=base, seed=seed, poison=poison, gap=gap, pad=pad, room=room)
+    return check(q, kv, chunk, facts, table, keys, page, block, base=base, **mods), q, kv, chunk
+
+
+@pytest.mark.parametrize("types", ALL)
+@pytest.mark.parametrize("rows,keys,H,KVH,D,page,block", [
+    ([1], [1], 4, 4, 64, 64, 16), ([1], [2], 1, 1, 16, 16, 16), ([1], [31], 4, 2, 128, 16, 16), ([1], [33], 8, 1, 128, 32, 32), ([1], [701], 32, 32, 128, 64, 16), ([1], [1500], 5, 5, 80, 64, 32),
+    ([1, 1, 1], [64, 1, 129], 8, 2, 32, 128, 128), ([2, 1, 5], [65, 700, 5], 6, 3, 48, 16, 16), ([7], [7], 4, 4, 128, 64, 64), ([33], [33], 2, 2, 64, 32, 16), ([5, 40], [300, 40], 8, 2, 128, 16, 16),
+    ([130], [200], 3, 1, 96, 64, 16), ([257], [257], 2, 2, 128, 64, 32), ([64, 1, 0, 3], [500, 90, 20, 3], 16, 2, 128, 128, 64), ([1], [2100], 64, 8, 128, 256, 128), ([20], [600], 12, 1, 112, 32, 16),
+    ([40], [300], 4, 2, 64, 64, 16), ([1, 2], [400, 1000], 8, 1, 96, 16, 16),
+])
+def test_causal(rows, keys, H, KVH, D, page, block, types):
+    run(rows, keys, H, KVH, D, types, page, block, poison=True)
+
+
+@pytest.mark.parametrize("types", ALL)
+@pytest.mark.parametrize("nodes,base,H,KVH,D", [([26], [674], 8, 8, 128), ([26, 8, 1], [100, 0, 63], 8, 2, 64), ([64], [65], 4, 1, 128), ([63, 40], [31, 300], 4, 4, 32)])
+def test_trees(nodes, base, H, KVH, D, types):
+    rng = np.random.default_rng(sum(nodes))
+    masks = [m for n in nodes for m in tree(n, rng)]
+    keys = [b + n for b, n in zip(base, nodes)]
+    run(nodes, keys, H, KVH, D, types, 64, 32, masks=masks, base=base, poison=True)
+    run(nodes, keys, H, KVH, D, types, 64, 16, masks=masks, base=base, window=9, slopes=True, softcap=20.0, prefix=[3] * len(nodes))
+
+
+@pytest.mark.parametrize("types", ALL)
+@pytest.mark.parametrize("mods", [dict(softcap=3.0), dict(slopes=True), dict(window=1), dict(window=17), dict(window=100), dict(prefix=[40, 0]), dict(prefix=[300, 2]),
+                                  dict(window=33, prefix=[5, 70], softcap=20.0, slopes=True), dict(scale=0.3), dict(scale=-0.2), dict(scale=0.0), dict(window=400)], ids=str)
+@pytest.mark.parametrize("rows,keys", [([1, 1], [300, 77]), ([50, 9], [300, 77]), ([150, 64], [260, 64])])
+def test_modified_scores_and_masks(rows, keys, mods, types):
+    run(rows, keys, 8, 2, 64, types, 32, 16, **mods)
+
+
+@pytest.mark.parametrize("types", ALL)
+@pytest.mark.parametrize("rows", [[1, 1, 2], [40, 3, 2]])
+def test_pages_that_are_not_there_and_rows_that_see_nothing(rows, types):
+    run(rows, [200, 64, 20], 8, 2, 64, types, 32, 32, gap=[(0, 1), (0, 4), (2, 0)], poison=True)
+    run(rows, [200, 64, 20], 8, 2, 64, types, 16, 16, gap=[(0, 11), (0, 12), (1, 3)], window=1, poison=True)
+
+
+@pytest.mark.parametrize("types", ALL)
+@pytest.mark.parametrize("rows", [[1, 3], [60, 40]])
+def test_strides_places_and_a_wide_bound(rows, types):
+    """Tokens further apart than their elements, queries and results among other heads, the result in the queries' place, bounds far beyond the lengths."""
+    keys = [90, 300]
+    run(rows, keys, 4, 2, 80, types, 64, 16, pad=16)
+    q, kv, chunk, facts, table = case(rows, keys, 4, 2, 64, types, 64, 16, room=100000)
+    wide = torch.zeros(q.shape[0], 8, 128, dtype=q.dtype, device=DEV)
+    wide[:, ::2, :64] = q
+    out = torch.zeros(4, q.shape[0], 64, dtype=q.dtype, device=DEV).transpose(0, 1)
+    a = check(wide[:, ::2, :64], kv, chunk, facts, table, keys, 64, 16, out=out)
+    b = check(q, kv, chunk, facts, table, keys, 64, 16, out=q)
+    assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("types", ["fp32/e4m3", "bf16/e4m3"])
+@pytest.mark.parametrize("rows", [[3], [70]])
+def test_nan_codes_stay_with_the_rows_that_see_them(rows, types):
+    keys = [100]
+    q, kv, chunk, facts, table = case(rows, keys, 4, 2, 64, types, 32, 16, seed=4)
+    clean = pkg().chunk_attention(q, kv, chunk)
+    n, at = rows[0], 98                                           # the last two rows see token 98
+    for which, name in enumerate(("k", "v")):
+        c = kv.both[which]
+        page = int(table[0][at // 32])
+        kept = c.view(torch.uint8)[page, 1, at % 32, 5].item()
+        c.view(torch.uint8)[page, 1, at % 32, 5] = 0x7F
+        got = pkg().chunk_attention(q, kv, chunk)
+        assert torch.equal(got[:n - 2], clean[:n - 2]) and torch.equal(got[:, :2], clean[:, :2])
+        seen = got[n - 2:, 2:]
+        assert seen.isnan().all() if which == 0 else (seen[..., 5].isnan().all() and torch.equal(seen[..., 6:], clean[n - 2:, 2:, 6:]) and torch.equal(seen[..., :5], clean[n - 2:, 2:, :5])), name
+        c.view(torch.uint8)[page, 1, at % 32, 5] = kept
+
+
+@pytest.mark.parametrize("types", ALL)
+@pytest.mark.parametrize("mods", [dict(), dict(softcap=4.0)], ids=str)
+@pytest.mark.parametrize("rows", [[20], [80]])
+def test_scales_that_are_zero_or_not_finite(rows, mods, types):
+    keys = [100]
+    q, kv, chunk, facts, table = case(rows, keys, 4, 2, 64, types, 32, 16, seed=4)
+    n, page = rows[0], int(table[0][3])                           # tokens 96 to 99, the first block of the last page
+    ks, vs = kv.both[2:]
+    clean = pkg().chunk_attention(q, kv, chunk, **mods)
+    for s in (ks, vs):
+        kept = s[page, 1, 0].item()
+        for bad in (float("nan"), float("inf")):
+            s[page, 1, 0] = bad
+            got = pkg().chunk_attention(q, kv, chunk, **mods)
+            assert torch.equal(got[:n - 4], clean[:n - 4]) and torch.equal(got[:, :2], clean[:, :2])
+            assert s is ks or not got[n - 4:, 2:].isfinite().any()
+            if s is ks and not mods:                              # (the cap of an infinite score is finite)
+                assert not got[n - 4:, 2:].isfinite().all()
+            if bad != bad:
+                assert not got[n - 4:, 2:].isfinite().any()
+        s[page, 1, 0] = -kept                                     # (a sign is not looked at)
+        assert torch.equal(pkg().chunk_attention(q, kv, chunk, **mods), clean)
+        s[page, 1, 0] = 0.0
+        check(q, kv, chunk, facts, table, keys, 32, 16, **mods)
+        s[page, 1, 0] = kept
+
+
+@pytest.mark.parametrize("types", ALL)
+@pytest.mark.parametrize("size", [2.0 ** -60, 2.0 ** 60])
+def test_scales_far_apart(size, types):
+    """Blocks of very different size side by side: the largest keys and values still count as they should."""
+    for rows in ([2], [70]):
+        q, kv, chunk, facts, table = case(rows, [150], 4, 2, 64, types, 32, 16, seed=9)
+        ks, vs = kv.both[2:]
+        vs[::2] *= size
+        ks[1::2] *= 2.0 ** -20
+        check(q, kv, chunk, facts, table, [150], 32, 16)
+
+
+def test_the_same_bits_every_time_and_in_a_graph():
+    p = pkg()
+    q, kv, chunk, facts, table = case([26, 3, 1], [700, 90, 1500], 16, 4, 128, "bf16/e4m3", 64, 32)
+    ws = torch.empty(p.chunk_attention_workspace(q, kv, chunk), dtype=torch.uint8, device=DEV)
+    out = torch.empty_like(q)
+    want = p.chunk_attention(q, kv, chunk, window=500)
+    p.chunk_attention(q, kv, chunk, window=500, out=out, workspace=ws)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        p.chunk_attention(q, kv, chunk, window=500, out=out, workspace=ws)
+    for seed in range(4):
+        out.zero_()
+        ws.fill_(255)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+        q.copy_(torch.randn(q.shape, device=DEV, generator=torch.Generator(device=DEV).manual_seed(seed)))
+        want = p.chunk_attention(q, kv, chunk, window=500)
+
+
+def test_a_cache_beyond_2_31_codes():
+    """Pages whose offsets do not fit in 32 bits, written and read."""
+    p = pkg()
+    n_pages, page = 40960, 64
+    kc = torch.empty(n_pages, 16, page, 64, dtype=torch.int8, device=DEV)
+    vc = torch.empty_like(kc)
+    ks, vs = (torch.ones(n_pages, 16, 4, device=DEV) for _ in range(2))
+    kv = p.PagedKV8(kc, vc, i32([[n_pages - 1, 17, n_pages - 2]]), ks, vs)
+    chunk = p.Chunk(i32([0, 150]), i32([150]), 150, 150, 150)
+    gen = torch.Generator(device=DEV).manual_seed(2)
+    q, k, v = (torch.randn(150, 16, 64, device=DEV, generator=gen).bfloat16() for _ in range(3))
+    q_out = torch.empty_like(q)
+    p.rope(p.rope_plan(64), q, k, v, chunk=chunk, kv=kv, q_out=q_out)
+    got = p.chunk_attention(q_out, kv, chunk)
+    near = [torch.empty(3, 16, page, 64, dtype=torch.int8, device=DEV) for _ in range(2)]
+    scales = [torch.ones(3, 16, 4, device=DEV) for _ in range(2)]
+    kv2 = p.PagedKV8(*near, i32([[1, 0, 2]]), *scales)
+    p.rope(p.rope_plan(64), q, k, v, chunk=chunk, kv=kv2, q_out=q_out)
+    assert torch.equal(kc[n_pages - 1], near[0][1]) and torch.equal(vc[n_pages - 2, :, :22], near[1][2, :, :22]) and torch.equal(ks[n_pages - 1], scales[0][1])
+    assert torch.equal(got, p.chunk_attention(q_out, kv2, chunk))
