@@ -404,6 +404,27 @@ typedef struct {
 } eagle_logits;
 int eagle_apply_logit_rules(const eagle_logits *logits, const eagle_logit_rules *rules, void *hip_stream);
 
+/* The choice of one token a row of logits [n_rows][vocab] of `dtype` (row stride in elements), from a given random number.  With the row's tokens in order of their logits, descending, equal ones
+ * by index, NaN as -inf, and w = exp((logit - largest) / temperature):
+ *   top_k > 0: the first top_k;  top_p < 1: of those the shortest run from the front that holds top_p of their mass;  min_p > 0: of those, w >= min_p;  the first in any case
+ *   token = the first in order whose running mass exceeds uniform * (mass of those kept), uniform in [0, 1);  logprob = ln(w / mass of those kept)
+ * A temperature that is not above 0 takes the first (logprob 0).  Logits of +inf, where there are any, count 1 each and all others 0.  A row of nothing but -inf: token -1, logprob -inf.
+ * Weights are rounded to whole multiples of 2^-b of the largest one, b = 62 - ceil(log2 vocab) (45 for 131072 tokens), and added up exactly: a call's result is the same every time.
+ * Parameters are arrays with an entry a row; null: 1, no top_k, no top_p, no min_p.  A parameter that is NaN is no filter.  Outputs lie apart from all inputs.
+ * workspace (dev, 256-byte aligned): eagle_sample_workspace() bytes, for the same arguments; its contents need not be kept or cleared. */
+typedef struct {
+  int32_t n_rows, vocab, dtype;
+  const void *logits;
+  int64_t stride;
+  const float *uniform, *temperature; /* dev [n_rows] */
+  const int32_t *top_k;
+  const float *top_p, *min_p;
+  int32_t *token;                     /* dev [n_rows] */
+  float *logprob;                     /* dev [n_rows] or null */
+} eagle_sample_args;
+size_t eagle_sample_workspace(const eagle_sample_args *args);
+int eagle_sample(const eagle_sample_args *args, void *workspace_dev, size_t workspace_bytes, void *hip_stream);
+
 /* ---- The same three inside a context ------------------------------------------------------------------------------
  * Positions: how the target's and the head's layers turn queries and keys (null: the default again, pairs (i, i + head_dim / 2) of the whole head by cfg.rope_theta).
  * theta of the given configuration counts, not cfg's.  Before the first EAGLE_W_Q / _K is loaded (they are laid out by pairs), EAGLE_ESTATE after that.  Keys are read

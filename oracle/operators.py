@@ -208,3 +208,37 @@ def append_codes(x, values, scale, facts, table, key_len, *, page, block, e4m3, 
                 values[pg, h, t % page] = nearest_code(x[r, h] / u, e4m3)
                 exact[pg, h, t % page] = x[r, h] / u
     return values, scale, exact
+
+
+def sample(x, u, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+    """One row -> (token, logprob, border): border is how close, in parts of the kept mass, the drawn number or the choice of what is kept comes to another answer."""
+    x = np.asarray(x, dtype=np.float64)
+    x = np.where(np.isnan(x), -np.inf, x)
+    order = np.lexsort((np.arange(len(x)), -x))
+    top = x[order[0]]
+    if top == -np.inf:
+        return -1, -np.inf, 1.0
+    if not temperature > 0:
+        return int(order[0]), 0.0, 1.0
+    y = x[order]
+    with np.errstate(invalid="ignore"):
+        t = np.where(y == top, 0.0, np.where(y == -np.inf, -np.inf, -np.inf if top == np.inf else (y - top) / temperature))
+    w, border = np.exp(t), 1.0
+    n = min(len(w), top_k) if top_k > 0 else len(w)
+    run = np.cumsum(w[:n])
+    if top_p < 1:
+        need = max(top_p, 0.0) * run[-1]
+        m = min(n, int(np.searchsorted(run, need)) + 1)
+        border = min(border, np.abs(run - need).min() / run[-1])
+        n = max(1, m)
+    if min_p > 0:
+        ok = t[:n] >= math.log(min_p)
+        border = min(border, np.abs(t[:n] - math.log(min_p)).min())
+        n = max(1, int(ok.sum()))
+    run = run[:n]
+    u = u if u > 0 else 0.0
+    at = min(int(np.searchsorted(run, u * run[-1], side="right")), n - 1)
+    while at > 0 and w[at] == 0:
+        at -= 1
+    border = min(border, np.abs(run - u * run[-1]).min() / run[-1] if u > 0 else 1.0)
+    return int(order[at]), float(t[at] - math.log(run[-1])), border

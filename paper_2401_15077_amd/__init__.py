@@ -31,7 +31,8 @@ EXPORTS = ["eagle_workspace_bytes", "eagle_init", "eagle_free", "eagle_load_weig
            "eagle_set_hint", "eagle_set_page_table", "eagle_set_buffer", "eagle_force_tree", "eagle_expand_level",
            "eagle_force_accept", "eagle_get_buffer", "eagle_get_kv_row", "eagle_set_profiling", "eagle_get_profile", "eagle_get_kernel_stats", "eagle_probe_stream_read",
            "eagle_head_loss", "eagle_feature_noise", "eagle_rope_plan_init", "eagle_rope", "eagle_chunk_attention_workspace", "eagle_chunk_attention",
-           "eagle_rope_coded", "eagle_chunk_attention_coded_workspace", "eagle_chunk_attention_coded", "eagle_apply_logit_rules", "eagle_set_rope", "eagle_set_attention", "eagle_set_logit_rules", "eagle_last_error", "eagle_version"]
+           "eagle_rope_coded", "eagle_chunk_attention_coded_workspace", "eagle_chunk_attention_coded", "eagle_apply_logit_rules",
+           "eagle_sample_workspace", "eagle_sample", "eagle_set_rope", "eagle_set_attention", "eagle_set_logit_rules", "eagle_last_error", "eagle_version"]
 
 
 class EagleConfig(ctypes.Structure):
@@ -456,7 +457,7 @@ class Eagle:
                  "launches": int(arr[i].launches), "bytes": arr[i].bytes} for i in range(n.value)]
 
 
-_OPERATORS = ("Chunk", "PagedKV", "PagedKV8", "LogitRules", "rope_plan", "rope", "chunk_attention", "chunk_attention_workspace", "apply_logit_rules")
+_OPERATORS = ("Chunk", "PagedKV", "PagedKV8", "LogitRules", "rope_plan", "rope", "chunk_attention", "chunk_attention_workspace", "apply_logit_rules", "sample", "sample_workspace")
 
 
 def __getattr__(name):

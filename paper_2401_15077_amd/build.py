@@ -6,8 +6,8 @@ import tempfile
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libeagle.so")
-SOURCES = ["eagle.hip", "operators.hip", "coded.hip"]
-HEADERS = ["kernels.h", "kernels2.h", "plans.h", "common.h", "host.h", "operators.h", "rows.h", "checks.h", "attention.h", "codes.h", "rope.h", "rope_coded.h", "chunk_attn.h", "logit_rules.h", os.path.join("..", "..", "include", "eagle.h")]
+SOURCES = ["eagle.hip", "operators.hip", "coded.hip", "sample.hip"]
+HEADERS = ["kernels.h", "kernels2.h", "plans.h", "common.h", "host.h", "operators.h", "rows.h", "checks.h", "attention.h", "codes.h", "rope.h", "rope_coded.h", "chunk_attn.h", "logit_rules.h", "sample.h", os.path.join("..", "..", "include", "eagle.h")]
 
 
 def needs_build() -> bool:

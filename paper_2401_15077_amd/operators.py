@@ -63,6 +63,11 @@ class EagleLogits(ctypes.Structure):
                 ("row_start", _vp), ("path_token", _vp), ("path_mask", _vp), ("allowed", _vp), ("allowed_row", _vp)]
 
 
+class EagleSampleArgs(ctypes.Structure):
+    _fields_ = [("n_rows", _i32), ("vocab", _i32), ("dtype", _i32), ("logits", _vp), ("stride", _i64), ("uniform", _vp), ("temperature", _vp), ("top_k", _vp), ("top_p", _vp), ("min_p", _vp),
+                ("token", _vp), ("logprob", _vp)]
+
+
 class EagleAttentionRules(ctypes.Structure):
     _fields_ = [("softcap", _f32), ("window", _i32), ("slopes_dev", _vp)]
 
@@ -84,6 +89,9 @@ def declare(lib) -> None:
     lib.eagle_chunk_attention_coded_workspace.argtypes = [P(EagleAttentionArgs), P(EagleChunk), P(EagleCodedKV)]
     lib.eagle_chunk_attention_coded_workspace.restype = ctypes.c_size_t
     lib.eagle_chunk_attention_coded.argtypes = [P(EagleAttentionArgs), P(EagleChunk), P(EagleCodedKV), _vp, ctypes.c_size_t, _vp]
+    lib.eagle_sample_workspace.argtypes = [P(EagleSampleArgs)]
+    lib.eagle_sample_workspace.restype = ctypes.c_size_t
+    lib.eagle_sample.argtypes = [P(EagleSampleArgs), _vp, ctypes.c_size_t, _vp]
     lib.eagle_set_rope.argtypes = [_vp, P(EagleRopeConfig)]
     lib.eagle_set_attention.argtypes = [_vp, P(EagleAttentionRules)]
     lib.eagle_set_logit_rules.argtypes = [_vp, P(EagleContextRules)]
@@ -408,3 +416,54 @@ def apply_logit_rules(logits: torch.Tensor, rules: LogitRules, *, row_start: Opt
         _call(_library().eagle_apply_logit_rules, dev, l, rules.c)
         _written((out,))
     return out
+
+
+def _sample_args(logits, uniform, temperature, top_k, top_p, min_p, token, logprob):
+    if logits.dim() != 2 or logits.dtype not in _TYPES or (logits.stride(1) != 1 and logits.shape[1] > 1):
+        raise ValueError("logits must be a float32 or bfloat16 [rows, vocab] tensor, its rows consecutive")
+    if logits.requires_grad:
+        _plain(logits, "logits")
+    (R, V), dev, f = logits.shape, logits.device, torch.float32
+    return EagleSampleArgs(R, V, _TYPES[logits.dtype], logits.data_ptr(), logits.stride(0) if R > 1 else V, _list(uniform, "uniform", f, R, dev), _list(temperature, "temperature", f, R, dev),
+                           _list(top_k, "top_k", torch.int32, R, dev), _list(top_p, "top_p", f, R, dev), _list(min_p, "min_p", f, R, dev), _list(token, "token", torch.int32, R, dev),
+                           _list(logprob, "logprob", f, R, dev))
+
+
+def sample_workspace(logits: torch.Tensor) -> int:
+    """Bytes of workspace sample needs for logits of this shape and type (whatever the filters)."""
+    lib = _library()
+    a = _sample_args(logits, None, None, None, None, None, None, None)
+    a.logits, a.uniform, a.token = 1 << 60, 1 << 58, 1 << 56      # (sizes alone count here)
+    n = lib.eagle_sample_workspace(a)
+    if n == 0:
+        raise EagleError(-1, lib.eagle_last_error().decode())
+    return n
+
+
+def sample(logits: torch.Tensor, uniform: torch.Tensor, *, temperature: Optional[torch.Tensor] = None, top_k: Optional[torch.Tensor] = None, top_p: Optional[torch.Tensor] = None,
+           min_p: Optional[torch.Tensor] = None, token: Optional[torch.Tensor] = None, logprob: Optional[torch.Tensor] = None,
+           workspace: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """A token of every row of logits [rows, vocab] (float32 or bfloat16), drawn by the row's number of float32 uniform [rows] in [0, 1) -> (int32 token [rows], float32 logprob [rows]), new
+    tensors where none are given.  float32 temperature, top_p, min_p and int32 top_k [rows] (None: no such filter): see eagle_sample.
+    workspace: a uint8 tensor of sample_workspace() bytes (None: one from torch's allocator for this call)."""
+    if uniform is None:
+        raise ValueError("uniform is needed: a random number for every row")
+    R, dev = logits.shape[0], logits.device
+    if token is None:
+        token = torch.empty(R, dtype=torch.int32, device=dev)
+    if logprob is None:
+        logprob = torch.empty(R, dtype=torch.float32, device=dev)
+    a = _sample_args(logits, uniform, temperature, top_k, top_p, min_p, token, logprob)
+    if R == 0:
+        return token, logprob
+    lib = _library()
+    if workspace is None:
+        n = lib.eagle_sample_workspace(a)
+        if n == 0:
+            raise EagleError(-1, lib.eagle_last_error().decode())
+        workspace = torch.empty(n, dtype=torch.uint8, device=dev)
+    elif workspace.dtype != torch.uint8 or not workspace.is_contiguous() or workspace.device != dev:
+        raise ValueError(f"workspace must be a contiguous uint8 tensor on {dev}")
+    _call(lib.eagle_sample, dev, a, workspace.data_ptr(), workspace.numel())
+    _written((token, logprob))
+    return token, logprob

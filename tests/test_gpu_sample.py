@@ -1,0 +1,184 @@
+"""The choice of a token against the oracle in 64 bits.
+
+Tolerances.  Weights are whole multiples of 2^-b of the largest (b >= 44 here), each rounded by half of one, so masses of up to 2^18 of them are off by 2^-27 of the largest weight and by no more than
+2^-27 of the mass: a token may differ from the oracle's only where the oracle's number falls as close as that to a border.  A log probability is worked out in 64 bits from such a mass and rounded
+to fp32: 2^-24 of itself and 2^-26."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import operators as ref
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = {"fp32": torch.float32, "bf16": torch.bfloat16}
+INF, NAN = float("inf"), float("nan")
+
+
+def pkg():
+    import paper_2401_15077_amd
+    return paper_2401_15077_amd
+
+
+def row(values, dtype=torch.float32):
+    return torch.tensor(np.asarray(values), dtype=dtype, device=DEV)
+
+
+def check(logits, u, **kw):
+    """kw: lists, an entry a row."""
+    R = logits.shape[0]
+    types = dict(temperature=torch.float32, top_k=torch.int32, top_p=torch.float32, min_p=torch.float32)
+    given = {n: row(v, types[n]) for n, v in kw.items()}
+    uniform = row(u)
+    token, logprob = pkg().sample(logits, uniform, **given)
+    again, _ = pkg().sample(logits, uniform, **given)
+    assert torch.equal(token, again)
+    x = logits.float().cpu().numpy()
+    token, logprob = token.tolist(), logprob.double().tolist()
+    near = 0
+    for r in range(R):
+        want, lp, border = ref.sample(x[r], float(uniform[r]), **{n: t[r].item() for n, t in given.items()})
+        if token[r] != want:
+            assert border < 2.0 ** -27, (r, token[r], want, border, {n: t[r].item() for n, t in given.items()})
+            near += 1
+        elif lp == -INF:
+            assert logprob[r] == -INF
+        else:
+            assert abs(logprob[r] - lp) <= 2.0 ** -24 * abs(lp) + 2.0 ** -26 or border < 2.0 ** -27, (r, logprob[r], lp)
+    assert near <= 1 + R // 50
+    return token
+
+
+def spread(R, V, dtype, seed=0, scale=3.0):
+    gen = torch.Generator(device=DEV).manual_seed(seed + 5)
+    x = torch.randn(R, V, device=DEV, generator=gen) * scale * (0.3 + torch.rand(R, 1, device=DEV, generator=gen))
+    return x.to(TYPES[dtype]), torch.rand(R, device=DEV, generator=gen).tolist()
+
+
+FILTERS = {"none": {}, "top_k": dict(top_k=[1, 2, 40, 200]), "many": dict(top_k=[257, 300, 900, 3000]), "top_p": dict(top_p=[0.1, 0.5, 0.9, 0.99]), "min_p": dict(min_p=[0.5, 0.1, 0.01, 1e-4]),
+           "all": dict(top_k=[50, 100, 20, 1000], top_p=[0.9, 0.5, 0.99, 0.95], min_p=[0.01, 0.02, 0.1, 0.001]), "two": dict(top_p=[0.99, 0.9, 0.999, 0.8], min_p=[0.1, 1e-3, 1e-5, 0.3])}
+
+
+@pytest.mark.parametrize("filters", FILTERS)
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("V", [1, 2, 3, 7, 63, 64, 65, 255, 1000, 1027, 4096, 32000, 50001, 131075])
+def test_filters(V, dtype, filters):
+    R = 12
+    x, u = spread(R, V, dtype, seed=V)
+    kw = {n: [v[r % 4] for r in range(R)] for n, v in FILTERS[filters].items()}
+    check(x, u, temperature=[(0.3, 0.7, 1.0, 1.7, 5.0)[r % 5] for r in range(R)], **kw)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("V", [10, 900, 5000, 40000, 140000])
+def test_equal_logits_go_by_index(V, dtype):
+    x = torch.zeros(8, V, device=DEV, dtype=TYPES[dtype])
+    x[1] = -0.0
+    x[1, ::3] = 0.0                                               # (the same number)
+    x[2:] = torch.randint(0, 3, (6, V), device=DEV, generator=torch.Generator(device=DEV).manual_seed(V)).to(x.dtype)
+    u = [0.37, 0.61, 0.2, 0.5, 0.9, 0.0, 0.99, 0.45]
+    check(x, u)
+    check(x, u, top_k=[5, V // 2, V // 3, V, V + 7, V - 1, 300, 2])
+    check(x, u, top_p=[0.5, 0.25, 0.7, 0.9, 0.99, 0.01, 0.4, 0.6])
+    check(x, u, top_k=[V // 2] * 8, top_p=[0.5] * 8, min_p=[0.5] * 8, temperature=[0.5, 1.0, 2.0, 0.1, 100.0, 1.0, 1.0, 1.0])
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_numbers_at_the_ends(dtype):
+    t = TYPES[dtype]
+    V = 777
+    x = torch.full((12, V), -INF, device=DEV, dtype=t)
+    x[1, 700] = -3e38                                             # one left
+    x[2, [5, 600]] = row([1.0, 2.0], t)
+    x[3] = NAN
+    x[4] = torch.arange(V, device=DEV).to(t)
+    x[4, ::2] = NAN
+    x[5, [3, 9, 400]] = INF
+    x[6] = 1.0
+    x[6, [3, 9, 400]] = INF
+    x[7, :3] = row([3e38, -3e38, 2.9e38], t)
+    x[8, :4] = row([1e-40, -1e-40, 0.0, -0.0], t)
+    x[9] = 5.0
+    x[9, 3] = NAN
+    x[10] = -INF
+    x[10, 776] = INF
+    u = [0.5, 0.9, 0.7, 0.1, 0.3, 0.5, 0.9, 0.5, 0.6, 0.999, 0.5, 0.5]
+    for kw in ({}, dict(top_k=[2] * 12), dict(top_p=[0.6] * 12), dict(min_p=[0.5] * 12), dict(top_k=[400] * 12, top_p=[0.5] * 12, min_p=[1e-3] * 12), dict(temperature=[0.0] * 12),
+               dict(temperature=[1e-38] * 12), dict(temperature=[3e38] * 12)):
+        got = check(x, u, **kw)
+        assert got[0] == got[3] == got[11] == -1 and got[1] == 700 and got[10] == 776
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_parameters_at_the_ends(dtype):
+    x, _ = spread(8, 3001, dtype, seed=3)
+    ends = [0.0, 1.0 - 2.0 ** -24, 1.0, 0.5, 1e-30, 0.25, 0.75, 0.999]
+    check(x, ends)
+    check(x, ends, temperature=[0.0, -1.0, NAN, 1e-6, 1e6, INF, 0.01, 50.0])
+    check(x, ends, top_k=[0, -5, 1, 3001, 3002, 1 << 30, 3000, 256])
+    check(x, ends, top_p=[0.0, -1.0, NAN, 1.0, 2.0, 1e-7, 0.9999999, 0.5])
+    check(x, ends, min_p=[0.0, -1.0, NAN, 1.0, 2.0, 1e-30, 0.999, 0.5])
+    # a number that is no number draws the first
+    token, _ = pkg().sample(x, row([NAN] * 8))
+    assert token.tolist() == x.float().cpu().numpy().argmax(1).tolist()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("V", [1000, 32001])
+def test_rows_of_a_wider_tensor(V, dtype):
+    x, u = spread(5, V + 11, dtype, seed=V)
+    for first in (0, 1, 3, 8):
+        check(x[:, first:first + V], u, top_p=[0.9] * 5)
+    check(x[::2, :V], u[:3], top_k=[30] * 3)
+
+
+def test_steep_and_flat_rows():
+    """One token that holds nearly all, and all tokens alike."""
+    x = torch.zeros(6, 60000, device=DEV)
+    x[0, 77], x[1, 5], x[2, 59999] = 40.0, 15.0, 11.0
+    x[3:] = torch.linspace(0, 1e-3, 60000, device=DEV)
+    u = [0.999, 0.99, 0.5, 0.1, 0.5, 0.95]
+    check(x, u)
+    check(x, u, top_p=[0.999999, 0.9, 0.7, 0.3, 0.999, 0.5])
+    check(x, u, min_p=[1e-9, 1e-3, 0.1, 0.9999, 0.9995, 0.5])
+
+
+def test_many_rows():
+    x, u = spread(700, 333, "fp32", seed=8)
+    check(x, u, top_p=[0.3 + 0.001 * r for r in range(700)], top_k=[r % 50 for r in range(700)])
+
+
+def test_the_numbers_of_a_distribution():
+    """u on a fine grid draws every token as often as its probability says."""
+    V, n = 50, 4000
+    x = torch.randn(1, V, device=DEV, generator=torch.Generator(device=DEV).manual_seed(1)).expand(n, V).contiguous()
+    u = (torch.arange(n, device=DEV) + 0.5) / n
+    token, logprob = pkg().sample(x, u.float())
+    share = torch.softmax(x[0].double(), 0).cpu()
+    count = torch.bincount(token.long().cpu(), minlength=V).double() / n
+    assert (count - share).abs().max() <= 1.5 / n
+    np.testing.assert_allclose(logprob.double().cpu().exp().numpy(), share[token.long().cpu()].numpy(), rtol=1e-5)
+
+
+def test_a_captured_call():
+    x, u = spread(20, 20000, "bf16", seed=1)
+    p = pkg()
+    uniform, t = row(u), torch.full((20,), 0.8, device=DEV)
+    top_k, top_p = torch.full((20,), 500, dtype=torch.int32, device=DEV), torch.full((20,), 0.95, device=DEV)
+    ws = torch.empty(p.sample_workspace(x), dtype=torch.uint8, device=DEV)
+    token, logprob = torch.empty(20, dtype=torch.int32, device=DEV), torch.empty(20, device=DEV)
+    call = lambda: p.sample(x, uniform, temperature=t, top_k=top_k, top_p=top_p, token=token, logprob=logprob, workspace=ws)
+    call()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call()
+    for i in range(5):
+        x.copy_(spread(20, 20000, "bf16", seed=10 + i)[0])
+        uniform.copy_(torch.rand(20, device=DEV, generator=torch.Generator(device=DEV).manual_seed(i)))
+        want, want_lp = p.sample(x, uniform, temperature=t, top_k=top_k, top_p=top_p)
+        ws.fill_(255)
+        token.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(token, want) and torch.equal(logprob, want_lp)
