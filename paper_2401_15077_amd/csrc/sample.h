@@ -2,17 +2,42 @@
 #pragma once
 #include "rows.h"
 #include "rope.h"
+#include <type_traits>
 
 typedef unsigned long long u64;
 
 struct SampleDev {
-  int n_rows, vocab, bits;                 // weights are multiples of 2^-bits of the largest one
+  int n_rows, vocab, bits, unit;           // masses are multiples of 2^-bits of the largest weight, parts of 2^-unit
   const void* logits;
   long long stride;
   const float *uniform, *temperature, *top_p, *min_p;
   const int* top_k;
   int* token; float* logprob;
 };
+
+// Sums and the like over a wave, by moves between neighbouring lanes (a step of a shuffle through LDS takes ten times as long).  What comes from outside the row of 16 is `none`.
+template <int MOVE, int ROWS = 0xF> __device__ __forceinline__ u64 moved(u64 x, u64 none) {
+  const uint32_t lo = __builtin_amdgcn_update_dpp((int)none, (int)x, MOVE, ROWS, 0xF, false), hi = __builtin_amdgcn_update_dpp((int)(none >> 32), (int)(x >> 32), MOVE, ROWS, 0xF, false);
+  return (u64)hi << 32 | lo;
+}
+// Lane l: f over lanes 0 .. l.  (Lanes 1, 2, 4, 8 back; the last lane of a row into the next; of the lower half into the upper.)
+template <typename F> __device__ __forceinline__ u64 wave_scan(u64 x, u64 none, F f) {
+  x = f(x, moved<0x111>(x, none));
+  x = f(x, moved<0x112>(x, none));
+  x = f(x, moved<0x114>(x, none));
+  x = f(x, moved<0x118>(x, none));
+  x = f(x, moved<0x142, 0xA>(x, none));
+  return f(x, moved<0x143, 0xC>(x, none));
+}
+__device__ __forceinline__ u64 last_lane(u64 x) {
+  return (u64)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), 63) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
+}
+struct Add { __device__ u64 operator()(u64 a, u64 b) const { return a + b; } };
+struct Least { __device__ u64 operator()(u64 a, u64 b) const { return min(a, b); } };
+struct Most { __device__ u64 operator()(u64 a, u64 b) const { return max(a, b); } };
+__device__ __forceinline__ u64 wave_sum(u64 x) { return last_lane(wave_scan(x, 0, Add())); }
+__device__ __forceinline__ u64 wave_min(u64 x) { return last_lane(wave_scan(x, ~0ull, Least())); }
+__device__ __forceinline__ u64 wave_max(u64 x) { return last_lane(wave_scan(x, 0, Most())); }
 
 // The order of the tokens, by value, descending, equal ones by index, as the order of 64-bit numbers.
 __device__ __forceinline__ uint32_t order_of(float x) {
@@ -25,206 +50,496 @@ __device__ __forceinline__ float value_of(uint32_t order) {
 }
 __device__ __forceinline__ u64 place_of(float x, int i) { return (u64)order_of(x) << 32 | (uint32_t)i; }
 
-// A work-group takes a row.  Nothing is sorted: what is looked for is the token in whose share of the running mass (or count) a given number falls.  A histogram of the masses over buckets of
-// equal width in log(weight), which keep the order, says the bucket; its tokens are listed, by histograms over ever smaller ranges of (value, index) until few are left, and those are ranked
-// pair by pair.  Masses are whole numbers (of 2^-bits of the largest weight) in 64 bits, so sums come out the same in any order.
-constexpr int SAMPLE_BUCKETS = 4096, SAMPLE_LIST = 1024, SAMPLE_PAIRS = 128, SAMPLE_TOP = 256;
+// Nothing is sorted: what is looked for is the token in whose share of the running mass (or count) a given number falls.  A histogram over buckets of equal width in log(weight), which keep the
+// order, says the bucket; its tokens are listed, through histograms over ever smaller ranges of (value, index) where they are many, and the last few are ranked pair by pair.  Where top-k or
+// min-p leaves few tokens, these are listed and ranked at once.
+//
+// A weight is 2^(-y / 64), y = (largest - logit) * 64 log2(e) / temperature, bucket b the nearest whole number to y, and what is added up is 2^((b - y) / 64) in whole multiples of 2^-unit, so
+// that no order of additions changes a sum: 13 operations a logit, in 64 bits, since y has to be known to far more than 24.  Four terms of the exponential series leave out 4 * 10^-14 of a weight.
+// A bucket's sum times 2^(-b / 64) is its mass, in multiples of 2^-bits of the largest weight.  The last bucket holds what lies 2^-64 below, which is as good as nothing.
+constexpr int SAMPLE_BUCKETS = 4096, SAMPLE_LIST = 1024, SAMPLE_PAIRS = 128, SAMPLE_FEW = 256;
+
+// What a row asks for.
+struct SampleRow {
+  bool greedy, top_k, top_p, min_p;
+  int k;
+  double rate, p, log_least, u;
+};
+// The same in every lane: kept in scalar registers.
+__device__ __forceinline__ double uniform(double x) {
+  const u64 b = __builtin_bit_cast(u64, x);
+  return __builtin_bit_cast(double, (u64)(uint32_t)__builtin_amdgcn_readfirstlane((int)(b >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)b));
+}
+__device__ __forceinline__ u64 uniform(u64 x) { return __builtin_bit_cast(u64, uniform(__builtin_bit_cast(double, x))); }
+__device__ __forceinline__ float uniform(float x) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x))); }
+__device__ inline SampleRow sample_row(const SampleDev& A, int r) {
+  SampleRow q;
+  const float temperature = A.temperature ? A.temperature[r] : 1.f, p = A.top_p ? A.top_p[r] : 1.f, least = A.min_p ? A.min_p[r] : 0.f, u = A.uniform[r];
+  q.k = A.top_k ? A.top_k[r] : 0;
+  q.greedy = !(temperature > 0.f);
+  q.top_k = q.k > 0 && q.k < A.vocab; q.top_p = p < 1.f; q.min_p = least > 0.f;
+  q.rate = uniform(1.0 / (double)temperature);
+  q.p = uniform(fmax((double)p, 0.0));
+  q.log_least = q.min_p ? uniform(log((double)least)) : 0.0;
+  q.u = uniform(u > 0.f ? fmin((double)u, 1.0) : 0.0);
+  return q;
+}
+
+// f(logits, first token, how many) of tokens first .. last - 1 of a row for the work-group's threads, a run at a time, in no order.  A run past the end is NaN.
+template <typename T, int NT, typename F>
+__device__ __forceinline__ void each_run(const T* row, int first, int last, F f) {
+  constexpr int VE = 16 / sizeof(T), GROUP = 16 / VE;
+  const int tid = threadIdx.x, n = last - first, head = min(n, (int)((16 - (uintptr_t)(row + first) % 16) % 16 / sizeof(T))), body = (n - head) / VE;
+  const uint4* p = (const uint4*)(row + first + head);
+  if (body > 0) {
+    uint4 raw[GROUP];
+    auto ask = [&](int i0) {
+#pragma unroll
+      for (int u = 0; u < GROUP; ++u) raw[u] = p[min(i0 + u * NT, body - 1)];
+    };
+    ask(tid);
+#pragma unroll 1
+    for (int i0 = tid; i0 - tid < body; i0 += NT * GROUP) {
+      uint4 now[GROUP];
+#pragma unroll
+      for (int u = 0; u < GROUP; ++u) now[u] = raw[u];
+      if (i0 - tid + NT * GROUP > body) {
+#pragma unroll
+        for (int u = 0; u < GROUP; ++u)
+          if (i0 + u * NT >= body) now[u] = uint4{~0u, ~0u, ~0u, ~0u};
+      }
+      ask(i0 + NT * GROUP);
+#pragma unroll
+      for (int u = 0; u < GROUP; ++u) {
+        float x[VE];
+        load_run<VE>((const T*)(now + u), x);
+        f(x, first + head + (i0 + u * NT) * VE, std::integral_constant<int, VE>());
+        __builtin_amdgcn_sched_barrier(0);                        // (a run after the other: all at once would take more registers than there are)
+      }
+    }
+  }
+  // what is in front of the first run and behind the last: a token each for some threads
+  const int t = tid < head ? first + tid : first + head + body * VE + (tid - 32);
+  if (tid < head || (tid >= 32 && t < last)) {
+    float x[1];
+    load_run<1>(row + t, x);
+    f(x, t, std::integral_constant<int, 1>());
+  }
+}
+
 template <typename T>
 __global__ __launch_bounds__(1024) void k_sample(const SampleDev A) {
-  __shared__ u64 hist[SAMPLE_BUCKETS], sub[SAMPLE_BUCKETS], list[2][SAMPLE_LIST], mass[SAMPLE_TOP], s_wave[16], s_low, s_high, s_found[3];
+  __shared__ u64 hist[SAMPLE_BUCKETS + 64], sub[SAMPLE_BUCKETS], list[2][SAMPLE_LIST], mass[SAMPLE_FEW], s_wave[16], s_low, s_high, s_found[3];
+  __shared__ double root[64];                                     // powers of 2^(-1 / 64)
   __shared__ int s_n, s_bucket;
-  constexpr int VE = 16 / sizeof(T);
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, V = A.vocab, r = blockIdx.x;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), V = A.vocab, r = blockIdx.x;
   const T* row = (const T*)A.logits + r * A.stride;
-  auto each = [&](auto f) {                                       // f(logit, token) of the row, NaN as -inf
-    auto clean = [](float x) { return x == x ? x : -INFINITY; };
-    const int head = min(V, (int)((16 - (uintptr_t)row % 16) % 16 / sizeof(T))), body = (V - head) / VE;
-    float x[VE];
-    if (tid < head) { load_run<1>(row + tid, x); f(clean(x[0]), tid); }
-    for (int i = tid; i < body; i += 1024) {
-      load_run<VE>(row + head + i * VE, x);
+  const SampleRow Q = sample_row(A, r);
+  auto runs = [&](auto f) { each_run<T, 1024>(row, 0, V, f); };
+  // f(first token, bits of those from `least` to `most`) of the runs that have such; few are expected.
+  auto between = [&](float least, float most, auto f) {
+    runs([&](const float* x, int t, auto n) {
+      uint32_t hits = 0;
 #pragma unroll
-      for (int j = 0; j < VE; ++j) f(clean(x[j]), head + i * VE + j);
-    }
-    const int t = head + body * VE + tid;
-    if (t < V) { load_run<1>(row + t, x); f(clean(x[0]), t); }
+      for (int j = 0; j < decltype(n)::value; ++j) hits |= __builtin_amdgcn_fmed3f(x[j], least, most) == x[j] ? 1u << j : 0u;
+      if (hits) f(t, hits);
+    });
   };
-  auto sum_all = [&](u64 x) -> u64 {                              // of the work-group
-    for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o, 64);
-    __syncthreads();
-    if (lane == 0) s_wave[wave] = x;
-    __syncthreads();
-    x = 0;
-    for (int i = 0; i < 16; ++i) x += s_wave[i];
-    return x;
+  auto logit = [&](int t) { float x; load_run<1>(row + t, &x); return x; };
+  auto each_bit = [&](int t, uint32_t hits, auto f) {             // f(logit, token)
+    for (; hits; hits &= hits - 1) f(logit(t + __builtin_ctz(hits)), t + __builtin_ctz(hits));
   };
-  float top = -INFINITY;
-  each([&](float x, int) { top = fmaxf(top, x); });
-  for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-  float* s_top = (float*)s_wave;
-  if (lane == 0) s_top[wave] = top;
-  __syncthreads();
-  for (int i = 0; i < 16; ++i) top = fmaxf(top, s_top[i]);
-  const float temperature = A.temperature ? A.temperature[r] : 1.f;
   auto answer = [&](int token, float logprob) {
-    if (tid > 0) return;
     A.token[r] = token;
     if (A.logprob) A.logprob[r] = logprob;
   };
-  if (top == -INFINITY) { answer(-1, -INFINITY); return; }
-  if (!(temperature > 0.f)) {                                     // the first of the largest
-    u64 best = ~0ull;
-    each([&](float x, int t) { if (x == top) best = min(best, (u64)t); });
-    if (tid == 0) s_low = ~0ull;
+  float top = -INFINITY;
+  runs([&](const float* x, int, auto n) {
+#pragma unroll
+    for (int j = 0; j < decltype(n)::value; ++j) top = fmaxf(top, x[j]);
+  });
+  {
+    const u64 first = wave_min(order_of(top));
+    if (tid < 64) root[tid] = exp2(tid * (-1.0 / 64.0));
+    if (lane == 0) s_wave[wave] = first;
+    if (tid == 0) { s_low = ~0ull; s_n = 0; }
     __syncthreads();
-    atomicMin(&s_low, best);
-    __syncthreads();
-    answer((int)s_low, 0.f);
+    u64 least = ~0ull;
+    for (int i = 0; i < 16; ++i) least = min(least, s_wave[i]);
+    top = uniform(value_of((uint32_t)least));
+  }
+  if (top == -INFINITY) {
+    if (tid == 0) answer(-1, -INFINITY);
     return;
   }
-  const double rate = 1.0 / (double)temperature, one = ldexp(1.0, A.bits);
-  auto weight = [&](float x) -> u64 {
-    if (x == -INFINITY) return 0;
-    if (top == INFINITY) return x == top ? 1ull << A.bits : 0ull;
-    return (u64)(exp(((double)x - (double)top) * rate) * one + 0.5);
+  if (Q.greedy) {                                                 // the first of the largest
+    u64 best = ~0ull;
+    between(top, top, [&](int t, uint32_t hits) { best = min(best, (u64)(t + __builtin_ctz(hits))); });
+    if (best != ~0ull) atomicMin(&s_low, best);
+    __syncthreads();
+    if (tid == 0) answer((int)s_low, 0.f);
+    return;
+  }
+  if (top == INFINITY) {                                          // those alone, all alike: the n-th of them
+    u64 n = 0;
+    between(top, top, [&](int, uint32_t hits) { n += __popc(hits); });
+    n = wave_sum(n);
+    __syncthreads();
+    if (lane == 0) s_wave[wave] = n;
+    __syncthreads();
+    n = 0;
+    for (int i = 0; i < 16; ++i) n += s_wave[i];
+    if (Q.top_k) n = min(n, (u64)Q.k);
+    if (Q.top_p) n = min(n, max(1ull, (u64)ceil(Q.p * (double)n)));
+    if (Q.min_p && Q.log_least > 0.0) n = 1;
+    u64 left = min((u64)(Q.u * (double)n), n - 1);
+    for (int t0 = 0; t0 < V; t0 += 1024) {
+      float x = 0.f;
+      if (t0 + tid < V) load_run<1>(row + t0 + tid, &x);
+      const uint64_t those = __ballot(x == top);
+      __syncthreads();
+      if (lane == 0) s_wave[wave] = __popcll(those);
+      __syncthreads();
+      u64 before = 0, all = 0;
+      for (int i = 0; i < 16; ++i) { if (i < wave) before += s_wave[i]; all += s_wave[i]; }
+      if (x == top && before + __popcll(those & ((1ull << lane) - 1)) == left) answer(t0 + tid, (float)-log((double)n));
+      if (left < all) return;
+      left -= all;
+    }
+    return;
+  }
+
+  const double step = uniform(fmax(Q.rate * (64 * 1.4426950408889634), 1e-290)), farthest = uniform((SAMPLE_BUCKETS - 1) / step), magic = 6755399441055744.0;   // 1.5 * 2^52: what is added to it is rounded to a whole number
+  const double top64 = uniform((double)top), one = uniform(ldexp(1.0, A.unit));
+  struct Bucket { int b; double rest; };
+  auto bucket_of = [&](double d) -> Bucket {                      // b and y - b
+    const double k = fma(d, step, magic);
+    return Bucket{(int)(uint32_t)__builtin_bit_cast(u64, k), fma(d, step, magic - k)};
   };
-  const float slope = fminf((float)(rate * (1.4426950408889634 * SAMPLE_BUCKETS / 32)), 3.4e38f);   // the last bucket begins 2^-32 below the largest weight
-  auto bucket = [&](float x) -> int { return x == -INFINITY ? SAMPLE_BUCKETS - 1 : x == top ? 0 : (int)fminf((top - x) * slope, SAMPLE_BUCKETS - 1.f); };
+  auto bucket = [&](float x) { return bucket_of(fmin(top64 - (double)x, farthest)); };
+  // 2^(-rest / 64): three terms behind the 1 leave out 4 * 10^-11.  The last sum is one with 2^52, so it ends on a whole number, in the lower 52 bits; what is above them is left to whoever adds up.
+  constexpr double L = 0.010830424696249145;                      // ln 2 / 64
+  const double first = uniform(one + 4503599627370496.0), c1 = uniform(-L * one), c2 = uniform(L * L / 2 * one), c3 = uniform(-L * L * L / 6 * one);
+  auto part_above = [&](double rest) -> u64 { return __builtin_bit_cast(u64, fma(fma(fma(rest, c3, c2), rest, c1), rest, first)); };
+  constexpr u64 LOWER = 0xFFFFFFFFFFFFFull;
+  auto part = [&](double rest) -> u64 { return part_above(rest) & LOWER; };
+  // Adds the parts of a run's tokens (or 1 each) to their buckets; what is far below, and NaN, goes to a place of the lane's behind them.
+  const float low = uniform((float)(top64 - farthest) - (fabsf(top) + (float)fmin(farthest, 1e30)) * 1e-6f);   // (a little below what is far below)
+  auto add_run = [&](const float* x, auto n, bool by_mass) {
+    constexpr int N = decltype(n)::value;
+    float most = x[0];
+#pragma unroll
+    for (int j = 1; j < N; ++j) most = fmaxf(most, x[j]);
+    if (!(most >= low)) return;
+    if (by_mass) {
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const double d = top64 - (double)x[j];
+        const Bucket b = bucket_of(d);
+        atomicAdd(&hist[d < farthest ? b.b : SAMPLE_BUCKETS + lane], part_above(b.rest));
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const double d = top64 - (double)x[j];
+        atomicAdd(&hist[d < farthest ? bucket_of(d).b : SAMPLE_BUCKETS + lane], 1ull);
+      }
+    }
+  };
+  auto exponent = [&](float x) -> double { return ((double)x - top64) * Q.rate; };   // ln(weight)
+  auto heavy = [&](float x) { return exponent(x) >= Q.log_least; };                  // min-p keeps it
+  // a little below the least that min-p keeps (at a temperature that is infinite, no bound)
+  const float scaled = (float)(top64 + Q.log_least / Q.rate), cut = uniform(Q.rate > 0.0 ? fminf(top, scaled - fabsf(scaled) * 1e-6f - 1e-30f) : -INFINITY);
+
+  auto scale_of = [&](int b) { return ldexp(root[b & 63], A.bits - A.unit - (b >> 6)); };   // a part of bucket b as a mass
   auto clear = [&](u64* h) {
-    for (int i = tid; i < SAMPLE_BUCKETS; i += 1024) h[i] = 0;
+    for (int i = 2 * tid; i < SAMPLE_BUCKETS; i += 2048) *(ulonglong2*)(h + i) = ulonglong2{0, 0};
     __syncthreads();
   };
-  // The bucket that the number falls into and what is in front of it.
-  auto find = [&](const u64* h, u64 target, u64* before) -> int {
-    constexpr int EACH = SAMPLE_BUCKETS / 1024;
-    u64 x[EACH], sum = 0;
+  // The running sums of a histogram, four buckets a thread.
+  constexpr int EACH = SAMPLE_BUCKETS / 1024;
+  struct Sums { u64 at, x[EACH], total; };
+  auto scan = [&](const u64* h, bool masses) -> Sums {
+    Sums s;
+    u64 sum = 0;
     __syncthreads();
-    for (int i = 0; i < EACH; ++i) { x[i] = h[tid * EACH + i]; sum += x[i]; }
-    u64 upto = sum;
-    for (int o = 1; o < 64; o <<= 1) { const u64 y = __shfl_up(upto, o, 64); if (lane >= o) upto += y; }
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      s.x[i] = h[tid * EACH + i] & LOWER;
+      if (masses) s.x[i] = (u64)((double)s.x[i] * scale_of(tid * EACH + i));
+      sum += s.x[i];
+    }
+    u64 upto = wave_scan(sum, 0, Add());
     if (lane == 63) s_wave[wave] = upto;
     __syncthreads();
-    for (int i = 0; i < wave; ++i) upto += s_wave[i];
-    u64 at = upto - sum;
-    if (at <= target && target < upto) {
-      int i = 0;
-      while (target >= at + x[i]) at += x[i++];
-      s_bucket = tid * EACH + i;
-      s_found[0] = at;
+    u64 total = 0;
+    for (int i = 0; i < 16; ++i) { const u64 y = s_wave[i]; if (i < wave) upto += y; total += y; }
+    s.at = upto - sum; s.total = uniform(total);
+    return s;
+  };
+  // The bucket that the number falls into -> s_bucket, what is in front of it -> s_found[0], what it holds -> s_found[1].
+  auto find = [&](const Sums& s, u64 target) {
+    u64 at = s.at;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      if (at <= target && target < at + s.x[i]) { s_bucket = tid * EACH + i; s_found[0] = at; s_found[1] = s.x[i]; }
+      at += s.x[i];
     }
     __syncthreads();
-    *before = s_found[0];
-    return s_bucket;
+  };
+  // The first place in the order whose bucket is at least b, for a whole wave.
+  auto edge = [&](int b) -> uint32_t {
+    uint32_t lo = order_of(top), hi = order_of(-INFINITY) + 1;
+    if (b <= 0) return lo;
+    while (hi - lo > 1) {
+      const uint32_t by = (hi - lo + 63) / 64, at = lo + by * (lane + 1);
+      const uint64_t yes = __ballot(at >= hi || bucket(value_of(at)).b >= b);
+      const int f = __builtin_ctzll(yes | 1ull << 63);
+      const uint32_t next = lo + by * (f + 1);
+      lo += by * f;
+      hi = min(hi, next);
+    }
+    return (uint32_t)__builtin_amdgcn_readfirstlane((int)hi);
+  };
+  auto mass_of = [&](float x) -> u64 {
+    const Bucket b = bucket(x);
+    return b.b < SAMPLE_BUCKETS - 1 ? (u64)((double)part(b.rest) * scale_of(b.b)) : 0ull;
   };
   struct Found { u64 place, before, share; };
-  // The token in whose share (its weight, or 1) of the tokens up to `limit` the number falls; h: histogram of those shares.
-  auto select = [&](const u64* h, u64 target, bool by_mass, u64 limit) -> Found {
-    auto share = [&](float x) -> u64 { return by_mass ? weight(x) : 1ull; };
-    u64 before;
-    const int b = find(h, target, &before);
-    u64 in_front = before, low = 0, high = 0;
-    bool ranged = false;
+  // Of the tokens up to `limit` in bucket b, the one in whose share (its part, or 1) the number falls.
+  auto select = [&](int b, u64 target, bool by_mass, u64 limit) -> Found {
+    auto share = [&](u64 place) -> u64 { return by_mass ? part(bucket(value_of((uint32_t)(place >> 32))).rest) : 1ull; };
+    u64 low = (u64)edge(b) << 32, high = min(limit, ((u64)edge(b + 1) << 32) - 1), in_front = 0;
+    auto narrow = [&](int shift) {                                // to the bucket of `sub` that the number falls into
+      const Sums s = scan(sub, false);
+      find(s, target - in_front);
+      in_front += uniform(s_found[0]);
+      low += (u64)__builtin_amdgcn_readfirstlane(s_bucket) << shift;
+      high = min(high, low + ((1ull << shift) - 1));
+    };
+    auto width = [&]() -> int {
+      const u64 range = high - low;
+      return max(0, 64 - __builtin_clzll(range | 1) - 12);        // (range >> width < 4096)
+    };
+    // f(logits, first token, bits of those in the range) of every run: where a value's tokens lie on both sides of an end
+    auto in_range = [&](auto f) {
+      runs([&](const float* x, int t, auto n) {
+        uint32_t hits = 0;
+#pragma unroll
+        for (int j = 0; j < decltype(n)::value; ++j) {
+          const u64 p = place_of(x[j], t + j);
+          hits |= x[j] == x[j] && p >= low && p <= high ? 1u << j : 0u;
+        }
+        if (hits) f(t, hits);
+      });
+    };
+    auto note = [&](int t, uint32_t hits) {
+      int i = atomicAdd(&s_n, __popc(hits));
+      for (; hits && i < SAMPLE_LIST; hits &= hits - 1) list[1][i++] = t + __builtin_ctz(hits);
+    };
     int n;
-    for (;;) {                                                    // list the bucket's tokens, or those of the range
+    for (bool ranged = false;; ranged = true) {                   // (every turn leaves a 2048th of the range at most, so that one of SAMPLE_LIST tokens is reached)
       if (tid == 0) { s_n = 0; s_low = ~0ull; s_high = 0; }
       __syncthreads();
-      u64 lo = ~0ull, hi = 0;
-      each([&](float x, int t) {
-        const u64 p = place_of(x, t);
-        if (p > limit || (ranged ? p < low || p > high : bucket(x) != b)) return;
-        const int i = atomicAdd(&s_n, 1);
-        if (i < SAMPLE_LIST) list[0][i] = p;
-        lo = min(lo, p); hi = max(hi, p);
-      });
-      if (hi) { atomicMin(&s_low, lo); atomicMax(&s_high, hi); }
+      if (!ranged) between(value_of((uint32_t)(high >> 32)), value_of((uint32_t)(low >> 32)), note);
+      else in_range(note);
       __syncthreads();
-      n = s_n; low = s_low; high = s_high;
+      n = __builtin_amdgcn_readfirstlane(s_n);
       if (n <= SAMPLE_LIST) break;
-      int shift = 0;
-      while ((high - low) >> shift >= SAMPLE_BUCKETS) ++shift;
+      const int shift = width();
       clear(sub);
-      each([&](float x, int t) {
-        const u64 p = place_of(x, t);
-        if (p >= low && p <= high && p <= limit) atomicAdd(&sub[(p - low) >> shift], share(x));
+      in_range([&](int t, uint32_t hits) {
+        for (; hits; hits &= hits - 1) {
+          const u64 p = place_of(logit(t + __builtin_ctz(hits)), t + __builtin_ctz(hits));
+          atomicAdd(&sub[(p - low) >> shift], share(p));
+        }
       });
-      const int c = find(sub, target - in_front, &before);
-      in_front += before;
-      low += (u64)c << shift;
-      high = min(high, low + ((1ull << shift) - 1));
-      ranged = true;
+      narrow(shift);
+    }
+    {
+      const int t = tid < n ? (int)list[1][tid] : 0;
+      const u64 p = place_of(logit(t), t);
+      const bool mine = tid < n && p >= low && p <= high;         // (of the last value some may lie behind the limit)
+      u64 lo = mine ? p : ~0ull, hi = mine ? p : 0;
+      lo = wave_min(lo);
+      hi = wave_max(hi);
+      __syncthreads();
+      if (tid == 0) s_n = 0;
+      if (lane == 0 && hi) { atomicMin(&s_low, lo); atomicMax(&s_high, hi); }
+      __syncthreads();
+      if (mine) list[0][atomicAdd(&s_n, 1)] = p;
+      __syncthreads();
+      n = __builtin_amdgcn_readfirstlane(s_n);
+      if (n > 0) { low = uniform(s_low); high = uniform(s_high); }
     }
     int from = 0;
     while (n > SAMPLE_PAIRS) {                                    // the same on the list
-      int shift = 0;
-      while ((high - low) >> shift >= SAMPLE_BUCKETS) ++shift;
+      const int shift = width();
       clear(sub);
       const u64 p = tid < n ? list[from][tid] : 0;
-      if (tid < n) atomicAdd(&sub[(p - low) >> shift], share(value_of((uint32_t)(p >> 32))));
-      const int c = find(sub, target - in_front, &before);
-      in_front += before;
+      if (tid < n) atomicAdd(&sub[(p - low) >> shift], share(p));
+      narrow(shift);
       if (tid == 0) s_n = 0;
       __syncthreads();
-      low += (u64)c << shift;
-      high = min(high, low + ((1ull << shift) - 1));
       if (tid < n && p >= low && p <= high) list[from ^ 1][atomicAdd(&s_n, 1)] = p;
       __syncthreads();
-      n = s_n;
+      n = __builtin_amdgcn_readfirstlane(s_n);
       from ^= 1;
       __syncthreads();
     }
     // what lies in front of each of the few, eight threads each
-    if (tid < n) mass[tid] = share(value_of((uint32_t)(list[from][tid] >> 32)));
+    if (tid < n) mass[tid] = share(list[from][tid]);
     __syncthreads();
     const int mine = tid >> 3;
     const u64 p = mine < n ? list[from][mine] : 0;
     u64 at = 0;
     for (int j = tid & 7; j < n; j += 8) at += list[from][j] < p ? mass[j] : 0;
-    for (int o = 4; o; o >>= 1) at += __shfl_xor(at, o, 64);
+    at += moved<0xB1>(at, 0);                                     // lanes two by two, four by four, and eight by eight
+    at += moved<0x4E>(at, 0);
+    at += moved<0x141>(at, 0);
     at += in_front;
     if (mine < n && (tid & 7) == 0 && at <= target && target < at + mass[mine]) { s_found[0] = p; s_found[1] = at; s_found[2] = mass[mine]; }
     __syncthreads();
-    const Found f{s_found[0], s_found[1], s_found[2]};
+    const Found f{uniform(s_found[0]), uniform(s_found[1]), uniform(s_found[2])};
     __syncthreads();
     return f;
   };
-  auto histogram = [&](bool by_mass, u64 limit) {
-    clear(hist);
-    each([&](float x, int t) {
-      if (limit != ~0ull && place_of(x, t) > limit) return;
-      const u64 w = by_mass ? weight(x) : 1ull;
-      if (w) atomicAdd(&hist[bucket(x)], w);
+  auto finish = [&](u64 place, u64 kept) {                        // one thread
+    const float x = value_of((uint32_t)(place >> 32));
+    answer((int)(uint32_t)place, (float)(exponent(x) - log(ldexp((double)kept, -A.bits))));
+  };
+  // All of at most SAMPLE_FEW tokens in list[0], or the first `most` of them in order, are what top-p, min-p and the number choose from.
+  auto few = [&](int n, int most) {
+    const int mine = tid >> 2;
+    const u64 p = mine < n ? list[0][mine] : 0;
+    int rank = 0;
+    for (int j = tid & 3; j < n; j += 4) rank += list[0][j] < p;
+    rank += (int)moved<0xB1>(rank, 0);
+    rank += (int)moved<0x4E>(rank, 0);
+    const float x = value_of((uint32_t)(p >> 32));
+    if (mine < n && (tid & 3) == 0) {
+      list[1][rank] = p;
+      mass[rank] = rank < most ? mass_of(x) : 0ull;
+    }
+    __syncthreads();
+    if (wave > 0) return;
+    u64 m[4], sum = 0, strong = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int j = 4 * lane + i;
+      m[i] = j < n ? mass[j] : 0;
+      sum += m[i];
+      if (Q.min_p && m[i] && heavy(value_of((uint32_t)(list[1][j] >> 32)))) strong += m[i];
+    }
+    const u64 upto = wave_scan(sum, 0, Add());
+    u64 kept = last_lane(upto);
+    if (Q.top_p) {
+      const u64 need = max(1ull, (u64)ceil(Q.p * (double)kept));
+      u64 at = upto - sum, least = ~0ull;
+#pragma unroll
+      for (int i = 3; i >= 0; --i) {                              // (from the end: the least running sum that reaches it)
+        u64 run = at;
+#pragma unroll
+        for (int j = 0; j <= i; ++j) run += m[j];
+        if (run >= need) least = run;
+      }
+      kept = min(kept, wave_min(least));
+    }
+    if (Q.min_p) {
+      kept = min(kept, max(wave_sum(strong), 1ull << A.bits));
+    }
+    const u64 target = min((u64)(Q.u * (double)kept), kept - 1);
+    u64 at = upto - sum;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (at <= target && target < at + m[i]) finish(list[1][4 * lane + i], kept);
+      at += m[i];
+    }
+  };
+  auto gather = [&](float least) -> int {                         // tokens of at least this value: into list[0], if they are few enough
+    if (tid == 0) s_n = 0;
+    __syncthreads();
+    between(least, top, [&](int t, uint32_t hits) {
+      int i = atomicAdd(&s_n, __popc(hits));
+      for (; hits && i < SAMPLE_FEW; hits &= hits - 1) list[1][i++] = t + __builtin_ctz(hits);
     });
     __syncthreads();
+    const int n = __builtin_amdgcn_readfirstlane(s_n);
+    if (tid < min(n, SAMPLE_FEW)) list[0][tid] = place_of(logit((int)list[1][tid]), (int)list[1][tid]);
+    __syncthreads();
+    return n;
   };
-  const int k = A.top_k ? A.top_k[r] : 0;
-  const float p = A.top_p ? A.top_p[r] : 1.f, least = A.min_p ? A.min_p[r] : 0.f, uniform = A.uniform[r];
-  const double u = uniform > 0.f ? fmin((double)uniform, 1.0) : 0.0;
-  const double log_least = least > 0.f ? log((double)least) : 0.0;
-  auto heavy = [&](float x) { return x == top || (top != INFINITY && ((double)x - (double)top) * rate >= log_least); };   // min-p keeps it
-  u64 limit = ~0ull;
-  if (k > 0 && k < V) {
-    histogram(false, ~0ull);
-    limit = select(hist, (u64)k - 1, false, ~0ull).place;
+
+  // Three boundaries, one after the other: the last token of top-k, the last of top-p, the token itself.
+  enum { LAST_K, LAST_P, TOKEN };
+  u64 limit = ~0ull, kept = 0;
+  Sums s;
+  bool tried = false;
+  float least = !Q.top_k && Q.min_p && !Q.top_p ? cut : NAN;      // tokens from here on may be few (NaN: not known)
+#pragma unroll 1
+  for (int stage = Q.top_k ? LAST_K : LAST_P;; ++stage) {
+    u64 target = (u64)Q.k - 1;
+    if (stage != TOKEN) {
+      if (least == least) {
+        const int n = gather(least);
+        if (n <= SAMPLE_FEW) { few(n, Q.top_k ? Q.k : V); return; }
+        __syncthreads();
+        least = NAN;
+      }
+      clear(hist);
+      if (limit == ~0ull) runs([&](const float* x, int, auto n) { add_run(x, n, stage == LAST_P); });
+      else runs([&](const float* x, int t, auto n) {
+        float y[decltype(n)::value];
+#pragma unroll
+        for (int j = 0; j < decltype(n)::value; ++j) y[j] = place_of(x[j], t + j) <= limit ? x[j] : NAN;
+        add_run(y, n, true);
+      });
+      s = scan(hist, stage == LAST_P);
+    }
+    if (stage == LAST_K) {
+      if (target >= s.total) continue;                            // (the last of them weighs nothing: no bound)
+    } else if (stage == LAST_P) {
+      kept = s.total;
+      if (!Q.top_p) stage = TOKEN;
+      else target = uniform(min(max(1ull, (u64)ceil(Q.p * (double)kept)), kept) - 1);
+    }
+    if (stage == TOKEN) {
+      if (Q.min_p) {
+        u64 m = 0;
+        between(cut, top, [&](int t, uint32_t hits) {
+          each_bit(t, hits, [&](float x, int i) {
+            if (heavy(x) && place_of(x, i) <= limit) m += mass_of(x);
+          });
+        });
+        m = wave_sum(m);
+        __syncthreads();
+        if (lane == 0) s_wave[wave] = m;
+        __syncthreads();
+        m = 0;
+        for (int i = 0; i < 16; ++i) m += s_wave[i];
+        kept = uniform(min(kept, max(m, 1ull << A.bits)));
+      }
+      target = uniform(min((u64)(Q.u * (double)kept), kept - 1));
+    }
+    find(s, target);
+    const int b = __builtin_amdgcn_readfirstlane(s_bucket);
+    const u64 before = uniform(s_found[0]), inside = uniform(hist[b] & LOWER);
+    if (stage == LAST_K && before + inside <= SAMPLE_FEW && !tried) {
+      tried = true;
+      least = value_of(edge(b + 1) - 1);
+      __syncthreads();
+      stage = LAST_K - 1;
+      continue;
+    }
+    __syncthreads();
+    // inside the bucket the number counts in the bucket's own units
+    const double scale = stage == LAST_K ? 1.0 : scale_of(b);
+    const Found f = select(b, min((u64)((double)(target - before) / scale), inside - 1), stage != LAST_K, limit);
+    if (stage == LAST_K) limit = f.place;
+    else if (stage == LAST_P) kept = uniform(min(kept, before + (u64)((double)(f.before + f.share) * scale)));
+    else {
+      if (tid == 0) finish(f.place, kept);
+      return;
+    }
   }
-  histogram(true, limit);
-  u64 total = 0;
-  for (int i = tid; i < SAMPLE_BUCKETS; i += 1024) total += hist[i];
-  total = sum_all(total);
-  u64 kept = total;
-  if (p < 1.f) {
-    const u64 need = (u64)ceil(fmax((double)p, 0.0) * (double)total);
-    const Found f = select(hist, need > 0 ? need - 1 : 0, true, limit);
-    kept = f.before + f.share;
-  }
-  if (least > 0.f) {
-    u64 m = 0;
-    each([&](float x, int t) { if (heavy(x) && (limit == ~0ull || place_of(x, t) <= limit)) m += weight(x); });
-    m = sum_all(m);
-    kept = min(kept, max(m, 1ull << A.bits));
-  }
-  const u64 target = min((u64)(u * (double)kept), kept - 1);
-  const Found f = select(hist, target, true, limit);
-  const float x = value_of((uint32_t)(f.place >> 32));
-  const double t = top == INFINITY ? 0.0 : ((double)x - (double)top) * rate;
-  answer((int)(uint32_t)f.place, (float)(t - log((double)kept / one)));
 }

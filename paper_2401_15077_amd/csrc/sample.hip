@@ -38,9 +38,9 @@ extern "C" int eagle_sample(const eagle_sample_args* a, void* workspace, size_t 
   const size_t need = eagle_sample_workspace(a);
   if (!workspace || !aligned(workspace, 256)) return fail(EAGLE_EINVAL, "sample: workspace must be a 256-byte aligned device pointer");
   if (workspace_bytes < need) return fail(EAGLE_ENOMEM, "sample: workspace of %zu bytes is smaller than the %zu needed", workspace_bytes, need);
-  int bits = 62;                                                  // (as many weights of at most 2^bits add up to at most 2^62)
+  int bits = 62;                                                  // (as many weights of at most 2^bits add up to at most 2^62, and parts to less than 2^52)
   while ((long long)a->vocab > 1ll << (62 - bits)) --bits;
-  const SampleDev d{a->n_rows, a->vocab, bits, a->logits, a->stride, a->uniform, a->temperature, a->top_p, a->min_p, a->top_k, a->token, a->logprob};
+  const SampleDev d{a->n_rows, a->vocab, bits, bits - 11, a->logits, a->stride, a->uniform, a->temperature, a->top_p, a->min_p, a->top_k, a->token, a->logprob};
   const hipStream_t stream = (hipStream_t)hip_stream;
   if (a->dtype == EAGLE_F32) k_sample<float><<<a->n_rows, 1024, 0, stream>>>(d);
   else k_sample<bf16_t><<<a->n_rows, 1024, 0, stream>>>(d);
