@@ -158,6 +158,7 @@ __global__ __launch_bounds__(1024) void k_sample(const SampleDev A) {
 #pragma unroll
     for (int j = 0; j < decltype(n)::value; ++j) top = fmaxf(top, x[j]);
   });
+  const float best_here = top;                                    // of this thread's tokens
   {
     const u64 first = wave_min(order_of(top));
     if (tid < 64) root[tid] = exp2(tid * (-1.0 / 64.0));
@@ -474,7 +475,7 @@ __global__ __launch_bounds__(1024) void k_sample(const SampleDev A) {
   enum { LAST_K, LAST_P, TOKEN };
   u64 limit = ~0ull, kept = 0;
   Sums s;
-  bool tried = false;
+  bool by_threads = Q.top_k && Q.k <= SAMPLE_FEW, tried = false;
   float least = !Q.top_k && Q.min_p && !Q.top_p ? cut : NAN;      // tokens from here on may be few (NaN: not known)
 #pragma unroll 1
   for (int stage = Q.top_k ? LAST_K : LAST_P;; ++stage) {
@@ -487,7 +488,9 @@ __global__ __launch_bounds__(1024) void k_sample(const SampleDev A) {
         least = NAN;
       }
       clear(hist);
-      if (limit == ~0ull) runs([&](const float* x, int, auto n) { add_run(x, n, stage == LAST_P); });
+      if (by_threads) {
+        if (top64 - (double)best_here < farthest) atomicAdd(&hist[bucket(best_here).b], 1ull);
+      } else if (limit == ~0ull) runs([&](const float* x, int, auto n) { add_run(x, n, stage == LAST_P); });
       else runs([&](const float* x, int t, auto n) {
         float y[decltype(n)::value];
 #pragma unroll
@@ -495,6 +498,17 @@ __global__ __launch_bounds__(1024) void k_sample(const SampleDev A) {
         add_run(y, n, true);
       });
       s = scan(hist, stage == LAST_P);
+    }
+    if (by_threads) {
+      // The k-th largest of the threads' own largest tokens is no larger than the k-th of all, and hardly smaller: what is not below its bucket is listed.
+      by_threads = false;
+      if (target < s.total) {
+        find(s, target);
+        least = value_of(edge(__builtin_amdgcn_readfirstlane(s_bucket) + 1) - 1);
+      }
+      __syncthreads();
+      stage = LAST_K - 1;
+      continue;
     }
     if (stage == LAST_K) {
       if (target >= s.total) continue;                            // (the last of them weighs nothing: no bound)
