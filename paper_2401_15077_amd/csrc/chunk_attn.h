@@ -173,24 +173,42 @@ __device__ __forceinline__ bf16x8 coded8(u32x2 u, int8_code_t) {
 template <int ROW> __device__ __forceinline__ int k_place(int t, int c) { return t * (ROW / 8) + (c ^ (ROW == 96 ? t >> 2 & 3 : t & 7)); }
 template <int ROW> __device__ __forceinline__ int v_place(int t, int c) { return t * (ROW / 8) + (c ^ (ROW == 128 ? (t & 3) << 2 : ROW == 64 ? (t & 2) << 1 : 0)); }
 
+// RAW: 16 codes (piece c) of token t lie in piece c ^ turn(t) of its row.  Keys are read a token a lane, 16 lanes at a time: 16 tokens' pieces lie in 16 different 16-byte columns; values
+// transposed, 16 tokens by 32 bytes at a time: twice in each of the 64 banks.
+template <int ROW> __device__ __forceinline__ int raw_k_turn(int t) { return ROW == 128 ? t >> 1 & 7 : t >> 2 & 3; }
+template <int ROW> __device__ __forceinline__ int raw_v_turn(int t) { return ROW == 128 ? (t >> 1 & 3) << 1 : (t >> 2 & 1) << 1; }
+// Lane l of 16 gets code l of the eight 16-code rows whose l / 2-th this address is in.
+__device__ __forceinline__ u32x2 read_transposed8(const char* p) {
+  typedef int i32x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2*)p));
+}
+// Not 0 if one of the e4m3 codes is NaN: seven ones carry into the sign's place.
+__device__ __forceinline__ uint32_t nan_codes(u32x4 v) {
+  uint32_t any = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) any |= (v[e] & 0x7F7F7F7Fu) + 0x01010101u;
+  return any & 0x80808080u;
+}
+
 __device__ __forceinline__ s16x4 read_transposed(const bf16_t* p) {   // lane l of 16 gets element l of the four 16-element rows whose l / 4-th this address is in
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p);
 }
 
 // Tokens of a tile, by shape, whether queries are fp32, and bytes of an element of the cache.
-constexpr int tile_tokens(bool wide, bool fp32, int bytes) { return wide && (bytes == 2 || (bytes == 1 && !fp32)) ? 64 : 32; }
+constexpr int tile_tokens(bool wide, bool fp32, int bytes) { return (bytes == 1 && !fp32) || (bytes == 2 && wide) ? 64 : 32; }
 
 template <typename T, typename CT, int DH_, bool WIDE_, bool MODS_>
 struct ChunkAttn {
   static constexpr int DH = DH_, NQ = sizeof(T) == 4 ? 3 : 1, NK = sizeof(CT) == 4 ? 3 : 1, NP = NQ > NK ? NQ : NK;
   static constexpr bool WIDE = WIDE_, MODS = MODS_, CODED = sizeof(CT) == 1;
   // bf16 caches go from memory to LDS without passing through registers (DIRECT); fp32 ones are split into their pieces on the way.  The narrow shape has fp32 keys in registers.
-  static constexpr bool DIRECT = sizeof(CT) == 2, KEYS_IN_LDS = WIDE || NK == 1;
+  // Codes do so in the narrow shape, as they are (RAW: a wave has its tile for itself, and makes bf16 of what it reads); in the wide one they become bf16 on the way, once for four waves.
+  static constexpr bool DIRECT = sizeof(CT) == 2, RAW = CODED && !WIDE, KEYS_IN_LDS = WIDE || NK == 1;
   static constexpr int KT = tile_tokens(WIDE, NQ == 3, sizeof(CT)), KB = KT / 32, KSN = DH / 16, DB = DH / 32;
   static constexpr int COLS = WIDE ? 128 : 32;
-  static constexpr int ROW = DIRECT && DH == 96 ? 128 : DH;       // elements of a token in LDS (a DIRECT load fills 1 KiB: whole tokens)
+  static constexpr int ROW = (DIRECT || RAW) && DH == 96 ? 128 : DH;   // elements of a token in LDS (a DIRECT load fills 1 KiB: whole tokens)
   static constexpr int PART = DH <= 64 ? 64 : 128;                // and in the workspace
-  static constexpr int TILE = KT * ROW;                           // elements of a piece of a tile
+  static constexpr int TILE = RAW ? KT * ROW / 2 : KT * ROW;      // elements (of 2 bytes) of a piece of a tile
   static constexpr int OWNERS = WIDE ? 1 : 4;                     // waves with a tile of their own
   static constexpr int K_ELTS = KEYS_IN_LDS ? OWNERS * NK * TILE : 8, V_ELTS = OWNERS * NK * TILE;   // of one buffer
   static constexpr bool TWO = WIDE;                               // buffers
@@ -205,8 +223,8 @@ struct ChunkAttn {
   static constexpr bool done_with(int n) { return NK == 3 ? n == 0 || n == 2 || n == 5 : n == PRODUCTS - 1; }   // the cache piece of product n
   static constexpr int WAVES = NK == 3 && (DH == 128 || (DH == 96 && !WIDE)) ? 1 : 2;      // a SIMD holds (by registers)
   static constexpr bool SPLIT = WIDE && NK == 3;                   // fp32 keys and values go through LDS in pieces
-  static constexpr int RUNS = DH == 64 ? 4 : 8, THREADS = WIDE ? 256 : 64;   // CODED: runs of 16 codes of a token, threads that fetch a tile
-  static constexpr int ITEMS = SPLIT ? KT * DH / 4 / 256 : CODED ? (KT * RUNS + THREADS - 1) / THREADS : KT * DH / 8 / 64;   // runs of 4 (SPLIT) or 8 elements a thread fetches of the values, and of the keys if they go through LDS
+  static constexpr int RUNS = DH == 64 ? 4 : 8;                   // CODED, WIDE: runs of 16 codes of a token
+  static constexpr int ITEMS = SPLIT ? KT * DH / 4 / 256 : CODED ? (KT * RUNS + 255) / 256 : KT * DH / 8 / 64;   // runs of 4 (SPLIT) or 8 elements a thread fetches of the values, and of the keys if they go through LDS
 };
 
 typedef __attribute__((address_space(3))) bf16_t* lds_ptr;
@@ -225,7 +243,7 @@ __device__ __forceinline__ void wait_lds() {
 template <typename P, typename T, typename CT>
 __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev A) {
   constexpr int DH = P::DH, ROW = P::ROW, NQ = P::NQ, NK = P::NK, KT = P::KT, KB = P::KB, KSN = P::KSN, DB = P::DB, COLS = P::COLS, TILE = P::TILE, ITEMS = P::ITEMS;
-  constexpr bool WIDE = P::WIDE, MODS = P::MODS, DIRECT = P::DIRECT, CODED = P::CODED;
+  constexpr bool WIDE = P::WIDE, MODS = P::MODS, DIRECT = P::DIRECT, CODED = P::CODED, RAW = P::RAW;
   // (arrays of their own: the compiler tells reads of one from loads on their way into another)
   __shared__ __attribute__((aligned(16))) bf16_t k_lds0[P::K_ELTS], k_lds1[P::TWO ? P::K_ELTS : 8], v_lds0[P::V0_ELTS], v_lds1[P::TWO ? P::V_ELTS : 8];
   __shared__ int s_bad[2];                                        // WIDE, not DIRECT: number of the last tile in a buffer whose values are not all finite
@@ -278,20 +296,28 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
   constexpr int STEP = WIDE ? 1 : 4;
   const int in_page = (1 << A.kv.page_shift) - 1;
   const CT *kb = (const CT*)A.kv.k + kvh * A.kv.head_stride, *vb = (const CT*)A.kv.v + kvh * A.kv.head_stride;
-  // Narrow and DIRECT: a wave has one buffer for keys and one for values; the next keys are on their way from the end of the scores on, the next values from the end of the products on.
-  constexpr bool STAGGERED = !WIDE && DIRECT;
+  // Narrow and DIRECT or RAW: a wave has one buffer for keys and one for values; the next keys are on their way from the end of the scores on, the next values from the end of the products on.
+  constexpr bool STAGGERED = !WIDE && (DIRECT || RAW);
   constexpr int MINE = WIDE ? 0 : NK * TILE;                      // a wave's place in a buffer: w * MINE
 
   // ---- DIRECT: a load instruction fills 1 KiB of LDS, RPI tokens of DH elements; lane -> (token, place), and the piece of 8 elements that belongs in the place.  What is not there (a page, a
   // token behind the last, elements from head_dim on) is whatever lies in page 0, or in the head's first piece: finite or not, it is masked like what a column may not see.
-  constexpr int RPI = 512 / ROW, INSTS = DIRECT ? KT / RPI / (WIDE ? 4 : 1) : 1;
-  const int tr = lane / (ROW / 8), place = lane % (ROW / 8);
-  // bytes from an instruction's first token to what this lane loads (the keys' order of pieces repeats every eight tokens, the values' every RPI)
-  uint32_t k_off[8 / RPI], v_off;
-  {
+  constexpr int RPI = (RAW ? 1024 : 512) / ROW, RUNS = ROW * (int)sizeof(CT) / 16, INSTS = DIRECT || RAW ? KT / RPI / (WIDE ? 4 : 1) : 1, ORDERS = DIRECT ? 8 / RPI : RAW ? 16 / RPI : 1;
+  const int tr = lane / RUNS, place = lane % RUNS;
+  // bytes from an instruction's first token to what this lane loads (the keys' order of pieces repeats every eight tokens (RAW: 16), the values' every RPI)
+  uint32_t k_off[ORDERS], v_off;
+  if constexpr (RAW) {
+#pragma unroll
+    for (int i = 0; i < ORDERS; ++i) {
+      const int kc = place ^ raw_k_turn<ROW>(i * RPI + tr);
+      k_off[i] = (uint32_t)(tr * (int)A.kv.token_stride + (kc * 16 < dh ? kc * 16 : 0));
+    }
+    const int vc = place ^ raw_v_turn<ROW>(tr);
+    v_off = (uint32_t)(tr * (int)A.kv.token_stride + (vc * 16 < dh ? vc * 16 : 0));
+  } else {
     const int vc = place ^ (v_place<ROW>(tr, 0) - tr * (ROW / 8));
 #pragma unroll
-    for (int i = 0; i < 8 / RPI; ++i) {
+    for (int i = 0; i < ORDERS; ++i) {
       const int t = i * RPI + tr, kc = place ^ (k_place<ROW>(t, 0) - t * (ROW / 8));
       k_off[i] = (uint32_t)(tr * (int)A.kv.token_stride + (kc * 8 < dh ? kc * 8 : 0)) * (uint32_t)sizeof(CT);
     }
@@ -322,16 +348,16 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
 #pragma unroll
       for (int u = 0; u < INSTS; ++u) {
         const int t0 = (first + u) * RPI;
-        if constexpr (K) load_lds((const char*)(kb + at[u]) + k_off[u % (8 / RPI)], kd + t0 * ROW);
-        if constexpr (V) load_lds((const char*)(vb + at[u]) + v_off, vd + t0 * ROW);
+        if constexpr (K) load_lds((const char*)(kb + at[u]) + k_off[u % ORDERS], kd + t0 * (RAW ? ROW / 2 : ROW));
+        if constexpr (V) load_lds((const char*)(vb + at[u]) + v_off, vd + t0 * (RAW ? ROW / 2 : ROW));
       }
     } else {
 #pragma unroll
       for (int u = 0; u < INSTS; ++u) {
         const int t0 = (first + u) * RPI, page = max(0, __shfl(pages, t0 + tr, 64));
         const long long at = page * A.kv.page_stride + (((k0 + t0 + tr) & in_page) - tr) * A.kv.token_stride;
-        if constexpr (K) load_lds((const char*)(kb + at) + k_off[u % (8 / RPI)], kd + t0 * ROW);
-        if constexpr (V) load_lds((const char*)(vb + at) + v_off, vd + t0 * ROW);
+        if constexpr (K) load_lds((const char*)(kb + at) + k_off[u % ORDERS], kd + t0 * (RAW ? ROW / 2 : ROW));
+        if constexpr (V) load_lds((const char*)(vb + at) + v_off, vd + t0 * (RAW ? ROW / 2 : ROW));
       }
     }
   };
@@ -340,24 +366,24 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
   f32x4 k4[P::SPLIT ? ITEMS : 1], v4[P::SPLIT ? ITEMS : 1];
   typedef Raw8<std::conditional_t<CODED, bf16_t, CT>> Raw;
   Raw kr[DIRECT || CODED || WIDE ? 1 : KSN], vr[DIRECT || CODED || WIDE ? 1 : ITEMS];
-  u32x4 k16[CODED ? ITEMS : 1], v16[CODED ? ITEMS : 1];
+  u32x4 k16[CODED && WIDE ? ITEMS : 1], v16[CODED && WIDE ? ITEMS : 1];
   float2 sc_fetched = {1.f, 1.f}, sc_next = {1.f, 1.f};           // CODED: scales of the keys and values of the lane's token of the fetched tile, of the one in LDS
+  auto scales = [&](int it, int pages) -> float2 {                // CODED: of the keys and values of the lane's token
+    if (pages < 0) return float2{1.f, 1.f};
+    const long long at = pages * A.scale_page + kvh * A.scale_head + (((tile_token(it) + (lane_now() & (KT - 1))) & in_page) >> A.block_shift);
+    return float2{fabsf(A.k_scale[at]), fabsf(A.v_scale[at])};
+  };
   auto fetch = [&](int it, int pages) {
     const int k0 = tile_token(it);
-    if constexpr (CODED) {
-      const int mine = WIDE ? tid : lane_now();
+    if constexpr (CODED && WIDE) {
 #pragma unroll
       for (int i = 0; i < ITEMS; ++i) {
-        const int item = i * P::THREADS + mine, t = item / P::RUNS, c = item % P::RUNS, page = __shfl(pages, t & (KT - 1), 64);
+        const int item = i * 256 + tid, t = item / P::RUNS, c = item % P::RUNS, page = __shfl(pages, t & (KT - 1), 64);
         const long long at = page * A.kv.page_stride + ((k0 + t) & in_page) * A.kv.token_stride + c * 16;
         k16[i] = v16[i] = u32x4{0, 0, 0, 0};
         if (t < KT && page >= 0 && c * 16 < dh) { k16[i] = *(const u32x4*)(kb + at); v16[i] = *(const u32x4*)(vb + at); }
       }
-      sc_fetched = float2{1.f, 1.f};
-      if (pages >= 0) {
-        const long long at = pages * A.scale_page + kvh * A.scale_head + (((k0 + (mine & (KT - 1))) & in_page) >> A.block_shift);
-        sc_fetched = float2{fabsf(A.k_scale[at]), fabsf(A.v_scale[at])};
-      }
+      sc_fetched = scales(it, pages);
     } else if constexpr (P::SPLIT) {                              // a token is eight threads': every eighth run of 4 elements
       const int l = lane_now(), t = 8 * w + (l >> 3), c = l & 7, page = __shfl(pages, t, 64);
       const long long at = page * A.kv.page_stride + ((k0 + t) & in_page) * A.kv.token_stride + 4 * c;
@@ -368,7 +394,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
         k4[i] = k;
         v4[i] = v;
       }
-    } else if constexpr (!WIDE) {
+    } else if constexpr (!WIDE && !CODED) {
 #pragma unroll
       for (int i = 0; i < ITEMS; ++i) {
         const int item = i * 64 + lane, t = item / (DH / 8), c = item % (DH / 8);
@@ -417,10 +443,9 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
 #pragma unroll
       for (int n = 0; n < 12 * ITEMS; ++n) bad |= put_step(kd, vd, n, pk);
     } else if constexpr (CODED) {
-      const int mine = WIDE ? tid : lane_now();
 #pragma unroll
       for (int i = 0; i < ITEMS; ++i) {
-        const int item = i * P::THREADS + mine, t = item / P::RUNS, c = item % P::RUNS;
+        const int item = i * 256 + tid, t = item / P::RUNS, c = item % P::RUNS;
         if (t >= KT || c * 16 >= DH) continue;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -455,6 +480,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
   }
   if constexpr (STAGGERED) {
     if (it < t_end) {
+      if constexpr (RAW) sc_next = scales(it, pages);
       dma((lds_ptr)k_lds0 + w * MINE, (lds_ptr)v_lds0, it, pages, KEYS());
       dma((lds_ptr)k_lds0, (lds_ptr)v_lds0 + w * MINE, it, pages, VALUES());
     }
@@ -468,7 +494,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
     const T* qp = (const T*)A.q + c.row * A.q_row + c.head * A.q_head;
 #pragma unroll
     for (int ks = 0; ks < KSN; ++ks) {
-      const int d = 16 * ks + 8 * hh;
+      const int d = RAW ? 32 * (ks >> 1) + 16 * hh + 8 * (ks & 1) : 16 * ks + 8 * hh;   // (RAW: a lane reads 16 codes of a key at once, for two steps)
       Raw8<T> x;
       x.zero();
       if (c.live && d < dh) x.load(qp + d);
@@ -504,11 +530,17 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
     for (int r = 0; r < 16; ++r) oacc[b][r] = 0.f;
 
   // Byte offsets in a buffer of what this lane reads of a tile: the keys' k-steps 0..3 (the others, and the second 32 tokens, lie a constant further on), the values' 32-wide blocks.
+  // RAW: of a key's pieces hh, 2 + hh, ..; of the values' blocks, a pair of 16-wide columns each.
   uint32_t k_at[4], v_at[DB];                                     // (rows of 96 elements: pieces 4 to 7 lie behind 0 to 3 in the same order)
 #pragma unroll
-  for (int i = 0; i < 4; ++i) k_at[i] = ROW == 96 && i > 1 ? k_at[i - 2] + 64 : 16 * k_place<ROW>(q, 2 * i + hh);
+  for (int i = 0; i < 4; ++i) k_at[i] = RAW ? (uint32_t)(q * ROW + 16 * (((2 * i + hh) ^ raw_k_turn<ROW>(q)) & (RUNS - 1))) : ROW == 96 && i > 1 ? k_at[i - 2] + 64 : 16 * k_place<ROW>(q, 2 * i + hh);
 #pragma unroll
   for (int b = 0; b < DB; ++b) {
+    if constexpr (RAW) {
+      const int r8 = (lane & 15) >> 1, t = 4 * hh + (r8 & 3) + 8 * (r8 >> 2), c = 2 * b + ((lane >> 4) & 1);
+      v_at[b] = t * ROW + 16 * ((c ^ raw_v_turn<ROW>(t)) & (RUNS - 1)) + 8 * (lane & 1);
+      continue;
+    }
     const int t = 4 * hh + ((lane & 15) >> 2), c = 4 * b + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
     v_at[b] = 16 * v_place<ROW>(t, c) + 8 * (lane & 1);
   }
@@ -532,10 +564,8 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
       if constexpr (WIDE) { __builtin_amdgcn_s_barrier(); asm volatile("" ::: "memory"); }
       if (it + STEP < t_end) dma((lds_ptr)kn, (lds_ptr)vn, it + STEP, pages_next, BOTH());
     } else if constexpr (CODED) {
-      if constexpr (!WIDE) sc = sc_fetched;
-      put(WIDE ? kn : kt, WIDE ? vn : vt);
-      if constexpr (WIDE) sc_next = sc_fetched;
-      else if (it + STEP < t_end) fetch(it + STEP, pages_next);
+      put(kn, vn);
+      sc_next = sc_fetched;
     } else if constexpr (WIDE) {
       bad = s_bad[which] == it;
     } else {
@@ -566,6 +596,26 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
           next_bad |= put_step(kn, vn, n, pk);
           __builtin_amdgcn_sched_barrier(0);
         }
+      } else if constexpr (RAW) {                                 // a read is two k-steps; as below
+        constexpr int PAIRS = KSN / 2, READS = KB * PAIRS, AHEAD = 2;
+        auto raw = [&](int n) -> u32x4 { return *(const u32x4*)((const char*)kt + k_at[n % PAIRS] + 32 * ROW * (n / PAIRS)); };
+        u32x4 kr[AHEAD];
+#pragma unroll
+        for (int n = 0; n < AHEAD; ++n) kr[n] = raw(n);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int n = 0; n < READS; ++n) {
+          const u32x4 k = kr[n % AHEAD];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const bf16x8 kf = coded8(u32x2{k[2 * h], k[2 * h + 1]}, CT());
+#pragma unroll
+            for (int u = 0; u < P::PRODUCTS; ++u)
+              sacc[n / PAIRS] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[P::column_piece(u)][2 * (n % PAIRS) + h], sacc[n / PAIRS], 0, 0, 0);
+          }
+          if (n + AHEAD < READS) kr[n % AHEAD] = raw(n + AHEAD);
+          __builtin_amdgcn_sched_barrier(0);
+        }
       } else if constexpr (P::KEYS_IN_LDS) {                      // reads some k-steps ahead of their products: LDS answers in the time of about four products
         constexpr int STEPS = KB * KSN, AHEAD = NQ == 3 ? 2 : 4;
         bf16x8 kf[AHEAD];
@@ -593,6 +643,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
       if (it + STEP < t_end) fetch(it + STEP, pages_next);        // (the keys' registers are free now)
     }
     if constexpr (STAGGERED && !LAST) {
+      if constexpr (RAW) sc_next = scales(it + STEP, pages_next);
       wait_lds();                                                 // the keys have been read
       dma((lds_ptr)kt, (lds_ptr)vt, it + STEP, pages_next, KEYS());
     }
@@ -754,13 +805,48 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
     }
     }
     if constexpr (STAGGERED) wait_loads<LAST ? 0 : INSTS>();   // the values have landed
-    if (NK == 1 && !full) {                                       // is there anything that is not finite among the values?
+    if (RAW && !full && std::is_same<CT, e4m3_t>::value) {        // is there a NaN among the values?
+      uint32_t any = 0;
+#pragma unroll 4
+      for (int i = 0; i < TILE / 512; ++i) any |= nan_codes(*(const u32x4*)(vt + i * 512 + lane * 8));
+      bad = __any(any != 0);
+    }
+    if (NK == 1 && !RAW && !full) {                                       // is there anything that is not finite among the values?
       uint32_t any = 0;
 #pragma unroll 4
       for (int i = 0; i < TILE / 512; ++i) any |= exponents(*(const u32x4*)(vt + i * 512 + lane * 8));
       bad = __any(any != 0);
     }
-    if (bad) {
+    if (RAW && bad) {
+      // 0 times NaN is not 0.  So it is added to the columns that see it, and zeroed for the product.
+      uint64_t spoilt = 0;
+#pragma unroll 1
+      for (int i = 0; i < TILE / 512; ++i) {
+        if (nan_codes(*(const u32x4*)(vt + i * 512 + lane * 8)) != 0) spoilt |= 1ull << ((i * 64 + lane) / RUNS);
+      }
+      for (int o = 32; o; o >>= 1) spoilt |= __shfl_xor((unsigned long long)spoilt, o, 64);
+      for (uint64_t left = spoilt & there; left; left &= left - 1) {
+        const int t = __builtin_ctzll(left);
+        const bool seen = vis >> t & 1;
+#pragma unroll
+        for (int b = 0; b < DB; ++b)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int d = 32 * b + 8 * i + 4 * hh;
+            const uint32_t v = *(const uint32_t*)((const char*)vt + t * ROW + 16 * (((d >> 4) ^ raw_v_turn<ROW>(t)) & (RUNS - 1)) + (d & 15));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) oacc[b][4 * i + e] += seen && (v >> (8 * e) & 0x7Fu) == 0x7Fu ? NAN : 0.f;
+            __builtin_amdgcn_sched_barrier(0);
+          }
+      }
+#pragma unroll 1
+      for (int i = 0; i < TILE / 512; ++i) {
+        u32x4 v = *(const u32x4*)(vt + i * 512 + lane * 8);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] &= ~((((v[e] & 0x7F7F7F7Fu) + 0x01010101u & 0x80808080u) >> 7) * 0xFFu);
+        *(u32x4*)(vt + i * 512 + lane * 8) = v;
+      }
+    } else if (bad) {
       // 0 times what is not finite is not 0.  So it is added to the columns that see it, and zeroed for the product.
       uint64_t spoilt = 0;
 #pragma unroll 1
@@ -819,6 +905,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
     u32x4 pf[2][NQ];
     constexpr int AHEAD = NK == 3 ? 1 : NQ == 3 ? 2 : 4;          // (of three pieces each is read again as soon as it is done with)
     bf16x8 vf[AHEAD][NK];
+    u32x2 vraw[AHEAD];                                            // RAW
     float sum = 0.f;
     auto weights = [&](int jj, int n) {                           // n of WORK steps: a pair's weights and their first piece, its second, its third
       const int pair = NQ == 3 ? n / 3 : n, j = NQ == 3 ? n % 3 : 0, a = jj >> 1, r = 8 * (jj & 1) + 2 * pair;
@@ -839,6 +926,10 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
       }
     };
     auto value = [&](int i, int j) {                              // piece j of block i % DB of 16 tokens
+      if constexpr (RAW) {
+        vraw[i % AHEAD] = read_transposed8((const char*)vt + v_at[i % DB] + 16 * ROW * (i / DB));
+        return;
+      }
       const char* p = (const char*)vt + v_at[i % DB] + (2 * j * TILE + 32 * ROW * (i / DB));
       const s16x4 lo = read_transposed((const bf16_t*)p), hi = read_transposed((const bf16_t*)(p + 16 * ROW));
       vf[i % AHEAD][j] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
@@ -852,6 +943,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
 #pragma unroll
     for (int i = 0; i < GROUPS; ++i) {
       const int jj = i / DB, b = i % DB;
+      if constexpr (RAW) vf[i % AHEAD][0] = coded8(vraw[i % AHEAD], CT());
 #pragma unroll
       for (int u = 0; u < P::PRODUCTS; ++u) {
         const int j = P::cache_piece(u), slot = b * P::PRODUCTS + u;
