@@ -224,8 +224,18 @@ struct ChunkAttn {
   static constexpr int WAVES = NK == 3 && (DH == 128 || (DH == 96 && !WIDE)) ? 1 : 2;      // a SIMD holds (by registers)
   static constexpr bool SPLIT = WIDE && NK == 3;                   // fp32 keys and values go through LDS in pieces
   static constexpr int RUNS = DH == 64 ? 4 : 8;                   // CODED, WIDE: runs of 16 codes of a token
+  static constexpr int PARKED = CODED && WIDE ? 2 * 8 * 256 * ((KT * RUNS + 255) / 256) : 8;
   static constexpr int ITEMS = SPLIT ? KT * DH / 4 / 256 : CODED ? (KT * RUNS + 255) / 256 : KT * DH / 8 / 64;   // runs of 4 (SPLIT) or 8 elements a thread fetches of the values, and of the keys if they go through LDS
 };
+
+struct ScoreRow {
+  float v[16];
+  __device__ __forceinline__ float& operator[](int i) { return v[i]; }
+};
+template <bool FIRST, typename A, typename B> __device__ __forceinline__ auto& one_of(A& a, B& b) {
+  if constexpr (FIRST) return a;
+  else return b;
+}
 
 typedef __attribute__((address_space(3))) bf16_t* lds_ptr;
 // At most N vector-memory operations of this wave under way; all of its LDS operations done.  No access to memory moves across.
@@ -246,6 +256,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
   constexpr bool WIDE = P::WIDE, MODS = P::MODS, DIRECT = P::DIRECT, CODED = P::CODED, RAW = P::RAW;
   // (arrays of their own: the compiler tells reads of one from loads on their way into another)
   __shared__ __attribute__((aligned(16))) bf16_t k_lds0[P::K_ELTS], k_lds1[P::TWO ? P::K_ELTS : 8], v_lds0[P::V0_ELTS], v_lds1[P::TWO ? P::V_ELTS : 8];
+  __shared__ __attribute__((aligned(16))) bf16_t parked[P::PARKED];  // CODED, WIDE: the codes of the tile after the next
   __shared__ int s_bad[2];                                        // WIDE, not DIRECT: number of the last tile in a buffer whose values are not all finite
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane & 31, hh = lane >> 5;
   // The lane, worked out anew: inside the loop, what can be had from the thread's number in an instruction or two is not kept (the widest shapes hold all 256 registers).
@@ -366,8 +377,8 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
   f32x4 k4[P::SPLIT ? ITEMS : 1], v4[P::SPLIT ? ITEMS : 1];
   typedef Raw8<std::conditional_t<CODED, bf16_t, CT>> Raw;
   Raw kr[DIRECT || CODED || WIDE ? 1 : KSN], vr[DIRECT || CODED || WIDE ? 1 : ITEMS];
-  u32x4 k16[CODED && WIDE ? ITEMS : 1], v16[CODED && WIDE ? ITEMS : 1];
-  float2 sc_fetched = {1.f, 1.f}, sc_next = {1.f, 1.f};           // CODED: scales of the keys and values of the lane's token of the fetched tile, of the one in LDS
+  float2 sc_next = {1.f, 1.f};                                    // CODED: scales of the keys and values of the lane's token of the next tile
+  const uint32_t run_off = CODED && WIDE ? lane / P::RUNS * (uint32_t)A.kv.token_stride + (lane % P::RUNS * 16 < dh ? lane % P::RUNS * 16u : 0u) : 0u;   // from a wave's first token to this lane's run
   auto scales = [&](int it, int pages) -> float2 {                // CODED: of the keys and values of the lane's token
     if (pages < 0) return float2{1.f, 1.f};
     const long long at = pages * A.scale_page + kvh * A.scale_head + (((tile_token(it) + (lane_now() & (KT - 1))) & in_page) >> A.block_shift);
@@ -375,15 +386,15 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
   };
   auto fetch = [&](int it, int pages) {
     const int k0 = tile_token(it);
-    if constexpr (CODED && WIDE) {
+    if constexpr (CODED && WIDE) {                                // (the tokens of a wave's 64 runs lie in one page, whose place stays in scalar registers; what is not there: as for DIRECT)
 #pragma unroll
       for (int i = 0; i < ITEMS; ++i) {
-        const int item = i * 256 + tid, t = item / P::RUNS, c = item % P::RUNS, page = __shfl(pages, t & (KT - 1), 64);
-        const long long at = page * A.kv.page_stride + ((k0 + t) & in_page) * A.kv.token_stride + c * 16;
-        k16[i] = v16[i] = u32x4{0, 0, 0, 0};
-        if (t < KT && page >= 0 && c * 16 < dh) { k16[i] = *(const u32x4*)(kb + at); v16[i] = *(const u32x4*)(vb + at); }
+        const int t0 = (i * 256 + 64 * w) / P::RUNS;
+        if (t0 >= KT) break;
+        const long long at = max(0, __builtin_amdgcn_readlane(pages, t0 & (KT - 1))) * A.kv.page_stride + ((k0 + t0) & in_page) * A.kv.token_stride;
+        load_lds((const char*)kb + at + run_off, (lds_ptr)parked + (2 * i * 256 + 64 * w) * 8);
+        load_lds((const char*)vb + at + run_off, (lds_ptr)parked + ((2 * i + 1) * 256 + 64 * w) * 8);
       }
-      sc_fetched = scales(it, pages);
     } else if constexpr (P::SPLIT) {                              // a token is eight threads': every eighth run of 4 elements
       const int l = lane_now(), t = 8 * w + (l >> 3), c = l & 7, page = __shfl(pages, t, 64);
       const long long at = page * A.kv.page_stride + ((k0 + t) & in_page) * A.kv.token_stride + 4 * c;
@@ -435,6 +446,21 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
     }
     return bad;
   };
+  // CODED, WIDE: the parked codes, and a step of 4 ITEMS that make bf16 of them: eight elements of the keys or values.
+  u32x4 held[CODED && WIDE ? 2 * ITEMS : 1];
+  auto take = [&]() {
+#pragma unroll
+    for (int i = 0; i < 2 * ITEMS; ++i) held[i] = *(const u32x4*)(parked + (i * 256 + tid) * 8);
+  };
+  auto code_step = [&](bf16_t* kd, bf16_t* vd, int n) {
+    const int i = n >> 2, h = n & 1, item = i * 256 + tid, t = item / P::RUNS, c = item % P::RUNS;
+    const bool values = n & 2;
+    const u32x4 u = held[2 * i + values];
+    if constexpr (CODED) {
+      const bf16x8 x = coded8(u32x2{u[2 * h], u[2 * h + 1]}, CT());
+      if (t < KT && c * 16 < DH) *(bf16x8*)(values ? vd + 8 * v_place<ROW>(t, 2 * c + h) : kd + 8 * k_place<ROW>(t, 2 * c + h)) = x;
+    }
+  };
   // the fetched tile to LDS; returns not 0 if a value is not finite (to this thread's knowledge)
   auto put = [&](bf16_t* kd, bf16_t* vd) -> uint32_t {
     uint32_t bad = 0;
@@ -442,18 +468,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
       u32x2 pk[3];
 #pragma unroll
       for (int n = 0; n < 12 * ITEMS; ++n) bad |= put_step(kd, vd, n, pk);
-    } else if constexpr (CODED) {
-#pragma unroll
-      for (int i = 0; i < ITEMS; ++i) {
-        const int item = i * 256 + tid, t = item / P::RUNS, c = item % P::RUNS;
-        if (t >= KT || c * 16 >= DH) continue;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          *(bf16x8*)(kd + 8 * k_place<ROW>(t, 2 * c + h)) = coded8(u32x2{k16[i][2 * h], k16[i][2 * h + 1]}, CT());
-          *(bf16x8*)(vd + 8 * v_place<ROW>(t, 2 * c + h)) = coded8(u32x2{v16[i][2 * h], v16[i][2 * h + 1]}, CT());
-        }
-      }
-    } else {
+    } else if constexpr (!CODED) {
 #pragma unroll
       for (int i = 0; i < ITEMS; ++i) {
         const int item = i * 64 + lane, t = item / (DH / 8), c = item % (DH / 8);
@@ -512,10 +527,14 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
     fetch(it + 1, pages1);
   }
   if constexpr (CODED && WIDE) {
-    put(k_lds0, v_lds0);
-    sc_next = sc_fetched;
+    wait_loads<0>();
+    take();
+#pragma unroll
+    for (int n = 0; n < 4 * ITEMS; ++n) code_step(k_lds0, v_lds0, n);
+    sc_next = scales(it, pages);
+    wait_lds();
+    if (it + 1 < t_end) fetch(it + 1, pages1);
     __syncthreads();
-    fetch(it + 1, pages1);
   }
 
   auto uniform = [](float x) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x))); };
@@ -555,7 +574,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
     const bool full = k0 + KT <= R.full_to && (k0 >= R.full_from || k0 + KT <= R.prefix) && there == low_ones(KT);
     bool bad = false;
     const int pages_next = AHEAD2 ? pages1 : page_of(it + STEP, entry_next);
-    float2 sc = sc_next;                                          // CODED: scales of the lane's token of this tile
+    const float2 sc = sc_next;                                    // CODED: scales of the lane's token of this tile
     if constexpr (STAGGERED) {
       wait_loads<INSTS>();                   // the keys have landed (the values are behind them)
     } else if constexpr (DIRECT) {
@@ -564,8 +583,9 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
       if constexpr (WIDE) { __builtin_amdgcn_s_barrier(); asm volatile("" ::: "memory"); }
       if (it + STEP < t_end) dma((lds_ptr)kn, (lds_ptr)vn, it + STEP, pages_next, BOTH());
     } else if constexpr (CODED) {
-      put(kn, vn);
-      sc_next = sc_fetched;
+      wait_loads<0>();
+      take();                                                     // (a wave's parked codes are its own; behind the last tile they are whatever they are)
+      sc_next = scales(it + 1, pages_next);
     } else if constexpr (WIDE) {
       bad = s_bad[which] == it;
     } else {
@@ -576,6 +596,9 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
     uint32_t next_bad = 0;
     if (idle) {
       if constexpr (P::SPLIT) next_bad = put(kn, vn);
+      if constexpr (CODED && WIDE)
+#pragma unroll
+        for (int n = 0; n < 4 * ITEMS; ++n) code_step(kn, vn, n);
     } else {
       auto key = [&](int a, int ks, int j) -> bf16x8 { return *(const bf16x8*)((const char*)kt + k_at[ks & 3] + (2 * j * TILE + 64 * ROW * a + 128 * (ks >> 2))); };
 #pragma unroll
@@ -627,6 +650,9 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
 #pragma unroll
           for (int u = 0; u < P::PRODUCTS; ++u) sacc[n / KSN] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[n % AHEAD], qf[P::column_piece(u)][n % KSN], sacc[n / KSN], 0, 0, 0);
           if (n + AHEAD < STEPS) kf[n % AHEAD] = key((n + AHEAD) / KSN, (n + AHEAD) % KSN, 0);
+          if constexpr (CODED)                                    // the next tile's codes, while the matrix unit works
+#pragma unroll
+            for (int i = n * 4 * ITEMS / STEPS; i < (n + 1) * 4 * ITEMS / STEPS; ++i) code_step(kn, vn, i);
           __builtin_amdgcn_sched_barrier(0);
         }
       } else {
@@ -648,37 +674,97 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
       dma((lds_ptr)kt, (lds_ptr)vt, it + STEP, pages_next, KEYS());
     }
     pages = pages_next;
-    if constexpr (AHEAD2) {
-      if (P::SPLIT && __any(next_bad != 0) && lane_now() == 0) s_bad[which ^ 1] = it + 1;
+    if constexpr (CODED && WIDE) {
+      pages1 = it + 2 < t_end ? page_of(it + 2, entry_next) : -1;
+      wait_lds();
+      if (it + 2 < t_end) fetch(it + 2, pages1);
+      entry_next = entry_of(it + 3);
+    }
+    if constexpr (P::SPLIT) {
+      if (__any(next_bad != 0) && lane_now() == 0) s_bad[which ^ 1] = it + 1;
       pages1 = it + 2 < t_end ? page_of(it + 2, entry_next) : -1;
       fetch(it + 2, pages1);
       entry_next = entry_of(it + 3);
-    } else if constexpr (!STAGGERED) entry_next = entry_of(it + 2 * STEP);
+    } else if constexpr (!STAGGERED && !CODED) entry_next = entry_of(it + 2 * STEP);
     const int lane = lane_now(), hh = lane >> 5;
+    // CODED: numbers of their own, since parts of an accumulator are moved about as a whole where branches meet (with a cap, 31 registers spilled less); for the others it costs more than it gives.
+    ScoreRow own_scores[CODED ? KB : 1];
+    auto& score = one_of<CODED>(own_scores, sacc);
+    if constexpr (CODED)
+#pragma unroll
+      for (int a = 0; a < KB; ++a)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) score[a][r] = sacc[a][r];
     uint64_t vis = ~0ull;                                         // tokens of the tile that the column sees
-    // CODED: a block is at least 16 tokens and begins at a multiple of 16, so each 16 tokens of a tile have one scale: the first one's.  k_by: to powers of two (MODS: of the score as it is).
+    // CODED: a block is at least 16 tokens and begins at a multiple of 16, so each 16 tokens of a tile have one scale: the first one's.  k_by: to powers of two, or to what the cap's tanh is taken of.
     constexpr int GROUPS16 = CODED ? KT / 16 : 1;
-    float k_by[GROUPS16], v_by[GROUPS16];
+    float k_by[GROUPS16], v_by[GROUPS16], v_out[GROUPS16];
     if constexpr (CODED) {
-      const float x = MODS ? sc.x : sc.x * c2;
+      const float x = sc.x * (MODS && A.softcap > 0.f ? cap_y : c2);
 #pragma unroll
       for (int i = 0; i < GROUPS16; ++i) {
         k_by[i] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 16 * i));
-        v_by[i] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, sc.y), 16 * i));
       }
       // a score of -inf must not meet a scale that is 0 or not finite: such a tile takes its scales before the mask
       if (!idle && (MODS || __any(!(x > 0.f && x < INFINITY)))) {
 #pragma unroll
         for (int a = 0; a < KB; ++a)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) sacc[a][r] *= k_by[2 * a + (r >> 3)];
+          for (int r = 0; r < 16; ++r) score[a][r] *= k_by[2 * a + (r >> 3)];
 #pragma unroll
         for (int i = 0; i < GROUPS16; ++i) k_by[i] = 1.f;
       }
     }
     if (!idle) {
     // cap and slopes
-    if constexpr (MODS) {
+    if constexpr (MODS && CODED) {                                // (as below, of what is the cap's y already)
+      if (A.softcap > 0.f) {
+        auto bent = [&](float y) -> float {
+          const float z = y * y;
+          float t = fmaf(cap_out * 0.01359966f, z, cap_out * -0.05067464f);
+          t = fmaf(t, z, cap_out * 0.13276915f);
+          t = fmaf(t, z, cap_out * -0.33330065f);
+          return y * fmaf(t, z, cap_out);
+        };
+        bool small = false;
+        if constexpr (NQ == 1) {
+          float far = 0.f;
+#pragma unroll
+          for (int a = 0; a < KB; ++a)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) far = fmaxf(far, fabsf(score[a][r]));
+          small = !__any(far > 0.7f);
+        }
+        if (small) {
+#pragma unroll
+          for (int a = 0; a < KB; ++a)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) score[a][r] = bent(score[a][r]);
+        } else {
+#pragma unroll
+          for (int a = 0; a < KB; ++a)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const float y = score[a][r], e = __builtin_amdgcn_exp2f(y * 2.88539008f);
+              float x = fmaf(-2.f * cap_out, __builtin_amdgcn_rcpf(e + 1.f), cap_out);
+              if constexpr (NQ == 3) {
+                const float z = y * y;
+                float t = 3.59212803657248102e-3f;
+                t = fmaf(t, z, -8.86323552990219657e-3f);
+                t = fmaf(t, z, 2.18694885361552028e-2f);
+                t = fmaf(t, z, -5.39682539682539683e-2f);
+                t = fmaf(t, z, 0.133333333333333333f);
+                t = fmaf(t, z, -0.333333333333333333f);
+                t = fmaf(t * z, y, y);
+                x = fabsf(y) < 0.35f ? cap_out * t : x;
+              } else {
+                x = fabsf(y) > 0.7f ? x : bent(y);
+              }
+              score[a][r] = x;
+            }
+        }
+      }
+    } else if constexpr (MODS) {
       // bf16 queries: a score up to 0.7 of the cap takes a polynomial, one beyond it the exponential, each by its own size alone; where no score of the wave is beyond (of those that no row sees
       // neither), the exponential is left out.
       const float k = cap_out * cap_y;
@@ -697,23 +783,23 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
 #pragma unroll
         for (int a = 0; a < KB; ++a)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) far = fmaxf(far, fabsf(sacc[a][r]));
+          for (int r = 0; r < 16; ++r) far = fmaxf(far, fabsf(score[a][r]));
         small = !__any(far * cap_y > 0.7f);
       }
       if (small) {
 #pragma unroll
         for (int a = 0; a < KB; ++a)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) sacc[a][r] = bent(sacc[a][r]);
+          for (int r = 0; r < 16; ++r) score[a][r] = bent(score[a][r]);
       } else if (A.softcap > 0.f) {
 #pragma unroll
         for (int a = 0; a < KB; ++a)
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
-            const float e = __builtin_amdgcn_exp2f(sacc[a][r] * cap_in);   // e^(2 x / cap); tanh = 1 - 2 / (e + 1)
+            const float e = __builtin_amdgcn_exp2f(score[a][r] * cap_in);   // e^(2 x / cap); tanh = 1 - 2 / (e + 1)
             float x = fmaf(-2.f * cap_out, __builtin_amdgcn_rcpf(e + 1.f), cap_out);
             if constexpr (NQ == 3) {                              // fp32: near 0 that cancels; the Taylor polynomial to y^13 is within 10^-9 below 0.35
-              const float y = sacc[a][r] * cap_y, z = y * y;
+              const float y = score[a][r] * cap_y, z = y * y;
               float t = 3.59212803657248102e-3f;
               t = fmaf(t, z, -8.86323552990219657e-3f);
               t = fmaf(t, z, 2.18694885361552028e-2f);
@@ -723,16 +809,18 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
               t = fmaf(t * z, y, y);
               x = fabsf(y) < 0.35f ? cap_out * t : x;
             } else {
-              x = fabsf(sacc[a][r]) * cap_y > 0.7f ? x : bent(sacc[a][r]);
+              x = fabsf(score[a][r]) * cap_y > 0.7f ? x : bent(score[a][r]);
             }
-            sacc[a][r] = x;
+            score[a][r] = x;
           }
       } else {
 #pragma unroll
         for (int a = 0; a < KB; ++a)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) sacc[a][r] *= c2;
+          for (int r = 0; r < 16; ++r) score[a][r] *= c2;
       }
+    }
+    if constexpr (MODS) {
       if (A.slopes) {
         if (R.tree && k0 + KT > R.base) {
           const unsigned long long tmask = A.chunk.tree_mask[column().row];
@@ -742,14 +830,14 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
             for (int r = 0; r < 16; ++r) {
               const int j = k0 + 32 * a + 8 * (r >> 2) + 4 * hh + (r & 3);
               const int pos = j > R.base ? R.base + __popcll(tmask & low_ones(j - R.base)) : j;
-              sacc[a][r] = fmaf(-slope, (float)abs(own - pos), sacc[a][r]);
+              score[a][r] = fmaf(-slope, (float)abs(own - pos), score[a][r]);
             }
         } else {
           const float d = (float)(own - k0 - 4 * hh);
 #pragma unroll
           for (int a = 0; a < KB; ++a)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) sacc[a][r] = fmaf(-slope, fabsf(d - (float)(32 * a + 8 * (r >> 2) + (r & 3))), sacc[a][r]);
+            for (int r = 0; r < 16; ++r) score[a][r] = fmaf(-slope, fabsf(d - (float)(32 * a + 8 * (r >> 2) + (r & 3))), score[a][r]);
         }
       }
     }
@@ -770,25 +858,25 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
 #pragma unroll
       for (int a = 0; a < KB; ++a)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) sacc[a][r] = (uint32_t)(mine >> (32 * a)) >> (8 * (r >> 2) + (r & 3)) & 1u ? sacc[a][r] : -INFINITY;
+        for (int r = 0; r < 16; ++r) score[a][r] = (uint32_t)(mine >> (32 * a)) >> (8 * (r >> 2) + (r & 3)) & 1u ? score[a][r] : -INFINITY;
     }
-    float top = sacc[0][0];
+    float top = score[0][0];
     if constexpr (CODED && !MODS) {
       top = -INFINITY;
 #pragma unroll
       for (int a = 0; a < KB; ++a)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          float x = sacc[a][8 * h];
+          float x = score[a][8 * h];
 #pragma unroll
-          for (int r = 1; r < 8; ++r) x = fmaxf(x, sacc[a][8 * h + r]);
+          for (int r = 1; r < 8; ++r) x = fmaxf(x, score[a][8 * h + r]);
           top = fmaxf(top, x * k_by[2 * a + h]);
         }
     } else {
 #pragma unroll
       for (int a = 0; a < KB; ++a)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) top = fmaxf(top, sacc[a][r]);
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, score[a][r]);
     }
     top = fmaxf(top, __shfl_xor(top, 32, 64));
     if constexpr (!MODS && !CODED) top *= c2;
@@ -885,17 +973,24 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
       if constexpr (WIDE) __syncthreads();
     }
     if constexpr (CODED) {                                        // a block of values whose scale is not finite: nothing finite for the columns that see one of them
-      if (__any(not_finite(sc.y)) && !idle) {
+      const bool odd_here = not_finite(sc.y);
+      if (__any(odd_here) && !idle) {
 #pragma unroll
         for (int i = 0; i < GROUPS16; ++i) {
-          const bool odd = not_finite(v_by[i]);
+          const bool odd = not_finite(__builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, sc.y), 16 * i)));
           const float add = odd && (vis & there) >> (16 * i) & 0xFFFFu ? NAN : 0.f;
 #pragma unroll
           for (int b = 0; b < DB; ++b)
 #pragma unroll
             for (int r = 0; r < 16; ++r) oacc[b][r] += add;
-          if (odd) v_by[i] = 0.f;
         }
+      }
+      // Weights take their block's value scale.  fp32 queries: by a product; bf16: in the exponent, as its logarithm (off by 2^-24 of it, the scale 2^-96 at least), and it is taken out of their sum again.
+      const float x = odd_here ? (NQ == 3 ? 0.f : 1.f) : NQ == 3 ? sc.y : fmaxf(sc.y, 1.26217745e-29f), y = NQ == 3 ? x : __builtin_amdgcn_logf(x), z = NQ == 3 ? 0.f : __builtin_amdgcn_rcpf(x);
+#pragma unroll
+      for (int i = 0; i < GROUPS16; ++i) {
+        v_by[i] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, y), 16 * i));
+        v_out[i] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, z), 16 * i));
       }
     }
     if (!idle) {
@@ -906,23 +1001,29 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
     constexpr int AHEAD = NK == 3 ? 1 : NQ == 3 ? 2 : 4;          // (of three pieces each is read again as soon as it is done with)
     bf16x8 vf[AHEAD][NK];
     u32x2 vraw[AHEAD];                                            // RAW
-    float sum = 0.f;
+    float sum = 0.f, block_sum = 0.f;
     auto weights = [&](int jj, int n) {                           // n of WORK steps: a pair's weights and their first piece, its second, its third
       const int pair = NQ == 3 ? n / 3 : n, j = NQ == 3 ? n % 3 : 0, a = jj >> 1, r = 8 * (jj & 1) + 2 * pair;
-      float x = sacc[a][r], y = sacc[a][r + 1];
+      float x = score[a][r], y = score[a][r + 1];
       if (j == 0) {
-        const float by = CODED ? k_by[CODED ? jj : 0] : c2;
-        x = __builtin_amdgcn_exp2f(MODS ? x - m_sub : fmaf(x, by, -m_sub));
-        y = __builtin_amdgcn_exp2f(MODS ? y - m_sub : fmaf(y, by, -m_sub));
-        sum += x;
-        sum += y;
-        if constexpr (CODED) { x *= v_by[jj]; y *= v_by[jj]; }
+        const float by = CODED ? k_by[CODED ? jj : 0] : c2, off = CODED && NQ == 1 ? m_sub - v_by[CODED ? jj : 0] : m_sub;
+        x = __builtin_amdgcn_exp2f(MODS ? x - off : fmaf(x, by, -off));
+        y = __builtin_amdgcn_exp2f(MODS ? y - off : fmaf(y, by, -off));
+        if constexpr (CODED && NQ == 1) {
+          block_sum = pair == 0 ? x : block_sum + x;
+          block_sum += y;
+          if (pair == 3) sum = fmaf(block_sum, v_out[jj], sum);
+        } else {
+          sum += x;
+          sum += y;
+          if constexpr (CODED) { x *= v_by[jj]; y *= v_by[jj]; }
+        }
       }
       const uint32_t h = bf16_pair(x, y);
       pf[jj & 1][j][pair] = h;
       if (j + 1 < NQ) {
-        sacc[a][r] = x - __builtin_bit_cast(float, h << 16);
-        sacc[a][r + 1] = y - __builtin_bit_cast(float, h & 0xFFFF0000u);
+        score[a][r] = x - __builtin_bit_cast(float, h << 16);
+        score[a][r + 1] = y - __builtin_bit_cast(float, h & 0xFFFF0000u);
       }
     };
     auto value = [&](int i, int j) {                              // piece j of block i % DB of 16 tokens

@@ -69,7 +69,7 @@ template <int VE> __device__ inline void store_run(bf16_t* p, const float* x) {
 // Bound by HBM, and by latency for a few rows: 8191 rows of 64 + 8 + 8 heads of 128 in bf16 take 63 us, 5.3 TB/s read and written (four rows a work-group 78: fewer, longer chains of loads;
 // elements instead of runs 190); 2011 fp32 rows of 64 + 8 heads in a loop over the same tensors 25; 104 rows of 32 + 8 + 8 heads 5.6 (four a work-group 8.1).
 template <typename T, typename CT, int VE>
-__device__ __forceinline__ void rope_row(const RopeDev& A, int r, int part) {
+__device__ __forceinline__ void rope_row(const RopeDev A, int r, int part) {
   __shared__ float2 cs[128];
   __shared__ int s_pos;
   __shared__ long long s_cell;                                    // the row's place in the cache: element offset of kv head 0, -1 none, -2: not a row of any sequence
