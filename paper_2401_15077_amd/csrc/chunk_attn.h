@@ -592,6 +592,12 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
       bad = __any(put(kt, vt) != 0);
     }
     const bool idle = WIDE && (!wave_live || k0 > wave_last);     // (the wave's part of moving data and the barriers stay)
+    auto ask_next = [&]() {                                       // CODED, WIDE: the parked codes have been read, the tile after the next may take their place
+      pages1 = it + 2 < t_end ? page_of(it + 2, entry_next) : -1;
+      wait_lds();
+      if (it + 2 < t_end) fetch(it + 2, pages1);
+      entry_next = entry_of(it + 3);
+    };
     f32x16 sacc[KB];
     uint32_t next_bad = 0;
     if (idle) {
@@ -599,6 +605,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
       if constexpr (CODED && WIDE)
 #pragma unroll
         for (int n = 0; n < 4 * ITEMS; ++n) code_step(kn, vn, n);
+      if constexpr (CODED && WIDE) ask_next();
     } else {
       auto key = [&](int a, int ks, int j) -> bf16x8 { return *(const bf16x8*)((const char*)kt + k_at[ks & 3] + (2 * j * TILE + 64 * ROW * a + 128 * (ks >> 2))); };
 #pragma unroll
@@ -653,6 +660,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
           if constexpr (CODED)                                    // the next tile's codes, while the matrix unit works
 #pragma unroll
             for (int i = n * 4 * ITEMS / STEPS; i < (n + 1) * 4 * ITEMS / STEPS; ++i) code_step(kn, vn, i);
+          if (CODED && n == 3) ask_next();
           __builtin_amdgcn_sched_barrier(0);
         }
       } else {
@@ -674,12 +682,6 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
       dma((lds_ptr)kt, (lds_ptr)vt, it + STEP, pages_next, KEYS());
     }
     pages = pages_next;
-    if constexpr (CODED && WIDE) {
-      pages1 = it + 2 < t_end ? page_of(it + 2, entry_next) : -1;
-      wait_lds();
-      if (it + 2 < t_end) fetch(it + 2, pages1);
-      entry_next = entry_of(it + 3);
-    }
     if constexpr (P::SPLIT) {
       if (__any(next_bad != 0) && lane_now() == 0) s_bad[which ^ 1] = it + 1;
       pages1 = it + 2 < t_end ? page_of(it + 2, entry_next) : -1;
@@ -739,7 +741,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
 #pragma unroll
           for (int a = 0; a < KB; ++a)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) score[a][r] = bent(score[a][r]);
+            for (int r = 0; r < 16; ++r) { score[a][r] = bent(score[a][r]); asm volatile("" : "+v"(score[a][r])); }
         } else {
 #pragma unroll
           for (int a = 0; a < KB; ++a)
@@ -761,6 +763,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
                 x = fabsf(y) > 0.7f ? x : bent(y);
               }
               score[a][r] = x;
+              asm volatile("" : "+v"(score[a][r]));
             }
         }
       }
@@ -1063,7 +1066,11 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
       wait_lds();                                                 // the values have been read
       dma((lds_ptr)kt, (lds_ptr)vt, it + STEP, pages, VALUES());
     }
-    if constexpr (AHEAD2) __syncthreads();
+    if constexpr (CODED && WIDE) {                                // (not __syncthreads, which would wait for the codes on their way)
+      wait_lds();
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+    } else if constexpr (AHEAD2) __syncthreads();
     it += STEP;
   };
   if constexpr (P::TWO) {
