@@ -49,17 +49,23 @@ static int check_attention(const eagle_attention_args* a, const eagle_chunk* chu
 // fp32 993, 1173, 1309, 986, 1124.  (Not in order: the sequences' own numbers of parts, hence the rounds of work-groups, change with the bound; six is the least of all three.)  Sixteen of those
 // sequences, bf16, with 1, 2, 4, 6, 8, 12, 16, 25: 215, 173, 172, 180, 171, 179, 177, 181; this bound makes it 25.  One token over 701 keys, 32 heads, fp32, 22 tiles: parts of 4 tiles 17.6, of 5 23.0, of 3 29.4.  Wide: one a CU (four trees of 26 nodes on 8 kv heads, fp32 queries, 37 tiles: 8 parts 27, 10 parts 32 to 38; 2011 fp32 rows on 32 heads, 512 work-groups: whole
 // 327, in two 339 and 26 more for joining).
+// Codes: the narrow shape up to 8192 columns, since a wave's tiles are then its own, without barriers, and what it reads beyond once comes from the L2 (D 128, a causal prompt on 8 kv heads, wide / narrow:
+// 1024 columns 15.8 / 10.0, 4096 40.5 / 31.4, 8192 77 / 77, 16384 209 / 222; with a cap 17.8 / 10.0, 47 / 32, 91 / 82, 252 / 249; fp32 queries 25 / 22, 67 / 47, 137 / 128, 392 / 427; int8 and bf16 16 / 10,
+// 41 / 32, 80 / 83, 208 / 251).  Two work-groups a CU where there are not as many units anyway (four trees of 26 nodes, fp32: 512 work-groups 33, 1024 38, 3200 59; 16 of them 103, 122, 130), else as above
+// (64 sequences of 1k to 16k tokens: 242, 242, 220).
+constexpr int ATTN_CODED_COLS = 8192, ATTN_CODED_WGS = 512;
 constexpr int ATTN_WIDE_WGS = 256, ATTN_NARROW_WGS = 3200, ATTN_MIN_TILES = 4, ATTN_MAX_PARTS = 64;
 
 // Columns and parts of a call; returns the bytes of workspace, at most `limit` of them if that is possible.
 static size_t plan_attention(ChunkAttnDev* d, int dtype, int kelt, size_t limit, bool* wide) {
   const int g = d->H / d->kv.n_kv_heads;
   const long long cols = (long long)d->chunk.max_rows * g;
-  *wide = cols > 32;
+  *wide = cols > (kelt == 1 ? ATTN_CODED_COLS : 32);
   const int KT = tile_tokens(*wide, dtype == EAGLE_F32, kelt), round = *wide ? 1 : 4;
   d->col_blocks = (int)((cols + (*wide ? 127 : 31)) / (*wide ? 128 : 32));
   const long long units = (long long)d->col_blocks * d->kv.n_kv_heads * d->chunk.n_seqs, tiles = ((long long)d->chunk.max_keys + KT - 1) / KT;
-  long long parts = std::min((*wide ? ATTN_WIDE_WGS : ATTN_NARROW_WGS) / units, (tiles + ATTN_MIN_TILES - 1) / ATTN_MIN_TILES);
+  const int wgs = *wide ? ATTN_WIDE_WGS : kelt == 1 && units < ATTN_CODED_WGS ? ATTN_CODED_WGS : ATTN_NARROW_WGS;
+  long long parts = std::min(wgs / units, (tiles + ATTN_MIN_TILES - 1) / ATTN_MIN_TILES);
   parts = std::max(1ll, std::min(parts, (long long)ATTN_MAX_PARTS));
   const size_t pairs = (size_t)d->chunk.n_rows * d->H, PART = d->kv.head_dim <= 64 ? 64 : 128;
   for (;; --parts) {

@@ -707,14 +707,15 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
       for (int i = 0; i < GROUPS16; ++i) {
         k_by[i] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 16 * i));
       }
-      // a score of -inf must not meet a scale that is 0 or not finite: such a tile takes its scales before the mask
+      // a score of -inf must not meet a scale that is 0 or not finite: such a block's scores (not its neighbours', whose rows' bits are theirs) take it before the mask
       if (!idle && (MODS || __any(!(x > 0.f && x < INFINITY)))) {
 #pragma unroll
-        for (int a = 0; a < KB; ++a)
+        for (int i = 0; i < GROUPS16; ++i) {
+          if (!MODS && k_by[i] > 0.f && k_by[i] < INFINITY) continue;
 #pragma unroll
-          for (int r = 0; r < 16; ++r) score[a][r] *= k_by[2 * a + (r >> 3)];
-#pragma unroll
-        for (int i = 0; i < GROUPS16; ++i) k_by[i] = 1.f;
+          for (int r = 0; r < 8; ++r) score[i >> 1][8 * (i & 1) + r] *= k_by[i];
+          k_by[i] = 1.f;
+        }
       }
     }
     if (!idle) {

@@ -262,3 +262,57 @@ def test_a_cache_beyond_2_31_codes():
     p.rope(p.rope_plan(64), q, k, v, chunk=chunk, kv=kv2, q_out=q_out)
     assert torch.equal(kc[n_pages - 1], near[0][1]) and torch.equal(vc[n_pages - 2, :, :22], near[1][2, :, :22]) and torch.equal(ks[n_pages - 1], scales[0][1])
     assert torch.equal(got, p.chunk_attention(q_out, kv2, chunk))
+
+
+def dense(q, kv, table, n, page, block, *, softcap=0.0, window=0, slopes=None):
+    """One sequence of n tokens that are all rows: (result, weighted mean of |v|, largest scale * sum |q k|) in 64 bits, all at once."""
+    kc, vc, ks, vs = kv.both
+    H, D = q.shape[1], q.shape[2]
+    g = H // kv.n_kv_heads
+    pages = torch.tensor(table[0][:-(-n // page)].tolist(), device=DEV)
+    k, v = ((c.float().double() * s.abs().double().repeat_interleave(block, 2)[..., None])[pages].transpose(0, 1).reshape(kv.n_kv_heads, -1, D)[:, :n] for c, s in ((kc, ks), (vc, vs)))
+    far = torch.arange(n, device=DEV)[:, None] - torch.arange(n, device=DEV)
+    seen = (far >= 0) & (far < (window or n + 1))
+    out, mean, big = (torch.empty(n, H, D, dtype=torch.float64, device=DEV) for _ in range(3))
+    for h in range(H):
+        x = q[:, h].double() @ k[h // g].T.contiguous() * D ** -0.5
+        size = (q[:, h].double().abs() @ k[h // g].T.contiguous().abs() * D ** -0.5).masked_fill(~seen, 0.0).amax(1)
+        if softcap:
+            x = softcap * torch.tanh(x / softcap)
+        if slopes is not None:
+            x = x - slopes[h].double() * far
+        w = torch.softmax(x.masked_fill(~seen, -float("inf")), 1)
+        out[:, h], mean[:, h], big[:, h] = w @ v[h // g], w @ v[h // g].abs(), size[:, None]
+    return out, mean, big
+
+
+@pytest.mark.parametrize("types", ALL)
+@pytest.mark.parametrize("D", [64, 80, 128])
+@pytest.mark.parametrize("mods", [dict(), dict(softcap=3.0, window=300, slopes=True)], ids=str)
+def test_more_than_8192_columns(mods, D, types):
+    """Four waves that share tiles: 1037 rows of eight heads on one kv head, and what is not finite among them."""
+    p = pkg()
+    n, H, page, block = 1037, 8, 64, 16
+    q, kv, chunk, facts, table = case([n], [n], H, 1, D, types, page, block, poison=True)
+    sl = torch.tensor(2.0 ** (-np.arange(1, H + 1)), dtype=torch.float32, device=DEV) if mods.get("slopes") else None
+    kw = dict(softcap=mods.get("softcap", 0.0), window=mods.get("window", 0), slopes=sl)
+    got = p.chunk_attention(q, kv, chunk, **kw)
+    want, mean, big = dense(q, kv, table, n, page, block, **kw)
+    count = torch.minimum(torch.arange(1, n + 1, device=DEV), torch.tensor(kw["window"] or n, device=DEV))[:, None, None].double()
+    extra = kw["softcap"] + (n * 0.5 if sl is not None else 0.0)
+    tol = (2 * (64 * U * big + 5 * U * (big + extra)) + (count / 8 + 33) * U) * mean + 1e-30
+    if q.dtype == torch.bfloat16:
+        tol = tol + 2.0 ** -8 * 1.001 * (mean + want.abs())
+    assert ((got.double() - want).abs() <= tol).all(), float(((got.double() - want).abs() / tol).max())
+    # a code and a scale that are not finite stay with the rows that see them: tokens 1000 and 1008 to 1023
+    for which, at in ((0, 1000), (1, 1000), (2, 1008), (3, 1008)):
+        t = kv.both[which]
+        spot = t.view(torch.uint8)[int(table[0][at // page]), 0, at % page] if which < 2 else t[int(table[0][at // page]), 0, at % page // block:at % page // block + 1]
+        kept = spot.clone()
+        if which < 2 and "int8" in types:
+            continue
+        spot.fill_(0x7F if which < 2 else float("nan"))
+        bad = p.chunk_attention(q, kv, chunk, **kw)
+        assert torch.equal(bad[:at], got[:at]) and bad[at:].isnan().all(), which
+        spot.copy_(kept)
+    assert torch.equal(p.chunk_attention(q, kv, chunk, **kw), got)
