@@ -131,7 +131,8 @@ template <typename T>
 __global__ __launch_bounds__(1024) void k_sample(const SampleDev A) {
   __shared__ u64 hist[SAMPLE_BUCKETS + 64], sub[SAMPLE_BUCKETS], list[2][SAMPLE_LIST], mass[SAMPLE_FEW], s_wave[16], s_low, s_high, s_found[3];
   __shared__ double root[64];                                     // powers of 2^(-1 / 64)
-  __shared__ int s_n, s_bucket;
+  __shared__ int noted[SAMPLE_LIST], s_n, s_bucket;
+  __shared__ uint32_t s_edge[4];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), V = A.vocab, r = blockIdx.x;
   const T* row = (const T*)A.logits + r * A.stride;
   const SampleRow Q = sample_row(A, r);
@@ -302,15 +303,27 @@ __global__ __launch_bounds__(1024) void k_sample(const SampleDev A) {
     }
     return (uint32_t)__builtin_amdgcn_readfirstlane((int)hi);
   };
+  // Those of two or four buckets, a wave each (all sixteen looking for the same would take each other's time: 1.1 us an edge).
+  struct Edges { uint32_t at[4]; };
+  auto edges = [&](int b0, int b1, int b2, int b3) -> Edges {
+    const int b = wave == 0 ? b0 : wave == 1 ? b1 : wave == 2 ? b2 : b3;
+    if (wave < 4 && b >= 0) { const uint32_t e = edge(b); if (lane == 0) s_edge[wave] = e; }
+    __syncthreads();
+    Edges e;
+    for (int i = 0; i < 4; ++i) e.at[i] = (uint32_t)__builtin_amdgcn_readfirstlane((int)s_edge[i]);
+    __syncthreads();
+    return e;
+  };
   auto mass_of = [&](float x) -> u64 {
     const Bucket b = bucket(x);
     return b.b < SAMPLE_BUCKETS - 1 ? (u64)((double)part(b.rest) * scale_of(b.b)) : 0ull;
   };
   struct Found { u64 place, before, share; };
-  // Of the tokens up to `limit` in bucket b, the one in whose share (its part, or 1) the number falls.
-  auto select = [&](int b, u64 target, bool by_mass, u64 limit) -> Found {
+  // Of the tokens up to `limit` from place `begin` up to `end` (a bucket's), the one in whose share (its part, or 1) the number falls.
+  // given >= 0: these are among the `given` tokens in `noted`.
+  auto select = [&](uint32_t begin, uint32_t end, u64 target, bool by_mass, u64 limit, int given) -> Found {
     auto share = [&](u64 place) -> u64 { return by_mass ? part(bucket(value_of((uint32_t)(place >> 32))).rest) : 1ull; };
-    u64 low = (u64)edge(b) << 32, high = min(limit, ((u64)edge(b + 1) << 32) - 1), in_front = 0;
+    u64 low = (u64)begin << 32, high = min(limit, ((u64)end << 32) - 1), in_front = 0;
     auto narrow = [&](int shift) {                                // to the bucket of `sub` that the number falls into
       const Sums s = scan(sub, false);
       find(s, target - in_front);
@@ -336,10 +349,12 @@ __global__ __launch_bounds__(1024) void k_sample(const SampleDev A) {
     };
     auto note = [&](int t, uint32_t hits) {
       int i = atomicAdd(&s_n, __popc(hits));
-      for (; hits && i < SAMPLE_LIST; hits &= hits - 1) list[1][i++] = t + __builtin_ctz(hits);
+      for (; hits && i < SAMPLE_LIST; hits &= hits - 1) noted[i++] = t + __builtin_ctz(hits);
     };
-    int n;
-    for (bool ranged = false;; ranged = true) {                   // (every turn leaves a 2048th of the range at most, so that one of SAMPLE_LIST tokens is reached)
+    int n = given;
+    if (given >= 0) {
+      if (tid == 0) { s_low = ~0ull; s_high = 0; }
+    } else for (bool ranged = false;; ranged = true) {                   // (every turn leaves a 2048th of the range at most, so that one of SAMPLE_LIST tokens is reached)
       if (tid == 0) { s_n = 0; s_low = ~0ull; s_high = 0; }
       __syncthreads();
       if (!ranged) between(value_of((uint32_t)(high >> 32)), value_of((uint32_t)(low >> 32)), note);
@@ -358,9 +373,9 @@ __global__ __launch_bounds__(1024) void k_sample(const SampleDev A) {
       narrow(shift);
     }
     {
-      const int t = tid < n ? (int)list[1][tid] : 0;
+      const int t = tid < n ? noted[tid] : 0;
       const u64 p = place_of(logit(t), t);
-      const bool mine = tid < n && p >= low && p <= high;         // (of the last value some may lie behind the limit)
+      const bool mine = tid < n && p >= low && p <= high;         // (of the last value some may lie behind the limit, and what is given may be of other buckets)
       u64 lo = mine ? p : ~0ull, hi = mine ? p : 0;
       lo = wave_min(lo);
       hi = wave_max(hi);
@@ -462,18 +477,19 @@ __global__ __launch_bounds__(1024) void k_sample(const SampleDev A) {
     __syncthreads();
     between(least, top, [&](int t, uint32_t hits) {
       int i = atomicAdd(&s_n, __popc(hits));
-      for (; hits && i < SAMPLE_FEW; hits &= hits - 1) list[1][i++] = t + __builtin_ctz(hits);
+      for (; hits && i < SAMPLE_FEW; hits &= hits - 1) noted[i++] = t + __builtin_ctz(hits);
     });
     __syncthreads();
     const int n = __builtin_amdgcn_readfirstlane(s_n);
-    if (tid < min(n, SAMPLE_FEW)) list[0][tid] = place_of(logit((int)list[1][tid]), (int)list[1][tid]);
+    if (tid < min(n, SAMPLE_FEW)) list[0][tid] = place_of(logit(noted[tid]), noted[tid]);
     __syncthreads();
     return n;
   };
 
   // Three boundaries, one after the other: the last token of top-k, the last of top-p, the token itself.
   enum { LAST_K, LAST_P, TOKEN };
-  u64 limit = ~0ull, kept = 0;
+  u64 limit = ~0ull, kept = 0, heavy_mass = ~0ull;
+  int given = -1, given_from = 0, given_to = -1;                  // tokens in `noted`: those of buckets given_from to given_to among them
   Sums s;
   bool by_threads = Q.top_k && Q.k <= SAMPLE_FEW, tried = false;
   float least = !Q.top_k && Q.min_p && !Q.top_p ? cut : NAN;      // tokens from here on may be few (NaN: not known)
@@ -504,7 +520,7 @@ __global__ __launch_bounds__(1024) void k_sample(const SampleDev A) {
       by_threads = false;
       if (target < s.total) {
         find(s, target);
-        least = value_of(edge(__builtin_amdgcn_readfirstlane(s_bucket) + 1) - 1);
+        least = value_of(edges(__builtin_amdgcn_readfirstlane(s_bucket) + 1, -1, -1, -1).at[0] - 1);
       }
       __syncthreads();
       stage = LAST_K - 1;
@@ -514,25 +530,33 @@ __global__ __launch_bounds__(1024) void k_sample(const SampleDev A) {
       if (target >= s.total) continue;                            // (the last of them weighs nothing: no bound)
     } else if (stage == LAST_P) {
       kept = s.total;
+      if (Q.min_p) {
+        // The buckets in front of the one that the least weight falls into are kept, and of this one and its neighbours what is heavy enough.
+        const int at = (int)fmin(-Q.log_least * (64 * 1.4426950408889634) + 0.5, SAMPLE_BUCKETS - 1.0), from = max(0, at - 1);
+        if (tid == 0) s_found[2] = 0;
+        __syncthreads();
+        if (tid == from / EACH) {
+          u64 m = s.at;
+#pragma unroll
+          for (int i = 0; i < EACH; ++i) m += i < from % EACH ? s.x[i] : 0;
+          atomicAdd(&s_found[2], m);
+        }
+        u64 m = 0;
+        const Edges e = edges(from, min(at + 2, SAMPLE_BUCKETS), -1, -1);
+        between(value_of(e.at[1] - 1), value_of(e.at[0]), [&](int t, uint32_t hits) {
+          each_bit(t, hits, [&](float x, int i) { if (heavy(x) && place_of(x, i) <= limit) m += mass_of(x); });
+        });
+        m = wave_sum(m);
+        if (lane == 0) atomicAdd(&s_found[2], m);
+        __syncthreads();
+        heavy_mass = uniform(max(s_found[2], 1ull << A.bits));
+        __syncthreads();
+      }
       if (!Q.top_p) stage = TOKEN;
       else target = uniform(min(max(1ull, (u64)ceil(Q.p * (double)kept)), kept) - 1);
     }
     if (stage == TOKEN) {
-      if (Q.min_p) {
-        u64 m = 0;
-        between(cut, top, [&](int t, uint32_t hits) {
-          each_bit(t, hits, [&](float x, int i) {
-            if (heavy(x) && place_of(x, i) <= limit) m += mass_of(x);
-          });
-        });
-        m = wave_sum(m);
-        __syncthreads();
-        if (lane == 0) s_wave[wave] = m;
-        __syncthreads();
-        m = 0;
-        for (int i = 0; i < 16; ++i) m += s_wave[i];
-        kept = uniform(min(kept, max(m, 1ull << A.bits)));
-      }
+      kept = min(kept, heavy_mass);
       target = uniform(min((u64)(Q.u * (double)kept), kept - 1));
     }
     find(s, target);
@@ -540,15 +564,40 @@ __global__ __launch_bounds__(1024) void k_sample(const SampleDev A) {
     const u64 before = uniform(s_found[0]), inside = uniform(hist[b] & LOWER);
     if (stage == LAST_K && before + inside <= SAMPLE_FEW && !tried) {
       tried = true;
-      least = value_of(edge(b + 1) - 1);
-      __syncthreads();
+      least = value_of(edges(b + 1, -1, -1, -1).at[0] - 1);
       stage = LAST_K - 1;
       continue;
     }
-    __syncthreads();
     // inside the bucket the number counts in the bucket's own units
     const double scale = stage == LAST_K ? 1.0 : scale_of(b);
-    const Found f = select(b, min((u64)((double)(target - before) / scale), inside - 1), stage != LAST_K, limit);
+    Edges e;
+    if (stage == LAST_P) {
+      // What is kept is known but for this bucket's mass, so the token's bucket is known too, or two or three that it may be: their tokens are noted on the way.
+      const u64 least_kept = min(before + 1, heavy_mass), most_kept = min(before + uniform(s_found[1]), heavy_mass);
+      __syncthreads();
+      find(s, min((u64)(Q.u * (double)least_kept), least_kept - 1));
+      given_from = __builtin_amdgcn_readfirstlane(s_bucket);
+      __syncthreads();
+      find(s, min((u64)(Q.u * (double)most_kept), most_kept - 1));
+      given_to = __builtin_amdgcn_readfirstlane(s_bucket);
+      if (tid == 0) s_n = 0;
+      e = edges(b, b + 1, given_from, given_to + 1);
+      const float most = value_of(e.at[0]), least = value_of(e.at[1] - 1), most_u = value_of(e.at[2]), least_u = value_of(e.at[3] - 1);
+      runs([&](const float* x, int t, auto n) {
+        uint32_t hits = 0;
+#pragma unroll
+        for (int j = 0; j < decltype(n)::value; ++j)
+          hits |= __builtin_amdgcn_fmed3f(x[j], least, most) == x[j] || __builtin_amdgcn_fmed3f(x[j], least_u, most_u) == x[j] ? 1u << j : 0u;
+        if (!hits) return;
+        int i = atomicAdd(&s_n, __popc(hits));
+        for (; hits && i < SAMPLE_LIST; hits &= hits - 1) noted[i++] = t + __builtin_ctz(hits);
+      });
+      __syncthreads();
+      given = __builtin_amdgcn_readfirstlane(s_n);
+      if (given > SAMPLE_LIST) given = -1;
+    } else e = edges(b, b + 1, -1, -1);
+    const bool noted_here = given >= 0 && (stage == LAST_P || (stage == TOKEN && b >= given_from && b <= given_to));
+    const Found f = select(e.at[0], e.at[1], min((u64)((double)(target - before) / scale), inside - 1), stage != LAST_K, limit, noted_here ? given : -1);
     if (stage == LAST_K) limit = f.place;
     else if (stage == LAST_P) kept = uniform(min(kept, before + (u64)((double)(f.before + f.share) * scale)));
     else {
