@@ -7,7 +7,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libeagle.so")
 SOURCES = ["eagle.hip", "operators.hip", "coded.hip", "sample.hip"]
-HEADERS = ["kernels.h", "kernels2.h", "plans.h", "common.h", "host.h", "operators.h", "rows.h", "checks.h", "attention.h", "codes.h", "rope.h", "rope_coded.h", "chunk_attn.h", "logit_rules.h", "sample.h", os.path.join("..", "..", "include", "eagle.h")]
+HEADERS = ["kernels.h", "kernels2.h", "plans.h", "common.h", "host.h", "operators.h", "rows.h", "checks.h", "attention.h", "codes.h", "wave.h", "rope.h", "rope_coded.h", "chunk_attn.h", "logit_rules.h", "sample.h", os.path.join("..", "..", "include", "eagle.h")]
 
 
 def needs_build() -> bool:

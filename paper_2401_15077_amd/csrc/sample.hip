@@ -14,6 +14,8 @@ static int check_sample(const eagle_sample_args* a) {
   if (!a->logits || !a->uniform || !a->token) return fail(EAGLE_EINVAL, "sample: logits, uniform or token is null");
   if (a->n_rows > 1 && a->stride < a->vocab) return fail(EAGLE_EINVAL, "sample: rows of %d entries need a stride of at least that", a->vocab);
   const int elt = elt_of(a->dtype);
+  for (const void* p : {(const void*)a->uniform, (const void*)a->temperature, (const void*)a->top_k, (const void*)a->top_p, (const void*)a->min_p, (const void*)a->token, (const void*)a->logprob})
+    if (!aligned(p, 4)) return fail(EAGLE_EINVAL, "sample: arrays must start on multiples of 4 bytes");
   if (!aligned(a->logits, elt)) return fail(EAGLE_EINVAL, "sample: logits must start on a multiple of an element");
   const size_t R = a->n_rows, all = (((size_t)R - 1) * (R > 1 ? a->stride : 0) + a->vocab) * elt;
   const void* out[2] = {a->token, a->logprob};

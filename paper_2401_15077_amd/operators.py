@@ -1,5 +1,5 @@
-"""Operators on the caller's own tensors: rotary positions with the append to a paged cache, attention of a chunk of new tokens over it, and the
-rules that logits pass before a token is chosen (argument marshalling only; include/eagle.h has the definitions).
+"""Operators on the caller's own tensors: rotary positions with the append to a paged cache, attention of a chunk of new tokens over it, both for caches of
+8-bit codes too, the rules that logits pass before a token is chosen, and the choice (argument marshalling only; include/eagle.h has the definitions).
 
 Every call is enqueued on torch's current stream of the tensors' device and does not synchronise.  Outputs are not recorded by autograd: tensors that
 require gradients (inputs, outputs, slopes, and what a cache's or rules' handle was made from) are refused while gradients are enabled."""
@@ -448,6 +448,8 @@ def sample(logits: torch.Tensor, uniform: torch.Tensor, *, temperature: Optional
     workspace: a uint8 tensor of sample_workspace() bytes (None: one from torch's allocator for this call)."""
     if uniform is None:
         raise ValueError("uniform is needed: a random number for every row")
+    if logits.dim() != 2:
+        raise ValueError("logits must be a float32 or bfloat16 [rows, vocab] tensor, its rows consecutive")
     R, dev = logits.shape[0], logits.device
     if token is None:
         token = torch.empty(R, dtype=torch.int32, device=dev)
