@@ -12,6 +12,7 @@ struct SampleDev {
   const float *uniform, *temperature, *top_p, *min_p;
   const int* top_k;
   int* token; float* logprob;
+  double part[4];                          // 2^-x/64 in units: the terms of its series, the first one with 2^52
 };
 
 // The order of the tokens, by value, descending, equal ones by index, as the order of 64-bit numbers.
@@ -34,11 +35,10 @@ __device__ __forceinline__ u64 place_of(float x, int i) { return (u64)order_of(x
 // A bucket's sum times 2^(-b / 64) is its mass, in multiples of 2^-bits of the largest weight.  The last bucket holds what lies 2^-64 below, which is as good as nothing.
 constexpr int SAMPLE_BUCKETS = 4096, SAMPLE_LIST = 1024, SAMPLE_PAIRS = 128, SAMPLE_FEW = 256;
 
-// What a row asks for.
+// What a row asks for; step: buckets a unit of logits, farthest: what the last bucket lies below the largest, reach: what the least weight does.
 struct SampleRow {
-  bool greedy, top_k, top_p, min_p;
-  int k;
-  double rate, p, log_least, u;
+  int greedy, top_k, top_p, min_p, k;
+  double rate, p, log_least, u, step, farthest, reach;
 };
 // The same in every lane: kept in scalar registers.
 __device__ __forceinline__ double uniform(double x) {
@@ -47,16 +47,18 @@ __device__ __forceinline__ double uniform(double x) {
 }
 __device__ __forceinline__ u64 uniform(u64 x) { return __builtin_bit_cast(u64, uniform(__builtin_bit_cast(double, x))); }
 __device__ __forceinline__ float uniform(float x) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x))); }
-__device__ inline SampleRow sample_row(const SampleDev& A, int r) {
+__device__ inline SampleRow sample_row(int vocab, float temperature, int k, float p, float least, float u) {
   SampleRow q;
-  const float temperature = A.temperature ? A.temperature[r] : 1.f, p = A.top_p ? A.top_p[r] : 1.f, least = A.min_p ? A.min_p[r] : 0.f, u = A.uniform[r];
-  q.k = A.top_k ? A.top_k[r] : 0;
+  q.k = k;
   q.greedy = !(temperature > 0.f);
-  q.top_k = q.k > 0 && q.k < A.vocab; q.top_p = p < 1.f; q.min_p = least > 0.f;
-  q.rate = uniform(1.0 / (double)temperature);
-  q.p = uniform(fmax((double)p, 0.0));
-  q.log_least = q.min_p ? uniform(log((double)least)) : 0.0;
-  q.u = uniform(u > 0.f ? fmin((double)u, 1.0) : 0.0);
+  q.top_k = k > 0 && k < vocab; q.top_p = p < 1.f; q.min_p = least > 0.f;
+  q.rate = 1.0 / (double)temperature;
+  q.p = fmax((double)p, 0.0);
+  q.log_least = q.min_p ? log((double)least) : 0.0;
+  q.u = u > 0.f ? fmin((double)u, 1.0) : 0.0;
+  q.step = fmax(q.rate * (64 * 1.4426950408889634), 1e-290);
+  q.farthest = (SAMPLE_BUCKETS - 1) / q.step;
+  q.reach = q.log_least / q.rate;
   return q;
 }
 
@@ -108,9 +110,11 @@ __global__ __launch_bounds__(1024) void k_sample(const SampleDev A) {
   __shared__ double root[64];                                     // powers of 2^(-1 / 64)
   __shared__ int noted[SAMPLE_LIST], s_n, s_bucket;
   __shared__ uint32_t s_edge[4];
+  __shared__ SampleRow s_row;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), V = A.vocab, r = blockIdx.x;
   const T* row = (const T*)A.logits + r * A.stride;
-  const SampleRow Q = sample_row(A, r);
+  const float temperature = A.temperature ? A.temperature[r] : 1.f, p_of_row = A.top_p ? A.top_p[r] : 1.f, min_of_row = A.min_p ? A.min_p[r] : 0.f, u_of_row = A.uniform[r];
+  const int k_of_row = A.top_k ? A.top_k[r] : 0;
   auto runs = [&](auto f) { each_run<T, 1024>(row, 0, V, f); };
   // f(first token, bits of those from `least` to `most`) of the runs that have such; few are expected.
   auto between = [&](float least, float most, auto f) {
@@ -129,6 +133,7 @@ __global__ __launch_bounds__(1024) void k_sample(const SampleDev A) {
     A.token[r] = token;
     if (A.logprob) A.logprob[r] = logprob;
   };
+  for (int i = 2 * tid; i < SAMPLE_BUCKETS; i += 2048) *(ulonglong2*)(hist + i) = ulonglong2{0, 0};
   float top = -INFINITY;
   runs([&](const float* x, int, auto n) {
 #pragma unroll
@@ -137,7 +142,9 @@ __global__ __launch_bounds__(1024) void k_sample(const SampleDev A) {
   const float best_here = top;                                    // of this thread's tokens
   {
     const u64 first = wave_min(order_of(top));
-    if (tid < 64) root[tid] = exp2(tid * (-1.0 / 64.0));
+    // (what is the same for all is worked out by a wave or two: sixteen would take each other's time)
+    if (wave == 1) root[lane] = exp2(lane * (-1.0 / 64.0));
+    if (wave == 2) { const SampleRow q = sample_row(V, temperature, k_of_row, p_of_row, min_of_row, u_of_row); if (lane == 0) s_row = q; }
     if (lane == 0) s_wave[wave] = first;
     if (tid == 0) { s_low = ~0ull; s_n = 0; }
     __syncthreads();
@@ -145,6 +152,10 @@ __global__ __launch_bounds__(1024) void k_sample(const SampleDev A) {
     for (int i = 0; i < 16; ++i) least = min(least, s_wave[i]);
     top = uniform(value_of((uint32_t)least));
   }
+  SampleRow Q = s_row;
+  Q.greedy = __builtin_amdgcn_readfirstlane(Q.greedy); Q.top_k = __builtin_amdgcn_readfirstlane(Q.top_k); Q.top_p = __builtin_amdgcn_readfirstlane(Q.top_p);
+  Q.min_p = __builtin_amdgcn_readfirstlane(Q.min_p); Q.k = __builtin_amdgcn_readfirstlane(Q.k);
+  Q.rate = uniform(Q.rate); Q.p = uniform(Q.p); Q.log_least = uniform(Q.log_least); Q.u = uniform(Q.u);
   if (top == -INFINITY) {
     if (tid == 0) answer(-1, -INFINITY);
     return;
@@ -186,8 +197,8 @@ __global__ __launch_bounds__(1024) void k_sample(const SampleDev A) {
     return;
   }
 
-  const double step = uniform(fmax(Q.rate * (64 * 1.4426950408889634), 1e-290)), farthest = uniform((SAMPLE_BUCKETS - 1) / step), magic = 6755399441055744.0;   // 1.5 * 2^52: what is added to it is rounded to a whole number
-  const double top64 = uniform((double)top), one = uniform(ldexp(1.0, A.unit));
+  const double step = uniform(Q.step), farthest = uniform(Q.farthest), magic = 6755399441055744.0;   // 1.5 * 2^52: what is added to it is rounded to a whole number
+  const double top64 = uniform((double)top);
   struct Bucket { int b; double rest; };
   auto bucket_of = [&](double d) -> Bucket {                      // b and y - b
     const double k = fma(d, step, magic);
@@ -195,8 +206,7 @@ __global__ __launch_bounds__(1024) void k_sample(const SampleDev A) {
   };
   auto bucket = [&](float x) { return bucket_of(fmin(top64 - (double)x, farthest)); };
   // 2^(-rest / 64): three terms behind the 1 leave out 4 * 10^-11.  The last sum is one with 2^52, so it ends on a whole number, in the lower 52 bits; what is above them is left to whoever adds up.
-  constexpr double L = 0.010830424696249145;                      // ln 2 / 64
-  const double first = uniform(one + 4503599627370496.0), c1 = uniform(-L * one), c2 = uniform(L * L / 2 * one), c3 = uniform(-L * L * L / 6 * one);
+  const double first = A.part[0], c1 = A.part[1], c2 = A.part[2], c3 = A.part[3];
   auto part_above = [&](double rest) -> u64 { return __builtin_bit_cast(u64, fma(fma(fma(rest, c3, c2), rest, c1), rest, first)); };
   constexpr u64 LOWER = 0xFFFFFFFFFFFFFull;
   auto part = [&](double rest) -> u64 { return part_above(rest) & LOWER; };
@@ -226,7 +236,7 @@ __global__ __launch_bounds__(1024) void k_sample(const SampleDev A) {
   auto exponent = [&](float x) -> double { return ((double)x - top64) * Q.rate; };   // ln(weight)
   auto heavy = [&](float x) { return exponent(x) >= Q.log_least; };                  // min-p keeps it
   // a little below the least that min-p keeps (at a temperature that is infinite, no bound)
-  const float scaled = (float)(top64 + Q.log_least / Q.rate), cut = uniform(Q.rate > 0.0 ? fminf(top, scaled - fabsf(scaled) * 1e-6f - 1e-30f) : -INFINITY);
+  const float scaled = (float)(top64 + uniform(Q.reach)), cut = uniform(Q.rate > 0.0 ? fminf(top, scaled - fabsf(scaled) * 1e-6f - 1e-30f) : -INFINITY);
 
   auto scale_of = [&](int b) { return ldexp(root[b & 63], A.bits - A.unit - (b >> 6)); };   // a part of bucket b as a mass
   auto clear = [&](u64* h) {
@@ -238,13 +248,19 @@ __global__ __launch_bounds__(1024) void k_sample(const SampleDev A) {
   struct Sums { u64 at, x[EACH], total; };
   auto scan = [&](const u64* h, bool masses) -> Sums {
     Sums s;
-    u64 sum = 0;
+    u64 sum = 0, any = 0;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
       s.x[i] = h[tid * EACH + i] & LOWER;
-      if (masses) s.x[i] = (u64)((double)s.x[i] * scale_of(tid * EACH + i));
-      sum += s.x[i];
+      any |= s.x[i];
+    }
+    if (any) {                                                    // (most of the buckets are empty)
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) {
+        if (masses) s.x[i] = (u64)((double)s.x[i] * scale_of(tid * EACH + i));
+        sum += s.x[i];
+      }
     }
     u64 upto = wave_scan(sum, 0, Add());
     if (lane == 63) s_wave[wave] = upto;
@@ -466,6 +482,7 @@ __global__ __launch_bounds__(1024) void k_sample(const SampleDev A) {
   u64 limit = ~0ull, kept = 0, heavy_mass = ~0ull;
   int given = -1, given_from = 0, given_to = -1;                  // tokens in `noted`: those of buckets given_from to given_to among them
   Sums s;
+  bool cleared = true;                                            // (hist is, from the start)
   bool by_threads = Q.top_k && Q.k <= SAMPLE_FEW, tried = false;
   float least = !Q.top_k && Q.min_p && !Q.top_p ? cut : NAN;      // tokens from here on may be few (NaN: not known)
 #pragma unroll 1
@@ -478,7 +495,8 @@ __global__ __launch_bounds__(1024) void k_sample(const SampleDev A) {
         __syncthreads();
         least = NAN;
       }
-      clear(hist);
+      if (!cleared) clear(hist);
+      cleared = false;
       if (by_threads) {
         if (top64 - (double)best_here < farthest) atomicAdd(&hist[bucket(best_here).b], 1ull);
       } else if (limit == ~0ull) runs([&](const float* x, int, auto n) { add_run(x, n, stage == LAST_P); });

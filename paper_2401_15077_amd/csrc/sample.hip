@@ -42,7 +42,9 @@ extern "C" int eagle_sample(const eagle_sample_args* a, void* workspace, size_t 
   if (workspace_bytes < need) return fail(EAGLE_ENOMEM, "sample: workspace of %zu bytes is smaller than the %zu needed", workspace_bytes, need);
   int bits = 62;                                                  // (as many weights of at most 2^bits add up to at most 2^62, and parts to less than 2^52)
   while ((long long)a->vocab > 1ll << (62 - bits)) --bits;
-  const SampleDev d{a->n_rows, a->vocab, bits, bits - 11, a->logits, a->stride, a->uniform, a->temperature, a->top_p, a->min_p, a->top_k, a->token, a->logprob};
+  const double one = std::ldexp(1.0, bits - 11), L = 0.010830424696249145;   // ln 2 / 64
+  const SampleDev d{a->n_rows, a->vocab, bits, bits - 11, a->logits, a->stride, a->uniform, a->temperature, a->top_p, a->min_p, a->top_k, a->token, a->logprob,
+                    {one + 4503599627370496.0, -L * one, L * L / 2 * one, -L * L * L / 6 * one}};
   const hipStream_t stream = (hipStream_t)hip_stream;
   if (a->dtype == EAGLE_F32) k_sample<float><<<a->n_rows, 1024, 0, stream>>>(d);
   else k_sample<bf16_t><<<a->n_rows, 1024, 0, stream>>>(d);
