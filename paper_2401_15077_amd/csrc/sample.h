@@ -525,7 +525,7 @@ __global__ __launch_bounds__(1024) void k_sample(const SampleDev A) {
       kept = s.total;
       if (Q.min_p) {
         // The buckets in front of the one that the least weight falls into are kept, and of this one and its neighbours what is heavy enough.
-        const int at = (int)fmin(-Q.log_least * (64 * 1.4426950408889634) + 0.5, SAMPLE_BUCKETS - 1.0), from = max(0, at - 1);
+        const int at = (int)fmax(0.0, fmin(-Q.log_least * (64 * 1.4426950408889634) + 0.5, SAMPLE_BUCKETS - 1.0)), from = max(0, at - 1);
         if (tid == 0) s_found[2] = 0;
         __syncthreads();
         if (tid == from / EACH) {

@@ -1,8 +1,9 @@
 """The choice of a token against the oracle in 64 bits.
 
-Tolerances.  Weights are whole multiples of 2^-b of the largest (b >= 44 here), each rounded by half of one, so masses of up to 2^18 of them are off by 2^-27 of the largest weight and by no more than
-2^-27 of the mass: a token may differ from the oracle's only where the oracle's number falls as close as that to a border.  A log probability is worked out in 64 bits from such a mass and rounded
-to fp32: 2^-24 of itself and 2^-26."""
+Tolerances.  A weight is 2^(-b / 64) times a part between 2^(-1 / 128) and 2^(1 / 128).  The part is off by 4e-11 of itself (three terms of its series) and by half a unit of 2^-(51 - ceil(log2 vocab)),
+2^-33 for the 140000 tokens here, so by less than 2^-32 of itself; a bucket's mass is cut to a multiple of 2^-44 of the largest weight, 2^-32 for all 4096 of them; weights below 2^-64, left out, are
+2^-46 together.  So a mass is off by less than 2^-27 of itself: a token may differ from the oracle's only where the oracle's number falls as close as that to a border.  A log probability is worked
+out in 64 bits from such a mass and rounded to fp32: 2^-24 of itself and 2^-26."""
 import numpy as np
 import pytest
 import torch
@@ -141,6 +142,17 @@ def test_steep_and_flat_rows():
     check(x, u)
     check(x, u, top_p=[0.999999, 0.9, 0.7, 0.3, 0.999, 0.5])
     check(x, u, min_p=[1e-9, 1e-3, 0.1, 0.9999, 0.9995, 0.5])
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("equal", [1, 200, 300, 5000])
+def test_a_least_weight_above_one_leaves_the_first(equal, dtype):
+    x = torch.zeros(8, 7001, device=DEV, dtype=TYPES[dtype])
+    x[:, 100:100 + equal] = 2.0
+    u = [0.0, 0.3, 0.999, 0.5, 0.7, 0.9, 0.2, 0.99]
+    least = [INF, 3e38, 2.0, 1.0 + 2.0 ** -23, INF, 1e30, 64.0, 1.5]
+    for kw in ({}, dict(top_p=[0.9, 0.5, 0.0, 0.99, 0.7, 0.1, 0.3, 0.6]), dict(top_k=[400] * 8), dict(top_k=[299] * 8, top_p=[0.95] * 8), dict(temperature=[INF, 1e30, 5.0, 1.0, 0.1, 1e-30, INF, 2.0])):
+        assert check(x, u, min_p=least, **kw) == [100] * 8
 
 
 def test_many_rows():
