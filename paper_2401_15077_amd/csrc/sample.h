@@ -111,7 +111,8 @@ __global__ __launch_bounds__(1024) void k_sample(const SampleDev A) {
   __shared__ int noted[SAMPLE_LIST], s_n, s_bucket;
   __shared__ uint32_t s_edge[4];
   __shared__ SampleRow s_row;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), V = A.vocab, r = blockIdx.x;
+  int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), V = A.vocab, r = blockIdx.x;
   const T* row = (const T*)A.logits + r * A.stride;
   const float temperature = A.temperature ? A.temperature[r] : 1.f, p_of_row = A.top_p ? A.top_p[r] : 1.f, min_of_row = A.min_p ? A.min_p[r] : 0.f, u_of_row = A.uniform[r];
   const int k_of_row = A.top_k ? A.top_k[r] : 0;
@@ -411,10 +412,7 @@ __global__ __launch_bounds__(1024) void k_sample(const SampleDev A) {
     __syncthreads();
     return f;
   };
-  auto finish = [&](u64 place, u64 kept) {                        // one thread
-    const float x = value_of((uint32_t)(place >> 32));
-    answer((int)(uint32_t)place, (float)(exponent(x) - log(ldexp((double)kept, -A.bits))));
-  };
+  u64 chosen = ~0ull, kept = 0;                                   // the thread that has it: the token's place, and the mass of all that are kept
   // All of at most SAMPLE_FEW tokens in list[0], or the first `most` of them in order, are what top-p, min-p and the number choose from.
   auto few = [&](int n, int most) {
     const int mine = tid >> 2;
@@ -439,7 +437,7 @@ __global__ __launch_bounds__(1024) void k_sample(const SampleDev A) {
       if (Q.min_p && m[i] && heavy(value_of((uint32_t)(list[1][j] >> 32)))) strong += m[i];
     }
     const u64 upto = wave_scan(sum, 0, Add());
-    u64 kept = last_lane(upto);
+    kept = last_lane(upto);
     if (Q.top_p) {
       const u64 need = max(1ull, (u64)ceil(Q.p * (double)kept));
       u64 at = upto - sum, least = ~0ull;
@@ -459,7 +457,7 @@ __global__ __launch_bounds__(1024) void k_sample(const SampleDev A) {
     u64 at = upto - sum;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      if (at <= target && target < at + m[i]) finish(list[1][4 * lane + i], kept);
+      if (at <= target && target < at + m[i]) chosen = list[1][4 * lane + i];
       at += m[i];
     }
   };
@@ -479,7 +477,7 @@ __global__ __launch_bounds__(1024) void k_sample(const SampleDev A) {
 
   // Three boundaries, one after the other: the last token of top-k, the last of top-p, the token itself.
   enum { LAST_K, LAST_P, TOKEN };
-  u64 limit = ~0ull, kept = 0, heavy_mass = ~0ull;
+  u64 limit = ~0ull, heavy_mass = ~0ull;
   int given = -1, given_from = 0, given_to = -1;                  // tokens in `noted`: those of buckets given_from to given_to among them
   Sums s;
   bool cleared = true;                                            // (hist is, from the start)
@@ -487,11 +485,13 @@ __global__ __launch_bounds__(1024) void k_sample(const SampleDev A) {
   float least = !Q.top_k && Q.min_p && !Q.top_p ? cut : NAN;      // tokens from here on may be few (NaN: not known)
 #pragma unroll 1
   for (int stage = Q.top_k ? LAST_K : LAST_P;; ++stage) {
+    asm volatile("" : "+v"(tid));                                  // (what can be had from the thread's number in an instruction or two is not kept: it would be spilled)
+    lane = tid & 63;
     u64 target = (u64)Q.k - 1;
     if (stage != TOKEN) {
       if (least == least) {
         const int n = gather(least);
-        if (n <= SAMPLE_FEW) { few(n, Q.top_k ? Q.k : V); return; }
+        if (n <= SAMPLE_FEW) { few(n, Q.top_k ? Q.k : V); break; }
         __syncthreads();
         least = NAN;
       }
@@ -594,8 +594,9 @@ __global__ __launch_bounds__(1024) void k_sample(const SampleDev A) {
     if (stage == LAST_K) limit = f.place;
     else if (stage == LAST_P) kept = uniform(min(kept, before + (u64)((double)(f.before + f.share) * scale)));
     else {
-      if (tid == 0) finish(f.place, kept);
-      return;
+      if (tid == 0) chosen = f.place;
+      break;
     }
   }
+  if (chosen != ~0ull) answer((int)(uint32_t)chosen, (float)(exponent(value_of((uint32_t)(chosen >> 32))) - log(ldexp((double)kept, -A.bits))));
 }
