@@ -245,8 +245,9 @@ int eagle_feature_noise(eagle_ctx *ctx, const float *in_dev, float *out_dev, int
 int eagle_probe_stream_read(const void *buf_dev, size_t bytes, int32_t iters, void *hip_stream, double *gb_per_s);
 
 /* ---- Operators on the caller's own tensors ----------------------------------------------------------------------
- * Rotary positions with the append to a paged cache, attention of a chunk of new tokens over it, and the rules logits pass before a token is
- * chosen: what a step does inside a context, for tensors of the caller (another head, a model of another layout, a scheduler of its own).
+ * Rotary positions with the append to a paged cache, attention of a chunk of new tokens over it, the rules logits pass before a token is
+ * chosen, and the choice: what a step does inside a context, for tensors of the caller (another head, a model of another layout, a scheduler of its own).  The cache holds fp32 or bf16, or
+ * 8-bit codes with scales.
  *   - They need no context.  Every tensor lies on the device that `hip_stream` belongs to, which must be the calling thread's current device; work
  *     is enqueued on that stream only, nothing is allocated and nothing synchronises, so the calls may be captured into graphs.
  *   - Calls on different streams or threads may overlap as long as they share no output and no workspace (two captured graphs that share a
@@ -365,7 +366,8 @@ typedef struct {
 int eagle_rope_coded(const eagle_rope_plan *plan, const eagle_rope_args *args, const eagle_chunk *chunk, const eagle_coded_kv *kv, void *hip_stream);
 
 /* eagle_chunk_attention over a cache of codes: k_j and v_j are code * scale, q and out EAGLE_F32 or EAGLE_BF16; codes and their products with the queries are exact as those of a bf16 cache are.
- * head_dim: a multiple of 16, 16..128; the cache's tokens start on multiples of 16 bytes.  What a scale that is not finite makes of scores and results stays with the rows that see a
+ * head_dim: a multiple of 16, 16..128; the cache's tokens start on multiples of 16 bytes.  With EAGLE_BF16 queries a value scale below 2^-96 counts as 2^-96, and the weight that is rounded to
+ * bf16 is the one times the scale.  What a scale that is not finite makes of scores and results stays with the rows that see a
  * token of its block: a value scale makes all of their result NaN, a key scale their scores infinite or NaN. */
 size_t eagle_chunk_attention_coded_workspace(const eagle_attention_args *args, const eagle_chunk *chunk, const eagle_coded_kv *kv);
 int eagle_chunk_attention_coded(const eagle_attention_args *args, const eagle_chunk *chunk, const eagle_coded_kv *kv, void *workspace_dev, size_t workspace_bytes, void *hip_stream);
@@ -409,8 +411,10 @@ int eagle_apply_logit_rules(const eagle_logits *logits, const eagle_logit_rules 
  *   top_k > 0: the first top_k;  top_p < 1: of those the shortest run from the front that holds top_p of their mass;  min_p > 0: of those, w >= min_p;  the first in any case
  *   token = the first in order whose running mass exceeds uniform * (mass of those kept), uniform in [0, 1);  logprob = ln(w / mass of those kept)
  * A temperature that is not above 0 takes the first (logprob 0).  Logits of +inf, where there are any, count 1 each and all others 0.  A row of nothing but -inf: token -1, logprob -inf.
- * Weights are rounded to whole multiples of 2^-b of the largest one, b = 62 - ceil(log2 vocab) (45 for 131072 tokens), and added up exactly: a call's result is the same every time.
+ * Weights are worked out in 64 bits, to 2^-33 of themselves for up to 131072 tokens (a bit less for each doubling beyond), and rounded to whole numbers that are added up exactly: a call's result is
+ * the same every time.  What weighs less than 2^-64 of the largest counts as nothing in sums.
  * Parameters are arrays with an entry a row; null: 1, no top_k, no top_p, no min_p.  A parameter that is NaN is no filter.  Outputs lie apart from all inputs.
+ * logits start on a multiple of an element, rows from 1 to 2^24, vocab to 2^30.  Row stride: at least vocab, where there is more than one row.
  * workspace (dev, 256-byte aligned): eagle_sample_workspace() bytes, for the same arguments; its contents need not be kept or cleared. */
 typedef struct {
   int32_t n_rows, vocab, dtype;
@@ -425,7 +429,7 @@ typedef struct {
 size_t eagle_sample_workspace(const eagle_sample_args *args);
 int eagle_sample(const eagle_sample_args *args, void *workspace_dev, size_t workspace_bytes, void *hip_stream);
 
-/* ---- The same three inside a context ------------------------------------------------------------------------------
+/* ---- Positions, attention and logit rules inside a context -------------------------------------------------
  * Positions: how the target's and the head's layers turn queries and keys (null: the default again, pairs (i, i + head_dim / 2) of the whole head by cfg.rope_theta).
  * theta of the given configuration counts, not cfg's.  Before the first EAGLE_W_Q / _K is loaded (they are laid out by pairs), EAGLE_ESTATE after that.  Keys are read
  * back (eagle_get_kv_row) in the model's own order of elements. */

@@ -41,6 +41,10 @@ template <bool E4M3> __device__ inline int least_exponent(double a) {
 // The work-groups in front append: one takes the new tokens of one block of a kv head, keys or values (it has to know the largest of them before it can write one).  The others rotate the
 // queries, as rope_row says.
 // Everything from the angle to the code is worked out in 64 bits, so that a code is what the definition says and no rounding on the way moves it: rounded to odd once for the conversion.
+//
+// What bounds it: 8191 rows, 64 / 8 heads of 128, bf16, take 95 us for 318 MB, where a copy of as much takes 66: keys and values alone 47, of which the vector unit works four fifths (64-bit
+// operations issue as 32-bit ones do here; in 32 bits with a 64-bit way out for what falls near a border: 108), queries alone 42, side by side in one launch.  (Queries in a launch of their own, or
+// heads in a loop of a work-group that keeps angles: 121 to 129.)  One row 8.5, 104 rows 10: the chain from lengths to page, tokens, largest, scale and code.
 template <typename T, bool E4M3, int VE>
 __global__ __launch_bounds__(256) void k_rope_coded(const AppendDev A) {
   const RopeDev& P = A.rope;
