@@ -23,7 +23,10 @@ template <bool E4M3> __device__ __forceinline__ uint32_t encode4(const float* x)
   constexpr float M = LARGEST_CODE<E4M3>;
   float y[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) y[i] = x[i] > M ? M : x[i] < -M ? -M : x[i];
+  for (int i = 0; i < 4; ++i) {                                   // (one choice after the other: nested they become branches)
+    y[i] = x[i] > M ? M : x[i];
+    y[i] = y[i] < -M ? -M : y[i];
+  }
   if constexpr (E4M3) {
     int u = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], u, true);

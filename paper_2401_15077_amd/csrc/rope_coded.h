@@ -9,7 +9,8 @@ struct AppendDev {
   const void *k, *v;
   long long k_row, k_head, v_row, v_head;
   int KVH, seq_blocks;                     // trees: blocks of a sequence at most
-  int kv_groups;                           // work-groups in front that append: (block, kv head, keys or values)
+  int kv_groups;                           // work-groups that append (each a block, kv head, keys or values): below i there are i * kv_share / 2^32 of them, until there are all
+  unsigned long long kv_share;
 };
 
 // Cosine and sine of position * turn in 64 bits: as cos_sin_turn takes whole and quarter turns off, with polynomials that leave out less than 2^-62.
@@ -38,18 +39,20 @@ template <bool E4M3> __device__ inline int least_exponent(double a) {
   return E4M3 ? e - 9 + (f > 0.875) : e - 7 + (f > 0.9921875);
 }
 
-// The work-groups in front append: one takes the new tokens of one block of a kv head, keys or values (it has to know the largest of them before it can write one).  The others rotate the
-// queries, as rope_row says.
+// Some work-groups append: one takes the new tokens of one block of a kv head, keys or values (it has to know the largest of them before it can write one).  The others rotate the queries, as
+// rope_row says.
 // Everything from the angle to the code is worked out in 64 bits, so that a code is what the definition says and no rounding on the way moves it: rounded to odd once for the conversion.
 //
-// What bounds it: 8191 rows, 64 / 8 heads of 128, bf16, take 95 us for 318 MB, where a copy of as much takes 66: keys and values alone 47, of which the vector unit works four fifths (64-bit
-// operations issue as 32-bit ones do here; in 32 bits with a 64-bit way out for what falls near a border: 108), queries alone 42, side by side in one launch.  (Queries in a launch of their own, or
-// heads in a loop of a work-group that keeps angles: 121 to 129.)  One row 8.5, 104 rows 10: the chain from lengths to page, tokens, largest, scale and code.
+// What bounds it: 8191 rows, 64 / 8 heads of 128, bf16, take 82 us for 318 MB, where a copy of as much takes 66.  Keys and values keep the vector unit busy (64-bit operations issue as 32-bit ones do
+// here; in 32 bits with a 64-bit way out for what falls near a border they took 13 more), queries the memory, so the two kinds are spread among each other, and five waves a SIMD hide what either
+// waits for: with four (all of a run's angles at once) 92, with six (by spilling) 89 to 121.  Queries in a launch of their own, or heads in a loop of a work-group that keeps angles: 121 to 129, then.
+// One row 8.5, 104 rows 10: the chain from lengths to page, tokens, largest, scale and code.
 template <typename T, bool E4M3, int VE>
 __global__ __launch_bounds__(256) void k_rope_coded(const AppendDev A) {
   const RopeDev& P = A.rope;
-  if ((int)blockIdx.x >= A.kv_groups) {
-    const int i = blockIdx.x - A.kv_groups;
+  const int nth = min((int)(blockIdx.x * A.kv_share >> 32), A.kv_groups);
+  if (min((int)((blockIdx.x + 1) * A.kv_share >> 32), A.kv_groups) == nth) {
+    const int i = blockIdx.x - nth;
     rope_row<T, T, VE>(P, i % P.n_rows, i / P.n_rows);
     return;
   }
@@ -58,8 +61,8 @@ __global__ __launch_bounds__(256) void k_rope_coded(const AppendDev A) {
   __shared__ int s_held[128];                                     // tree: the slot is written
   __shared__ double s_max[4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const bool values = A.v && (blockIdx.x & 1);
-  int id = A.v ? blockIdx.x >> 1 : blockIdx.x;
+  const bool values = A.v && (nth & 1);
+  int id = A.v ? nth >> 1 : nth;
   const int kvh = id % A.KVH;
   id /= A.KVH;
   // the block: sequence and number
@@ -168,26 +171,24 @@ __global__ __launch_bounds__(256) void k_rope_coded(const AppendDev A) {
     for (int j = 0; j < VE; ++j) { a[j] = fa[j]; b[j] = fb[j]; }
     if (values || u >= rot_units) return;
     const int pos = s_pos[t];
-    double2 c[VE];
+    auto turned = [](double& x, double& y, double2 c) { const double x0 = x; x = x0 * c.x - y * c.y; y = y * c.x + x0 * c.y; };
 #pragma unroll
     for (int j = 0; j < VE; ++j) {
-      c[j] = cos_sin_turn64(P.turn[u * VE + j], pos);
-      c[j].x *= P.mscale; c[j].y *= P.mscale;
-    }
-    auto turned = [](double& x, double& y, double2 c) { const double x0 = x; x = x0 * c.x - y * c.y; y = y * c.x + x0 * c.y; };
-    if (P.interleaved && VE > 1) {
-#pragma unroll
-      for (int j = 0; j < VE / 2; ++j) { turned(a[2 * j], a[2 * j + 1], c[j]); turned(b[2 * j], b[2 * j + 1], c[VE / 2 + j]); }
-    } else {
-#pragma unroll
-      for (int j = 0; j < VE; ++j) turned(a[j], b[j], c[j]);
+      double2 c = cos_sin_turn64(P.turn[u * VE + j], pos);
+      c.x *= P.mscale; c.y *= P.mscale;
+      if (P.interleaved && VE > 1) {
+        double* x = 2 * j < VE ? a + 2 * j : b + 2 * j - VE;
+        turned(x[0], x[1], c);
+      } else turned(a[j], b[j], c);
+      __builtin_amdgcn_sched_barrier(0);                          // (an angle at a time: all of them at once take the registers of a further wave of five)
     }
   };
   double a[VE], b[VE], top = 0.0;
   auto largest = [&](const double* x) {
 #pragma unroll
-    for (int j = 0; j < VE; ++j) { const double m = fabs(x[j]); top = m > top && m < INFINITY ? m : top; }
+    for (int j = 0; j < VE; ++j) { const double m = fabs(x[j]); top = ((m > top) & (m < INFINITY)) ? m : top; }
   };
+#pragma unroll 1
   for (int i = tid; i < all; i += 256) {
     unit(i, a, b);
     largest(a); largest(b);
@@ -214,7 +215,8 @@ __global__ __launch_bounds__(256) void k_rope_coded(const AppendDev A) {
   if (tid == 0 && (!kept || grown > 0)) *scale_at = (float)scale;
   const double inv = 1.0 / scale, bound = 2.0 * M * scale;
   auto code = [&](double x) -> float {
-    x = x > bound ? bound : x < -bound ? -bound : x;
+    x = x > bound ? bound : x;
+    x = x < -bound ? -bound : x;
     double y = x * inv;
     y = fma(fma(-y, scale, x), inv, y);                           // (put right by what the quotient leaves, so that a tie is a tie)
     return odd_f32(y);
@@ -226,6 +228,7 @@ __global__ __launch_bounds__(256) void k_rope_coded(const AppendDev A) {
     } else if constexpr (VE == 4) *(uint32_t*)p = encode4<E4M3>(y);
     else *(u32x2*)p = u32x2{encode4<E4M3>(y), encode4<E4M3>(y + 4)};
   };
+#pragma unroll 1
   for (int i = tid; i < all; i += 256) {
     if (all > 256) unit(i, a, b);
     const Place p = place(i % units);
@@ -243,6 +246,7 @@ __global__ __launch_bounds__(256) void k_rope_coded(const AppendDev A) {
   // the block's other tokens: their codes in the new scale, or 0 where the old one stood for nothing
   const double shrink = kept ? ldexp(1.0, -grown) : 0.0;
   const int runs = P.head_dim / VE;
+#pragma unroll 1
   for (int i = tid; i < held * runs; i += 256) {
     const int slot = i / runs;
     if (s_held[slot]) continue;

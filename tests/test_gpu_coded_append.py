@@ -155,6 +155,15 @@ def test_bounds_gaps_positions_and_strides(kw, cache):
 
 
 @pytest.mark.parametrize("cache", ["e4m3", "int8"])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("v", [False, True])
+def test_more_than_4096_work_groups(v, inter, dtype, cache):
+    """Those that append are spread among those that rotate queries."""
+    run([1300, 1, 900], [1310, 77, 900], 2, 16 if v else 32, 16, dtype, cache, 64, 16, inter=inter, v=v)
+
+
+@pytest.mark.parametrize("cache", ["e4m3", "int8"])
 @pytest.mark.parametrize("scale", [0.0, -0.01, float("inf"), float("nan"), 2.0 ** -140, 3e38, 2.0 ** 100, 1.5 * 2.0 ** 99])
 def test_scales_of_all_kinds(scale, cache):
     run([1, 40], [40, 70], 2, 2, 64, "fp32", cache, 64, 32, scales=lambda s: torch.full_like(s, scale))
