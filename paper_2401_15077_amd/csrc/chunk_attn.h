@@ -22,10 +22,10 @@
 //
 // 8-bit codes are exact in bf16, so the products are those of a bf16 cache.  A block has at least 16 tokens: 16 scores share a key scale, which stands in the constant that takes scores to powers of
 // two (or to the cap's tangent), and their weights a value scale.  fp32 weights are multiplied with it before they become pieces; a bf16 weight takes it as log2 in its exponent, so that it is rounded
-// once (scales below 2^-96 count as 2^-96: none is lost to the least exponent).  The narrow shape brings codes to LDS as they are and makes bf16 of what each wave reads (RAW); in the wide one four
+// once (scales below 2^-96 count as 2^-96: none is lost to the least exponent), and the sum takes it rounded: 0.0019 to 0.0023 of the result's norm off, where the unrounded sum gave 0.0022 to 0.0025.  The narrow shape brings codes to LDS as they are and makes bf16 of what each wave reads (RAW); in the wide one four
 // waves would do so four times, so a tile's codes are parked in LDS and become bf16 between the products of the tile before.  64 tokens over 1k to 16k each, 64 / 8 heads, e4m3: 221 us, 5.1 TB/s of
-// cache (lengths all alike 5.4 to 5.8); 470 vector instructions a tile beside 32 products, the matrix unit busy 14 %.  1536 and 509 rows behind a window and a cap, bf16: 211, 716 vector instructions
-// a tile, 128 of them what makes bf16 of the codes; busy 23 %.  Four trees of 26 nodes, fp32 over int8: 33, 5 of it joining.  One token over 701, fp32: 12.6.
+// cache (lengths all alike 5.4 to 5.8); 470 vector instructions a tile beside 32 products, the matrix unit busy 14 %.  1536 and 509 rows behind a window and a cap, bf16: 220, 750 vector instructions
+// a tile, 128 of them what makes bf16 of the codes; busy 22 %.  Four trees of 26 nodes, fp32 over int8: 33, 5 of it joining.  One token over 701, fp32: 12.6.
 //
 // Registers: fp32 queries over a bf16 cache of 128 hold all 256 and spill (3 and, with cap or slopes, 17 of the wide shape, 7 and 6 of the narrow), which is a few of their loads a tile; over codes of 128
 // three at most; no other shape spills vector registers.
@@ -1020,17 +1020,19 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
         const float by = CODED ? k_by[CODED ? jj : 0] : c2, off = CODED && NQ == 1 ? m_sub - v_by[CODED ? jj : 0] : m_sub;
         x = __builtin_amdgcn_exp2f(MODS ? x - off : fmaf(x, by, -off));
         y = __builtin_amdgcn_exp2f(MODS ? y - off : fmaf(y, by, -off));
-        if constexpr (CODED && NQ == 1) {
-          block_sum = pair == 0 ? x : block_sum + x;
-          block_sum += y;
-          if (pair == 3) sum = fmaf(block_sum, v_out[jj], sum);
-        } else {
+        if constexpr (!(CODED && NQ == 1)) {
           sum += x;
           sum += y;
           if constexpr (CODED) { x *= v_by[jj]; y *= v_by[jj]; }
         }
       }
       const uint32_t h = bf16_pair(x, y);
+      if constexpr (CODED && NQ == 1) {                           // (of the rounded ones: a scale is no power of two, so the largest weight is rounded too, and where it is most of the sum that cancels)
+        const float xr = __builtin_bit_cast(float, h << 16), yr = __builtin_bit_cast(float, h & 0xFFFF0000u);
+        block_sum = pair == 0 ? xr : block_sum + xr;
+        block_sum += yr;
+        if (pair == 3) sum = fmaf(block_sum, v_out[jj], sum);
+      }
       pf[jj & 1][j][pair] = h;
       if (j + 1 < NQ) {
         score[a][r] = x - __builtin_bit_cast(float, h << 16);
