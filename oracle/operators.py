@@ -233,7 +233,7 @@ def sample(x, u, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
         n = max(1, m)
     if min_p > 0:
         ok = t[:n] >= math.log(min_p)
-        border = min(border, np.abs(t[:n] - math.log(min_p)).min())
+        border = min(border, np.abs(t[:n] - math.log(min_p))[y[:n] != top].min(initial=1.0))   # (the largest weigh 1, whoever works it out)
         n = max(1, int(ok.sum()))
     run = run[:n]
     u = u if u > 0 else 0.0

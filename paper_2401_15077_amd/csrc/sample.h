@@ -124,7 +124,7 @@ __global__ __launch_bounds__(1024) void k_sample(const SampleDev A) {
   const float temperature = A.temperature ? A.temperature[r] : 1.f, p_of_row = A.top_p ? A.top_p[r] : 1.f, min_of_row = A.min_p ? A.min_p[r] : 0.f, u_of_row = A.uniform[r];
   const int k_of_row = A.top_k ? A.top_k[r] : 0;
   auto runs = [&](auto f) { each_run<T, 1024>(row, 0, V, f); };
-  // f(first token, bits of those from `least` to `most`) of the runs that have such; few are expected.
+  // f(first token, bits of those from `least` to `most`, least <= most) of the runs that have such; few are expected.
   auto between = [&](float least, float most, auto f) {
     runs([&](const float* x, int t, auto n) {
       uint32_t hits = 0;
@@ -543,7 +543,7 @@ __global__ __launch_bounds__(1024) void k_sample(const SampleDev A) {
         }
         u64 m = 0;
         const Edges e = edges(from, min(at + 2, SAMPLE_BUCKETS), -1, -1);
-        between(value_of(e.at[1] - 1), value_of(e.at[0]), [&](int t, uint32_t hits) {
+        if (e.at[0] < e.at[1]) between(value_of(e.at[1] - 1), value_of(e.at[0]), [&](int t, uint32_t hits) {   // (numbers may lie further apart than these buckets: then none falls into them)
           each_bit(t, hits, [&](float x, int i) { if (heavy(x) && place_of(x, i) <= limit) m += mass_of(x); });
         });
         m = wave_sum(m);
