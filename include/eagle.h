@@ -366,8 +366,9 @@ typedef struct {
 int eagle_rope_coded(const eagle_rope_plan *plan, const eagle_rope_args *args, const eagle_chunk *chunk, const eagle_coded_kv *kv, void *hip_stream);
 
 /* eagle_chunk_attention over a cache of codes: k_j and v_j are code * scale, q and out EAGLE_F32 or EAGLE_BF16; codes and their products with the queries are exact as those of a bf16 cache are.
- * head_dim: a multiple of 16, 16..128; the cache's tokens start on multiples of 16 bytes.  With EAGLE_BF16 queries a value scale below 2^-96 counts as 2^-96, and the weight that is rounded to
- * bf16 is the one times the scale.  What a scale that is not finite makes of scores and results stays with the rows that see a
+ * head_dim: a multiple of 16, 16..128; the cache's tokens start on multiples of 16 bytes.  With EAGLE_BF16 queries a value scale below 2^-96 counts as 2^-96 (one below
+ * 2^-64 may count as 2^-64 where the sequence has one above 2^96), and the weight that is rounded to bf16 is the one times the scale.  Value scales may be as large as fp32 has them: where codes times
+ * scales are finite, so are sums of them times weights.  What a scale that is not finite makes of scores and results stays with the rows that see a
  * token of its block: a value scale makes all of their result NaN, a key scale their scores infinite or NaN. */
 size_t eagle_chunk_attention_coded_workspace(const eagle_attention_args *args, const eagle_chunk *chunk, const eagle_coded_kv *kv);
 int eagle_chunk_attention_coded(const eagle_attention_args *args, const eagle_chunk *chunk, const eagle_coded_kv *kv, void *workspace_dev, size_t workspace_bytes, void *hip_stream);

@@ -22,7 +22,7 @@
 //
 // 8-bit codes are exact in bf16, so the products are those of a bf16 cache.  A block has at least 16 tokens: 16 scores share a key scale, which stands in the constant that takes scores to powers of
 // two (or to the cap's tangent), and their weights a value scale.  fp32 weights are multiplied with it before they become pieces; a bf16 weight takes it as log2 in its exponent, so that it is rounded
-// once (scales below 2^-96 count as 2^-96: none is lost to the least exponent), and the sum takes it rounded: 0.0019 to 0.0023 of the result's norm off, where the unrounded sum gave 0.0022 to 0.0025.  The narrow shape brings codes to LDS as they are and makes bf16 of what each wave reads (RAW); in the wide one four
+// once (scales below 2^-96 count as 2^-96, or below 2^-64 as 2^-64 beside one above 2^96: none is lost to the least exponent), and the sum takes it rounded: 0.0019 to 0.0023 of the result's norm off, where the unrounded sum gave 0.0022 to 0.0025.  The narrow shape brings codes to LDS as they are and makes bf16 of what each wave reads (RAW); in the wide one four
 // waves would do so four times, so a tile's codes are parked in LDS and become bf16 between the products of the tile before.  64 tokens over 1k to 16k each, 64 / 8 heads, e4m3: 221 us, 5.1 TB/s of
 // cache (lengths all alike 5.4 to 5.8); 470 vector instructions a tile beside 32 products, the matrix unit busy 14 %.  1536 and 509 rows behind a window and a cap, bf16: 220, 750 vector instructions
 // a tile, 128 of them what makes bf16 of the codes; busy 22 %.  Four trees of 26 nodes, fp32 over int8: 33, 5 of it joining.  One token over 701, fp32: 12.6.
@@ -548,6 +548,8 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
   const float c2 = uniform(A.scale * 1.44269504088896341f);       // scores to powers of two
   const float cap_in = uniform(MODS && A.softcap > 0.f ? 2.f * c2 / A.softcap : 0.f), cap_out = uniform(A.softcap * 1.44269504088896341f);
   const float cap_y = uniform(cap_in * 0.34657359027997264f);     // scale / cap
+  constexpr float V_FAR = 0x1p96f, V_LIFT = 32.f, V_LEAST = 0x1p-96f;
+  float v_least = V_LEAST;                                        // CODED, bf16 queries: the least value scale that is told from smaller ones
   float m_run = -INFINITY, l_run = 0.f;                           // maximum (in powers of two) of the column, sum of this lane's half of the tokens
   f32x16 oacc[DB];
 #pragma unroll
@@ -708,7 +710,11 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
     // CODED: a block is at least 16 tokens and begins at a multiple of 16, so each 16 tokens of a tile have one scale: the first one's.  k_by: to powers of two, or to what the cap's tanh is taken of.
     constexpr int GROUPS16 = CODED ? KT / 16 : 1;
     float k_by[GROUPS16], v_by[GROUPS16], v_out[GROUPS16];
+    // A value scale above V_FAR (or none that is a number) is in this tile.  It stands inside the weights, of up to 2^8, and would take them and their sums out of range.  So the maximum is put
+    // V_LIFT above what it is, which makes all weights so much smaller and changes nothing else; the least scale of bf16 queries is as much larger from then on.
+    bool far = false;
     if constexpr (CODED) {
+      far = __any(!(sc.y <= V_FAR));
       const float x = sc.x * (MODS && A.softcap > 0.f ? cap_y : c2);
 #pragma unroll
       for (int i = 0; i < GROUPS16; ++i) {
@@ -891,6 +897,18 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
     }
     top = fmaxf(top, __shfl_xor(top, 32, 64));
     if constexpr (!MODS && !CODED) top *= c2;
+    if constexpr (CODED) {
+      if (far) {                                                  // the columns that see a token of such a block
+        bool lifted = false;
+#pragma unroll
+        for (int i = 0; i < GROUPS16; ++i) {
+          const float y = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, sc.y), 16 * i));
+          lifted |= y > V_FAR && (vis & there) >> (16 * i) & 0xFFFFu;
+        }
+        top += lifted ? V_LIFT : 0.f;
+        if (__any(lifted)) v_least = V_LEAST * 0x1p32f;
+      }
+    }
     // The maximum moves only when it grows by more than 8 (weights up to 2^8 lose nothing in fp32 or bf16), and lane by lane, so that a column's bits are its own.
     const bool moved = top > m_run + 8.f || (m_run == -INFINITY && top > -INFINITY);
     if (__any(moved)) {
@@ -985,7 +1003,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
     }
     if constexpr (CODED) {                                        // a block of values whose scale is not finite: nothing finite for the columns that see one of them
       const bool odd_here = not_finite(sc.y);
-      if (__any(odd_here) && !idle) {
+      if (far && !idle && __any(odd_here)) {
 #pragma unroll
         for (int i = 0; i < GROUPS16; ++i) {
           const bool odd = not_finite(__builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, sc.y), 16 * i)));
@@ -996,8 +1014,10 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
             for (int r = 0; r < 16; ++r) oacc[b][r] += add;
         }
       }
-      // Weights take their block's value scale.  fp32 queries: by a product; bf16: in the exponent, as its logarithm (off by 2^-24 of it, the scale 2^-96 at least), and it is taken out of their sum again.
-      const float x = odd_here ? (NQ == 3 ? 0.f : 1.f) : NQ == 3 ? sc.y : fmaxf(sc.y, 1.26217745e-29f), y = NQ == 3 ? x : __builtin_amdgcn_logf(x), z = NQ == 3 ? 0.f : __builtin_amdgcn_rcpf(x);
+      // Weights take their block's value scale.  fp32 queries: by a product; bf16: in the exponent, as its logarithm (off by 2^-24 of it, the scale v_least at least), and it is taken out of their sum again.
+      const float x = odd_here ? (NQ == 3 ? 0.f : 1.f) : NQ == 3 ? sc.y : fmaxf(sc.y, v_least), y = NQ == 3 ? x : __builtin_amdgcn_logf(x);
+      float z = NQ == 3 ? 0.f : __builtin_amdgcn_rcpf(x);
+      if (NQ == 1 && far) z = x > V_FAR ? __builtin_amdgcn_rcpf(x * 0x1p-32f) * 0x1p-32f : z;   // (the instruction makes 0 of what is below the least normal number)
 #pragma unroll
       for (int i = 0; i < GROUPS16; ++i) {
         v_by[i] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, y), 16 * i));
