@@ -361,7 +361,8 @@ typedef struct {
  *     -100..100 with a <= M 2^e; codes of other tokens become 0
  *   - else scale = its scale times 2^n, n the least whole number >= 0 with a <= M scale 2^n, which stays within 2^100; codes of other tokens are rounded again where n > 0
  *   - code = element / scale, to nearest, ties to even, within -M..M (an infinity is M); NaN stays NaN in EAGLE_E4M3 and becomes 0 in EAGLE_INT8
- * with everything from the position to the code worked out in 64 bits.  Codes at or behind key_len, of pages that are not there and of blocks without new tokens stay as they are.
+ * with everything from the position to the code worked out in 64 bits.  Codes at or behind key_len, of pages that are not there and of blocks without new tokens stay as they are:
+ * a tree's node that lies there is not stored and counts for no scale.
  * Two sequences of one call must not append to the same block. */
 int eagle_rope_coded(const eagle_rope_plan *plan, const eagle_rope_args *args, const eagle_chunk *chunk, const eagle_coded_kv *kv, void *hip_stream);
 

@@ -184,7 +184,7 @@ def append_codes(x, values, scale, facts, table, key_len, *, page, block, e4m3, 
     M = 448.0 if e4m3 else 127.0
     blocks = {}
     for r, s, t, _, _ in facts:
-        if r - int(row_start[s]) < max_rows and 0 <= t < max_keys and t // page < len(table[s]) and 0 <= table[s][t // page] < len(values):
+        if r - int(row_start[s]) < max_rows and 0 <= t < min(max_keys, int(key_len[s])) and t // page < len(table[s]) and 0 <= table[s][t // page] < len(values):
             blocks.setdefault((s, t // block), []).append((r, t))
     for (s, b), new in blocks.items():
         pg, first = int(table[s][b * block // page]), b * block

@@ -114,7 +114,7 @@ __global__ __launch_bounds__(256) void k_rope_coded(const AppendDev A) {
   int r0, n_all;
   rows_of(s, &r0, &n_all);
   const int keys = min(max(0, C.key_len[s]), 1 << 30), n_rows = min(n_all, C.max_rows);
-  const long long end = min((long long)C.max_keys, room);         // tokens from here on are not stored
+  const long long end = min((long long)min(C.max_keys, keys), room);   // tokens from here on are not stored (a tree's nodes may lie behind the sequence's last token)
   const int held = (int)max(0ll, min((long long)B, min((long long)keys, room) - t0));   // slots of tokens of the sequence
   if (tid < 128) s_held[tid] = 0;
   if (tid == 0) s_n = 0;
