@@ -17,7 +17,7 @@ struct AppendDev {
 __device__ inline double2 cos_sin_turn64(unsigned long long turn, int position) {
   const unsigned long long t = turn * (unsigned long long)(long long)position;
   const unsigned long long quarter = (t + (1ull << 61)) >> 62;
-  const double x = (double)(long long)(t - (quarter << 62)) * 3.4061215800656670e-19;   // 2 pi / 2^64
+  const double x = (double)(long long)(t - (quarter << 62)) * 3.4061215800865545e-19;   // 2 pi / 2^64
   const double z = x * x;
   double s = 2.8114572543455206e-15, c = 4.7794773323873853e-14;                        // 1 / 17!, 1 / 16!
   s = fma(s, z, -7.6471637318198165e-13); c = fma(c, z, -1.1470745597729725e-11);
