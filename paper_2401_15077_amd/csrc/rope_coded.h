@@ -13,7 +13,8 @@ struct AppendDev {
   unsigned long long kv_share;
 };
 
-// Cosine and sine of position * turn in 64 bits: as cos_sin_turn takes whole and quarter turns off, with polynomials that leave out less than 2^-62.
+// Cosine and sine of position * turn in 64 bits: as cos_sin_turn takes whole and quarter turns off, with the series' terms up to x^17 and x^16, which leave out less than 2^-63 of a sine and 2^-58 of a
+// cosine (|x| <= pi / 4; a term more would be lost in the sum's own roundings of 2^-53).  The turn is rounded to a multiple of 2^-64: the angle is off by less than 2^-62 a position.
 __device__ inline double2 cos_sin_turn64(unsigned long long turn, int position) {
   const unsigned long long t = turn * (unsigned long long)(long long)position;
   const unsigned long long quarter = (t + (1ull << 61)) >> 62;
@@ -22,7 +23,7 @@ __device__ inline double2 cos_sin_turn64(unsigned long long turn, int position) 
   double s = 2.8114572543455206e-15, c = 4.7794773323873853e-14;                        // 1 / 17!, 1 / 16!
   s = fma(s, z, -7.6471637318198165e-13); c = fma(c, z, -1.1470745597729725e-11);
   s = fma(s, z, 1.6059043836821613e-10); c = fma(c, z, 2.0876756987868099e-9);
-  s = fma(s, z, -2.5052108385441718e-8); c = fma(c, z, -2.7557319223985891e-7);
+  s = fma(s, z, -2.505210838544172e-8); c = fma(c, z, -2.755731922398589e-7);
   s = fma(s, z, 2.7557319223985893e-6); c = fma(c, z, 2.4801587301587302e-5);
   s = fma(s, z, -1.9841269841269841e-4); c = fma(c, z, -1.3888888888888889e-3);
   s = fma(s, z, 8.3333333333333333e-3); c = fma(c, z, 4.1666666666666667e-2);
@@ -41,7 +42,8 @@ template <bool E4M3> __device__ inline int least_exponent(double a) {
 
 // Some work-groups append: one takes the new tokens of one block of a kv head, keys or values (it has to know the largest of them before it can write one).  The others rotate the queries, as
 // rope_row says.
-// Everything from the angle to the code is worked out in 64 bits, so that a code is what the definition says and no rounding on the way moves it: rounded to odd once for the conversion.
+// Everything from the angle to the code is worked out in 64 bits and rounded to odd once for the conversion.  So a code is what the definition says, but where the exact number lies as near to the border
+// between two codes as the angle's error and a few roundings of 2^-53 move it: there it may be the neighbour.
 //
 // What bounds it: 8191 rows, 64 / 8 heads of 128, bf16, take 82 us for 318 MB, where a copy of as much takes 66.  Keys and values keep the vector unit busy (64-bit operations issue as 32-bit ones do
 // here; in 32 bits with a 64-bit way out for what falls near a border they took 13 more), queries the memory, so the two kinds are spread among each other, and five waves a SIMD hide what either
