@@ -417,7 +417,7 @@ int eagle_apply_logit_rules(const eagle_logits *logits, const eagle_logit_rules 
  * the same every time.  What weighs less than 2^-64 of the largest counts as nothing in sums.
  * Parameters are arrays with an entry a row; null: 1, no top_k, no top_p, no min_p.  A parameter that is NaN is no filter.  Outputs lie apart from all inputs.
  * logits start on a multiple of an element, rows from 1 to 2^24, vocab to 2^30.  Row stride: at least vocab, where there is more than one row.
- * workspace (dev, 256-byte aligned): eagle_sample_workspace() bytes, for the same arguments; its contents need not be kept or cleared. */
+ * workspace (dev, 256-byte aligned): eagle_sample_workspace() bytes, for the same arguments; its contents need not be kept or cleared (reserved: nothing uses it today). */
 typedef struct {
   int32_t n_rows, vocab, dtype;
   const void *logits;

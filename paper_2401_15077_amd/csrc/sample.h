@@ -6,7 +6,7 @@
 #include <type_traits>
 
 struct SampleDev {
-  int n_rows, vocab, bits, unit;           // masses are multiples of 2^-bits of the largest weight, parts of 2^-unit
+  int vocab, bits, unit;                   // masses are multiples of 2^-bits of the largest weight, parts of 2^-unit
   const void* logits;
   long long stride;
   const float *uniform, *temperature, *top_p, *min_p;

@@ -31,7 +31,7 @@ static int check_sample(const eagle_sample_args* a) {
 
 extern "C" size_t eagle_sample_workspace(const eagle_sample_args* a) {
   if (check_sample(a)) return 0;
-  return 256;
+  return 256;                                                     // (reserved: a row is one work-group, which has all it needs in LDS)
 }
 
 extern "C" int eagle_sample(const eagle_sample_args* a, void* workspace, size_t workspace_bytes, void* hip_stream) {
@@ -43,7 +43,7 @@ extern "C" int eagle_sample(const eagle_sample_args* a, void* workspace, size_t 
   int bits = 62;                                                  // (as many weights of at most 2^bits add up to at most 2^62, and parts to less than 2^52)
   while ((long long)a->vocab > 1ll << (62 - bits)) --bits;
   const double one = std::ldexp(1.0, bits - 11), L = 0.010830424696249145;   // ln 2 / 64
-  const SampleDev d{a->n_rows, a->vocab, bits, bits - 11, a->logits, a->stride, a->uniform, a->temperature, a->top_p, a->min_p, a->top_k, a->token, a->logprob,
+  const SampleDev d{a->vocab, bits, bits - 11, a->logits, a->stride, a->uniform, a->temperature, a->top_p, a->min_p, a->top_k, a->token, a->logprob,
                     {one + 4503599627370496.0, -L * one, L * L / 2 * one, -L * L * L / 6 * one}};
   const hipStream_t stream = (hipStream_t)hip_stream;
   if (a->dtype == EAGLE_F32) k_sample<float><<<a->n_rows, 1024, 0, stream>>>(d);

@@ -27,11 +27,3 @@ struct Most { __device__ u64 operator()(u64 a, u64 b) const { return max(a, b); 
 __device__ __forceinline__ u64 wave_sum(u64 x) { return last_lane(wave_scan(x, 0, Add())); }
 __device__ __forceinline__ u64 wave_min(u64 x) { return last_lane(wave_scan(x, ~0ull, Least())); }
 __device__ __forceinline__ u64 wave_max(u64 x) { return last_lane(wave_scan(x, 0, Most())); }
-__device__ __forceinline__ int wave_scan_sum(int x) {
-  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);
-  return x + __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
-}
