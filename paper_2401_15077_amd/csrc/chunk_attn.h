@@ -22,7 +22,10 @@
 //
 // 8-bit codes are exact in bf16, so the products are those of a bf16 cache.  A block has at least 16 tokens: 16 scores share a key scale, which stands in the constant that takes scores to powers of
 // two (or to the cap's tangent), and their weights a value scale.  fp32 weights are multiplied with it before they become pieces; a bf16 weight takes it as log2 in its exponent, so that it is rounded
-// once (scales below 2^-96 count as 2^-96, or below 2^-64 as 2^-64 beside one above 2^96: none is lost to the least exponent), and the sum takes it rounded: 0.0019 to 0.0023 of the result's norm off, where the unrounded sum gave 0.0022 to 0.0025.  The narrow shape brings codes to LDS as they are and makes bf16 of what each wave reads (RAW); in the wide one four
+// once (scales below 2^-96 count as 2^-96, or below 2^-64 as 2^-64 beside one above 2^96: none is lost to the least exponent).  The sum takes weights as they are: with rounded ones a row of few tokens
+// can be off by 2^-7 of its weights, twice what a weight's rounding is.  The maximum stands where the largest weight times its scale is a power of two, and is not rounded: 0.0018 to 0.0019 of the
+// result's norm off, 0.0017 of which is the output's rounding; standing at the largest score 0.0022 to 0.0026, with rounded weights in the sum 0.0020 to 0.0024 (and two instructions a weight more:
+// 2045 rows 221 us for 214); weights of two pieces 0.0017, 254 us.  The narrow shape brings codes to LDS as they are and makes bf16 of what each wave reads (RAW); in the wide one four
 // waves would do so four times, so a tile's codes are parked in LDS and become bf16 between the products of the tile before.  64 tokens over 1k to 16k each, 64 / 8 heads, e4m3: 221 us, 5.1 TB/s of
 // cache (lengths all alike 5.4 to 5.8); 470 vector instructions a tile beside 32 products, the matrix unit busy 14 %.  1536 and 509 rows behind a window and a cap, bf16: 220, 750 vector instructions
 // a tile, 128 of them what makes bf16 of the codes; busy 22 %.  Four trees of 26 nodes, fp32 over int8: 33, 5 of it joining.  One token over 701, fp32: 12.6.
@@ -897,6 +900,7 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
     }
     top = fmaxf(top, __shfl_xor(top, 32, 64));
     if constexpr (!MODS && !CODED) top *= c2;
+    const float top_seen = top;
     if constexpr (CODED) {
       if (far) {                                                  // the columns that see a token of such a block
         bool lifted = false;
@@ -912,6 +916,19 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
     // The maximum moves only when it grows by more than 8 (weights up to 2^8 lose nothing in fp32 or bf16), and lane by lane, so that a column's bits are its own.
     const bool moved = top > m_run + 8.f || (m_run == -INFINITY && top > -INFINITY);
     if (__any(moved)) {
+      if constexpr (CODED && NQ == 1) {
+        // With the scale of its block the largest weight is no power of two, as it is without, and would be rounded.  So the maximum is put up to 1 higher, where it is one.
+        const float in_block = __builtin_amdgcn_fractf(__builtin_amdgcn_logf(not_finite(sc.y) ? 1.f : fmaxf(sc.y, V_LEAST)));
+        float up = 0.f;
+#pragma unroll
+        for (int i = 0; i < GROUPS16; ++i) {
+          float x = score[i >> 1][8 * (i & 1)];
+#pragma unroll
+          for (int r = 1; r < 8; ++r) x = fmaxf(x, score[i >> 1][8 * (i & 1) + r]);
+          if ((MODS ? x : x * k_by[i]) >= top_seen) up = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, in_block), 16 * i));
+        }
+        top += fmaxf(up, __shfl_xor(up, 32, 64));
+      }
       const float f = moved ? __builtin_amdgcn_exp2f(m_run - top) : 1.f;
       m_run = moved ? top : m_run;
       l_run *= f;
@@ -1040,19 +1057,17 @@ __global__ __launch_bounds__(256, P::WAVES) void k_chunk_attn(const ChunkAttnDev
         const float by = CODED ? k_by[CODED ? jj : 0] : c2, off = CODED && NQ == 1 ? m_sub - v_by[CODED ? jj : 0] : m_sub;
         x = __builtin_amdgcn_exp2f(MODS ? x - off : fmaf(x, by, -off));
         y = __builtin_amdgcn_exp2f(MODS ? y - off : fmaf(y, by, -off));
-        if constexpr (!(CODED && NQ == 1)) {
+        if constexpr (CODED && NQ == 1) {
+          block_sum = pair == 0 ? x : block_sum + x;
+          block_sum += y;
+          if (pair == 3) sum = fmaf(block_sum, v_out[jj], sum);
+        } else {
           sum += x;
           sum += y;
           if constexpr (CODED) { x *= v_by[jj]; y *= v_by[jj]; }
         }
       }
       const uint32_t h = bf16_pair(x, y);
-      if constexpr (CODED && NQ == 1) {                           // (of the rounded ones: a scale is no power of two, so the largest weight is rounded too, and where it is most of the sum that cancels)
-        const float xr = __builtin_bit_cast(float, h << 16), yr = __builtin_bit_cast(float, h & 0xFFFF0000u);
-        block_sum = pair == 0 ? xr : block_sum + xr;
-        block_sum += yr;
-        if (pair == 3) sum = fmaf(block_sum, v_out[jj], sum);
-      }
       pf[jj & 1][j][pair] = h;
       if (j + 1 < NQ) {
         score[a][r] = x - __builtin_bit_cast(float, h << 16);
