@@ -22,13 +22,14 @@
 //
 // 8-bit codes are exact in bf16, so the products are those of a bf16 cache.  A block has at least 16 tokens: 16 scores share a key scale, which stands in the constant that takes scores to powers of
 // two (or to the cap's tangent), and their weights a value scale.  fp32 weights are multiplied with it before they become pieces; a bf16 weight takes it as log2 in its exponent, so that it is rounded
-// once (scales below 2^-96 count as 2^-96, or below 2^-64 as 2^-64 beside one above 2^96: none is lost to the least exponent).  The sum takes weights as they are: with rounded ones a row of few tokens
-// can be off by 2^-7 of its weights, twice what a weight's rounding is.  The maximum stands where the largest weight times its scale is a power of two, and is not rounded: 0.0018 to 0.0019 of the
-// result's norm off, 0.0017 of which is the output's rounding; standing at the largest score 0.0022 to 0.0026, with rounded weights in the sum 0.0020 to 0.0024 (and two instructions a weight more:
-// 2045 rows 221 us for 214); weights of two pieces 0.0017, 254 us.  The narrow shape brings codes to LDS as they are and makes bf16 of what each wave reads (RAW); in the wide one four
-// waves would do so four times, so a tile's codes are parked in LDS and become bf16 between the products of the tile before.  64 tokens over 1k to 16k each, 64 / 8 heads, e4m3: 221 us, 5.1 TB/s of
-// cache (lengths all alike 5.4 to 5.8); 470 vector instructions a tile beside 32 products, the matrix unit busy 14 %.  1536 and 509 rows behind a window and a cap, bf16: 220, 750 vector instructions
-// a tile, 128 of them what makes bf16 of the codes; busy 22 %.  Four trees of 26 nodes, fp32 over int8: 33, 5 of it joining.  One token over 701, fp32: 12.6.
+// once (scales below 2^-96 count as 2^-96, or below 2^-64 as 2^-64 beside one above 2^96: none is lost to the least exponent).  The sum takes weights as they are: with rounded ones a row of
+// few tokens can be off by 2^-7 of its weights, twice what a weight's rounding is.  The maximum stands where the largest weight times its scale is a power of two, and is not rounded: 0.0019
+// of the result's norm off where some hundred tokens are seen, 0.0017 of which is the output's rounding, and 0.0022 to 0.0023 where thousands weigh about alike; standing at the largest score
+// 0.0022 to 0.0026 and 0.0025, with rounded weights in the sum 0.0020 to 0.0024 and 0.0023 (and two instructions a pair of weights more: 2045 rows 221 us for 214); weights of two pieces
+// 0.0017, 254 us.  The narrow shape brings codes to LDS as they are and makes bf16 of what each wave reads (RAW); in the wide one four waves would do so four times, so a tile's codes are
+// parked in LDS and become bf16 between the products of the tile before.  64 tokens over 1k to 16k each, 64 / 8 heads, e4m3: 222 us, 5.1 TB/s of cache (lengths all alike 5.4 to 5.8); 510
+// vector instructions a tile beside 32 products, the matrix unit busy 14 %.  1536 and 509 rows behind a window and a cap, bf16: 217, 760 vector instructions a tile, 128 of them what makes
+// bf16 of the codes; busy 22 %.  Four trees of 26 nodes, fp32 over int8: 33, 5 of it joining.  One token over 701, fp32: 12.6.
 //
 // Registers: fp32 queries over a bf16 cache of 128 hold all 256 and spill (3 and, with cap or slopes, 17 of the wide shape, 7 and 6 of the narrow), which is a few of their loads a tile; over codes of 128
 // three at most; no other shape spills vector registers.

@@ -45,7 +45,7 @@ template <bool E4M3> __device__ inline int least_exponent(double a) {
 // Everything from the angle to the code is worked out in 64 bits and rounded to odd once for the conversion.  So a code is what the definition says, but where the exact number lies as near to the border
 // between two codes as the angle's error and a few roundings of 2^-53 move it: there it may be the neighbour.
 //
-// What bounds it: 8191 rows, 64 / 8 heads of 128, bf16, take 82 us for 318 MB, where a copy of as much takes 66.  Keys and values keep the vector unit busy (64-bit operations issue as 32-bit ones do
+// What bounds it: 8191 rows, 64 / 8 heads of 128, bf16, take 84 us for 318 MB, where a copy of as much takes 66.  Keys and values keep the vector unit busy (64-bit operations issue as 32-bit ones do
 // here; in 32 bits with a 64-bit way out for what falls near a border they took 13 more), queries the memory, so the two kinds are spread among each other, and five waves a SIMD hide what either
 // waits for: with four (all of a run's angles at once) 92, with six (by spilling) 89 to 121.  Queries in a launch of their own, or heads in a loop of a work-group that keeps angles: 121 to 129, then.
 // One row 8.5, 104 rows 10: the chain from lengths to page, tokens, largest, scale and code.

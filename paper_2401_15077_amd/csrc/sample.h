@@ -37,7 +37,7 @@ __device__ __forceinline__ u64 place_of(float x, int i) { return (u64)order_of(x
 //
 // A row is one work-group of 16 waves, which holds the CU's LDS and registers, in one launch.  What bounds it: the work-group's chain of passes and barriers, not memory (160 rows of 100003, bf16,
 // are 32 MB and take 47 us; of one row's time 4 are the largest, 17 the histogram, 2.5 finding buckets and their edges, 9 the pass that lists, 8 the two rankings).  With all filters 104 rows of
-// 32000 in fp32 take 24, one row of 32000 13, three rows of 128256 35.  Rows divided over several work-groups need a launch for every pass: three rows of 128256 32, but one of 16384 26 in place of
+// 32000 in fp32 take 25, one row of 32000 13, three rows of 128256 35.  Rows divided over several work-groups need a launch for every pass: three rows of 128256 32, but one of 16384 26 in place of
 // 16 and one of 32000 with top-p 41 in place of 27.  What is the same for a row (parameters, the edges of buckets) is worked out by one wave: sixteen that do so at once take each other's time
 // (1.1 us an edge).
 constexpr int SAMPLE_BUCKETS = 4096, SAMPLE_LIST = 1024, SAMPLE_PAIRS = 128, SAMPLE_FEW = 256;
